@@ -422,6 +422,137 @@ aoh_status aoh_classify(const void* w_q, const void* w_k, int32_t n_layers, int3
                         int32_t n_kv_heads, int32_t d_head, int32_t d_model, int32_t sparsity_pct,
                         double* er_out, uint8_t* labels_out, void* stream);
 
+/* ------------------------------------------------------------ paged cache
+ *
+ * Serving many requests at once: their keys and values lie in pages of a fixed
+ * number of tokens, which the caller deals out, and a call serves all sequences,
+ * whatever their lengths. (The paper has no counterpart; head labels, the sink +
+ * window rule and the grouping of heads are those of the calls above.)
+ *
+ *   aoh_paged_prefill  attention over packed prompts
+ *   aoh_paged_append   new keys and values written to the pages
+ *   aoh_paged_decode   attention of one new token of every sequence
+ *   aoh_paged_read     cached keys and values back as dense bf16 rows, e.g. the
+ *                      prefix of a prompt that aoh_paged_prefill continues
+ *
+ * A server's step: aoh_paged_append with lens = lengths including the new
+ * tokens, then aoh_paged_decode with the same lens and table.
+ *
+ * Pages. Page p of the pool holds, for K and V and every KV head, page_size rows
+ * of d_head numbers: [n_pages][K, V][n_kv_heads][page_size][d_head]. A sequence's
+ * position t lies in row t % page_size of the page that its row of the table
+ * names at t / page_size. With AOH_PAGES_E4M3 the numbers are 8-bit (e4m3: sign, 4 bits
+ * of exponent, 3 of mantissa), and behind them lie powers of two, int8
+ * [n_pages][n_kv_heads][K, V][page_size]: code c of a row with power e stands for
+ * c * 2^e. e is the least power for which the row's largest finite magnitude is at
+ * most 448 * 2^e, within [-80, 120]; a code is the nearest one (ties to even) to the
+ * number * 2^-e; an infinity or NaN is stored as NaN. What was never written may
+ * hold anything.
+ *
+ * Tables and lengths are device arrays, read when the kernels run: a captured graph
+ * sees their contents at replay. Entries of a table past a sequence's pages are not read. A page
+ * outside [0, n_pages) or a length outside [0, table_stride * page_size] is out
+ * of range: nothing outside the pool is accessed, outputs that depend on it are
+ * unspecified, nothing is appended there, and aoh_paged_check reports INVALID.
+ *
+ * Calls on one handle must be ordered on one stream (or synchronised by the
+ * caller); the handle belongs to the device that was current at its creation.
+ */
+#define AOH_PAGES_BF16 0
+#define AOH_PAGES_E4M3 1
+
+typedef struct aoh_paged_config {
+  int32_t n_q_heads;  /* Hq, a multiple of n_kv_heads, at most 16 times it        */
+  int32_t n_kv_heads; /* Hkv, at most 64                                          */
+  int32_t d_head;     /* 64 or 128                                                */
+  int32_t page_size;  /* tokens of a page: 16, 32, 64 or 128                      */
+  int32_t n_pages;    /* pages of the pool, >= 1                                  */
+  int32_t form;       /* AOH_PAGES_BF16 or AOH_PAGES_E4M3                         */
+  int32_t max_seqs;   /* sequences of one call at most, 1 .. 65535                */
+  int32_t sink;       /* S, 0 .. 2^30, of streaming heads                         */
+  int32_t window;     /* W, 1 .. 2^30                                             */
+} aoh_paged_config;
+
+typedef struct aoh_paged aoh_paged; /* opaque handle */
+
+/* Bytes of the pool of `cfg`; 0 if it is invalid (message in aoh_last_error()). Host only. */
+size_t aoh_paged_bytes(const aoh_paged_config* cfg);
+
+/*
+ * Bind a caller-owned device buffer as the pool (256-byte aligned; not freed by the
+ * library; contents need not be initialised). head_labels: host [n_kv_heads], copied. Allocates the handle's
+ * small device arrays and synchronises the device once; no later call
+ * allocates. Errors: INVALID, CAPACITY, UNSUPPORTED, CUDA.
+ */
+aoh_status aoh_paged_init(const aoh_paged_config* cfg, const uint8_t* head_labels, void* pool, size_t pool_bytes,
+                          aoh_paged** out);
+
+/*
+ * Causal attention over packed prompts. The rows of sequence b, q_lens[b] of
+ * them, follow those of sequence b - 1, in q and out, and its k_lens[b] keys and
+ * values likewise in k and v. Row i sits at position k_lens[b] - q_lens[b] + i of
+ * the sequence's keys and sees keys by the rule above; with k_lens equal to q_lens
+ * that is a whole prompt, with more keys the rows continue a prompt whose earlier
+ * keys come first in k and v. A row that sees no key gives zeros.
+ *   q            rows of [n_q_heads][d_head], q_stride elements apart (a multiple of 8,
+ *                at least n_q_heads * d_head: slices of a fused projection will do)
+ *   k, v         rows of [n_kv_heads][d_head], k_stride and v_stride apart
+ *   q_lens, k_lens  host [n_seqs], >= 0; k_lens NULL: as q_lens
+ *   out          [rows][n_q_heads][d_head]
+ * The pages are not touched. The lengths travel as kernel arguments: a captured call
+ * replays with the same ones. Errors: INVALID, CUDA.
+ */
+aoh_status aoh_paged_prefill(aoh_paged* cache, const void* q, const void* k, const void* v, int64_t q_stride,
+                             int64_t k_stride, int64_t v_stride, const int32_t* q_lens, const int32_t* k_lens,
+                             int32_t n_seqs, void* out, void* stream);
+
+/*
+ * Write rows to the pages. Sequence b's rows are rows cu_rows[b] .. cu_rows[b + 1] - 1
+ * of k and v, and become the last ones of its lens[b] tokens (lens counts them
+ * already).
+ *   k, v     rows of [n_kv_heads][d_head], k_stride and v_stride elements apart
+ *   cu_rows  device [n_seqs + 1], cu_rows[0] = 0, or NULL: one row a sequence
+ *   lens     device [n_seqs]
+ *   n_rows   rows in all (cu_rows[n_seqs])
+ *   table    device [n_seqs][table_stride]
+ * No two rows may name the same place. Errors: INVALID, CUDA.
+ */
+aoh_status aoh_paged_append(aoh_paged* cache, const void* k, const void* v, int64_t k_stride, int64_t v_stride,
+                            const int32_t* cu_rows, const int32_t* lens, int32_t n_seqs, int32_t n_rows,
+                            const int32_t* table, int32_t table_stride, void* stream);
+
+/*
+ * Read positions first[b] .. first[b] + (cu_rows[b + 1] - cu_rows[b]) - 1 of every
+ * sequence as rows cu_rows[b] .. of k_out and v_out, dense bf16
+ * [n_rows][n_kv_heads][d_head]. first: device [n_seqs], or NULL: from position 0. The
+ * other arguments as for aoh_paged_append. Errors: INVALID, CUDA.
+ */
+aoh_status aoh_paged_read(aoh_paged* cache, const int32_t* cu_rows, const int32_t* first, int32_t n_seqs,
+                          int32_t n_rows, const int32_t* table, int32_t table_stride, void* k_out, void* v_out,
+                          void* stream);
+
+/*
+ * Attention of one query token of every sequence, at position lens[b] - 1, over its
+ * lens[b] cached positions (a streaming head: the sinks and the window among them).
+ * lens[b] = 0 gives zeros.
+ *   q     rows of [n_q_heads][d_head], q_stride elements apart
+ *   lens  device [n_seqs];  table  device [n_seqs][table_stride]
+ *   out   [n_seqs][n_q_heads][d_head]
+ * Errors: INVALID, CUDA.
+ */
+aoh_status aoh_paged_decode(aoh_paged* cache, const void* q, int64_t q_stride, const int32_t* lens, int32_t n_seqs,
+                            const int32_t* table, int32_t table_stride, void* out, void* stream);
+
+/*
+ * Synchronise `stream` and read the device error word of the handle's calls: AOH_OK,
+ * AOH_ERR_TIMEOUT (a kernel's bounded wait ran out) or AOH_ERR_INVALID (a page or a
+ * length was out of range); clears the word.
+ */
+aoh_status aoh_paged_check(aoh_paged* cache, void* stream);
+
+/* Release the handle and its device arrays (not the pool). NULL is a no-op. */
+void aoh_paged_destroy(aoh_paged* cache);
+
 /* Library ABI version (major * 100 + minor); 101 added aoh_config.chunk, 102
  * aoh_cache_reserve and aoh_decode_step_noalloc_status. */
 int32_t aoh_version(void);

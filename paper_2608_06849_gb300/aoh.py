@@ -46,6 +46,14 @@ EXPORTS = [
     "aoh_decode_step_reuse",
     "aoh_cache_selftest_wait",
     "aoh_h2share_map",
+    "aoh_paged_bytes",
+    "aoh_paged_init",
+    "aoh_paged_prefill",
+    "aoh_paged_append",
+    "aoh_paged_read",
+    "aoh_paged_decode",
+    "aoh_paged_check",
+    "aoh_paged_destroy",
 ]
 
 
@@ -60,6 +68,13 @@ class aoh_config(ctypes.Structure):
                 ("batch", "n_q_heads", "n_kv_heads", "d_head", "max_seq", "sink", "window", "chunk")]
 
 
+class aoh_paged_config(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("n_q_heads", "n_kv_heads", "d_head", "page_size", "n_pages", "form", "max_seqs", "sink", "window")]
+
+
+PAGE_FORMS = {"bf16": 0, "e4m3": 1}
+
 _lib = None
 
 
@@ -73,6 +88,8 @@ def load():
     lib = ctypes.CDLL(LIB_PATH)
     P = ctypes.c_void_p
     i32 = ctypes.c_int32
+    i64 = ctypes.c_int64
+    pcfgp = ctypes.POINTER(aoh_paged_config)
     cfgp = ctypes.POINTER(aoh_config)
     u8p = ctypes.POINTER(ctypes.c_uint8)
     i32p = ctypes.POINTER(ctypes.c_int32)
@@ -99,6 +116,14 @@ def load():
         "aoh_decode_step_noalloc_status": (i32, [ctypes.POINTER(ctypes.c_uint32), P]),
         "aoh_decode_step_noalloc_selftest": (i32, [cfgp, u8p, P, i32p, i32, P, P, P, P, P]),
         "aoh_classify": (i32, [P, P, i32, i32, i32, i32, i32, i32, ctypes.POINTER(ctypes.c_double), u8p, P]),
+        "aoh_paged_bytes": (ctypes.c_size_t, [pcfgp]),
+        "aoh_paged_init": (i32, [pcfgp, u8p, P, ctypes.c_size_t, ctypes.POINTER(P)]),
+        "aoh_paged_prefill": (i32, [P, P, P, P, i64, i64, i64, i32p, i32p, i32, P, P]),
+        "aoh_paged_append": (i32, [P, P, P, i64, i64, P, P, i32, i32, P, i32, P]),
+        "aoh_paged_read": (i32, [P, P, P, i32, i32, P, i32, P, P, P]),
+        "aoh_paged_decode": (i32, [P, P, i64, P, i32, P, i32, P, P]),
+        "aoh_paged_check": (i32, [P, P]),
+        "aoh_paged_destroy": (None, [P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -327,6 +352,84 @@ def aoh_cache_destroy(cache):
     load().aoh_cache_destroy(cache)
 
 
+def make_paged_config(n_q_heads, n_kv_heads, d_head, page_size, n_pages, form, max_seqs, sink, window):
+    if form not in PAGE_FORMS:
+        raise ValueError(f"form {form!r} is none of {sorted(PAGE_FORMS)}")
+    return aoh_paged_config(n_q_heads, n_kv_heads, d_head, page_size, n_pages, PAGE_FORMS[form], max_seqs, sink, window)
+
+
+def aoh_paged_bytes(cfg):
+    n = load().aoh_paged_bytes(ctypes.byref(cfg))
+    if n == 0:
+        raise AohError(1, load().aoh_last_error().decode())
+    return n
+
+
+def aoh_paged_init(cfg, labels, pool):
+    """pool: a CUDA uint8 tensor of at least aoh_paged_bytes() bytes."""
+    if len(labels) != cfg.n_kv_heads:
+        raise ValueError(f"labels need {cfg.n_kv_heads} entries (one per KV head)")
+    h = ctypes.c_void_p()
+    _check(load().aoh_paged_init(ctypes.byref(cfg), _labels_arr(labels), _ptr(pool, "pool", torch.uint8), pool.numel(),
+                                 ctypes.byref(h)))
+    return h
+
+
+def _rows(t, name, heads, d):
+    """Pointer, token stride and rows of a [rows, heads, d] bf16 CUDA tensor
+    whose rows are dense and may lie any distance apart (a slice of a fused
+    projection's output)."""
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != d:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}; expected [rows, {heads}, {d}]")
+    if not t.is_cuda or t.dtype != torch.bfloat16:
+        raise ValueError(f"{name} must be a torch.bfloat16 CUDA tensor")
+    n, stride = t.shape[0], t.stride()
+    if n <= 1:
+        stride = (heads * d,) + stride[1:]
+    if stride[2] != 1 or (heads > 1 and stride[1] != d) or stride[0] < heads * d:
+        raise ValueError(f"{name} must have dense rows of {heads} x {d}, not strides {t.stride()}")
+    return t.data_ptr(), stride[0], n
+
+
+def _lens_arr(lens):
+    return (ctypes.c_int32 * max(1, len(lens)))(*lens)
+
+
+# The argument checks of the aoh_paged_* calls that need sizes are PagedCache's.
+
+def aoh_paged_prefill(cache, q, k, v, q_lens, k_lens, out, stream=None):
+    """q, k, v, out: (pointer, token stride) pairs but for out, a pointer;
+    q_lens, k_lens (or None): host lists."""
+    _check(load().aoh_paged_prefill(cache, q[0], k[0], v[0], q[1], k[1], v[1], _lens_arr(q_lens),
+                                    None if k_lens is None else _lens_arr(k_lens), len(q_lens), out,
+                                    _stream_ptr(stream)))
+
+
+def aoh_paged_append(cache, k, v, cu_rows, lens, n_seqs, n_rows, table, table_stride, stream=None):
+    """k, v: (pointer, token stride) pairs; cu_rows (or None), lens, table: pointers."""
+    _check(load().aoh_paged_append(cache, k[0], v[0], k[1], v[1], cu_rows, lens, n_seqs, n_rows, table, table_stride,
+                                   _stream_ptr(stream)))
+
+
+def aoh_paged_read(cache, cu_rows, first, n_seqs, n_rows, table, table_stride, k_out, v_out, stream=None):
+    """Pointers throughout; cu_rows and first may be None."""
+    _check(load().aoh_paged_read(cache, cu_rows, first, n_seqs, n_rows, table, table_stride, k_out, v_out,
+                                 _stream_ptr(stream)))
+
+
+def aoh_paged_decode(cache, q, lens, n_seqs, table, table_stride, out, stream=None):
+    """q: (pointer, token stride); lens, table, out: pointers."""
+    _check(load().aoh_paged_decode(cache, q[0], q[1], lens, n_seqs, table, table_stride, out, _stream_ptr(stream)))
+
+
+def aoh_paged_check(cache, stream=None):
+    _check(load().aoh_paged_check(cache, _stream_ptr(stream)))
+
+
+def aoh_paged_destroy(cache):
+    load().aoh_paged_destroy(cache)
+
+
 # ------------------------------------------------------------- convenience
 
 def _need(t, name, n):
@@ -413,6 +516,107 @@ class Cache:
     def close(self):
         if getattr(self, "handle", None):
             aoh_cache_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class PagedCache:
+    """A pool of pages on the current CUDA device plus its library handle:
+    attention for many sequences of different lengths, whose keys and values the
+    caller deals to pages (include/aoh.h documents the layout).
+
+    ``form`` is "bf16", or "e4m3": 8-bit numbers with a power of two for each
+    row. ``pool`` may be a uint8 CUDA tensor of the caller's. Tables are int32
+    CUDA tensors [sequences, pages], lengths int32 CUDA tensors [sequences].
+    Every tensor is checked against the configuration before the library is
+    called."""
+
+    def __init__(self, n_pages, page_size, n_q_heads, n_kv_heads, d_head, sink, window, labels, form="bf16",
+                 max_seqs=256, pool=None, device=None):
+        self.handle = None
+        self.cfg = make_paged_config(n_q_heads, n_kv_heads, d_head, page_size, n_pages, form, max_seqs, sink, window)
+        self.labels = [int(x) for x in labels]
+        self.nbytes = aoh_paged_bytes(self.cfg)
+        self.pool = torch.empty(self.nbytes, dtype=torch.uint8, device=device or "cuda") if pool is None else pool
+        self.handle = aoh_paged_init(self.cfg, self.labels, self.pool)
+        self.n_pages, self.page_size, self.form, self.max_seqs = n_pages, page_size, form, max_seqs
+        self.n_q_heads, self.n_kv_heads, self.d_head = n_q_heads, n_kv_heads, d_head
+        self.sink, self.window = sink, window
+
+    def _ints(self, t, name, n):
+        if t.dim() != 1 or t.shape[0] != n:
+            raise ValueError(f"{name} has shape {tuple(t.shape)}; expected [{n}]")
+        return _ptr(t, name, torch.int32)
+
+    def _table(self, table):
+        if table.dim() != 2 or table.shape[0] > self.max_seqs:
+            raise ValueError(f"table has shape {tuple(table.shape)}; expected [sequences <= {self.max_seqs}, pages]")
+        return _ptr(table, "table", torch.int32), table.shape[0], table.shape[1]
+
+    def _out(self, t, name, rows, heads):
+        if tuple(t.shape) != (rows, heads, self.d_head):
+            raise ValueError(f"{name} has shape {tuple(t.shape)}; expected [{rows}, {heads}, {self.d_head}]")
+        return _ptr(t, name)
+
+    def prefill(self, q, k, v, q_lens, out, k_lens=None, stream=None):
+        """Causal attention over packed prompts: q, out [rows, Hq, d], k, v [keys, Hkv, d]
+        (q, k and v with any distance between tokens); q_lens, k_lens host
+        lists. Sequence b's rows are the last q_lens[b] of its k_lens[b] (default:
+        q_lens[b]) positions. The pages are not touched."""
+        qp, kp = _rows(q, "q", self.n_q_heads, self.d_head), _rows(k, "k", self.n_kv_heads, self.d_head)
+        vp = _rows(v, "v", self.n_kv_heads, self.d_head)
+        op = self._out(out, "out", qp[2], self.n_q_heads)
+        if len(q_lens) > self.max_seqs or (k_lens is not None and len(k_lens) != len(q_lens)):
+            raise ValueError(f"q_lens and k_lens hold one length a sequence, at most {self.max_seqs}")
+        if sum(q_lens) != qp[2] or sum(q_lens if k_lens is None else k_lens) != kp[2] or kp[2] != vp[2]:
+            raise ValueError(f"q, k and v hold {qp[2]}, {kp[2]} and {vp[2]} rows; q_lens and k_lens say otherwise")
+        aoh_paged_prefill(self.handle, qp, kp, vp, q_lens, k_lens, op, stream)
+
+    def append(self, k, v, lens, table, cu_rows=None, stream=None):
+        """Write k, v [rows, Hkv, d] (any distance between tokens): rows cu_rows[b] ..
+        cu_rows[b + 1] - 1 (without cu_rows: row b) become the last of sequence b's
+        lens[b] tokens."""
+        kp, vp = _rows(k, "k", self.n_kv_heads, self.d_head), _rows(v, "v", self.n_kv_heads, self.d_head)
+        tp, n, width = self._table(table)
+        if kp[2] != vp[2] or (cu_rows is None and kp[2] != n):
+            raise ValueError(f"k and v hold {kp[2]} and {vp[2]} rows for {n} sequences")
+        aoh_paged_append(self.handle, kp, vp, None if cu_rows is None else self._ints(cu_rows, "cu_rows", n + 1),
+                         self._ints(lens, "lens", n), n, kp[2], tp, width, stream)
+
+    def read(self, table, cu_rows, k_out, v_out, first=None, stream=None):
+        """Positions first[b] (default 0) on of every sequence as rows cu_rows[b] ..
+        cu_rows[b + 1] - 1 (None: row b alone) of k_out, v_out [rows, Hkv, d]."""
+        tp, n, width = self._table(table)
+        rows = k_out.shape[0]
+        kp, vp = self._out(k_out, "k_out", rows, self.n_kv_heads), self._out(v_out, "v_out", rows, self.n_kv_heads)
+        if cu_rows is None and rows != n:
+            raise ValueError(f"k_out and v_out hold {rows} rows for {n} sequences")
+        aoh_paged_read(self.handle, None if cu_rows is None else self._ints(cu_rows, "cu_rows", n + 1),
+                       None if first is None else self._ints(first, "first", n), n, rows, tp, width, kp, vp, stream)
+
+    def decode(self, q, lens, table, out, stream=None):
+        """Attention of one new token of every sequence, q, out [sequences, Hq, d] (q
+        with any distance between tokens), over the sequence's lens[b] cached
+        positions, the token's own among them (append it first)."""
+        qp = _rows(q, "q", self.n_q_heads, self.d_head)
+        tp, n, width = self._table(table)
+        if qp[2] != n:
+            raise ValueError(f"q holds {qp[2]} rows for {n} sequences")
+        aoh_paged_decode(self.handle, qp, self._ints(lens, "lens", n), n, tp, width,
+                         self._out(out, "out", n, self.n_q_heads), stream)
+
+    def check(self, stream=None):
+        """Synchronise and raise if a kernel reported an error."""
+        aoh_paged_check(self.handle, stream)
+
+    def close(self):
+        if getattr(self, "handle", None):
+            aoh_paged_destroy(self.handle)
             self.handle = None
 
     def __del__(self):

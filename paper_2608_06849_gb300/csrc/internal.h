@@ -18,6 +18,7 @@ constexpr int kMaxKvHeads = 64;
 // sticky status word).
 constexpr uint32_t kErrTimeout = 1u;   // a kernel's bounded wait ran out
 constexpr uint32_t kErrCapacity = 2u;  // a decode step found a sequence already holding max_seq tokens
+constexpr uint32_t kErrPages = 4u;     // a length or a page of a paged cache's tables is out of range
 
 // Cache geometry as the kernels see it. Offsets are in bf16 elements from the
 // cache base; see include/aoh.h for the layout.
@@ -154,6 +155,87 @@ struct PrefillTcArgs {
   float scale_log2;
 };
 
+// Packed prompts: a sequence's rows are {first query row, rows, first key row, keys}; by
+// value up to kMost sequences, in device memory above.
+struct PackedSeqs {
+  static constexpr int kMost = 64;
+  int4 by_value[kMost];
+  const int4* table;  // device, or null: by value
+  __host__ __device__ int4 of(int b) const { return table ? table[b] : by_value[b]; }
+};
+
+// Arguments of the prefill kernels on packed prompts: tensor maps over q / k / v (rows of
+// [heads][D], box 128 rows x 64 columns, 128-byte swizzle). Work items travel by value.
+struct PackedArgs {
+  CUtensorMap tq, tk, tv;
+  CacheGeom geom;  // heads, S and W (no cache)
+  void* out;       // [rows][Hq][D]
+  PackedSeqs seqs;
+  const uint64_t* work;  // unused
+  uint32_t* err;
+  float scale_log2;
+};
+
+// Sequences that travel to the device as a kernel's arguments: unlike a copy from
+// pageable memory it waits for nothing and may be captured.
+struct PackedUpload {
+  static constexpr int kMost = 1024;
+  int first, n;
+  int4 seq[kMost];
+};
+
+// The pages of a paged cache (include/aoh.h gives the layout).
+struct PagePool {
+  void* data;      // [n_pages][K, V][Hkv][ps][D], bf16 or e4m3
+  int8_t* powers;  // e4m3: [n_pages][Hkv][K, V][ps]
+  int n_pages, ps, lg_ps;
+  int form;        // 0: bf16, 1: e4m3 rows with a power of two each
+  int Hkv, D;
+};
+
+// Rows of a call in a paged cache: sequence b's rows are cu[b] .. cu[b + 1] - 1 (cu
+// null: row b alone).
+struct PageRows {
+  const int32_t* cu;     // device [n_seqs + 1], or null
+  const int32_t* table;  // device [n_seqs][table_stride]: the sequence's pages
+  int table_stride, n_seqs, n_rows;
+};
+
+// Writes rows k, v ([Hkv][D] at token strides of so many elements) as the last rows of
+// sequences of lens[b] tokens.
+struct PagedAppendArgs {
+  PagePool pool;
+  PageRows rows;
+  const void* k;
+  const void* v;
+  long long k_stride, v_stride;
+  const int32_t* lens;
+  uint32_t* err;
+};
+
+// Reads positions first[b] .. (0 .. when first is null) into dense bf16 rows k, v.
+struct PagedReadArgs {
+  PagePool pool;
+  PageRows rows;
+  void* k;
+  void* v;
+  const int32_t* first;
+  uint32_t* err;
+};
+
+struct PagedDecodeArgs {
+  PagePool pool;
+  CacheGeom geom;
+  const void* q;  // rows of [Hq][D] q_stride elements apart
+  long long q_stride;
+  void* out;      // [n_seqs][Hq][D]
+  const int32_t* lens;
+  const int32_t* table;
+  int table_stride, n_seqs;
+  uint32_t* err;
+  float scale_log2;
+};
+
 // One warp waits on an mbarrier nothing arrives at, for limit_ns; the timeout
 // lands in *err; *elapsed_ns receives how long the wait lasted (0 if it did
 // not give up).
@@ -210,6 +292,18 @@ cudaError_t launch_prefill_tc(const PrefillTcArgs& a, const std::vector<uint64_t
 // One CTA an SM through all items in one pipeline (prefill_short.cu).
 cudaError_t launch_prefill_short(const PrefillTcArgs& a, const std::vector<uint64_t>& items, int num_sms,
                                  cudaStream_t s);
+// 4D map over a [B][T][H][D] bf16 tensor whose rows lie `stride` elements apart (0: H * D),
+// box [1][128][1][64], 128-byte swizzle.
+bool make_rows_map(CUtensorMap* map, const void* base, int B, long long T, int H, int D, long long stride);
+// Fills the first seqs.size() entries of the device table.
+cudaError_t launch_packed_seqs(int4* table, const std::vector<int4>& seqs, cudaStream_t s);
+// The items of packed prompts: `pairs` as in launch_prefill_tc; is_short: one CTA an SM
+// through all items.
+cudaError_t launch_prefill_packed(const PackedArgs& a, const std::vector<uint64_t>& items,
+                                  const std::vector<uint64_t>& pairs, bool is_short, int num_sms, cudaStream_t s);
+cudaError_t launch_paged_append(const PagedAppendArgs& a, int num_sms, cudaStream_t s);
+cudaError_t launch_paged_read(const PagedReadArgs& a, int num_sms, cudaStream_t s);
+cudaError_t launch_paged_decode(const PagedDecodeArgs& a, cudaStream_t s);
 // The CUDA-core decode kernel: the H2Share reuse step of d_head 64, with its
 // CTA count.
 cudaError_t launch_decode_cc(const DecodeArgs& a, cudaStream_t s);

@@ -1,0 +1,98 @@
+// Packed prompts on the prefill kernels (prefill_tc.cuh, prefill_short.cuh): the rows
+// of all sequences lie one behind the other, queries in one tensor, keys and values in
+// others, and row i of a sequence of q_len rows and k_len keys sits at position
+// k_len - q_len + i among its keys. There is no cache: every KV tile is 128 keys of the
+// sequence from its first key on, whatever row of the tensor that is, so a tile's first
+// key is always the tile's first row. Rows past a sequence's last key belong to the
+// next one; they are hidden by the mask and, as V rows, zeroed.
+#pragma once
+
+#include "prefill_tile.cuh"
+
+namespace aoh {
+namespace pf {
+
+struct PackedItem {
+  static constexpr int n_c = 0;  // no cached tiles
+  int h, kvh, q0, len, qrow, krow, klen, off, a_end, c_begin, c_end;
+  bool streaming, two_heads;
+  __device__ __forceinline__ PackedItem(const PackedArgs& a, uint64_t code) {
+    const CacheGeom& g = a.geom;
+    two_heads = (code & kPrefillTwoHeads) != 0;
+    code &= ~kPrefillTwoHeads;
+    h = (int)(code >> 24) & 1023;
+    q0 = (int)(code & 0xffffffu) * (two_heads ? kBM : 2 * kBM);
+    kvh = h / g.G;
+    streaming = g.kind[kvh] != 0;
+    const int4 s = a.seqs.of((int)(code >> 34));
+    qrow = s.x;
+    len = s.y;
+    krow = s.z;
+    klen = s.w;
+    off = klen - len;
+    const int end = max(off + min(q0 + (two_heads ? kBM : 2 * kBM), len), 0);
+    const int tiles = (end + kBN - 1) / kBN;
+    if (!streaming) {
+      a_end = c_begin = c_end = tiles;
+    } else {
+      a_end = (min(g.S, end) + kBN - 1) / kBN;
+      c_begin = max(a_end, max(0, g.wstart(off + q0)) / kBN);
+      c_end = max(c_begin, tiles);
+    }
+  }
+  __device__ __forceinline__ int row0(int x) const { return two_heads ? q0 : q0 + x * kBM; }
+  __device__ __forceinline__ int head(int x) const { return two_heads ? h + x : h; }
+  __device__ __forceinline__ int tiles() const { return a_end + (c_end - c_begin); }
+  __device__ __forceinline__ int chunk_tile(int i) const { return i < a_end ? i : c_begin + (i - a_end); }
+  __device__ __forceinline__ int valid(const CacheGeom&, int i) const { return klen - chunk_tile(i) * kBN; }
+  __device__ __forceinline__ size_t out_row0(const PackedArgs&) const { return (size_t)qrow; }
+  __device__ __forceinline__ int rot(const CacheGeom&) const { return 0; }
+};
+
+template <int D>
+__device__ __forceinline__ void load_kv(const PackedArgs& a, const PackedItem& t, int i, int sel, uint8_t* dst,
+                                        uint64_t* bar) {
+  using C = PfCfg<D>;
+  mbar_arrive_expect_tx(bar, C::KVBYTES);
+  const CUtensorMap* map = sel ? &a.tv : &a.tk;
+  for (int db = 0; db < C::DBLK; ++db)
+    tma_load_4d(dst + db * C::BOX, map, db * 64, t.kvh, t.krow + t.chunk_tile(i) * kBN, 0, bar);
+}
+
+template <int D>
+__device__ __forceinline__ void load_q(const PackedArgs& a, const PackedItem& t, int x, uint8_t* dst, uint64_t* bar) {
+  using C = PfCfg<D>;
+  mbar_arrive_expect_tx(bar, C::QBYTES);
+  for (int db = 0; db < C::DBLK; ++db)
+    tma_load_4d(dst + db * C::BOX, &a.tq, db * 64, t.head(x), t.qrow + t.row0(x), 0, bar);
+}
+
+// The keys of tile ja that row i (position off + i) sees, as in Mask.
+struct PackedMask {
+  bool need;
+  int e_hi, a0 = 0, a1 = 0;
+  static constexpr int b0 = 0, b1 = 0;
+  __device__ __forceinline__ PackedMask(const CacheGeom& g, const PackedItem& t, int ja, int i, int qx0, int) {
+    const int j0 = t.chunk_tile(ja) * kBN, jl = j0 + kBN - 1, pos = t.off + i;
+    need = !(jl <= t.off + qx0 && jl < t.klen &&
+             (!t.streaming || jl < g.S || j0 >= g.wstart(t.off + qx0 + kBM - 1)));
+    const int kmax = min(pos, t.klen - 1) - j0;
+    e_hi = kmax + 1;
+    if (t.streaming) {
+      e_hi = min(e_hi, g.S - j0);
+      a0 = g.wstart(pos) - j0;
+      a1 = kmax + 1;
+    }
+  }
+};
+
+template <>
+struct CallOf<PackedArgs> {
+  using ItemT = PackedItem;
+  using MaskT = PackedMask;
+  static constexpr bool kEmptyRows = true;  // fewer keys than rows
+  static constexpr bool kChained = true;
+};
+
+}  // namespace pf
+}  // namespace aoh

@@ -1,0 +1,184 @@
+// The host's plan of a prefill call: its work items, how clusters share them, and the
+// kernel that runs them. Host code alone.
+#pragma once
+
+#include <algorithm>
+#include <functional>
+#include <vector>
+
+#include "internal.h"
+
+namespace aoh {
+
+// Prefill work: items of two 128-row query tiles, heaviest first so the
+// hardware block scheduler fills the machine longest-processing-time first. An
+// item is one query tile of two heads of a group, or, for the last head of an
+// odd group, two consecutive tiles of that head. Two heads see the same keys;
+// two tiles visit the union of their KV tiles, so that each pair of tiles has one
+// KV tile that the first does not see, and a sequence's last pair may lack the
+// second: 8 ragged sequences of up to 2,999 tokens, 32/8 heads of 128 of which
+// half stream (S = 64, W = 512), 298 -> 277 us; 32K tokens of 28/4 streaming heads
+// (S = 128, W = 1024) 517 -> 480, 32K with half of them retrieval 2504 -> 2468.
+// The cost, the number of KV tiles visited, is the same for all items of a kind,
+// so (b, index, kind) entries are sorted and then expanded. *costs receives each
+// item's cost; rows_of(b) is sequence b's number of rows, cost(b, q0, q_end, streaming) that
+// of the KV tiles that rows q0 .. q_end - 1 visit.
+template <class Rows, class Cost>
+std::vector<uint64_t> prefill_items(const CacheGeom& g, int B, Rows rows_of, Cost cost, std::vector<int>* costs) {
+  constexpr int BM = 128;
+  struct Entry {
+    int cost, b, index;
+    bool streaming, two_heads;
+  };
+  std::vector<Entry> entries;
+  for (int b = 0; b < B; ++b) {
+    const int len = rows_of(b);
+    for (int streaming = 0; streaming < 2; ++streaming) {
+      if ((streaming ? g.n_s : g.n_r) == 0) continue;
+      for (int two_heads = 0; two_heads < 2; ++two_heads) {
+        if ((two_heads ? g.G / 2 : g.G % 2) == 0) continue;
+        const int rows = two_heads ? BM : 2 * BM;
+        for (int q0 = 0; q0 < len; q0 += rows)
+          entries.push_back({cost(b, q0, std::min(q0 + rows, len), streaming != 0), b, q0 / rows, streaming != 0,
+                             two_heads != 0});
+      }
+    }
+  }
+  std::stable_sort(entries.begin(), entries.end(), [](const Entry& x, const Entry& y) { return x.cost > y.cost; });
+  std::vector<uint64_t> items;
+  const size_t most = entries.size() * (size_t)(g.Hq / 2 + g.Hkv);
+  items.reserve(most);
+  costs->reserve(most);
+  for (const Entry& e : entries)
+    for (int i = 0; i < (e.streaming ? g.n_s : g.n_r); ++i) {
+      const int kvh = e.streaming ? g.s_head[i] : g.r_head[i];
+      const int first = e.two_heads ? 0 : g.G - 1, step = e.two_heads ? 2 : 1;
+      for (int h = first; h + step <= g.G; h += step) {
+        items.push_back(prefill_item(e.b, kvh * g.G + h, e.index) | (e.two_heads ? kPrefillTwoHeads : 0));
+        costs->push_back(e.cost);
+      }
+    }
+  return items;
+}
+
+// A cache's chunk: the cached tiles, then those of the chunk itself.
+inline std::vector<uint64_t> prefill_schedule(const CacheGeom& g, const std::vector<int32_t>& base,
+                                              const std::vector<int32_t>& lens, std::vector<int>* costs) {
+  constexpr int BN = 128;
+  return prefill_items(
+      g, g.B, [&](int b) { return (int)lens[b]; },
+      [&](int b, int q0, int q_end, bool streaming) {
+        const int Lb = base[b];
+        const int n_c = Lb == 0 ? 0 : ((streaming ? std::min(Lb, g.S + g.W) : Lb) + BN - 1) / BN;
+        if (!streaming) return n_c + (q_end + BN - 1) / BN;
+        const int a_end = (std::min(std::max(g.S - Lb, 0), q_end) + BN - 1) / BN;
+        const int c_begin = std::max(a_end, std::max(0, g.wstart(q0)) / BN);
+        const int c_end = std::max(c_begin, (q_end + BN - 1) / BN);
+        return n_c + a_end + (c_end - c_begin);
+      },
+      costs);
+}
+
+// Packed prompts (PackedSeqs): row i of a sequence is the last but q_len - 1 - i of its
+// k_len positions. No tiles where every row lies before the first key.
+inline std::vector<uint64_t> packed_schedule(const CacheGeom& g, const std::vector<int4>& seqs, std::vector<int>* costs) {
+  constexpr int BN = 128;
+  return prefill_items(
+      g, (int)seqs.size(), [&](int b) { return seqs[b].y; },
+      [&](int b, int q0, int q_end, bool streaming) {
+        const int off = seqs[b].w - seqs[b].y;
+        const int end = std::max(off + q_end, 0);
+        if (!streaming) return (end + BN - 1) / BN;
+        const int a_end = (std::min(g.S, end) + BN - 1) / BN;
+        const int c_begin = std::max(a_end, std::max(0, g.wstart(off + q0)) / BN);
+        return a_end + std::max(0, (end + BN - 1) / BN - c_begin);
+      },
+      costs);
+}
+
+// The work of clusters of two CTAs, two entries a cluster: two items, or one item
+// twice, with kPrefillHalf, that its CTAs share (kPrefillNone fills the last
+// cluster). Nothing when one CTA an item is as good.
+//
+// When every item's cluster runs at once, the call lasts as long as its longest
+// item, and sharing all halves that. Measured (8 heads of 128, one sequence, us of
+// a call without / with): 512 rows (4 tiles) 17 / 18, 640 19 / 20, 1024 22 / 21, 2048
+// 33 / 26; heads of 64: 512 16 / 16, 1024 20 / 18, 2048 30 / 22.
+//
+// In a few waves, as in a chunk after a long prefix whose heavy items all read it,
+// a last wave of heavy items that leaves many SMs idle is shared, while the
+// lighter items behind it are not. k + 1 of the first k * num_sms + 1 items meet
+// on one SM; where that ends a tenth later than the work spread evenly, the ends
+// of longest-first schedules decide, in visited tiles, with 4 tiles' time added
+// to an item and 8 to a half: nothing shared, or half a wave or a whole one from
+// item k * num_sms on (from the even one below, with an odd count of SMs). Past four items an SM the last wave matters little. 28
+// heads of 128, half of them streaming (S = 128, W = 2048), us of a call without /
+// with: 4096 rows after 16K tokens 388 / 388 (not shared), 20K 471 / 461, 24K 555 /
+// 526, 28K 638 / 585; 1024 rows after 24K 272 / 151.
+inline std::vector<uint64_t> prefill_pairs(const std::vector<uint64_t>& items, const std::vector<int>& costs, int num_sms) {
+  const int n = (int)items.size(), slots = num_sms / 2;
+  int first = 0, last = 0;  // items [first, last) are shared
+  if (n <= slots) {
+    if (n > 0 && costs[0] >= 7) last = n;
+  } else if (n <= std::min(4 * num_sms, kPrefillSplitMost)) {
+    long long work = 0, meet = 0;
+    for (int c : costs) work += c + 4;
+    for (int a = 0; a < n; a += num_sms)
+      if ((a / num_sms + 1) * (long long)(costs[a] + 4) > meet) {
+        meet = (a / num_sms + 1) * (long long)(costs[a] + 4);
+        first = a;
+      }
+    first &= ~1;  // the halves of an item are entries 2 i and 2 i + 1 at any count of SMs
+    if (meet * num_sms * 10 > work * 11) {
+      std::vector<int> free_at;  // a min-heap
+      auto end_of = [&](int count, int shared_end) {
+        free_at.assign(count, 0);
+        int end = 0;
+        for (int i = 0; i < n;) {
+          const bool half = i >= first && i < shared_end;
+          std::pop_heap(free_at.begin(), free_at.end(), std::greater<int>());
+          end = std::max(end, free_at.back() += half ? (costs[i] + 1) / 2 + 8 : costs[i] + 4);
+          std::push_heap(free_at.begin(), free_at.end(), std::greater<int>());
+          i += count == num_sms || half ? 1 : 2;
+        }
+        return end;
+      };
+      int best = end_of(num_sms, 0);
+      for (int window = slots; window <= 2 * slots; window += slots) {
+        const int end = end_of(slots, first + window);
+        if (end < best) {
+          best = end;
+          last = std::min(first + window, n);
+        }
+      }
+    }
+  }
+  std::vector<uint64_t> pairs;
+  if (last == 0) return pairs;
+  pairs.reserve(n + last - first + 2);
+  for (int i = 0; i < n; ++i) {
+    const bool half = i >= first && i < last;
+    if (half) pairs.push_back(items[i] | kPrefillHalf);
+    pairs.push_back(items[i] | (half ? kPrefillHalf : 0));
+  }
+  if (pairs.size() & 1) pairs.push_back(kPrefillNone);
+  return pairs;
+}
+
+// Whether one CTA an SM goes through all items in one pipeline instead of a CTA an
+// item: many short items, whose starts and ends it overlaps. It deals them out
+// beforehand, which needs several for an SM to even out, and its loop over KV tiles
+// is a few percent slower. Measured, us of a call with a CTA an item / so (32/8 heads
+// of 128, half streaming, S = 64, W = 512; items an SM, tiles an item): 8 x 512 (3.4,
+// 2.5) 41 / 38, 16 x 512 (6.7, 2.5) 78 / 62, 8 x 1024 (6.7, 4.3) 94 / 79, 2 x 2048
+// (3.4, 6.8) 60 / 62, 8 x 2048 (13.5, 6.8) 220 / 191, 1 x 4096 (3.4, 11) 80 / 87, 2 x 4096
+// (6.7, 11) 154 / 146, 1 x 8192 (6.7, 19) 224 / 238, 2 x 8192 (13.5, 19) 439 / 433; 4 x 512
+// (1.7, 2.5) 24 / 25; 32K tokens of 28/4 heads (24, 73) 2469 / 2609.
+inline bool prefill_is_short(const std::vector<int>& costs, int num_sms) {
+  const long long n = (long long)costs.size();
+  long long tiles = 0;
+  for (int c : costs) tiles += c;
+  return n >= 3 * num_sms && tiles <= 20 * n && tiles * num_sms * 10 <= 19 * n * n;
+}
+
+}  // namespace aoh

@@ -1,7 +1,9 @@
-// The parts of the prefill kernels (prefill_tc.cu: a CTA an item, or half of one;
-// prefill_short.cu: one pipeline through many short items): shapes, the geometry of
+// The parts of the prefill kernels (prefill_tc.cuh: a CTA an item, or half of one;
+// prefill_short.cuh: one pipeline through many short items): shapes, the geometry of
 // a work item and its copies, the MMAs and the softmax of one tile, and the output
-// rows.
+// rows. The kernels serve two kinds of call, told apart by the type of their
+// arguments: a chunk of a cache's sequences (PrefillTcArgs, below) and packed
+// prompts (PackedArgs, prefill_packed.cuh).
 #pragma once
 
 #include <math.h>
@@ -89,6 +91,10 @@ struct Item {
   __device__ __forceinline__ int row0(int x) const { return two_heads ? q0 : q0 + x * kBM; }
   __device__ __forceinline__ int head(int x) const { return two_heads ? h + x : h; }
   __device__ __forceinline__ int tiles() const { return n_c + a_end + (c_end - c_begin); }
+  // row 0 of the sequence among the output's rows
+  __device__ __forceinline__ size_t out_row0(const PrefillTcArgs& a) const { return (size_t)b * a.T; }
+  // oldest ring slot of a wrapped cached ring
+  __device__ __forceinline__ int rot(const CacheGeom& g) const { return (streaming && Lb > g.S + g.W) ? (Lb - g.S) % g.W : 0; }
   // visited tile i: the chunk tile, for i >= n_c
   __device__ __forceinline__ int chunk_tile(int i) const { return i - n_c < a_end ? i - n_c : c_begin + (i - n_c - a_end); }
   // keys of visited tile i that hold data (the rest: cache rows not yet written,
@@ -216,6 +222,18 @@ struct Mask {
   }
 };
 
+// What the kernels need to know of a kind of call: its items and masks, and
+// whether rows may see no key at all (their outputs are zeros).
+template <class A>
+struct CallOf;
+template <>
+struct CallOf<PrefillTcArgs> {
+  using ItemT = Item;
+  using MaskT = Mask;
+  static constexpr bool kEmptyRows = false;
+  static constexpr bool kChained = false;  // launches that follow one another without a wait between
+};
+
 // The softmax of one landed S tile, one row (TMEM lane) a thread: reads the row,
 // hides keys, moves the running max m (rescaling O in TMEM when it grew by more
 // than 2^8, once the PV before, phase pv_parity of pv_done, has landed), writes P
@@ -231,8 +249,8 @@ struct Mask {
 // 2504 us so. Announcing the first half before the third quarter's exponentials
 // waits for the stores to TMEM with nothing to do: 2572 us; forming the first
 // quarter with the old max while the new one is found: 2567 us.
-template <int D>
-__device__ __forceinline__ bool softmax_tile(const PrefillTcArgs& a, const Mask& mask,
+template <int D, class A, class M>
+__device__ __forceinline__ bool softmax_tile(const A& a, const M& mask,
                                              uint32_t tl, uint32_t s_col, uint32_t o_col, bool first, float& m,
                                              float& l, uint64_t* pv_done, uint32_t pv_parity,
                                              uint64_t* p_full, volatile int* abort_flag) {
@@ -364,13 +382,13 @@ __device__ __forceinline__ void put_row(uint8_t* stage, int lane, int chunk, con
 
 // COLS columns, from col0 on, of rows i0 .. i0 + 31 of the chunk (those below len), query
 // tile x's head, from the warp's `stage`.
-template <int D, int COLS>
-__device__ __forceinline__ void write_rows(const PrefillTcArgs& a, const Item& t, int x, int i0, int col0,
+template <int D, int COLS, class A, class T>
+__device__ __forceinline__ void write_rows(const A& a, const T& t, int x, int i0, int col0,
                                            const uint8_t* stage, int lane) {
   constexpr int CH = COLS / 8, RPI = 32 / CH;  // chunks a row, rows a step
   __syncwarp();
   const int c = lane % CH;
-  bf16* out = static_cast<bf16*>(a.out) + ((size_t)t.b * a.T * a.geom.Hq + t.head(x)) * D + col0 + c * 8;
+  bf16* out = static_cast<bf16*>(a.out) + (t.out_row0(a) * a.geom.Hq + t.head(x)) * D + col0 + c * 8;
 #pragma unroll
   for (int r0 = 0; r0 < 32; r0 += RPI) {
     const int r = r0 + lane / CH;
@@ -381,10 +399,12 @@ __device__ __forceinline__ void write_rows(const PrefillTcArgs& a, const Item& t
 
 // Write a warp's 32 finished rows of query tile x's O (each lane's times its inv), the
 // first of them row i0 of the chunk, COLS columns at a time. taddr: O's first
-// column, stage: 32 * COLS * 2 bytes.
-template <int D, int COLS>
-__device__ __forceinline__ void store_o(const PrefillTcArgs& a, const Item& t, int x, int i0, uint32_t taddr, float inv,
+// column, stage: 32 * COLS * 2 bytes, l: the row's sum (0: it saw no key).
+template <int D, int COLS, class A, class T>
+__device__ __forceinline__ void store_o(const A& a, const T& t, int x, int i0, uint32_t taddr, float l,
                                         uint8_t* stage, int lane) {
+  const float inv = 1.f / l;
+  const bool none = CallOf<A>::kEmptyRows && l == 0.f;
 #pragma unroll
   for (int c = 0; c < D / 32; ++c) {
     uint32_t v[32];
@@ -394,7 +414,7 @@ __device__ __forceinline__ void store_o(const PrefillTcArgs& a, const Item& t, i
     for (int e = 0; e < 32; e += 8) {
       float y[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) y[k] = __uint_as_float(v[e + k]) * inv;
+      for (int k = 0; k < 8; ++k) y[k] = none ? 0.f : __uint_as_float(v[e + k]) * inv;
       put_row<COLS>(stage, lane, c % (COLS / 32) * 4 + e / 8, y);
     }
     if ((c + 1) * 32 % COLS == 0) {

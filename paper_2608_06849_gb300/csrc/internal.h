@@ -224,6 +224,7 @@ struct PagedReadArgs {
 };
 
 struct PagedDecodeArgs {
+  CUtensorMap pages;  // the pool as [page, K or V, head][row][D]
   PagePool pool;
   CacheGeom geom;
   const void* q;  // rows of [Hq][D] q_stride elements apart
@@ -232,6 +233,8 @@ struct PagedDecodeArgs {
   const int32_t* lens;
   const int32_t* table;
   int table_stride, n_seqs;
+  float* states;       // [CTAs][4] states of shared items
+  uint32_t* counters;  // [CTAs][3] arrivals: groups of its first and last item, groups of its last
   uint32_t* err;
   float scale_log2;
 };
@@ -303,7 +306,10 @@ cudaError_t launch_prefill_packed(const PackedArgs& a, const std::vector<uint64_
                                   const std::vector<uint64_t>& pairs, bool is_short, int num_sms, cudaStream_t s);
 cudaError_t launch_paged_append(const PagedAppendArgs& a, int num_sms, cudaStream_t s);
 cudaError_t launch_paged_read(const PagedReadArgs& a, int num_sms, cudaStream_t s);
-cudaError_t launch_paged_decode(const PagedDecodeArgs& a, cudaStream_t s);
+bool make_pages_map(CUtensorMap* map, const PagePool& p);
+// Floats of PagedDecodeArgs::states.
+size_t paged_state_floats(int num_sms, int D);
+cudaError_t launch_paged_decode(const PagedDecodeArgs& a, int num_sms, cudaStream_t s);
 // The CUDA-core decode kernel: the H2Share reuse step of d_head 64, with its
 // CTA count.
 cudaError_t launch_decode_cc(const DecodeArgs& a, cudaStream_t s);

@@ -22,6 +22,9 @@ struct aoh_paged {
   void* meta = nullptr;  // the device arrays below
   int4* d_seqs = nullptr;
   uint32_t* d_err = nullptr;
+  uint32_t* d_counters = nullptr;  // decode: arrivals, zero between calls
+  float* d_states = nullptr;       // decode: states of items that CTAs share
+  CUtensorMap pages;               // of the pool, which does not move
 };
 
 namespace {
@@ -52,7 +55,8 @@ aoh_status check_config(const aoh_paged_config* cfg) {
   if (c.d_head != 64 && c.d_head != 128) return fail(AOH_ERR_UNSUPPORTED, "d_head must be 64 or 128");
   if (c.page_size != 16 && c.page_size != 32 && c.page_size != 64 && c.page_size != 128)
     return fail(AOH_ERR_UNSUPPORTED, "page_size must be 16, 32, 64 or 128");
-  if (c.n_pages < 1) return fail(AOH_ERR_INVALID, "n_pages must be >= 1");
+  if (c.n_pages < 1 || (int64_t)c.n_pages * 2 * c.n_kv_heads > (1 << 30))
+    return fail(AOH_ERR_INVALID, "n_pages must be >= 1, and at most 2^29 / n_kv_heads");
   if (c.form != AOH_PAGES_BF16 && c.form != AOH_PAGES_E4M3)
     return fail(AOH_ERR_INVALID, "form %d is neither bf16 (0) nor e4m3 (1)", c.form);
   if (c.max_seqs < 1 || c.max_seqs > 65535) return fail(AOH_ERR_INVALID, "max_seqs must be in [1, 65535]");
@@ -180,7 +184,9 @@ aoh_status aoh_paged_init(const aoh_paged_config* cfg, const uint8_t* head_label
 
   cudaError_t e = cudaGetDevice(&h->device);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&h->num_sms, cudaDevAttrMultiProcessorCount, h->device);
-  const size_t meta = 256 + (size_t)c.max_seqs * sizeof(int4);
+  const size_t counters = ((size_t)h->num_sms * 3 * 4 + 255) / 256 * 256;
+  const size_t seqs = ((size_t)c.max_seqs * sizeof(int4) + 255) / 256 * 256;
+  const size_t meta = 256 + counters + seqs + paged_state_floats(h->num_sms, c.d_head) * 4;
   if (e == cudaSuccess) e = cudaMalloc(&h->meta, meta);
   if (e == cudaSuccess) e = cudaMemset(h->meta, 0, meta);
   if (e == cudaSuccess) e = cudaDeviceSynchronize();
@@ -189,8 +195,16 @@ aoh_status aoh_paged_init(const aoh_paged_config* cfg, const uint8_t* head_label
     delete h;
     return cuda_fail(e, "metadata allocation");
   }
-  h->d_err = static_cast<uint32_t*>(h->meta);
-  h->d_seqs = reinterpret_cast<int4*>(static_cast<uint8_t*>(h->meta) + 256);
+  uint8_t* base = static_cast<uint8_t*>(h->meta);
+  h->d_err = reinterpret_cast<uint32_t*>(base);
+  h->d_counters = reinterpret_cast<uint32_t*>(base + 256);
+  h->d_seqs = reinterpret_cast<int4*>(base + 256 + counters);
+  h->d_states = reinterpret_cast<float*>(base + 256 + counters + seqs);
+  if (!make_pages_map(&h->pages, h->pool)) {
+    cudaFree(h->meta);
+    delete h;
+    return fail(AOH_ERR_CUDA, "cuTensorMapEncodeTiled failed for the pages");
+  }
   *out = h;
   return AOH_OK;
 }
@@ -257,6 +271,9 @@ aoh_status aoh_paged_decode(aoh_paged* cache, const void* q, int64_t q_stride, c
   if (st != AOH_OK) return st;
   if (!lens) return fail(AOH_ERR_INVALID, "lens must not be NULL");
   PagedDecodeArgs a;
+  a.pages = cache->pages;
+  a.states = cache->d_states;
+  a.counters = cache->d_counters;
   a.pool = cache->pool;
   a.geom = cache->geom;
   a.q = q;
@@ -268,7 +285,7 @@ aoh_status aoh_paged_decode(aoh_paged* cache, const void* q, int64_t q_stride, c
   a.n_seqs = n_seqs;
   a.err = cache->d_err;
   a.scale_log2 = (float)(1.4426950408889634 / sqrt((double)c.d_head));
-  const cudaError_t e = launch_paged_decode(a, (cudaStream_t)stream);
+  const cudaError_t e = launch_paged_decode(a, cache->num_sms, (cudaStream_t)stream);
   return e == cudaSuccess ? AOH_OK : cuda_fail(e, "paged decode launch");
 }
 
@@ -336,6 +353,8 @@ aoh_status aoh_paged_check(aoh_paged* cache, void* stream) {
   if (e != cudaSuccess) return cuda_fail(e, "cudaStreamSynchronize");
   uint32_t err = 0;
   e = cudaMemcpy(&err, cache->d_err, sizeof(err), cudaMemcpyDeviceToHost);
+  // a launch that gave up may have left arrivals behind
+  if (e == cudaSuccess && (err & kErrTimeout)) e = cudaMemset(cache->d_counters, 0, (size_t)cache->num_sms * 3 * 4);
   if (e == cudaSuccess && err) e = cudaMemset(cache->d_err, 0, sizeof(err));
   if (e != cudaSuccess) return cuda_fail(e, "error word");
   if (err & kErrTimeout) return fail(AOH_ERR_TIMEOUT, "a kernel's bounded wait ran out (error word 0x%x)", err);

@@ -61,6 +61,25 @@ __device__ __forceinline__ void tc_mma(uint32_t d_tmem, uint64_t adesc, uint64_t
       : "memory");
 }
 
+// As tc_mma, with 8-bit floating-point A and B (kind::f8f6f4; K = 32 a call).
+__device__ __forceinline__ void tc_mma_f8(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
+                                          uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+template <bool F8>
+__device__ __forceinline__ void tc_mma_any(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
+                                           uint32_t accumulate) {
+  if constexpr (F8)
+    tc_mma_f8(d_tmem, adesc, bdesc, idesc, accumulate);
+  else
+    tc_mma(d_tmem, adesc, bdesc, idesc, accumulate);
+}
+
 // D(tmem) (+)= A(tmem) * B(smem desc), kind::f16. A is M lanes x K columns
 // of packed bf16 pairs (element k of a row in column k / 2, even k in the low
 // half), K-major.
@@ -125,11 +144,29 @@ __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&v)[8])
                "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
                : "memory");
 }
+__device__ __forceinline__ void tmem_st4(uint32_t taddr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(taddr), "r"(a), "r"(b), "r"(c), "r"(d)
+               : "memory");
+}
+__device__ __forceinline__ void tmem_st2(uint32_t taddr, uint32_t a, uint32_t b) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x2.b32 [%0], {%1,%2};" ::"r"(taddr), "r"(a), "r"(b) : "memory");
+}
 // The load or store of as many columns as v holds.
+__device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&v)[32]) { tmem_ld32(taddr, v); }
 __device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&v)[8]) { tmem_ld8(taddr, v); }
 __device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&v)[16]) { tmem_ld16(taddr, v); }
 __device__ __forceinline__ void tmem_st(uint32_t taddr, const uint32_t (&v)[8]) { tmem_st8(taddr, v); }
 __device__ __forceinline__ void tmem_st(uint32_t taddr, const uint32_t (&v)[16]) { tmem_st16(taddr, v); }
+// The first N of v (2, 4, 8 or 16).
+template <int N, int M>
+__device__ __forceinline__ void tmem_st_n(uint32_t taddr, const uint32_t (&v)[M]) {
+  if constexpr (N == 2)
+    tmem_st2(taddr, v[0], v[1]);
+  else if constexpr (N == 4)
+    tmem_st4(taddr, v[0], v[1], v[2], v[3]);
+  else
+    tmem_st(taddr, v);
+}
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -144,6 +181,15 @@ __device__ __forceinline__ uint64_t sdesc_sw128(uint32_t saddr, uint32_t lbo, ui
   d |= 1ull << 46;
   d |= 2ull << 61;
   return d;
+}
+
+// The same for rows of 128 bytes, or of 64 (64-byte swizzle: 16-byte chunk c of row r
+// stored at chunk c ^ (r / 2 % 4), 8-row atoms of 512 bytes; layout bits 4).
+template <int ROW_BYTES>
+__device__ __forceinline__ uint64_t sdesc_rows(uint32_t saddr, uint32_t lbo, uint32_t sbo) {
+  static_assert(ROW_BYTES == 128 || ROW_BYTES == 64, "swizzle width");
+  const uint64_t d = sdesc_sw128(saddr, lbo, sbo);
+  return ROW_BYTES == 128 ? d : (d & ~(7ull << 61)) | 4ull << 61;
 }
 
 // Descriptors of one operand's K-steps (and of tiles at constant distances) differ
@@ -164,7 +210,21 @@ __host__ __device__ constexpr uint32_t idesc_bf16(int M, int N, bool b_mn_major,
          | ((uint32_t)(M >> 4) << 24);          // M / 16
 }
 
+// The same of kind::f8f6f4: A e4m3, B e4m3 (b_format 0) or e5m2 (1).
+__host__ __device__ constexpr uint32_t idesc_f8(int M, int N, bool a_mn_major, uint32_t b_format) {
+  return (1u << 4) | (b_format << 10) | ((a_mn_major ? 1u : 0u) << 15) | ((uint32_t)(N >> 3) << 17) |
+         ((uint32_t)(M >> 4) << 24);
+}
+
 // ------------------------------------------------------------ tensor TMA
+__device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, int c0, int c1, int c2, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+      "[%0], [%1, {%2, %3, %4}], [%5];" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(smem_u32(bar))
+      : "memory");
+}
+
 __device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, int c0, int c1, int c2, int c3,
                                             uint64_t* bar) {
   asm volatile(

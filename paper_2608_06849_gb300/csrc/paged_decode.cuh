@@ -24,7 +24,7 @@
 // state (O, max, sum), and the last to arrive adds them up (groups of 16 first).
 // A streaming head's tiles are the pages of its sinks and then those of its window.
 //
-// Warps: 4 NK softmax (a thread a key of the tile), one producer, one MMA issuer.
+// Warps: 4 NK softmax (a thread a key of the tile), two producers, one MMA issuer.
 #pragma once
 
 #include <cuda_fp8.h>
@@ -66,7 +66,7 @@ struct Lay {
   static constexpr int OCOL = 2 * SBUF;
   static constexpr int TMEM_COLS = next_pow2(cmax(OCOL + NPV, 32));
   static constexpr int SOFT = 128 * NK;                    // softmax threads
-  static constexpr int THREADS = SOFT + 64;
+  static constexpr int THREADS = SOFT + 96;
   static constexpr int QBLK = SN * ROWB, QBUF = DBLK * QBLK;
   static constexpr int PBLK = NPV * 128;                   // weights of 128 bytes of keys
   static constexpr int PSET = PBLK * ES;
@@ -82,7 +82,7 @@ struct Lay {
   static constexpr int OFF_X = OFF_LSUM + 4 * NK * GP * 4;  // [GP][64] the upper rows of O (d_head 64)
   static constexpr int OFF_QF = OFF_X + (D == 64 ? GP * 64 * 4 : 0);  // [2][16] factors of the scores
   static constexpr int OFF_BAR = OFF_QF + 128;
-  static constexpr int NBAR = 2 * kNS + 10 + 2;
+  static constexpr int NBAR = 3 * kNS + 10 + 2;
   static constexpr int OFF_MISC = OFF_BAR + NBAR * 8;
   static constexpr int OFF_LENS = OFF_MISC + 64 + 8 * 32;
   static constexpr int SMEM = OFF_LENS + kLensCap * 4 + 1024;
@@ -266,7 +266,7 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
   constexpr int NK = C::NK, LG = NK == 1 ? 7 : NK == 2 ? 8 : 9;
   static_assert(1 << LG == C::KEYS, "keys of a tile");
   constexpr int NT = C::THREADS, NW = C::SOFT / 32;
-  constexpr int kProducer = NW, kMma = NW + 1;
+  constexpr int kLoadK = NW, kLoadV = NW + 1, kMma = NW + 2;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
   uint8_t* sQ = smem + C::OFF_Q;
@@ -276,8 +276,9 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
   float* lsum = reinterpret_cast<float*>(smem + C::OFF_LSUM);
   float* upper = reinterpret_cast<float*>(smem + C::OFF_X);
   float* qfac = reinterpret_cast<float*>(smem + C::OFF_QF);
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR);
-  uint64_t* empty = full + kNS;
+  uint64_t* k_full = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR);  // K and powers of a stage landed
+  uint64_t* v_full = k_full + kNS;
+  uint64_t* empty = v_full + kNS;
   uint64_t* s_full = empty + kNS;  // [2] S(j) in TMEM
   uint64_t* s_free = s_full + 2;   // [2] S(j) read by the softmax
   uint64_t* p_full = s_free + 2;   // [2] P(j) written
@@ -304,7 +305,8 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
   if (threadIdx.x < 32) qfac[threadIdx.x] = 0.f;
   if (threadIdx.x == 0) {
     for (int s = 0; s < kNS; ++s) {
-      mbar_init(&full[s], 1);
+      mbar_init(&k_full[s], 1);
+      mbar_init(&v_full[s], 1);
       mbar_init(&empty[s], 1);
     }
     for (int x = 0; x < 2; ++x) {
@@ -320,7 +322,7 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
     *first_b = 0;
     fence_mbar_init();
   }
-  if (warp == kProducer && lane == 0) prefetch_tmap(&a.pages);
+  if (warp == kLoadK && lane == 0) prefetch_tmap(&a.pages);
   if (warp == kMma) {
     tmem_alloc(tmem_slot, C::TMEM_COLS);
     tmem_relinquish();
@@ -382,48 +384,60 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
   __syncthreads();
   Walk<LG> walk(a, mirrored ? lens_s : nullptr, start, end, *first_b, p < P ? sh64[0] : total);
 
-  if (warp == kProducer) {
-    // ------------------------------------------------------------ producer
-    // A lane a page of the tile: its K, V (and powers).
+  if (warp == kLoadK || warp == kLoadV) {
+    // ------------------------------------------------------------ producers
+    // One for K (and the powers), one for V; a lane a page of the tile. A copy takes its warp
+    // some 80 clocks, its operands being per-lane values that have to become uniform, and
+    // 16-token pages of 8-bit numbers 32 of them a tile: with one producer, which copied the
+    // powers page by page too, 16 sequences of 32K took 230 us at such pages, 165 at 64 tokens.
+    const bool is_v = warp == kLoadV;
+    uint64_t* full = is_v ? v_full : k_full;
     const int spt = C::KEYS >> lg;  // pages of a tile, at most 32
-    const int page_rows = 1 << lg;
     int it = 0;
     bool ok = true;
     while (ok && walk.next()) {
       const Item& t = walk.t;
       const int32_t* row = a.table + (size_t)walk.b * a.table_stride;
-      const int slots = (int)(((long long)t.len + page_rows - 1) >> lg) - t.gap;
+      const int slots = (int)(((long long)t.len + a.pool.ps - 1) >> lg) - t.gap;
       for (int j = walk.lo; j < walk.hi; ++j, ++it) {
         const int st = it % kNS;
         const int n = min(spt, slots - j * spt);
         int page = 0;
         if (lane < n) page = __ldg(row + page_of_slot(t, j * spt + lane));
-        bool bad = (unsigned)page >= (unsigned)a.pool.n_pages;
-        if (bad) atomicOr(a.err, kErrPages);
-        if (lane == 0) {
-          if (it >= kNS) ok = wait_bar(&empty[st], ((it / kNS) & 1) ^ 1, a.err, abort_flag);
-          if (ok) mbar_arrive_expect_tx(&full[st], (uint32_t)(n << lg) * (2 * D * C::ES + (F8 ? 2 : 0)));
-        }
-        ok = __shfl_sync(0xffffffffu, ok, 0);
+        const bool bad = (unsigned)page >= (unsigned)a.pool.n_pages;
+        if (bad && !is_v) atomicOr(a.err, kErrPages);
+        if (it >= kNS) ok = __all_sync(0xffffffffu, wait_bar(&empty[st], ((it / kNS) & 1) ^ 1, a.err, abort_flag));
         if (!ok) break;
+        if constexpr (F8) {
+          if (!is_v) {
+            // the pages' powers, 16 bytes a lane
+#pragma unroll
+            for (int c0 = 0; c0 < C::POWB / 16; c0 += 32) {
+              const int c = c0 + lane, slot = c >> (lg - 3);
+              const int pg = __shfl_sync(0xffffffffu, bad ? 0 : page, slot);
+              if (slot < n)
+                cp_async16(sPow + st * C::POWB + c * 16,
+                           a.pool.powers + (((size_t)pg * g.Hkv + t.kvh) << (lg + 1)) + (c & ((1 << (lg - 3)) - 1)) * 16);
+            }
+            cp_async_mbar_arrive(&full[st]);
+            __syncwarp();
+          }
+        }
+        if (lane == 0) mbar_arrive_expect_tx(&full[st], (uint32_t)(n << lg) * (D * C::ES));
+        __syncwarp();
         if (lane < n) {
           const int key = lane << lg;  // of the tile
-          uint8_t* dst = smem + st * C::STAGE + (key >> 7) * C::GRP + (key & 127) * C::ROWB;
+          uint8_t* dst = smem + st * C::STAGE + (is_v ? C::HALF : 0) + (key >> 7) * C::GRP + (key & 127) * C::ROWB;
           // a page out of range reads as zeros (its coordinate is past the map's end)
-          const int block = bad ? 2 * g.Hkv * a.pool.n_pages : page * 2 * g.Hkv + t.kvh;
+          const int block = bad ? 2 * g.Hkv * a.pool.n_pages : (page * 2 + (is_v ? 1 : 0)) * g.Hkv + t.kvh;
 #pragma unroll
-          for (int sel = 0; sel < 2; ++sel)
-#pragma unroll
-            for (int db = 0; db < C::DBLK; ++db)
-              tma_load_3d(dst + sel * C::HALF + db * C::BOX, &a.pages, db * 64, 0, block + sel * (bad ? 0 : g.Hkv), &full[st]);
-          if constexpr (F8)
-            bulk_g2s(sPow + st * C::POWB + (key << 1),
-                     a.pool.powers + (((size_t)(bad ? 0 : page) * g.Hkv + t.kvh) << (lg + 1)), 2u << lg, &full[st]);
+          for (int db = 0; db < C::DBLK; ++db) tma_load_3d(dst + db * C::BOX, &a.pages, db * 64, 0, block, &full[st]);
         }
         __syncwarp();
       }
     }
     // every issued copy lands before the CTA can exit
+    if (F8) asm volatile("cp.async.wait_all;" ::: "memory");
     if (lane == 0)
       for (int j = it > kNS ? it - kNS : 0; j < it; ++j) drain_wait(&full[j % kNS], (j / kNS) & 1, a.err);
     __syncwarp();
@@ -447,6 +461,7 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
       for (; ok && ofw < n; ++ofw) wait_warp(o_free, ofw & 1);
     };
     auto issue_pv = [&](int j, bool first, int item) {
+      wait_warp(&v_full[j % kNS], (j / kNS) & 1);
       wait_warp(&p_full[j & 1], (j >> 1) & 1);
       if (first) wait_ofree(item);
       if (!ok) return;
@@ -528,7 +543,7 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
       if (F8 && lane == 0) mbar_arrive(&q_set[item & 1]);
       for (int j = walk.lo; j < walk.hi; ++j, ++it) {
         const int st = it % kNS;
-        wait_warp(&full[st], (it / kNS) & 1);
+        wait_warp(&k_full[st], (it / kNS) & 1);
         if (it >= 2) wait_warp(&s_free[it & 1], ((it >> 1) - 1) & 1);
         if (!ok) break;
         if (elect_one()) {
@@ -578,7 +593,7 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
         const long long pos = ((long long)page_of_slot(w, slot) << lg) + (t & (a.pool.ps - 1));
         const bool see = pos < w.len && (!w.strm || pos < g.S || pos >= w.w0);
         const unsigned hidden = __ballot_sync(0xffffffffu, !see);
-        if (F8 || hidden) local_ok = wait_bar(&full[st], (it / kNS) & 1, a.err, abort_flag) && local_ok;
+        if (F8) local_ok = wait_bar(&k_full[st], (it / kNS) & 1, a.err, abort_flag) && local_ok;
         int ek = 0, ev = 0;
         if constexpr (F8) {
           const int8_t* pw = sPow + st * C::POWB + ((t >> lg) << (lg + 1)) + (t & (a.pool.ps - 1));
@@ -588,6 +603,7 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
         if (hidden) {
           // V rows that no weight may meet (0 times a NaN is NaN), while S is formed
           constexpr int CH = C::ROWB / 16;
+          local_ok = wait_bar(&v_full[st], (it / kNS) & 1, a.err, abort_flag) && local_ok;
 #pragma unroll
           for (int db = 0; db < C::DBLK; ++db) {
             uint4* v4 = reinterpret_cast<uint4*>(smem + st * C::STAGE + C::HALF + y * C::GRP + db * C::BOX + (warp & 3) * 32 * C::ROWB);

@@ -270,6 +270,10 @@ aoh_status aoh_paged_decode(aoh_paged* cache, const void* q, int64_t q_stride, c
   if (st == AOH_OK) st = check_table(cache, table, table_stride);
   if (st != AOH_OK) return st;
   if (!lens) return fail(AOH_ERR_INVALID, "lens must not be NULL");
+  // the split counts tiles of at least 128 keys in 32 bits
+  if ((int64_t)n_seqs * c.n_kv_heads * (((int64_t)table_stride * c.page_size + 127) / 128) > INT32_MAX)
+    return fail(AOH_ERR_INVALID, "%d sequences of up to %lld tokens are too many for one call", n_seqs,
+                (long long)table_stride * c.page_size);
   PagedDecodeArgs a;
   a.pages = cache->pages;
   a.states = cache->d_states;

@@ -20,11 +20,13 @@
 //
 // The items, (sequence, KV head), are cut into tiles of 64 KB of K and V; all tiles, item
 // after item, are dealt to the CTAs in equal runs, so that every CTA streams as many bytes
-// whatever the lengths. A CTA joins the runs of an item that it shares: each stores its
-// state (O, max, sum), and the last to arrive adds them up (groups of 16 first).
-// A streaming head's tiles are the pages of its sinks and then those of its window.
+// whatever the lengths. Where CTAs share an item each stores its state (O, max, sum), and the
+// last to arrive adds them up (groups of 16 first). A streaming head's tiles are the pages
+// of its sinks and then those of its window.
 //
-// Warps: 4 NK softmax (a thread a key of the tile), two producers, one MMA issuer.
+// Warps: 4 or 8 of softmax (a thread one or two keys of the tile), 4 that finish items, two
+// producers, one MMA issuer. O and the sums have two buffers, so that a CTA's next item goes
+// on while its last one is finished, stored and joined.
 #pragma once
 
 #include <cuda_fp8.h>
@@ -64,9 +66,11 @@ struct Lay {
   static constexpr int SN = F8 ? (2 * GP + 15) / 16 * 16 : 16;
   static constexpr int SBUF = NK * SN;                     // TMEM columns of one tile's S
   static constexpr int OCOL = 2 * SBUF;
-  static constexpr int TMEM_COLS = next_pow2(cmax(OCOL + NPV, 32));
-  static constexpr int SOFT = 128 * NK;                    // softmax threads
-  static constexpr int THREADS = SOFT + 96;
+  static constexpr int TMEM_COLS = next_pow2(cmax(OCOL + 2 * NPV, 32));
+  static constexpr int KP = NK == 4 ? 2 : 1;               // keys of a softmax thread
+  static constexpr int SOFT = 128 * NK / KP;               // softmax threads
+  static constexpr int NW = SOFT / 32;
+  static constexpr int THREADS = SOFT + 128 + 96;
   static constexpr int QBLK = SN * ROWB, QBUF = DBLK * QBLK;
   static constexpr int PBLK = NPV * 128;                   // weights of 128 bytes of keys
   static constexpr int PSET = PBLK * ES;
@@ -77,14 +81,14 @@ struct Lay {
   static constexpr int OFF_Q = kNS * STAGE;
   static constexpr int OFF_P = OFF_Q + 2 * QBUF;
   static constexpr int OFF_POW = OFF_P + NPB * PBUF;
-  static constexpr int OFF_RED = OFF_POW + kNS * POWB;     // [2][GP][4 NK] warp maxima
-  static constexpr int OFF_LSUM = OFF_RED + 2 * GP * 4 * NK * 4;  // [4 NK][GP]
-  static constexpr int OFF_X = OFF_LSUM + 4 * NK * GP * 4;  // [GP][64] the upper rows of O (d_head 64)
+  static constexpr int OFF_RED = OFF_POW + kNS * POWB;     // [2][GP][NW] warp maxima
+  static constexpr int OFF_SUM = OFF_RED + 2 * GP * NW * 4;  // [2][GP][NW] sums of an item, [2][16] maxima
+  static constexpr int OFF_X = OFF_SUM + 2 * GP * NW * 4 + 128;  // [GP][64] the upper rows of O (d_head 64)
   static constexpr int OFF_QF = OFF_X + (D == 64 ? GP * 64 * 4 : 0);  // [2][16] factors of the scores
   static constexpr int OFF_BAR = OFF_QF + 128;
-  static constexpr int NBAR = 3 * kNS + 10 + 2;
+  static constexpr int NBAR = 3 * kNS + 16 + 1;
   static constexpr int OFF_MISC = OFF_BAR + NBAR * 8;
-  static constexpr int OFF_LENS = OFF_MISC + 64 + 8 * 32;
+  static constexpr int OFF_LENS = OFF_MISC + 32 + 4 * 32 + kMaxKvHeads;
   static constexpr int SMEM = OFF_LENS + kLensCap * 4 + 1024;
   // kind::f16 with bf16, or kind::f8f6f4 with e4m3 (weights: e5m2); V is MN-major
   static constexpr uint32_t IDESC_S = F8 ? idesc_f8(128, SN, false, 0) : idesc_bf16(128, SN, false, false);
@@ -96,33 +100,29 @@ struct Lay {
   static_assert(TMEM_COLS <= 512, "TMEM columns");
 };
 
-// An item: the keys of one KV head of a sequence that its queries see, as tiles.
-struct Item {
-  int len, kvh, w0, gslot, gap, tiles;
-  bool strm;
+// What the heads of a sequence of len tokens see, as tiles of 2^LG keys: a retrieval head every
+// page (tr tiles), a streaming head the pages of its sinks and those of its window (ts tiles; from
+// its gslot-th page on, gap pages are left out; w0: first position of the window).
+struct Seq {
+  int len, tr, ts, w0, gslot, gap;
 };
-// Head k of a sequence of len tokens, retrieval heads before streaming ones.
-// LG: log2 of the keys of a tile.
 template <int LG>
-__device__ __forceinline__ Item make_item(const PagedDecodeArgs& a, int len, int k) {
+__device__ __forceinline__ Seq make_seq(const PagedDecodeArgs& a, int len) {
   const CacheGeom& g = a.geom;
-  Item t;
-  t.len = len;
-  t.strm = k >= g.n_r;
-  t.kvh = t.strm ? g.s_head[k - g.n_r] : g.r_head[k];
-  t.w0 = t.gslot = t.gap = 0;
-  const int lg = a.pool.lg_ps;
-  if (t.strm && len - g.W > g.S) {
-    t.w0 = len - g.W;
-    t.gslot = (g.S + a.pool.ps - 1) >> lg;
-    t.gap = max((t.w0 >> lg) - t.gslot, 0);
+  const int lg = a.pool.lg_ps, round = (1 << (LG - lg)) - 1;
+  Seq q;
+  q.len = len;
+  q.w0 = q.gslot = q.gap = 0;
+  const int slots = (int)(((unsigned)len + a.pool.ps - 1) >> lg);
+  if (len - g.W > g.S) {
+    q.w0 = len - g.W;
+    q.gslot = (g.S + a.pool.ps - 1) >> lg;
+    q.gap = max((q.w0 >> lg) - q.gslot, 0);
   }
-  const int slots = (int)(((long long)len + a.pool.ps - 1) >> lg) - t.gap;
-  t.tiles = (slots + (1 << (LG - lg)) - 1) >> (LG - lg);
-  return t;
+  q.tr = (slots + round) >> (LG - lg);
+  q.ts = (slots - q.gap + round) >> (LG - lg);
+  return q;
 }
-// Page of the item (a slot) -> page of the sequence.
-__device__ __forceinline__ int page_of_slot(const Item& t, int slot) { return slot < t.gslot ? slot : slot + t.gap; }
 
 // The tokens of sequence b, within what its table holds.
 __device__ __forceinline__ int seq_len(const PagedDecodeArgs& a, int b, bool report) {
@@ -132,38 +132,77 @@ __device__ __forceinline__ int seq_len(const PagedDecodeArgs& a, int b, bool rep
   return n < 0 ? 0 : most;
 }
 
-// The items of a CTA's run of tiles [start, end), in order.
+// x / d for 0 <= x, 0 < d: by a reciprocal, put right, where floats hold x.
+__device__ __forceinline__ int quotient(int x, int d) {
+  if (x >= 1 << 23) return (int)((unsigned)x / (unsigned)d);
+  const int q = (int)__fdividef((float)x, (float)d), r = x - q * d;
+  return q + (r >= d ? 1 : 0) - (r < 0 ? 1 : 0);
+}
+
+// How the tiles are dealt: CTA p < P has tiles first(p) .. first(p + 1) - 1 of `total`.
+struct Deal {
+  int P, per, rem;
+  int total;
+  __device__ __forceinline__ int first(int p) const { return p * per + min(p, rem); }
+  __device__ __forceinline__ int cta_of(int x) const {
+    const int wide = rem * (per + 1);
+    return x < wide ? quotient(x, per + 1) : rem + quotient(x - wide, per);
+  }
+};
+
+// The items of a CTA's run of tiles [start, end), in order; used by whole warps. Head k of a
+// sequence: retrieval heads before streaming ones.
 template <int LG>
 struct Walk {
   const PagedDecodeArgs& a;
-  const int* lens_s;
-  long long start, end, off;  // off: the first tile of the item
-  int b, k, lo, hi;
-  Item t;
-  __device__ __forceinline__ Walk(const PagedDecodeArgs& a_, const int* ls, long long s, long long e, int b0, long long off0)
-      : a(a_), lens_s(ls), start(s), end(e), off(off0), b(b0), k(-1) {
-    t.tiles = 0;
+  const int* lens_s;       // the lengths in shared memory, or null: lane b of the warp has sequence b's
+  const uint8_t* heads_s;  // KV head of head k
+  int len_reg;             // (neither above kLensCap sequences: they are loaded)
+  int start, end, off;     // off: the first tile of the item
+  int b, k, lo, hi, tiles = 0;
+  Seq q;
+  // seq_off: the first tile of sequence b, which holds tile `start`
+  __device__ __forceinline__ Walk(const PagedDecodeArgs& a_, const int* ls, const uint8_t* hs, int lr, int s, int e, int b0,
+                                  int seq_off)
+      : a(a_), lens_s(ls), heads_s(hs), len_reg(lr), start(s), end(e), off(seq_off), b(b0), k(-1) {
+    if (start >= end) return;
+    enter();
+    // the item that holds it: the last one that starts at or before it, a lane an item
+    const int lane = threadIdx.x & 31, x = start - off;
+    k = __popc(__ballot_sync(0xffffffffu, lane + 1 < a.geom.Hkv && first_tile(lane + 1) <= x)) - 1;
+    if (a.geom.Hkv > 32) k += __popc(__ballot_sync(0xffffffffu, lane + 33 < a.geom.Hkv && first_tile(lane + 33) <= x));
+    off += first_tile(k + 1);
   }
-  __device__ __forceinline__ int len() const { return lens_s ? lens_s[b] : seq_len(a, b, false); }
+  __device__ __forceinline__ int first_tile(int i) const {
+    const int n_r = a.geom.n_r;
+    return min(i, n_r) * q.tr + max(i - n_r, 0) * q.ts;
+  }
+  __device__ __forceinline__ void enter() {
+    q = make_seq<LG>(a, a.n_seqs <= 32 ? __shfl_sync(0xffffffffu, len_reg, b) : lens_s ? lens_s[b] : seq_len(a, b, false));
+  }
+  __device__ __forceinline__ bool streaming() const { return k >= a.geom.n_r; }
+  __device__ __forceinline__ int kvh() const { return heads_s[k]; }
+  // page of the item (a slot) -> page of the sequence
+  __device__ __forceinline__ int page_of_slot(int slot) const { return !streaming() || slot < q.gslot ? slot : slot + q.gap; }
+  __device__ __forceinline__ int slots() const {
+    return (int)(((unsigned)q.len + a.pool.ps - 1) >> a.pool.lg_ps) - (streaming() ? q.gap : 0);
+  }
   __device__ __forceinline__ bool next() {
     while (true) {
-      off += t.tiles;
+      off += tiles;
       if (off >= end) return false;
       if (++k == a.geom.Hkv) {
         k = 0;
         ++b;
+        enter();
       }
-      t = make_item<LG>(a, len(), k);
-      lo = (int)(max(start, off) - off);
-      hi = (int)min(end - off, (long long)t.tiles);
+      tiles = streaming() ? q.ts : q.tr;
+      lo = max(start - off, 0);
+      hi = min(end - off, tiles);
       if (lo < hi) return true;
     }
   }
 };
-
-__device__ __forceinline__ int cta_of(long long x, long long total, int P) {
-  return (int)(((x + 1) * (long long)P - 1) / total);
-}
 
 // A state of an item that CTAs share: O [G][D], then the maxima and sums [G] each. Slots of
 // a CTA: 0, 1 the state of its first and of its last item, 2, 3 the states joined by the group
@@ -173,46 +212,50 @@ __device__ __forceinline__ float* state_slot(const PagedDecodeArgs& a, int cta, 
   return a.states + ((size_t)cta * 4 + slot) * state_floats(D);
 }
 
-// Adds up n states and stores the outputs (out) or the sum (dst); 128 threads.
-template <int D, class Part>
-__device__ __forceinline__ void join(int n, Part part, int G, bf16* out, float* dst) {
+// Adds up n <= kGroup states and stores the outputs (out) or the sum (dst); 4 warps. State 0
+// is at `first`, state j > 0 at rest + j * stride. A lane owns four values at a time, and
+// the lanes of a head hold the states' maxima and sums between them.
+template <int D>
+__device__ __forceinline__ void join(int n, const float* first, const float* rest, int stride, int G, bf16* out, float* dst) {
   constexpr int U = 8;
-  for (int v = threadIdx.x; v < G * (D / 4); v += 128) {
-    const int h = v / (D / 4);
-    float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
-    float M = -INFINITY, L = 0.f;
-    for (int j = 0; j < n; j += U) {
-      float4 x[U];
-      float mj[U], lj[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const float* p = part(min(j + u, n - 1));
-        x[u] = __ldcg(reinterpret_cast<const float4*>(p) + v);
-        mj[u] = __ldcg(p + G * D + h);
-        lj[u] = __ldcg(p + G * D + G + h);
-      }
-      float top = M;
+  const int lane = threadIdx.x & 31, src = lane & 16;
+  auto part = [&](int j) { return j == 0 ? first : rest + (size_t)j * stride; };
+#pragma unroll 1
+  for (int v = threadIdx.x & 127; v < (G * (D / 4) + 31) / 32 * 32; v += 128) {
+    const bool mine = v < G * (D / 4);  // d_head 64, odd G: the last half-warp has no head
+    const int h = mine ? v / (D / 4) : 0, vv = mine ? v : 0;
+    float4 x[U];
+    auto load = [&](int j0) {
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (j + u < n) top = fmaxf(top, mj[u]);
-      const float sc = M == -INFINITY ? 0.f : fast_exp2(M - top);
-      O.x *= sc;
-      O.y *= sc;
-      O.z *= sc;
-      O.w *= sc;
-      L *= sc;
+        if (j0 + u < n) x[u] = __ldcg(reinterpret_cast<const float4*>(part(j0 + u)) + vv);
+    };
+    const float* p = part(min(lane & 15, n - 1)) + G * D + h;
+    const float mj = (lane & 15) < n ? __ldcg(p) : -INFINITY, lj = __ldcg(p + G);
+    load(0);
+    float M = mj;
+#pragma unroll
+    for (int o = 8; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+    const float w = mj == -INFINITY ? 0.f : fast_exp2(mj - M);
+    float L = mj == -INFINITY ? 0.f : w * lj;
+#pragma unroll
+    for (int o = 8; o >= 1; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
+    float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+    for (int j0 = 0; j0 < n; j0 += U) {
+      if (j0 > 0) load(j0);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        if (j + u >= n || mj[u] == -INFINITY) continue;
-        const float w = fast_exp2(mj[u] - top);
-        O.x += w * x[u].x;
-        O.y += w * x[u].y;
-        O.z += w * x[u].z;
-        O.w += w * x[u].w;
-        L += w * lj[u];
+        const float f = __shfl_sync(0xffffffffu, w, src | (j0 + u));
+        if (j0 + u < n) {
+          O.x += f * x[u].x;
+          O.y += f * x[u].y;
+          O.z += f * x[u].z;
+          O.w += f * x[u].w;
+        }
       }
-      M = top;
     }
+    if (!mine) continue;
     if (out) {
       const float inv = 1.f / L;
       *reinterpret_cast<uint2*>(out + v * 4) =
@@ -237,7 +280,7 @@ __device__ __forceinline__ void join_item(const PagedDecodeArgs& a, int p, int f
   const int gslot = p0 == f ? 1 : 0;
   auto arrive = [&](uint32_t* counter, int of) {
     named_barrier_sync(2, 128);
-    if (threadIdx.x == 0) {
+    if ((threadIdx.x & 127) == 0) {
       const bool done = atom_add_acq_rel_gpu(counter, 1u) == (uint32_t)(of - 1);
       if (done) *counter = 0u;
       *flag = done;
@@ -246,14 +289,15 @@ __device__ __forceinline__ void join_item(const PagedDecodeArgs& a, int p, int f
     return *flag != 0;
   };
   if (!arrive(&a.counters[3 * p0 + gslot], size)) return;
-  auto own = [&](int j) { return state_slot(a, p0 + j, p0 + j == f ? 1 : 0, D); };
+  constexpr int kCta = 4 * state_floats(D);
+  const float *own = state_slot(a, p0, gslot, D), *own_rest = state_slot(a, p0, 0, D);
   if (groups == 1) {
-    join<D>(size, own, G, out, nullptr);
+    join<D>(size, own, own_rest, kCta, G, out, nullptr);
     return;
   }
-  join<D>(size, own, G, nullptr, state_slot(a, p0, 2 + gslot, D));
+  join<D>(size, own, own_rest, kCta, G, nullptr, state_slot(a, p0, 2 + gslot, D));
   if (!arrive(&a.counters[3 * f + 2], groups)) return;
-  join<D>(groups, [&](int j) { return state_slot(a, f + j * kGroup, 2 + (j == 0 ? 1 : 0), D); }, G, out, nullptr);
+  join<D>(groups, state_slot(a, f, 3, D), state_slot(a, f, 2, D), kGroup * kCta, G, out, nullptr);
 }
 
 // Powers of two as floats.
@@ -263,17 +307,18 @@ template <int D, bool F8, int GP>
 __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
     paged_decode_kernel(const __grid_constant__ PagedDecodeArgs a) {
   using C = Lay<D, F8, GP>;
-  constexpr int NK = C::NK, LG = NK == 1 ? 7 : NK == 2 ? 8 : 9;
+  constexpr int NK = C::NK, NW = C::NW, KP = C::KP, LG = NK == 1 ? 7 : NK == 2 ? 8 : 9;
   static_assert(1 << LG == C::KEYS, "keys of a tile");
-  constexpr int NT = C::THREADS, NW = C::SOFT / 32;
-  constexpr int kLoadK = NW, kLoadV = NW + 1, kMma = NW + 2;
+  constexpr int NT = C::THREADS;
+  constexpr int kFinish = NW, kLoadK = NW + 4, kLoadV = NW + 5, kMma = NW + 6;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
   uint8_t* sQ = smem + C::OFF_Q;
   uint8_t* sP = smem + C::OFF_P;
   int8_t* sPow = reinterpret_cast<int8_t*>(smem + C::OFF_POW);
   float* red = reinterpret_cast<float*>(smem + C::OFF_RED);
-  float* lsum = reinterpret_cast<float*>(smem + C::OFF_LSUM);
+  float* lsum = reinterpret_cast<float*>(smem + C::OFF_SUM);  // [2][GP][NW]
+  float* mfin = lsum + 2 * GP * NW;                           // [2][16]
   float* upper = reinterpret_cast<float*>(smem + C::OFF_X);
   float* qfac = reinterpret_cast<float*>(smem + C::OFF_QF);
   uint64_t* k_full = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR);  // K and powers of a stage landed
@@ -284,14 +329,16 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
   uint64_t* p_full = s_free + 2;   // [2] P(j) written
   uint64_t* p_free = p_full + 2;   // [2] O += P(j) V(j) done
   uint64_t* q_set = p_free + 2;    // [2] the item's factors written
-  uint64_t* o_free = q_set + 2;    // the item's O read
-  uint64_t* drain = o_free + 1;
+  uint64_t* l_full = q_set + 2;    // [2] the item's sums and maxima written
+  uint64_t* o_full = l_full + 2;   // [2] the item's O final
+  uint64_t* o_free = o_full + 2;   // [2] the item's O, sums and maxima read
+  uint64_t* drain = o_free + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::OFF_MISC);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   volatile int* flag = reinterpret_cast<volatile int*>(tmem_slot + 2);
-  int* first_b = reinterpret_cast<int*>(tmem_slot + 3);
-  long long* sh64 = reinterpret_cast<long long*>(smem + C::OFF_MISC + 16);  // total, first offset
-  long long* wsum = reinterpret_cast<long long*>(smem + C::OFF_MISC + 64);
+  int* first_s = reinterpret_cast<int*>(tmem_slot + 3);  // [2] the run's first sequence, and its first tile
+  int* wsum = reinterpret_cast<int*>(smem + C::OFF_MISC + 32);
+  uint8_t* heads_s = smem + C::OFF_MISC + 32 + 128;
   int* lens_s = reinterpret_cast<int*>(smem + C::OFF_LENS);
 
   const CacheGeom& g = a.geom;
@@ -303,6 +350,8 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
     reinterpret_cast<uint4*>(sQ)[i] = make_uint4(0, 0, 0, 0);
   fence_proxy_async_smem();
   if (threadIdx.x < 32) qfac[threadIdx.x] = 0.f;
+  if (threadIdx.x < g.Hkv)
+    heads_s[threadIdx.x] = (int)threadIdx.x < g.n_r ? g.r_head[threadIdx.x] : g.s_head[threadIdx.x - g.n_r];
   if (threadIdx.x == 0) {
     for (int s = 0; s < kNS; ++s) {
       mbar_init(&k_full[s], 1);
@@ -315,11 +364,13 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
       mbar_init(&p_full[x], NW);
       mbar_init(&p_free[x], 1);
       mbar_init(&q_set[x], 1);
+      mbar_init(&l_full[x], NW);
+      mbar_init(&o_full[x], 1);
+      mbar_init(&o_free[x], 4);
     }
-    mbar_init(o_free, 4);
     mbar_init(drain, 1);
     *abort_flag = 0;
-    *first_b = 0;
+    first_s[0] = first_s[1] = 0;
     fence_mbar_init();
   }
   if (warp == kLoadK && lane == 0) prefetch_tmap(&a.pages);
@@ -327,62 +378,84 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
     tmem_alloc(tmem_slot, C::TMEM_COLS);
     tmem_relinquish();
   }
-  // everything earlier kernels wrote is visible from here on
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-
-  // ---- this CTA's run: a prefix sum of the sequences' tiles
-  auto seq_tiles = [&](int len) {
-    long long n = 0;
-    if (g.n_r > 0) n += (long long)g.n_r * make_item<LG>(a, len, 0).tiles;
-    if (g.n_s > 0) n += (long long)g.n_s * make_item<LG>(a, len, g.n_r).tiles;
-    return n;
-  };
-  const bool mirrored = a.n_seqs <= kLensCap;
-  const int per = (a.n_seqs + NT - 1) / NT;
-  const int b0 = min(a.n_seqs, (int)threadIdx.x * per), b1 = min(a.n_seqs, b0 + per);
-  long long mine = 0;
-  for (int b = b0; b < b1; ++b) {
-    const int len = seq_len(a, b, blockIdx.x == 0);
-    if (mirrored) lens_s[b] = len;
-    mine += seq_tiles(len);
-  }
-  long long inc = mine;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const long long y = __shfl_up_sync(0xffffffffu, inc, o);
-    if (lane >= o) inc += y;
-  }
-  if (lane == 31) wsum[warp] = inc;
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  long long before = inc - mine, total = 0;
-  for (int w = 0; w < NT / 32; ++w) {
-    if (w < warp) before += wsum[w];
-    total += wsum[w];
-  }
-  const int P = (int)min((long long)gridDim.x, total), p = blockIdx.x;
-  const long long start = p < P ? (long long)p * total / P : total, end = p < P ? (long long)(p + 1) * total / P : total;
-  if (before <= start && start < before + mine) {
-    int b = b0;
-    while (true) {
-      const long long n = seq_tiles(mirrored ? lens_s[b] : seq_len(a, b, false));
-      if (start < before + n) break;
-      before += n;
-      ++b;
+  // everything earlier kernels wrote is visible from here on
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+  // ---- this CTA's run: a prefix sum of the sequences' tiles; up to 32 sequences every warp
+  // forms it for itself, a lane a sequence, without a barrier
+  auto seq_tiles = [&](int len) {
+    const Seq q = make_seq<LG>(a, len);
+    return g.n_r * q.tr + g.n_s * q.ts;
+  };
+  auto scan = [&](int x, int n) {  // over the first n lanes
+    for (int o = 1; o < n; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
     }
-    *first_b = b;
-    sh64[0] = before;
+    return x;
+  };
+  const int p = blockIdx.x;
+  const bool few = a.n_seqs <= 32, mirrored = !few && a.n_seqs <= kLensCap;
+  Deal deal;
+  int len_reg = 0, b_first = 0, seq_off = 0;
+  auto set_deal = [&](int total, int most) {  // most: at least the longest item's tiles
+    deal.total = total;
+    // an item on more than kGroup CTAs is joined in two levels, which a short step does not do
+    // for less: several tiles a CTA there
+    const int least = max(1, (most + kGroup - 1) / kGroup);
+    deal.P = min((int)gridDim.x, quotient(total + least - 1, least));
+    deal.per = quotient(total, max(deal.P, 1));
+    deal.rem = total - deal.per * deal.P;
+  };
+  if (few) {
+    if (lane < a.n_seqs) len_reg = seq_len(a, lane, p == 0 && warp == 0);
+    const int mine = lane < a.n_seqs ? seq_tiles(len_reg) : 0;
+    const Seq q = make_seq<LG>(a, len_reg);
+    const int most = lane >= a.n_seqs ? 0 : g.n_r > 0 ? q.tr : q.ts;
+    set_deal(__reduce_add_sync(0xffffffffu, mine), __reduce_max_sync(0xffffffffu, most));
+    const int inc = scan(mine, a.n_seqs);
+    const unsigned past = __ballot_sync(0xffffffffu, lane < a.n_seqs && inc > deal.first(p));
+    b_first = past ? __ffs(past) - 1 : 0;
+    seq_off = __shfl_sync(0xffffffffu, inc - mine, b_first);
+  } else {
+    const int per = (a.n_seqs + NT - 1) / NT;
+    const int b0 = min(a.n_seqs, (int)threadIdx.x * per), b1 = min(a.n_seqs, b0 + per);
+    int mine = 0;
+    for (int b = b0; b < b1; ++b) {
+      const int len = seq_len(a, b, p == 0);
+      if (mirrored) lens_s[b] = len;
+      mine += seq_tiles(len);
+    }
+    const int inc = scan(mine, 32);
+    if (lane == 31) wsum[warp] = inc;
+    __syncthreads();
+    const int part = lane < NT / 32 ? wsum[lane] : 0, upto = scan(part, 32);
+    set_deal(__shfl_sync(0xffffffffu, upto, 31), 1);
+    int before = __shfl_sync(0xffffffffu, upto - part, warp) + inc - mine;
+    const int start = deal.first(p);
+    if (p < deal.P && before <= start && start < before + mine) {
+      int b = b0;
+      while (true) {
+        const int n = seq_tiles(mirrored ? lens_s[b] : seq_len(a, b, false));
+        if (start < before + n) break;
+        before += n;
+        ++b;
+      }
+      first_s[0] = b;
+      first_s[1] = before;
+    }
+    __syncthreads();
+    b_first = first_s[0];
+    seq_off = first_s[1];
   }
-  // sequences without a token
-  for (int b = p; b < a.n_seqs; b += gridDim.x)
-    if ((mirrored ? lens_s[b] : seq_len(a, b, false)) == 0)
-      for (int i = threadIdx.x; i < g.Hq * D / 8; i += NT)
-        reinterpret_cast<uint4*>(static_cast<bf16*>(a.out) + (size_t)b * g.Hq * D)[i] = make_uint4(0, 0, 0, 0);
-  __syncthreads();
-  Walk<LG> walk(a, mirrored ? lens_s : nullptr, start, end, *first_b, p < P ? sh64[0] : total);
+  const bool any = p < deal.P;
+  Walk<LG> walk(a, mirrored ? lens_s : nullptr, heads_s, len_reg, any ? deal.first(p) : deal.total,
+                any ? deal.first(p + 1) : deal.total, b_first, any ? seq_off : deal.total);
 
   if (warp == kLoadK || warp == kLoadV) {
     // ------------------------------------------------------------ producers
@@ -396,14 +469,13 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
     int it = 0;
     bool ok = true;
     while (ok && walk.next()) {
-      const Item& t = walk.t;
       const int32_t* row = a.table + (size_t)walk.b * a.table_stride;
-      const int slots = (int)(((long long)t.len + a.pool.ps - 1) >> lg) - t.gap;
+      const int slots = walk.slots(), kvh = walk.kvh();
       for (int j = walk.lo; j < walk.hi; ++j, ++it) {
         const int st = it % kNS;
         const int n = min(spt, slots - j * spt);
         int page = 0;
-        if (lane < n) page = __ldg(row + page_of_slot(t, j * spt + lane));
+        if (lane < n) page = __ldg(row + walk.page_of_slot(j * spt + lane));
         const bool bad = (unsigned)page >= (unsigned)a.pool.n_pages;
         if (bad && !is_v) atomicOr(a.err, kErrPages);
         if (it >= kNS) ok = __all_sync(0xffffffffu, wait_bar(&empty[st], ((it / kNS) & 1) ^ 1, a.err, abort_flag));
@@ -417,7 +489,7 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
               const int pg = __shfl_sync(0xffffffffu, bad ? 0 : page, slot);
               if (slot < n)
                 cp_async16(sPow + st * C::POWB + c * 16,
-                           a.pool.powers + (((size_t)pg * g.Hkv + t.kvh) << (lg + 1)) + (c & ((1 << (lg - 3)) - 1)) * 16);
+                           a.pool.powers + (((size_t)pg * g.Hkv + kvh) << (lg + 1)) + (c & ((1 << (lg - 3)) - 1)) * 16);
             }
             cp_async_mbar_arrive(&full[st]);
             __syncwarp();
@@ -429,7 +501,7 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
           const int key = lane << lg;  // of the tile
           uint8_t* dst = smem + st * C::STAGE + (is_v ? C::HALF : 0) + (key >> 7) * C::GRP + (key & 127) * C::ROWB;
           // a page out of range reads as zeros (its coordinate is past the map's end)
-          const int block = bad ? 2 * g.Hkv * a.pool.n_pages : (page * 2 + (is_v ? 1 : 0)) * g.Hkv + t.kvh;
+          const int block = bad ? 2 * g.Hkv * a.pool.n_pages : (page * 2 + (is_v ? 1 : 0)) * g.Hkv + kvh;
 #pragma unroll
           for (int db = 0; db < C::DBLK; ++db) tma_load_3d(dst + db * C::BOX, &a.pages, db * 64, 0, block, &full[st]);
         }
@@ -450,50 +522,58 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
     const uint64_t p_desc0 = sdesc_rows<128>(smem_u32(sP), 16, 1024);
     constexpr int KSTEPS = D * C::ES / 32;        // 32 bytes of d a step
     constexpr int PSTEPS = 128 * C::ES / 32;      // 32 bytes of keys a step
-    int it = 0, ofw = 0, item = 0;
+    int it = 0, item = 0;
     bool ok = true;
     auto wait_warp = [&](uint64_t* bar, uint32_t parity) {
       if (ok) ok = __all_sync(0xffffffffu, wait_bar(bar, parity, a.err, abort_flag));
       return ok;
     };
-    // the O of the first n items has been read
-    auto wait_ofree = [&](int n) {
-      for (; ok && ofw < n; ++ofw) wait_warp(o_free, ofw & 1);
-    };
-    auto issue_pv = [&](int j, bool first, int item) {
+    // P V of tile j, which waits behind the S of the tile after it
+    int pend = -1, pend_item = 0;
+    bool pend_first = false, pend_last = false;
+    auto issue_pv = [&]() {
+      const int j = pend;
+      pend = -1;
       wait_warp(&v_full[j % kNS], (j / kNS) & 1);
       wait_warp(&p_full[j & 1], (j >> 1) & 1);
-      if (first) wait_ofree(item);
       if (!ok) return;
       if (elect_one()) {
         tc_fence_after();
+        const uint32_t o = tmem + C::OCOL + (pend_item & 1) * C::NPV;
         const uint64_t v_desc = v_desc0 + (uint32_t)((j % kNS) * sdesc_step(C::STAGE));
         const uint64_t p_desc = p_desc0 + (uint32_t)((j % C::NPB) * sdesc_step(C::PBUF));
 #pragma unroll
         for (int z = 0; z < C::SETS; ++z)
 #pragma unroll
           for (int kk = 0; kk < PSTEPS; ++kk)
-            tc_mma_any<F8>(tmem + C::OCOL, v_desc + sdesc_step(z * C::MB * C::GRP + kk * (32 / C::ES) * C::ROWB),
+            tc_mma_any<F8>(o, v_desc + sdesc_step(z * C::MB * C::GRP + kk * (32 / C::ES) * C::ROWB),
                            p_desc + sdesc_step(z * C::PSET + (kk >> 2) * C::PBLK + (kk & 3) * 32), C::IDESC_PV,
-                           first && z == 0 && kk == 0 ? 0u : 1u);
+                           pend_first && z == 0 && kk == 0 ? 0u : 1u);
         tc_commit(&p_free[j & 1]);
         tc_commit(&empty[j % kNS]);
+        if (pend_last) tc_commit(&o_full[pend_item & 1]);
       }
       __syncwarp();
     };
-    constexpr int CPR = D / 8;                    // 16-byte pieces of a query row
+    // An item's queries: piece c of the G x D block; CPR neighbouring lanes hold a row. Those
+    // of the next item are on their way while this one's tiles are multiplied.
+    constexpr int CPR = D / 8;
     constexpr int QV = (GP * CPR + 31) / 32;
-    while (ok && walk.next()) {
-      // the item's queries: piece c of the G x D block; CPR neighbouring lanes hold a row
-      uint4 qr[QV];
-      const bf16* qg = static_cast<const bf16*>(a.q) + (size_t)walk.b * a.q_stride + (size_t)walk.t.kvh * G * D;
+    uint4 qr[QV];
+    auto fetch = [&](int b, int kvh) {
+      const bf16* qg = static_cast<const bf16*>(a.q) + (size_t)b * a.q_stride + (size_t)kvh * G * D;
 #pragma unroll
       for (int i = 0; i < QV; ++i) {
         const int c = lane + 32 * i;
         qr[i] = c < G * CPR ? *reinterpret_cast<const uint4*>(qg + c * 8) : make_uint4(0, 0, 0, 0);
       }
-      // buffer item & 1 was last read by the MMAs of item - 2
-      wait_ofree(item - 1);
+    };
+    bool more = walk.next();
+    if (more) fetch(walk.b, walk.kvh());
+    while (ok && more) {
+      const int lo = walk.lo, hi = walk.hi;
+      // Q's buffer and O's were last in use by item - 2
+      if (item >= 2) wait_warp(&o_free[item & 1], ((item >> 1) - 1) & 1);
       if (!ok) break;
       uint8_t* qs = sQ + (item & 1) * C::QBUF;
 #pragma unroll
@@ -541,8 +621,12 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
       fence_proxy_async_smem();
       __syncwarp();
       if (F8 && lane == 0) mbar_arrive(&q_set[item & 1]);
-      for (int j = walk.lo; j < walk.hi; ++j, ++it) {
+      more = walk.next();
+      if (more) fetch(walk.b, walk.kvh());
+      for (int j = lo; j < hi; ++j, ++it) {
         const int st = it % kNS;
+        // (a P V does not wait behind a tile that is still on its way)
+        if (pend >= 0 && !__all_sync(0xffffffffu, mbar_test(&k_full[st], (it / kNS) & 1))) issue_pv();
         wait_warp(&k_full[st], (it / kNS) & 1);
         if (it >= 2) wait_warp(&s_free[it & 1], ((it >> 1) - 1) & 1);
         if (!ok) break;
@@ -560,26 +644,103 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
           tc_commit(&s_full[it & 1]);
         }
         __syncwarp();
-        // P V of the tile before, behind this tile's S
-        if (j > walk.lo) issue_pv(it - 1, j - 1 == walk.lo, item);
+        if (pend >= 0) issue_pv();
+        pend = it;
+        pend_item = item;
+        pend_first = j == lo;
+        pend_last = j == hi - 1;
       }
-      if (ok) issue_pv(it - 1, walk.hi - 1 == walk.lo, item);
       ++item;
     }
+    if (pend >= 0 && ok) issue_pv();
     if (elect_one()) tc_commit(drain);
     __syncwarp();
     drain_wait(drain, 0, a.err);
     __syncwarp();
+  } else if (warp >= kFinish) {
+    // ------------------------------------------------------------ finishing items
+    const int r = threadIdx.x & 127;  // row of O^T
+    const uint32_t tl = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+    // sequences without a token
+    for (int b = p; b < a.n_seqs; b += gridDim.x)
+      if ((few ? __shfl_sync(0xffffffffu, len_reg, b) : mirrored ? lens_s[b] : seq_len(a, b, false)) == 0)
+        for (int i = r; i < g.Hq * D / 8; i += 128)
+          reinterpret_cast<uint4*>(static_cast<bf16*>(a.out) + (size_t)b * g.Hq * D)[i] = make_uint4(0, 0, 0, 0);
+    int item = 0;
+    bool ok = true;
+    while (ok && walk.next()) {
+      const int x = item & 1;
+      const int f = deal.cta_of(walk.off), last = deal.cta_of(walk.off + walk.tiles - 1);
+      bf16* out = static_cast<bf16*>(a.out) + ((size_t)walk.b * g.Hq + (size_t)walk.kvh() * G) * D;
+      ok = wait_bar(&l_full[x], (item >> 1) & 1, a.err, abort_flag);
+      ok = wait_bar(&o_full[x], (item >> 1) & 1, a.err, abort_flag) && ok;
+      tc_fence_after();
+      float o[GP];
+      {
+        uint32_t part[C::PARTS][cmax(GP, 8)];
+#pragma unroll
+        for (int q = 0; q < C::PARTS; ++q) tmem_ld(tl + C::OCOL + x * C::NPV + (q * C::MB + r / D) * GP, part[q]);
+        tmem_ld_wait();
+#pragma unroll
+        for (int h = 0; h < GP; ++h) {
+          o[h] = __uint_as_float(part[0][h]);
+#pragma unroll
+          for (int q = 1; q < C::PARTS; ++q) o[h] += __uint_as_float(part[q][h]);
+        }
+      }
+      if (D == 64 && r >= 64) {
+#pragma unroll
+        for (int h = 0; h < GP; ++h) upper[h * 64 + r - 64] = o[h];
+      }
+      ok = named_barrier_and(2, 128, ok);
+      if (!ok) break;
+      if (D == 64 && r < 64) {
+#pragma unroll
+        for (int h = 0; h < GP; ++h) o[h] += upper[h * 64 + r];
+      }
+      auto sum_of = [&](int h) {
+        float L = 0.f;
+#pragma unroll
+        for (int u = 0; u < NW; u += 4) {
+          const float4 s4 = *reinterpret_cast<const float4*>(lsum + (x * GP + h) * NW + u);
+          L += (s4.x + s4.y) + (s4.z + s4.w);
+        }
+        return L;
+      };
+      if (f == last) {
+#pragma unroll
+        for (int h = 0; h < GP; ++h)
+          if (r < D && h < G) out[h * D + r] = __float2bfloat16_rn(__fdividef(o[h], sum_of(h)));
+        if (D == 64) named_barrier_sync(2, 128);  // `upper` has been read
+      } else {
+        float* slot = state_slot(a, p, p == f ? 1 : 0, D);
+#pragma unroll
+        for (int h = 0; h < GP; ++h)
+          if (r < D && h < G) __stcg(slot + h * D + r, o[h]);
+        if (r < G) {
+          __stcg(slot + G * D + r, mfin[x * 16 + r]);
+          __stcg(slot + G * D + G + r, sum_of(r));
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&o_free[x]);
+      ++item;
+      if (f != last) {
+        join_item<D>(a, p, f, last, G, out, flag);
+      }
+    }
   } else {
     // ------------------------------------------------------------ softmax
-    const int t = threadIdx.x;            // key of the tile
-    const int y = t >> 7, r = t & 127;    // its group, and its row there (and row r of O^T, threads 0-127)
+    const int t = threadIdx.x;            // key of the tile (and key t + SOFT)
+    const int r = t & 127;                // its row in its group (and row r of O^T, threads 0-127)
     const uint32_t tl = tmem + ((uint32_t)((warp & 3) * 32) << 16);
     int it = 0, item = 0;
     // ok: the softmax threads' common verdict, set at a barrier; local_ok: this thread's waits since
     bool ok = true, local_ok = true;
     while (ok && walk.next()) {
-      const Item& w = walk.t;
+      const Seq& w = walk.q;
+      const bool strm = walk.streaming();
       float m[GP], l[GP];
 #pragma unroll
       for (int h = 0; h < GP; ++h) {
@@ -588,69 +749,86 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
       }
       for (int j = walk.lo; j < walk.hi; ++j, ++it) {
         const int x = it & 1, st = it % kNS;
-        const long long vrow = ((long long)j << LG) + t;
-        const int slot = (int)(vrow >> lg);
-        const long long pos = ((long long)page_of_slot(w, slot) << lg) + (t & (a.pool.ps - 1));
-        const bool see = pos < w.len && (!w.strm || pos < g.S || pos >= w.w0);
-        const unsigned hidden = __ballot_sync(0xffffffffu, !see);
+        const bool first = j == walk.lo;
+        bool see[KP];
+        int ek[KP], ev[KP];
         if (F8) local_ok = wait_bar(&k_full[st], (it / kNS) & 1, a.err, abort_flag) && local_ok;
-        int ek = 0, ev = 0;
-        if constexpr (F8) {
-          const int8_t* pw = sPow + st * C::POWB + ((t >> lg) << (lg + 1)) + (t & (a.pool.ps - 1));
-          ek = see ? pw[0] : 0;
-          ev = see ? pw[a.pool.ps] : 0;
-        }
-        if (hidden) {
-          // V rows that no weight may meet (0 times a NaN is NaN), while S is formed
-          constexpr int CH = C::ROWB / 16;
-          local_ok = wait_bar(&v_full[st], (it / kNS) & 1, a.err, abort_flag) && local_ok;
 #pragma unroll
-          for (int db = 0; db < C::DBLK; ++db) {
-            uint4* v4 = reinterpret_cast<uint4*>(smem + st * C::STAGE + C::HALF + y * C::GRP + db * C::BOX + (warp & 3) * 32 * C::ROWB);
-            for (int c = lane; c < 32 * CH; c += 32)
-              if (hidden >> (c / CH) & 1) v4[c] = make_uint4(0, 0, 0, 0);
+        for (int c = 0; c < KP; ++c) {
+          const int key = t + c * C::SOFT, y = key >> 7;
+          const int slot = (j << (LG - lg)) + (key >> lg);
+          const long long pos = ((long long)walk.page_of_slot(slot) << lg) + (key & (a.pool.ps - 1));
+          see[c] = pos < w.len && (!strm || pos < g.S || pos >= w.w0);
+          const unsigned hidden = __ballot_sync(0xffffffffu, !see[c]);
+          ek[c] = ev[c] = 0;
+          if constexpr (F8) {
+            const int8_t* pw = sPow + st * C::POWB + ((key >> lg) << (lg + 1)) + (key & (a.pool.ps - 1));
+            ek[c] = see[c] ? pw[0] : 0;
+            ev[c] = see[c] ? pw[a.pool.ps] : 0;
+          }
+          if (hidden) {
+            // V rows that no weight may meet (0 times a NaN is NaN), while S is formed
+            constexpr int CH = C::ROWB / 16;
+            local_ok = wait_bar(&v_full[st], (it / kNS) & 1, a.err, abort_flag) && local_ok;
+#pragma unroll
+            for (int db = 0; db < C::DBLK; ++db) {
+              uint4* v4 = reinterpret_cast<uint4*>(smem + st * C::STAGE + C::HALF + y * C::GRP + db * C::BOX +
+                                                   (warp & 3) * 32 * C::ROWB);
+              for (int i = lane; i < 32 * CH; i += 32)
+                if (hidden >> (i / CH) & 1) v4[i] = make_uint4(0, 0, 0, 0);
+            }
           }
         }
-        if (F8 && j == walk.lo)
-          local_ok = wait_bar(&q_set[item & 1], (item >> 1) & 1, a.err, abort_flag) && local_ok;
+        if (F8 && first) local_ok = wait_bar(&q_set[item & 1], (item >> 1) & 1, a.err, abort_flag) && local_ok;
         local_ok = wait_bar(&s_full[x], (it >> 1) & 1, a.err, abort_flag) && local_ok;
         tc_fence_after();
         constexpr int SC = F8 ? cmax(2 * GP, 8) : cmax(GP, 8);  // columns read
-        uint32_t v[SC];
-        tmem_ld(tl + x * C::SBUF + y * C::SN, v);
+        uint32_t v[KP][SC];
+#pragma unroll
+        for (int c = 0; c < KP; ++c) tmem_ld(tl + x * C::SBUF + ((t + c * C::SOFT) >> 7) * C::SN, v[c]);
         tmem_ld_wait();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&s_free[x]);
-        float s[GP];
-        const float kf = pow2i(ek);
+        float s[KP][GP];
 #pragma unroll
-        for (int h = 0; h < GP; ++h) {
-          if constexpr (F8)
-            s[h] = fmaf(__uint_as_float(v[h]) + __uint_as_float(v[GP + h]), kf * qfac[(item & 1) * 16 + h], (float)ev);
-          else
-            s[h] = __uint_as_float(v[h]) * a.scale_log2;
-          if (!see) s[h] = -INFINITY;
+        for (int c = 0; c < KP; ++c) {
+          const float kf = pow2i(ek[c]);
+#pragma unroll
+          for (int h = 0; h < GP; ++h) {
+            if constexpr (F8)
+              s[c][h] = fmaf(__uint_as_float(v[c][h]) + __uint_as_float(v[c][GP + h]), kf * qfac[(item & 1) * 16 + h],
+                             (float)ev[c]);
+            else
+              s[c][h] = __uint_as_float(v[c][h]) * a.scale_log2;
+            if (!see[c]) s[c][h] = -INFINITY;
+          }
         }
         // the running maximum moves only when a key is far above it; all threads agree
-        float wm[GP];
+        auto top_of = [&](int h) { return warp_max(KP == 2 ? fmaxf(s[0][h], s[KP - 1][h]) : s[0][h]); };
         bool below = local_ok;
+        if (!first) {
+          float wm[GP];
 #pragma unroll
-        for (int h = 0; h < GP; ++h) {
-          wm[h] = warp_max(s[h]);
-          below = below && wm[h] <= m[h] + C::kLag;
+          for (int h = 0; h < GP; ++h) wm[h] = top_of(h);
+#pragma unroll
+          for (int h = 0; h < GP; ++h) below = below && wm[h] <= m[h] + C::kLag;
         }
-        const bool first = j == walk.lo;
-        bool resc = false;
-        float alpha[GP];
-        if (!named_barrier_and(1, C::SOFT, below && !first)) {
+        if (first || !named_barrier_and(1, C::SOFT, below)) {
           float* rx = red + x * (GP * NW);
-          if (lane == 0) {
+          {
+            float wm[GP];
 #pragma unroll
-            for (int h = 0; h < GP; ++h) rx[h * NW + warp] = wm[h];
+            for (int h = 0; h < GP; ++h) wm[h] = top_of(h);
+            if (lane == 0) {
+#pragma unroll
+              for (int h = 0; h < GP; ++h) rx[h * NW + warp] = wm[h];
+            }
           }
           ok = named_barrier_and(1, C::SOFT, local_ok);
           if (!ok) break;
+          bool resc = false;
+          float alpha[GP];
 #pragma unroll
           for (int h = 0; h < GP; ++h) {
             float top = -INFINITY;
@@ -669,58 +847,63 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
               resc = true;
             }
           }
+          if (resc && warp < 4) {
+            // row r of O^T, once O += P(it - 1) V has landed
+            local_ok = wait_bar(&p_free[x ^ 1], ((it - 1) >> 1) & 1, a.err, abort_flag) && local_ok;
+            tc_fence_after();
+#pragma unroll
+            for (int q = 0; q < C::MB * C::PARTS; ++q) {
+              const uint32_t col = tl + C::OCOL + (item & 1) * C::NPV + q * GP;
+              uint32_t o[cmax(GP, 8)];
+              tmem_ld(col, o);
+              tmem_ld_wait();
+#pragma unroll
+              for (int h = 0; h < GP; ++h) o[h] = __float_as_uint(__uint_as_float(o[h]) * alpha[h]);
+              tmem_st_n<GP>(col, o);
+            }
+            tmem_st_wait();
+          }
         }
         // the P buffer is free once O += P(it - NPB) V is done
         if (it >= C::NPB)
           local_ok = wait_bar(&p_free[(it - C::NPB) & 1], ((it - C::NPB) >> 1) & 1, a.err, abort_flag) && local_ok;
-        if (resc && y == 0) {
-          // row r of O^T, once O += P(it - 1) V has landed
-          local_ok = wait_bar(&p_free[x ^ 1], ((it - 1) >> 1) & 1, a.err, abort_flag) && local_ok;
-          tc_fence_after();
 #pragma unroll
-          for (int q = 0; q < C::MB * C::PARTS; ++q) {
-            uint32_t o[cmax(GP, 8)];
-            tmem_ld(tl + C::OCOL + q * GP, o);
-            tmem_ld_wait();
+        for (int c = 0; c < KP; ++c) {
+          const int y = (t + c * C::SOFT) >> 7;
+          float pr[GP];
 #pragma unroll
-            for (int h = 0; h < GP; ++h) o[h] = __float_as_uint(__uint_as_float(o[h]) * alpha[h]);
-            tmem_st_n<GP>(tl + C::OCOL + q * GP, o);
-          }
-          tmem_st_wait();
-        }
-        float pr[GP];
+          for (int h = 0; h < GP; ++h) pr[h] = see[c] ? fast_exp2(s[c][h] - m[h] + C::kRaise) : 0.f;
+          // weights of key r of group y -> column r of the K-major [NPV][128 keys] buffer of its set
+          uint8_t* pb = sP + (it % C::NPB) * C::PBUF + (y / C::MB) * C::PSET;
+          const int n0 = (y % C::MB) * GP;
+          if constexpr (F8) {
+            const float un = pow2i(-ev[c]);
 #pragma unroll
-        for (int h = 0; h < GP; ++h) pr[h] = see ? fast_exp2(s[h] - m[h] + C::kRaise) : 0.f;
-        // weights of key r of group y -> column r of the K-major [NPV][128 keys] buffer of its set
-        uint8_t* pb = sP + (it % C::NPB) * C::PBUF + (y / C::MB) * C::PSET;
-        const int n0 = (y % C::MB) * GP;
-        if constexpr (F8) {
-          const float un = pow2i(-ev);
+            for (int h = 0; h < GP; h += 2) {
+              float2 rest = make_float2(pr[h], pr[h + 1]);
+              l[h] = fmaf(rest.x, un, l[h]);
+              l[h + 1] = fmaf(rest.y, un, l[h + 1]);
 #pragma unroll
-          for (int h = 0; h < GP; h += 2) {
-            float2 rest = make_float2(pr[h], pr[h + 1]);
-            l[h] = fmaf(rest.x, un, l[h]);
-            l[h + 1] = fmaf(rest.y, un, l[h + 1]);
-#pragma unroll
-            for (int q = 0; q < C::PARTS; ++q) {
-              const uint32_t c2 = __nv_cvt_float2_to_fp8x2(rest, __NV_SATFINITE, __NV_E5M2);
-              const int n = q * C::MB * GP + n0 + h;
-              pb[n * 128 + (((r >> 4) ^ (n & 7)) << 4) + (r & 15)] = (uint8_t)c2;
-              pb[(n + 1) * 128 + (((r >> 4) ^ ((n + 1) & 7)) << 4) + (r & 15)] = (uint8_t)(c2 >> 8);
-              if (q + 1 < C::PARTS) {
-                const float2 f = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)c2, __NV_E5M2)));
-                rest.x -= f.x;
-                rest.y -= f.y;
+              for (int q = 0; q < C::PARTS; ++q) {
+                const uint32_t c2 = __nv_cvt_float2_to_fp8x2(rest, __NV_SATFINITE, __NV_E5M2);
+                const int n = q * C::MB * GP + n0 + h;
+                pb[n * 128 + (((r >> 4) ^ (n & 7)) << 4) + (r & 15)] = (uint8_t)c2;
+                pb[(n + 1) * 128 + (((r >> 4) ^ ((n + 1) & 7)) << 4) + (r & 15)] = (uint8_t)(c2 >> 8);
+                if (q + 1 < C::PARTS) {
+                  const float2 f = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)c2, __NV_E5M2)));
+                  rest.x -= f.x;
+                  rest.y -= f.y;
+                }
               }
             }
-          }
-        } else {
+          } else {
 #pragma unroll
-          for (int h = 0; h < GP; ++h) {
-            l[h] += pr[h];
-            const int n = n0 + h;
-            *reinterpret_cast<bf16*>(pb + (r >> 6) * C::PBLK + n * 128 + ((((r & 63) >> 3) ^ (n & 7)) << 4) + (r & 7) * 2) =
-                __float2bfloat16_rn(pr[h]);
+            for (int h = 0; h < GP; ++h) {
+              l[h] += pr[h];
+              const int n = n0 + h;
+              *reinterpret_cast<bf16*>(pb + (r >> 6) * C::PBLK + n * 128 + ((((r & 63) >> 3) ^ (n & 7)) << 4) + (r & 7) * 2) =
+                  __float2bfloat16_rn(pr[h]);
+            }
           }
         }
         fence_proxy_async_smem();
@@ -730,70 +913,23 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
       }
       if (!ok) break;
 
-      // ---- the item's state: row r of O^T (threads 0-127), m, and l summed over the keys
+      // ---- the item's sums and maxima, for the warps that finish it
+      if (item >= 2) local_ok = wait_bar(&o_free[item & 1], ((item >> 1) - 1) & 1, a.err, abort_flag) && local_ok;
 #pragma unroll
-      for (int h = 0; h < GP; ++h) {
-        float sum = l[h];
+      for (int o = 16; o >= 1; o >>= 1) {
 #pragma unroll
-        for (int o = 16; o >= 1; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        if (lane == 0) lsum[warp * GP + h] = sum;
+        for (int h = 0; h < GP; ++h) l[h] += __shfl_xor_sync(0xffffffffu, l[h], o);
       }
-      float o[GP];
-      if (y == 0) {
-        const int last = it - 1;
-        local_ok = wait_bar(&p_free[last & 1], (last >> 1) & 1, a.err, abort_flag) && local_ok;
-        tc_fence_after();
+      if (lane == 0) {
 #pragma unroll
-        for (int q = 0; q < C::PARTS; ++q) {
-          uint32_t part[cmax(GP, 8)];
-          tmem_ld(tl + C::OCOL + (q * C::MB + r / D) * GP, part);
-          tmem_ld_wait();
-#pragma unroll
-          for (int h = 0; h < GP; ++h) o[h] = (q == 0 ? 0.f : o[h]) + __uint_as_float(part[h]);
-        }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(o_free);
-        if (D == 64 && r >= 64) {
-#pragma unroll
-          for (int h = 0; h < GP; ++h) upper[h * 64 + r - 64] = o[h];
+        for (int h = 0; h < GP; ++h) {
+          lsum[((item & 1) * GP + h) * NW + warp] = l[h];
+          if (warp == 0) mfin[(item & 1) * 16 + h] = m[h];
         }
       }
-      ok = named_barrier_and(1, C::SOFT, local_ok);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&l_full[item & 1]);
       ++item;
-      if (!ok) break;
-      if (y != 0) continue;
-      if (D == 64 && r < 64) {
-#pragma unroll
-        for (int h = 0; h < GP; ++h) o[h] += upper[h * 64 + r];
-      }
-      float L[GP];
-#pragma unroll
-      for (int h = 0; h < GP; ++h) {
-        L[h] = 0.f;
-#pragma unroll
-        for (int u = 0; u < NW; ++u) L[h] += lsum[u * GP + h];
-      }
-      bf16* out = static_cast<bf16*>(a.out) + ((size_t)walk.b * g.Hq + (size_t)w.kvh * G) * D;
-      const int f = cta_of(walk.off, total, P), lst = cta_of(walk.off + w.tiles - 1, total, P);
-      if (f == lst) {
-#pragma unroll
-        for (int h = 0; h < GP; ++h)
-          if (r < D && h < G) out[h * D + r] = __float2bfloat16_rn(o[h] / L[h]);
-      } else {
-        float* slot = state_slot(a, p, p == f ? 1 : 0, D);
-#pragma unroll
-        for (int h = 0; h < GP; ++h)
-          if (h < G) {
-            if (r < D) __stcg(slot + h * D + r, o[h]);
-            if (r == h) {
-              __stcg(slot + G * D + h, m[h]);
-              __stcg(slot + G * D + G + h, L[h]);
-            }
-          }
-        join_item<D>(a, p, f, lst, G, out, flag);
-      }
-      named_barrier_sync(2, 128);  // `upper` and the flag have been read
     }
   }
 

@@ -9,9 +9,11 @@
 // the exact quotient, and c 2^e is exact in bf16, so that a row read back is the stored
 // one. NaN and infinities become the NaN code and do not count for e.
 //
-// Both kernels only move bytes: a lane holds 16 bytes of bf16 and D / 8 neighbouring lanes
-// one row of one head, the heads of a token next to each other, so that a token's K (or V)
-// is read as one run of Hkv * D * 2 bytes, while each head's row goes to its own page block.
+// Both kernels only move bytes: a lane holds 16 numbers (32 bytes of bf16) and D / 16
+// neighbouring lanes one row of one head, the heads of a token next to each other, so that a
+// token's K (or V) is read as one run of Hkv * D * 2 bytes, while each head's row goes to its
+// own page block. With 8 numbers a lane the 8-bit append was bound by its integer
+// instructions (132 for 8 numbers, 61% of their rate).
 #include <cuda_fp8.h>
 
 #include "common.cuh"
@@ -21,23 +23,26 @@ namespace aoh {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMostRows = 8;  // rows of a block
+constexpr int kMostRows = 16;  // rows of a block
 
 // Where row r of the call lies: its page, or -1, and its place in it.
 struct Place {
   int page, row;
 };
 
-__device__ __forceinline__ int seq_of(const PageRows& rows, int r) {
+// Sequence of row r, for rows r0 .. r0 + 31 in the lanes of a warp (r0 and cu alike): the
+// sequence of r0 by a search that splits in 32 at each step, and a few steps on from there.
+__device__ __forceinline__ int seq_of(const PageRows& rows, int r0, int r) {
   if (rows.cu == nullptr) return r;
-  int lo = 0, hi = rows.n_seqs;  // cu[lo] <= r < cu[hi]
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (__ldg(rows.cu + mid) <= r)
-      lo = mid;
-    else
-      hi = mid;
+  const int lane = threadIdx.x & 31;
+  int lo = 0, n = rows.n_seqs;  // cu[lo] <= r0 < cu[lo + n]
+  while (n > 1) {
+    const int step = (n + 31) / 32, at = lo + (lane + 1) * step;
+    const int past = __popc(__ballot_sync(0xffffffffu, at < lo + n && __ldg(rows.cu + at) <= r0));
+    lo += past * step;
+    n = min(step, n - past * step);
   }
+  while (lo + 1 < rows.n_seqs && __ldg(rows.cu + lo + 1) <= r) ++lo;
   return lo;
 }
 
@@ -61,131 +66,280 @@ __device__ __forceinline__ size_t power_at(const PagePool& pool, const Place& p,
   return ((((size_t)p.page * pool.Hkv + h) * 2 + sel) << pool.lg_ps) + p.row;
 }
 
-// 8 numbers of a row of CPR lanes as e4m3 codes; *e: the row's power.
-template <int CPR>
-__device__ __forceinline__ uint2 encode(const uint4& x, int* e) {
-  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-  uint32_t most = 0;  // bits of the largest finite |x|
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t a = w[i] & 0x7fffu, b = (w[i] >> 16) & 0x7fffu;
-    most = max(most, a < 0x7f80u ? a : 0u);
-    most = max(most, b < 0x7f80u ? b : 0u);
+// 16 bf16 numbers: 32 aligned bytes, but for tensors that are only 16-byte aligned.
+struct Sixteen {
+  uint32_t w[8];
+};
+template <bool WIDE>
+__device__ __forceinline__ Sixteen load16(const void* p) {
+  Sixteen x;
+  if constexpr (WIDE) {
+    asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(x.w[0]), "=r"(x.w[1]), "=r"(x.w[2]), "=r"(x.w[3]), "=r"(x.w[4]), "=r"(x.w[5]), "=r"(x.w[6]),
+                   "=r"(x.w[7])
+                 : "l"(p)
+                 : "memory");
+  } else {
+    const uint4 a = *static_cast<const uint4*>(p), b = *(static_cast<const uint4*>(p) + 1);
+    x = Sixteen{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
   }
+  return x;
+}
+template <bool WIDE>
+__device__ __forceinline__ void store16(void* p, const Sixteen& x) {
+  if constexpr (WIDE) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(x.w[0]), "r"(x.w[1]), "r"(x.w[2]),
+                 "r"(x.w[3]), "r"(x.w[4]), "r"(x.w[5]), "r"(x.w[6]), "r"(x.w[7])
+                 : "memory");
+  } else {
+    *static_cast<uint4*>(p) = make_uint4(x.w[0], x.w[1], x.w[2], x.w[3]);
+    *(static_cast<uint4*>(p) + 1) = make_uint4(x.w[4], x.w[5], x.w[6], x.w[7]);
+  }
+}
+
+// 16 numbers of a row of LPR lanes as e4m3 codes; *e: the row's power. Magnitudes of bf16
+// numbers are ordered as their bits, two to a word; a row with an infinity or NaN is looked
+// at again number by number.
+template <int LPR>
+__device__ __forceinline__ uint4 encode(const Sixteen& x, int* e) {
+  // the row's lanes (another row of the warp may have ended)
+  const unsigned lanes = ((1u << LPR) - 1u) << (threadIdx.x & 31 & ~(LPR - 1));
+  auto row_max = [&](uint32_t two) {
 #pragma unroll
-  for (int o = CPR / 2; o >= 1; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+    for (int o = LPR / 2; o >= 1; o >>= 1) two = __vmaxu2(two, __shfl_xor_sync(lanes, two, o));
+    return max(two & 0xffffu, two >> 16);
+  };
+  uint32_t two = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) two = __vmaxu2(two, x.w[i] & 0x7fff7fffu);
+  uint32_t most = row_max(two);
+  const bool odd = most >= 0x7f80u;
+  if (odd) {
+    two = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t a = x.w[i] & 0x7fff7fffu;
+      two = __vmaxu2(two, a & ~__vcmpgeu2(a, 0x7f807f80u));
+    }
+    most = row_max(two);
+  }
   // most = 1.f * 2^(E - 127): 448 = 1.75 * 2^8
   *e = min(max((int)(most >> 7) - ((most & 0x7fu) <= 0x60u ? 135 : 134), -80), 120);
   const float scale = __uint_as_float((uint32_t)(127 - *e) << 23);
-  uint32_t c[4];
+  uint32_t c[8];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float2 f = bf16x2_to_float2(w[i]);
-    if ((w[i] & 0x7f80u) == 0x7f80u) f.x = __uint_as_float(0x7fffffffu);
-    if ((w[i] & 0x7f800000u) == 0x7f800000u) f.y = __uint_as_float(0x7fffffffu);
-    c[i] = __nv_cvt_float2_to_fp8x2(make_float2(f.x * scale, f.y * scale), __NV_SATFINITE, __NV_E4M3);
+  for (int i = 0; i < 8; ++i) {
+    float2 f = __fmul2_rn(bf16x2_to_float2(x.w[i]), make_float2(scale, scale));
+    if (odd) {  // infinities: NaN
+      if ((x.w[i] & 0x7f80u) == 0x7f80u) f.x = __uint_as_float(0x7fffffffu);
+      if ((x.w[i] & 0x7f800000u) == 0x7f800000u) f.y = __uint_as_float(0x7fffffffu);
+    }
+    c[i] = __nv_cvt_float2_to_fp8x2(f, __NV_SATFINITE, __NV_E4M3);
   }
-  return make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
+  return make_uint4(__byte_perm(c[0], c[1], 0x5410), __byte_perm(c[2], c[3], 0x5410), __byte_perm(c[4], c[5], 0x5410),
+                    __byte_perm(c[6], c[7], 0x5410));
 }
 
-__device__ __forceinline__ uint4 decode(const uint2& c, int e) {
+__device__ __forceinline__ Sixteen decode(const uint4& c, int e) {
   const float scale = __uint_as_float((uint32_t)(127 + e) << 23);
-  uint32_t w[4];
+  const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+  Sixteen x;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t two = (i < 2 ? c.x : c.y) >> (16 * (i & 1));
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t two = w[i / 2] >> (16 * (i & 1));
     const float2 f = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(two & 0xffffu), __NV_E4M3)));
-    w[i] = float2_to_bf16x2(f.x * scale, f.y * scale);
+    const float2 y = __fmul2_rn(f, make_float2(scale, scale));
+    x.w[i] = float2_to_bf16x2(y.x, y.y);
   }
-  return make_uint4(w[0], w[1], w[2], w[3]);
+  return x;
 }
 
-template <int D, bool E4M3>
-__global__ void __launch_bounds__(kThreads) append_kernel(const __grid_constant__ PagedAppendArgs a, int rows_per_block) {
-  constexpr int CPR = D / 8;
+// A block's threads as (row of several at a time, vector of a token, 16 numbers of it): the
+// vectors of a token side by side, up to as many as the block holds, and several tokens where
+// it holds more. Each thread has U rows on their way at once.
+template <int LPR>
+struct Split {
+  static constexpr int U = 4;
+  int ch, vec, sub, vecs, rows;
+  __device__ __forceinline__ explicit Split(int per_row) {
+    vecs = kThreads / LPR;
+    while (vecs >= 2 * per_row) vecs >>= 1;
+    rows = kThreads / LPR / vecs;
+    const int v = threadIdx.x / LPR;
+    ch = threadIdx.x % LPR;
+    sub = v / vecs;
+    vec = v - sub * vecs;
+  }
+};
+
+// What earlier kernels wrote is visible from here on; the next one may start its prologue.
+__device__ __forceinline__ void after_the_last_kernel() {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
+// WIDE: k, v and the strides are multiples of 32 bytes. The first rows are on their way while
+// warp 0 looks up where they go, a chain of three or four loads.
+template <int D, bool E4M3, bool WIDE>
+__global__ void __launch_bounds__(kThreads, 4) append_kernel(const __grid_constant__ PagedAppendArgs a, int rows_per_block) {
+  constexpr int LPR = D / 16, U = Split<LPR>::U;
   __shared__ Place place[kMostRows];
+  __shared__ int8_t power[E4M3 ? 2 * kMaxKvHeads * kMostRows : 1];
   const int r0 = blockIdx.x * rows_per_block, n = min(rows_per_block, a.rows.n_rows - r0);
-  if ((int)threadIdx.x < n) {
-    const int r = r0 + threadIdx.x, b = seq_of(a.rows, r);
+  const int per_row = 2 * a.pool.Hkv;
+  const Split<LPR> t(per_row);
+  after_the_last_kernel();
+  Sixteen x[U];
+  auto load = [&](int vec, int i0) {
+    const bool is_v = vec >= a.pool.Hkv;
+    const long long stride = is_v ? a.v_stride : a.k_stride;
+    const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(is_v ? a.v : a.k) + (r0 + i0) * stride +
+                               (is_v ? vec - a.pool.Hkv : vec) * D + t.ch * 16;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (i0 + u * t.rows < n) x[u] = load16<WIDE>(src + u * t.rows * stride);
+  };
+  auto store = [&](int vec, int i0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * t.rows;  // alike for a row's lanes
+      if (i >= n) continue;
+      const Place p = place[i];
+      if constexpr (E4M3) {
+        int e;
+        const uint4 c = encode<LPR>(x[u], &e);
+        if (t.ch == 0) power[vec * kMostRows + i] = (int8_t)e;
+        if (p.page < 0) continue;
+        *reinterpret_cast<uint4*>(static_cast<uint8_t*>(a.pool.data) + data_row(a.pool, p, vec) * D + t.ch * 16) = c;
+      } else {
+        if (p.page < 0) continue;
+        store16<true>(static_cast<__nv_bfloat16*>(a.pool.data) + data_row(a.pool, p, vec) * D + t.ch * 16, x[u]);
+      }
+    }
+  };
+  int vec = t.vec, i0 = t.sub;
+  if (vec < per_row) load(vec, i0);
+  if (threadIdx.x < 32) {
+    const int r = r0 + min((int)threadIdx.x, n - 1), b = seq_of(a.rows, r0, r);
     const int end = a.rows.cu ? __ldg(a.rows.cu + b + 1) : r + 1;
-    place[threadIdx.x] = place_of(a.pool, a.rows, b, (long long)__ldg(a.lens + b) - (end - r), a.err);
+    if ((int)threadIdx.x < n)
+      place[threadIdx.x] = place_of(a.pool, a.rows, b, (long long)__ldg(a.lens + b) - (end - r), a.err);
   }
   __syncthreads();
-  const int ch = threadIdx.x % CPR, per_row = 2 * a.pool.Hkv;
-  for (int u = threadIdx.x / CPR; u < n * per_row; u += kThreads / CPR) {
-    const int i = u / per_row, vec = u - i * per_row;
-    const bool is_v = vec >= a.pool.Hkv;
-    const int h = is_v ? vec - a.pool.Hkv : vec;
-    const __nv_bfloat16* src =
-        is_v ? static_cast<const __nv_bfloat16*>(a.v) + (r0 + i) * a.v_stride : static_cast<const __nv_bfloat16*>(a.k) + (r0 + i) * a.k_stride;
-    const uint4 x = *reinterpret_cast<const uint4*>(src + h * D + ch * 8);
-    const Place p = place[i];
-    if constexpr (E4M3) {
-      int e;
-      const uint2 c = encode<CPR>(x, &e);
-      if (p.page < 0) continue;
-      *reinterpret_cast<uint2*>(static_cast<uint8_t*>(a.pool.data) + data_row(a.pool, p, vec) * D + ch * 8) = c;
-      if (ch == 0) a.pool.powers[power_at(a.pool, p, vec)] = (int8_t)e;
-    } else {
-      if (p.page < 0) continue;
-      *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.pool.data) + data_row(a.pool, p, vec) * D + ch * 8) = x;
+  while (vec < per_row) {
+    store(vec, i0);
+    i0 += U * t.rows;
+    if (i0 >= n) {
+      i0 = t.sub;
+      vec += t.vecs;
+    }
+    if (vec < per_row) load(vec, i0);
+  }
+  if constexpr (E4M3) {
+    // a head's powers of neighbouring tokens lie side by side: stored by neighbouring lanes
+    __syncthreads();
+    for (int u = threadIdx.x; u < per_row * kMostRows; u += kThreads) {
+      const int v = u / kMostRows, i = u % kMostRows;
+      if (i < n && place[i].page >= 0) a.pool.powers[power_at(a.pool, place[i], v)] = power[u];
     }
   }
+}
+
+template <int D, bool E4M3, bool WIDE>
+__global__ void __launch_bounds__(kThreads, 4) read_kernel(const __grid_constant__ PagedReadArgs a, int rows_per_block) {
+  constexpr int LPR = D / 16, U = Split<LPR>::U;
+  __shared__ Place place[kMostRows];
+  const int r0 = blockIdx.x * rows_per_block, n = min(rows_per_block, a.rows.n_rows - r0);
+  after_the_last_kernel();
+  if (threadIdx.x < 32) {
+    const int r = r0 + min((int)threadIdx.x, n - 1), b = seq_of(a.rows, r0, r);
+    const long long pos = (a.first ? __ldg(a.first + b) : 0) + (long long)(a.rows.cu ? r - __ldg(a.rows.cu + b) : 0);
+    if ((int)threadIdx.x < n) place[threadIdx.x] = place_of(a.pool, a.rows, b, pos, a.err);
+  }
+  __syncthreads();
+  const int per_row = 2 * a.pool.Hkv;
+  const Split<LPR> t(per_row);
+  for (int vec = t.vec; vec < per_row; vec += t.vecs) {
+    const bool is_v = vec >= a.pool.Hkv;
+    __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(is_v ? a.v : a.k) +
+                         ((size_t)r0 * a.pool.Hkv + (is_v ? vec - a.pool.Hkv : vec)) * D + t.ch * 16;
+    for (int i0 = t.sub; i0 < n; i0 += U * t.rows) {
+      Sixteen x[U];  // e4m3: 16 codes in the first four words
+      int e[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int i = i0 + u * t.rows;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) x[u].w[w] = 0;
+        e[u] = 0;
+        if (i >= n) continue;
+        const Place p = place[i];
+        if (p.page < 0) continue;
+        const size_t at = data_row(a.pool, p, vec) * D + t.ch * 16;
+        if constexpr (E4M3) {
+          const uint4 c = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(a.pool.data) + at);
+          x[u].w[0] = c.x;
+          x[u].w[1] = c.y;
+          x[u].w[2] = c.z;
+          x[u].w[3] = c.w;
+          e[u] = a.pool.powers[power_at(a.pool, p, vec)];
+        } else {
+          x[u] = load16<true>(static_cast<const __nv_bfloat16*>(a.pool.data) + at);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int i = i0 + u * t.rows;
+        if (i >= n) continue;
+        if constexpr (E4M3) x[u] = decode(make_uint4(x[u].w[0], x[u].w[1], x[u].w[2], x[u].w[3]), e[u]);
+        store16<WIDE>(dst + (size_t)i * a.pool.Hkv * D, x[u]);
+      }
+    }
+  }
+}
+
+// Rows of a block: the call's rows on four blocks an SM (which run at once), up to
+// kMostRows. The launch overlaps the end of the kernel before it.
+template <class K, class A>
+cudaError_t launch(K kernel, const A& a, int num_sms, cudaStream_t s) {
+  const int n = a.rows.n_rows, even = (n + 4 * num_sms - 1) / (4 * num_sms), per = even < kMostRows ? even : kMostRows;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((n + per - 1) / per));
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, a, per);
+}
+
+bool whole(const void* p, long long elements) {  // of 32 bytes
+  return reinterpret_cast<uintptr_t>(p) % 32 == 0 && elements % 16 == 0;
 }
 
 template <int D, bool E4M3>
-__global__ void __launch_bounds__(kThreads) read_kernel(const __grid_constant__ PagedReadArgs a, int rows_per_block) {
-  constexpr int CPR = D / 8;
-  __shared__ Place place[kMostRows];
-  const int r0 = blockIdx.x * rows_per_block, n = min(rows_per_block, a.rows.n_rows - r0);
-  if ((int)threadIdx.x < n) {
-    const int r = r0 + threadIdx.x, b = seq_of(a.rows, r);
-    const long long pos = (a.first ? __ldg(a.first + b) : 0) + (long long)(a.rows.cu ? r - __ldg(a.rows.cu + b) : 0);
-    place[threadIdx.x] = place_of(a.pool, a.rows, b, pos, a.err);
-  }
-  __syncthreads();
-  const int ch = threadIdx.x % CPR, per_row = 2 * a.pool.Hkv;
-  for (int u = threadIdx.x / CPR; u < n * per_row; u += kThreads / CPR) {
-    const int i = u / per_row, vec = u - i * per_row;
-    const bool is_v = vec >= a.pool.Hkv;
-    const int h = is_v ? vec - a.pool.Hkv : vec;
-    const Place p = place[i];
-    uint4 x = make_uint4(0, 0, 0, 0);
-    if (p.page >= 0) {
-      const size_t at = data_row(a.pool, p, vec) * D + ch * 8;
-      if constexpr (E4M3)
-        x = decode(*reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(a.pool.data) + at),
-                   a.pool.powers[power_at(a.pool, p, vec)]);
-      else
-        x = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.pool.data) + at);
-    }
-    *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(is_v ? a.v : a.k) + ((size_t)(r0 + i) * a.pool.Hkv + h) * D + ch * 8) = x;
-  }
+cudaError_t append(const PagedAppendArgs& a, int num_sms, cudaStream_t s) {
+  return whole(a.k, a.k_stride) && whole(a.v, a.v_stride) ? launch(append_kernel<D, E4M3, true>, a, num_sms, s)
+                                                          : launch(append_kernel<D, E4M3, false>, a, num_sms, s);
 }
-
-// Rows of a block: one while the blocks of eight would leave SMs idle.
-int rows_per_block(int n_rows, int num_sms) { return n_rows >= 4 * kMostRows * num_sms ? kMostRows : 1; }
+template <int D, bool E4M3>
+cudaError_t read(const PagedReadArgs& a, int num_sms, cudaStream_t s) {
+  return whole(a.k, 0) && whole(a.v, 0) ? launch(read_kernel<D, E4M3, true>, a, num_sms, s)
+                                        : launch(read_kernel<D, E4M3, false>, a, num_sms, s);
+}
 
 }  // namespace
 
 cudaError_t launch_paged_append(const PagedAppendArgs& a, int num_sms, cudaStream_t s) {
-  const int per = rows_per_block(a.rows.n_rows, num_sms);
-  const int grid = (a.rows.n_rows + per - 1) / per;
-  if (a.pool.D == 128)
-    (a.pool.form ? append_kernel<128, true> : append_kernel<128, false>)<<<grid, kThreads, 0, s>>>(a, per);
-  else
-    (a.pool.form ? append_kernel<64, true> : append_kernel<64, false>)<<<grid, kThreads, 0, s>>>(a, per);
-  return cudaGetLastError();
+  if (a.pool.D == 128) return a.pool.form ? append<128, true>(a, num_sms, s) : append<128, false>(a, num_sms, s);
+  return a.pool.form ? append<64, true>(a, num_sms, s) : append<64, false>(a, num_sms, s);
 }
 
 cudaError_t launch_paged_read(const PagedReadArgs& a, int num_sms, cudaStream_t s) {
-  const int per = rows_per_block(a.rows.n_rows, num_sms);
-  const int grid = (a.rows.n_rows + per - 1) / per;
-  if (a.pool.D == 128)
-    (a.pool.form ? read_kernel<128, true> : read_kernel<128, false>)<<<grid, kThreads, 0, s>>>(a, per);
-  else
-    (a.pool.form ? read_kernel<64, true> : read_kernel<64, false>)<<<grid, kThreads, 0, s>>>(a, per);
-  return cudaGetLastError();
+  if (a.pool.D == 128) return a.pool.form ? read<128, true>(a, num_sms, s) : read<128, false>(a, num_sms, s);
+  return a.pool.form ? read<64, true>(a, num_sms, s) : read<64, false>(a, num_sms, s);
 }
 
 }  // namespace aoh

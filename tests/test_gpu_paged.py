@@ -241,6 +241,24 @@ def test_append_and_read_one_row_each(form):
 
 
 @pytest.mark.parametrize("form", ["bf16", "e4m3"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_rows_aligned_to_16_bytes_alone(form, d):
+    lens, hkv, page = [50, 3], 3, 16
+    p = Pages(lens, hkv, hkv, d, page, form, [0] * hkv)
+    n, width = sum(lens), hkv * d
+    raw = randn((2 * n + 1, width + 8), 1)
+    rows = [raw.as_strided((n, hkv, d), (width + 8, d, 1), 8 + i * n * (width + 8)) for i in range(2)]
+    assert rows[0].data_ptr() % 32 == 16
+    cu = ints(sums(lens))
+    p.cache.append(rows[0], rows[1], ints(lens), p.table, cu_rows=cu)
+    outs = [torch.empty(n * width + 8, dtype=torch.bfloat16, device="cuda")[8:].view(n, hkv, d) for _ in range(2)]
+    p.cache.read(p.table, cu, *outs)
+    p.cache.check()
+    for out, x in zip(outs, rows):
+        assert np.array_equal(f64(out), p.held(f64(x)))
+
+
+@pytest.mark.parametrize("form", ["bf16", "e4m3"])
 def test_append_many_rows(form):
     """Enough rows for blocks of several."""
     lens, hkv, d, page = [3001, 1, 2500], 2, 64, 32

@@ -375,51 +375,8 @@ def aoh_paged_init(cfg, labels, pool):
     return h
 
 
-def _rows(t, name, heads, d):
-    """Pointer, token stride and rows of a [rows, heads, d] bf16 CUDA tensor
-    whose rows are dense and may lie any distance apart (a slice of a fused
-    projection's output)."""
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != d:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}; expected [rows, {heads}, {d}]")
-    if not t.is_cuda or t.dtype != torch.bfloat16:
-        raise ValueError(f"{name} must be a torch.bfloat16 CUDA tensor")
-    n, stride = t.shape[0], t.stride()
-    if n <= 1:
-        stride = (heads * d,) + stride[1:]
-    if stride[2] != 1 or (heads > 1 and stride[1] != d) or stride[0] < heads * d:
-        raise ValueError(f"{name} must have dense rows of {heads} x {d}, not strides {t.stride()}")
-    return t.data_ptr(), stride[0], n
-
-
 def _lens_arr(lens):
     return (ctypes.c_int32 * max(1, len(lens)))(*lens)
-
-
-# The argument checks of the aoh_paged_* calls that need sizes are PagedCache's.
-
-def aoh_paged_prefill(cache, q, k, v, q_lens, k_lens, out, stream=None):
-    """q, k, v, out: (pointer, token stride) pairs but for out, a pointer;
-    q_lens, k_lens (or None): host lists."""
-    _check(load().aoh_paged_prefill(cache, q[0], k[0], v[0], q[1], k[1], v[1], _lens_arr(q_lens),
-                                    None if k_lens is None else _lens_arr(k_lens), len(q_lens), out,
-                                    _stream_ptr(stream)))
-
-
-def aoh_paged_append(cache, k, v, cu_rows, lens, n_seqs, n_rows, table, table_stride, stream=None):
-    """k, v: (pointer, token stride) pairs; cu_rows (or None), lens, table: pointers."""
-    _check(load().aoh_paged_append(cache, k[0], v[0], k[1], v[1], cu_rows, lens, n_seqs, n_rows, table, table_stride,
-                                   _stream_ptr(stream)))
-
-
-def aoh_paged_read(cache, cu_rows, first, n_seqs, n_rows, table, table_stride, k_out, v_out, stream=None):
-    """Pointers throughout; cu_rows and first may be None."""
-    _check(load().aoh_paged_read(cache, cu_rows, first, n_seqs, n_rows, table, table_stride, k_out, v_out,
-                                 _stream_ptr(stream)))
-
-
-def aoh_paged_decode(cache, q, lens, n_seqs, table, table_stride, out, stream=None):
-    """q: (pointer, token stride); lens, table, out: pointers."""
-    _check(load().aoh_paged_decode(cache, q[0], q[1], lens, n_seqs, table, table_stride, out, _stream_ptr(stream)))
 
 
 def aoh_paged_check(cache, stream=None):
@@ -428,6 +385,38 @@ def aoh_paged_check(cache, stream=None):
 
 def aoh_paged_destroy(cache):
     load().aoh_paged_destroy(cache)
+
+
+# The other aoh_paged_* calls take sizes and strides, which PagedCache reads off its
+# tensors, checks and passes on. An attribute of a tensor costs 0.05 - 0.11 us on a
+# Grace core and the 13 arguments of a call 1 us: an append of four tensors through
+# layers of checks took 7.2 us where the library's own part is 1.8.
+
+def _rows(t, name, heads, d):
+    """Pointer, token stride and rows of a [rows, heads, d] bf16 CUDA tensor
+    whose rows are dense and may lie any distance apart (a slice of a fused
+    projection's output)."""
+    shape = t.shape
+    if len(shape) != 3 or shape[1] != heads or shape[2] != d:
+        raise ValueError(f"{name} has shape {tuple(shape)}; expected [rows, {heads}, {d}]")
+    if t.dtype is not torch.bfloat16 or not t.is_cuda:
+        raise ValueError(f"{name} must be a torch.bfloat16 CUDA tensor")
+    n = shape[0]
+    s0, s1, s2 = t.stride()
+    if n <= 1:
+        s0 = heads * d
+    if s2 != 1 or (s1 != d and heads > 1) or s0 < heads * d:
+        raise ValueError(f"{name} must have dense rows of {heads} x {d}, not strides {t.stride()}")
+    return t.data_ptr(), s0, n
+
+
+def _dense(t, name, shape, dtype):
+    """Pointer of a contiguous CUDA tensor of that shape."""
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}; expected {list(shape)}")
+    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} CUDA tensor")
+    return t.data_ptr()
 
 
 # ------------------------------------------------------------- convenience
@@ -548,67 +537,75 @@ class PagedCache:
         self.n_q_heads, self.n_kv_heads, self.d_head = n_q_heads, n_kv_heads, d_head
         self.sink, self.window = sink, window
 
-    def _ints(self, t, name, n):
-        if t.dim() != 1 or t.shape[0] != n:
-            raise ValueError(f"{name} has shape {tuple(t.shape)}; expected [{n}]")
-        return _ptr(t, name, torch.int32)
-
     def _table(self, table):
-        if table.dim() != 2 or table.shape[0] > self.max_seqs:
-            raise ValueError(f"table has shape {tuple(table.shape)}; expected [sequences <= {self.max_seqs}, pages]")
-        return _ptr(table, "table", torch.int32), table.shape[0], table.shape[1]
-
-    def _out(self, t, name, rows, heads):
-        if tuple(t.shape) != (rows, heads, self.d_head):
-            raise ValueError(f"{name} has shape {tuple(t.shape)}; expected [{rows}, {heads}, {self.d_head}]")
-        return _ptr(t, name)
+        shape = table.shape
+        if len(shape) != 2 or shape[0] > self.max_seqs:
+            raise ValueError(f"table has shape {tuple(shape)}; expected [sequences <= {self.max_seqs}, pages]")
+        return _dense(table, "table", shape, torch.int32), shape[0], shape[1]
 
     def prefill(self, q, k, v, q_lens, out, k_lens=None, stream=None):
         """Causal attention over packed prompts: q, out [rows, Hq, d], k, v [keys, Hkv, d]
         (q, k and v with any distance between tokens); q_lens, k_lens host
         lists. Sequence b's rows are the last q_lens[b] of its k_lens[b] (default:
         q_lens[b]) positions. The pages are not touched."""
-        qp, kp = _rows(q, "q", self.n_q_heads, self.d_head), _rows(k, "k", self.n_kv_heads, self.d_head)
-        vp = _rows(v, "v", self.n_kv_heads, self.d_head)
-        op = self._out(out, "out", qp[2], self.n_q_heads)
-        if len(q_lens) > self.max_seqs or (k_lens is not None and len(k_lens) != len(q_lens)):
+        hq, hkv, d = self.n_q_heads, self.n_kv_heads, self.d_head
+        qp, qs, nq = _rows(q, "q", hq, d)
+        kp, ks, nk = _rows(k, "k", hkv, d)
+        vp, vs, nv = _rows(v, "v", hkv, d)
+        op = _dense(out, "out", (nq, hq, d), torch.bfloat16)
+        n = len(q_lens)
+        if n > self.max_seqs or (k_lens is not None and len(k_lens) != n):
             raise ValueError(f"q_lens and k_lens hold one length a sequence, at most {self.max_seqs}")
-        if sum(q_lens) != qp[2] or sum(q_lens if k_lens is None else k_lens) != kp[2] or kp[2] != vp[2]:
-            raise ValueError(f"q, k and v hold {qp[2]}, {kp[2]} and {vp[2]} rows; q_lens and k_lens say otherwise")
-        aoh_paged_prefill(self.handle, qp, kp, vp, q_lens, k_lens, op, stream)
+        if sum(q_lens) != nq or sum(q_lens if k_lens is None else k_lens) != nk or nk != nv:
+            raise ValueError(f"q, k and v hold {nq}, {nk} and {nv} rows; q_lens and k_lens say otherwise")
+        st = _lib.aoh_paged_prefill(self.handle, qp, kp, vp, qs, ks, vs, _lens_arr(q_lens),
+                                    None if k_lens is None else _lens_arr(k_lens), n, op, _stream_ptr(stream))
+        if st:
+            _check(st)
 
     def append(self, k, v, lens, table, cu_rows=None, stream=None):
         """Write k, v [rows, Hkv, d] (any distance between tokens): rows cu_rows[b] ..
         cu_rows[b + 1] - 1 (without cu_rows: row b) become the last of sequence b's
         lens[b] tokens."""
-        kp, vp = _rows(k, "k", self.n_kv_heads, self.d_head), _rows(v, "v", self.n_kv_heads, self.d_head)
+        kp, ks, rows = _rows(k, "k", self.n_kv_heads, self.d_head)
+        vp, vs, rows_v = _rows(v, "v", self.n_kv_heads, self.d_head)
         tp, n, width = self._table(table)
-        if kp[2] != vp[2] or (cu_rows is None and kp[2] != n):
-            raise ValueError(f"k and v hold {kp[2]} and {vp[2]} rows for {n} sequences")
-        aoh_paged_append(self.handle, kp, vp, None if cu_rows is None else self._ints(cu_rows, "cu_rows", n + 1),
-                         self._ints(lens, "lens", n), n, kp[2], tp, width, stream)
+        if rows != rows_v or (cu_rows is None and rows != n):
+            raise ValueError(f"k and v hold {rows} and {rows_v} rows for {n} sequences")
+        cp = None if cu_rows is None else _dense(cu_rows, "cu_rows", (n + 1,), torch.int32)
+        st = _lib.aoh_paged_append(self.handle, kp, vp, ks, vs, cp, _dense(lens, "lens", (n,), torch.int32), n, rows, tp,
+                                   width, _stream_ptr(stream))
+        if st:
+            _check(st)
 
     def read(self, table, cu_rows, k_out, v_out, first=None, stream=None):
         """Positions first[b] (default 0) on of every sequence as rows cu_rows[b] ..
         cu_rows[b + 1] - 1 (None: row b alone) of k_out, v_out [rows, Hkv, d]."""
         tp, n, width = self._table(table)
         rows = k_out.shape[0]
-        kp, vp = self._out(k_out, "k_out", rows, self.n_kv_heads), self._out(v_out, "v_out", rows, self.n_kv_heads)
+        shape = (rows, self.n_kv_heads, self.d_head)
+        kp, vp = _dense(k_out, "k_out", shape, torch.bfloat16), _dense(v_out, "v_out", shape, torch.bfloat16)
         if cu_rows is None and rows != n:
             raise ValueError(f"k_out and v_out hold {rows} rows for {n} sequences")
-        aoh_paged_read(self.handle, None if cu_rows is None else self._ints(cu_rows, "cu_rows", n + 1),
-                       None if first is None else self._ints(first, "first", n), n, rows, tp, width, kp, vp, stream)
+        cp = None if cu_rows is None else _dense(cu_rows, "cu_rows", (n + 1,), torch.int32)
+        fp = None if first is None else _dense(first, "first", (n,), torch.int32)
+        st = _lib.aoh_paged_read(self.handle, cp, fp, n, rows, tp, width, kp, vp, _stream_ptr(stream))
+        if st:
+            _check(st)
 
     def decode(self, q, lens, table, out, stream=None):
         """Attention of one new token of every sequence, q, out [sequences, Hq, d] (q
         with any distance between tokens), over the sequence's lens[b] cached
         positions, the token's own among them (append it first)."""
-        qp = _rows(q, "q", self.n_q_heads, self.d_head)
+        qp, qs, rows = _rows(q, "q", self.n_q_heads, self.d_head)
         tp, n, width = self._table(table)
-        if qp[2] != n:
-            raise ValueError(f"q holds {qp[2]} rows for {n} sequences")
-        aoh_paged_decode(self.handle, qp, self._ints(lens, "lens", n), n, tp, width,
-                         self._out(out, "out", n, self.n_q_heads), stream)
+        if rows != n:
+            raise ValueError(f"q holds {rows} rows for {n} sequences")
+        st = _lib.aoh_paged_decode(self.handle, qp, qs, _dense(lens, "lens", (n,), torch.int32), n, tp, width,
+                                   _dense(out, "out", (n, self.n_q_heads, self.d_head), torch.bfloat16),
+                                   _stream_ptr(stream))
+        if st:
+            _check(st)
 
     def check(self, stream=None):
         """Synchronise and raise if a kernel reported an error."""

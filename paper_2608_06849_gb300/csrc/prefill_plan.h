@@ -46,7 +46,8 @@ std::vector<uint64_t> prefill_items(const CacheGeom& g, int B, Rows rows_of, Cos
   }
   std::stable_sort(entries.begin(), entries.end(), [](const Entry& x, const Entry& y) { return x.cost > y.cost; });
   std::vector<uint64_t> items;
-  const size_t most = entries.size() * (size_t)(g.Hq / 2 + g.Hkv);
+  size_t most = 0;
+  for (const Entry& e : entries) most += (size_t)(e.streaming ? g.n_s : g.n_r) * (e.two_heads ? g.G / 2 : 1);
   items.reserve(most);
   costs->reserve(most);
   for (const Entry& e : entries)

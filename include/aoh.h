@@ -535,13 +535,15 @@ aoh_status aoh_paged_read(aoh_paged* cache, const int32_t* cu_rows, const int32_
  * Attention of one query token of every sequence, at position lens[b] - 1, over its
  * lens[b] cached positions (a streaming head: the sinks and the window among them).
  * lens[b] = 0 gives zeros.
- *   q     rows of [n_q_heads][d_head], q_stride elements apart
- *   lens  device [n_seqs];  table  device [n_seqs][table_stride]
- *   out   [n_seqs][n_q_heads][d_head]
+ *   q        rows of [n_q_heads][d_head], q_stride elements apart
+ *   lens     device [n_seqs];  table  device [n_seqs][table_stride]
+ *   max_len  the host's upper bound of lens, or 0: what the table holds. It decides how the
+ *            work is split; with a bound that is too low the outputs are still right.
+ *   out      [n_seqs][n_q_heads][d_head]
  * Errors: INVALID, CUDA.
  */
 aoh_status aoh_paged_decode(aoh_paged* cache, const void* q, int64_t q_stride, const int32_t* lens, int32_t n_seqs,
-                            const int32_t* table, int32_t table_stride, void* out, void* stream);
+                            int32_t max_len, const int32_t* table, int32_t table_stride, void* out, void* stream);
 
 /*
  * Synchronise `stream` and read the device error word of the handle's calls: AOH_OK,

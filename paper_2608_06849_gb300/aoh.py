@@ -121,7 +121,7 @@ def load():
         "aoh_paged_prefill": (i32, [P, P, P, P, i64, i64, i64, i32p, i32p, i32, P, P]),
         "aoh_paged_append": (i32, [P, P, P, i64, i64, P, P, i32, i32, P, i32, P]),
         "aoh_paged_read": (i32, [P, P, P, i32, i32, P, i32, P, P, P]),
-        "aoh_paged_decode": (i32, [P, P, i64, P, i32, P, i32, P, P]),
+        "aoh_paged_decode": (i32, [P, P, i64, P, i32, i32, P, i32, P, P]),
         "aoh_paged_check": (i32, [P, P]),
         "aoh_paged_destroy": (None, [P]),
     }
@@ -533,9 +533,14 @@ class PagedCache:
         self.nbytes = aoh_paged_bytes(self.cfg)
         self.pool = torch.empty(self.nbytes, dtype=torch.uint8, device=device or "cuda") if pool is None else pool
         self.handle = aoh_paged_init(self.cfg, self.labels, self.pool)
+        self.device = self.pool.device.index
         self.n_pages, self.page_size, self.form, self.max_seqs = n_pages, page_size, form, max_seqs
         self.n_q_heads, self.n_kv_heads, self.d_head = n_q_heads, n_kv_heads, d_head
         self.sink, self.window = sink, window
+
+    def _stream(self, stream):
+        """As _stream_ptr, of the pool's device (which has to be the current one)."""
+        return torch._C._cuda_getCurrentRawStream(self.device) if stream is None else stream.cuda_stream
 
     def _table(self, table):
         shape = table.shape
@@ -559,7 +564,7 @@ class PagedCache:
         if sum(q_lens) != nq or sum(q_lens if k_lens is None else k_lens) != nk or nk != nv:
             raise ValueError(f"q, k and v hold {nq}, {nk} and {nv} rows; q_lens and k_lens say otherwise")
         st = _lib.aoh_paged_prefill(self.handle, qp, kp, vp, qs, ks, vs, _lens_arr(q_lens),
-                                    None if k_lens is None else _lens_arr(k_lens), n, op, _stream_ptr(stream))
+                                    None if k_lens is None else _lens_arr(k_lens), n, op, self._stream(stream))
         if st:
             _check(st)
 
@@ -574,7 +579,7 @@ class PagedCache:
             raise ValueError(f"k and v hold {rows} and {rows_v} rows for {n} sequences")
         cp = None if cu_rows is None else _dense(cu_rows, "cu_rows", (n + 1,), torch.int32)
         st = _lib.aoh_paged_append(self.handle, kp, vp, ks, vs, cp, _dense(lens, "lens", (n,), torch.int32), n, rows, tp,
-                                   width, _stream_ptr(stream))
+                                   width, self._stream(stream))
         if st:
             _check(st)
 
@@ -589,21 +594,23 @@ class PagedCache:
             raise ValueError(f"k_out and v_out hold {rows} rows for {n} sequences")
         cp = None if cu_rows is None else _dense(cu_rows, "cu_rows", (n + 1,), torch.int32)
         fp = None if first is None else _dense(first, "first", (n,), torch.int32)
-        st = _lib.aoh_paged_read(self.handle, cp, fp, n, rows, tp, width, kp, vp, _stream_ptr(stream))
+        st = _lib.aoh_paged_read(self.handle, cp, fp, n, rows, tp, width, kp, vp, self._stream(stream))
         if st:
             _check(st)
 
-    def decode(self, q, lens, table, out, stream=None):
+    def decode(self, q, lens, table, out, max_len=0, stream=None):
         """Attention of one new token of every sequence, q, out [sequences, Hq, d] (q
         with any distance between tokens), over the sequence's lens[b] cached
-        positions, the token's own among them (append it first)."""
+        positions, the token's own among them (append it first). max_len: the
+        host's bound of the lengths (0: what the table holds), by which the work is
+        split; right at any value, fastest at a close one."""
         qp, qs, rows = _rows(q, "q", self.n_q_heads, self.d_head)
         tp, n, width = self._table(table)
         if rows != n:
             raise ValueError(f"q holds {rows} rows for {n} sequences")
-        st = _lib.aoh_paged_decode(self.handle, qp, qs, _dense(lens, "lens", (n,), torch.int32), n, tp, width,
-                                   _dense(out, "out", (n, self.n_q_heads, self.d_head), torch.bfloat16),
-                                   _stream_ptr(stream))
+        st = _lib.aoh_paged_decode(self.handle, qp, qs, _dense(lens, "lens", (n,), torch.int32), n, max_len, tp,
+                                   width, _dense(out, "out", (n, self.n_q_heads, self.d_head), torch.bfloat16),
+                                   self._stream(stream))
         if st:
             _check(st)
 

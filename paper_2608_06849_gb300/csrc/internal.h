@@ -233,6 +233,7 @@ struct PagedDecodeArgs {
   const int32_t* lens;
   const int32_t* table;
   int table_stride, n_seqs;
+  int max_len;         // the host's bound of the lengths, for the choice of the split alone
   float* states;       // [CTAs][4] states of shared items
   uint32_t* counters;  // [CTAs][3] arrivals: groups of its first and last item, groups of its last
   uint32_t* err;

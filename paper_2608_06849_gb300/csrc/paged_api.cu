@@ -260,7 +260,7 @@ aoh_status aoh_paged_read(aoh_paged* cache, const int32_t* cu_rows, const int32_
 }
 
 aoh_status aoh_paged_decode(aoh_paged* cache, const void* q, int64_t q_stride, const int32_t* lens, int32_t n_seqs,
-                            const int32_t* table, int32_t table_stride, void* out, void* stream) {
+                            int32_t max_len, const int32_t* table, int32_t table_stride, void* out, void* stream) {
   aoh_status st = check_handle(cache);
   if (st == AOH_OK) st = check_seqs(cache, n_seqs);
   if (st != AOH_OK || n_seqs == 0) return st;
@@ -270,6 +270,7 @@ aoh_status aoh_paged_decode(aoh_paged* cache, const void* q, int64_t q_stride, c
   if (st == AOH_OK) st = check_table(cache, table, table_stride);
   if (st != AOH_OK) return st;
   if (!lens) return fail(AOH_ERR_INVALID, "lens must not be NULL");
+  if (max_len < 0) return fail(AOH_ERR_INVALID, "max_len must be >= 0");
   // the split counts tiles of at least 128 keys in 32 bits
   if ((int64_t)n_seqs * c.n_kv_heads * (((int64_t)table_stride * c.page_size + 127) / 128) > INT32_MAX)
     return fail(AOH_ERR_INVALID, "%d sequences of up to %lld tokens are too many for one call", n_seqs,
@@ -287,6 +288,8 @@ aoh_status aoh_paged_decode(aoh_paged* cache, const void* q, int64_t q_stride, c
   a.table = table;
   a.table_stride = table_stride;
   a.n_seqs = n_seqs;
+  const int32_t holds = table_stride * c.page_size;
+  a.max_len = max_len > 0 && max_len < holds ? max_len : holds;
   a.err = cache->d_err;
   a.scale_log2 = (float)(1.4426950408889634 / sqrt((double)c.d_head));
   const cudaError_t e = launch_paged_decode(a, cache->num_sms, (cudaStream_t)stream);

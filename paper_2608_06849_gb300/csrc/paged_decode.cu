@@ -4,10 +4,10 @@
 
 namespace aoh {
 
-cudaError_t launch_paged_decode_f8_128(const PagedDecodeArgs& a, int num_sms, cudaStream_t s);
-cudaError_t launch_paged_decode_f8_64(const PagedDecodeArgs& a, int num_sms, cudaStream_t s);
-cudaError_t launch_paged_decode_bf16_128(const PagedDecodeArgs& a, int num_sms, cudaStream_t s);
-cudaError_t launch_paged_decode_bf16_64(const PagedDecodeArgs& a, int num_sms, cudaStream_t s);
+cudaError_t launch_paged_decode_f8_128(const PagedDecodeArgs& a, int num_sms, int cluster, cudaStream_t s);
+cudaError_t launch_paged_decode_f8_64(const PagedDecodeArgs& a, int num_sms, int cluster, cudaStream_t s);
+cudaError_t launch_paged_decode_bf16_128(const PagedDecodeArgs& a, int num_sms, int cluster, cudaStream_t s);
+cudaError_t launch_paged_decode_bf16_64(const PagedDecodeArgs& a, int num_sms, int cluster, cudaStream_t s);
 
 // 3D map over a pool as [page, K or V, head][row][D], box one block of up to 128 bytes a row,
 // swizzled over that width.
@@ -28,10 +28,40 @@ bool make_pages_map(CUtensorMap* map, const PagePool& p) {
 
 size_t paged_state_floats(int num_sms, int D) { return (size_t)num_sms * 4 * pdec::state_floats(D); }
 
+// CTAs of a cluster an item, or 0: all SMs in equal runs, by what they take in tenths of a
+// microsecond beyond what both do, with sequences of at most a.max_len tokens: a tile of 64 KB
+// 0.95 us on an SM whose neighbours leave it the bandwidth, 1.47 us on all SMs at once; joining
+// an item's states through global memory 3.3 us, 5.5 in two levels. Measured, us a step in
+// equal runs / on clusters (8-bit, 32/8 heads of 128): 1 x 4096 9.4 / 6.0, 4 x 8192 15.7 /
+// 11.5, 8 streaming heads (S = 64, W = 2048) of 8 x 20000 13.1 / 8.9; bf16, 28/4 heads, half
+// streaming, 1 x 4096 9.8 / 6.0.
+static int cluster_size(const PagedDecodeArgs& a, int num_sms) {
+  const CacheGeom& g = a.geom;
+  if (g.G > pdec::kClusterHeads) return 0;
+  const long long items = (long long)a.n_seqs * g.Hkv;
+  const long long keys = 32768 / (g.D * (a.pool.form ? 1 : 2)), ring = (long long)g.S + g.W + 2 * a.pool.ps;
+  const long long tr = (a.max_len + keys - 1) / keys, ts = ((a.max_len < ring ? a.max_len : ring) + keys - 1) / keys;
+  const long long widest = g.n_r > 0 ? tr : ts, total = a.n_seqs * (g.n_r * tr + g.n_s * ts);
+  const bool two_levels = widest * num_sms > pdec::kGroup * (total > num_sms ? total : num_sms);
+  double best = 14.7 * (double)((total + num_sms - 1) / num_sms) + (two_levels ? 55 : 33);
+  int pick = 0;
+  for (int c = pdec::kClusterMost; c >= 2; c /= 2) {
+    if (items > num_sms / c) continue;
+    const double share = 14.7 * (double)(items * c) / num_sms, tile = share > 9.5 ? share : 9.5;
+    const double cost = tile * (double)((widest + c - 1) / c);
+    if (cost < best && items <= decode_tc_max_clusters(c)) {
+      best = cost;
+      pick = c;
+    }
+  }
+  return pick;
+}
+
 cudaError_t launch_paged_decode(const PagedDecodeArgs& a, int num_sms, cudaStream_t s) {
+  const int c = cluster_size(a, num_sms);
   if (a.pool.D == 128)
-    return a.pool.form ? launch_paged_decode_f8_128(a, num_sms, s) : launch_paged_decode_bf16_128(a, num_sms, s);
-  return a.pool.form ? launch_paged_decode_f8_64(a, num_sms, s) : launch_paged_decode_bf16_64(a, num_sms, s);
+    return a.pool.form ? launch_paged_decode_f8_128(a, num_sms, c, s) : launch_paged_decode_bf16_128(a, num_sms, c, s);
+  return a.pool.form ? launch_paged_decode_f8_64(a, num_sms, c, s) : launch_paged_decode_bf16_64(a, num_sms, c, s);
 }
 
 }  // namespace aoh

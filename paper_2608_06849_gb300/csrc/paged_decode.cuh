@@ -24,6 +24,10 @@
 // last to arrive adds them up (groups of 16 first). A streaming head's tiles are the pages
 // of its sinks and then those of its window.
 //
+// Short steps of few items run on whole clusters instead (CL): a cluster an item, whose CTAs
+// add up their states through distributed shared memory, each finishing D / C values of every
+// head.
+//
 // Warps: 4 or 8 of softmax (a thread one or two keys of the tile), 4 that finish items, two
 // producers, one MMA issuer. O and the sums have two buffers, so that a CTA's next item goes
 // on while its last one is finished, stored and joined.
@@ -32,6 +36,7 @@
 #include <cuda_fp8.h>
 #include <math.h>
 
+#include "cluster.cuh"
 #include "common.cuh"
 #include "internal.h"
 #include "tc.cuh"
@@ -43,9 +48,11 @@ using bf16 = __nv_bfloat16;
 constexpr int kNS = 3;              // ring stages
 constexpr int kGroup = 16;          // states joined at a time
 constexpr int kLensCap = 1024;      // lengths mirrored in shared memory
+constexpr int kClusterMost = 16;    // CTAs of a cluster
+constexpr int kClusterHeads = 8;    // query heads a KV head there: the states of 16 do not fit
 
 // Shapes of one head size, format and (padded) number of query heads a KV head.
-template <int D_, bool F8_, int GP_>
+template <int D_, bool F8_, int GP_, bool CL = false>
 struct Lay {
   static constexpr int D = D_, GP = GP_;
   static constexpr bool F8 = F8_;
@@ -76,20 +83,25 @@ struct Lay {
   static constexpr int PSET = PBLK * ES;
   static constexpr int PBUF = SETS * PSET;
   static constexpr int POWB = F8 ? 2 * KEYS : 0;           // a stage's powers
-  static constexpr int FIXED = kNS * STAGE + 2 * QBUF + kNS * POWB + 8192 + 2048;
-  static constexpr int NPB = FIXED + 2 * PBUF <= 225 * 1024 ? 2 : 1;
+  static constexpr int NBAR = 3 * kNS + 16 + 1;
+  // behind the barriers, lengths; with clusters the others' states: [C][G][D / C] values, then
+  // [C][16] (m, l)
+  static constexpr int TAIL = CL ? GP * D * 4 + kClusterMost * 16 * 8 : kLensCap * 4;
+  static constexpr int XBYTES = D == 64 ? GP * 64 * 4 : 0;
+  static constexpr int FIXED = kNS * STAGE + 2 * QBUF + kNS * POWB + 4 * GP * NW * 4 + 128 + XBYTES + 128 + NBAR * 8 + 32 +
+                               4 * 32 + kMaxKvHeads + TAIL + 1024;
+  static constexpr int NPB = FIXED + 2 * PBUF <= 232448 ? 2 : 1;  // P buffers that fit
   static constexpr int OFF_Q = kNS * STAGE;
   static constexpr int OFF_P = OFF_Q + 2 * QBUF;
   static constexpr int OFF_POW = OFF_P + NPB * PBUF;
   static constexpr int OFF_RED = OFF_POW + kNS * POWB;     // [2][GP][NW] warp maxima
   static constexpr int OFF_SUM = OFF_RED + 2 * GP * NW * 4;  // [2][GP][NW] sums of an item, [2][16] maxima
   static constexpr int OFF_X = OFF_SUM + 2 * GP * NW * 4 + 128;  // [GP][64] the upper rows of O (d_head 64)
-  static constexpr int OFF_QF = OFF_X + (D == 64 ? GP * 64 * 4 : 0);  // [2][16] factors of the scores
+  static constexpr int OFF_QF = OFF_X + XBYTES;            // [2][16] factors of the scores
   static constexpr int OFF_BAR = OFF_QF + 128;
-  static constexpr int NBAR = 3 * kNS + 16 + 1;
   static constexpr int OFF_MISC = OFF_BAR + NBAR * 8;
   static constexpr int OFF_LENS = OFF_MISC + 32 + 4 * 32 + kMaxKvHeads;
-  static constexpr int SMEM = OFF_LENS + kLensCap * 4 + 1024;
+  static constexpr int SMEM = OFF_LENS + TAIL + 1024;
   // kind::f16 with bf16, or kind::f8f6f4 with e4m3 (weights: e5m2); V is MN-major
   static constexpr uint32_t IDESC_S = F8 ? idesc_f8(128, SN, false, 0) : idesc_bf16(128, SN, false, false);
   static constexpr uint32_t IDESC_PV = F8 ? idesc_f8(128, NPV, true, 1) : idesc_bf16(128, NPV, false, true);
@@ -204,6 +216,37 @@ struct Walk {
   }
 };
 
+// The one item of a cluster: its CTAs have equal runs of its tiles.
+template <int LG>
+struct ClusterWalk {
+  const PagedDecodeArgs& a;
+  const uint8_t* heads_s;
+  int b, k, lo, hi, tiles, off = 0;
+  bool left;
+  Seq q;
+  __device__ __forceinline__ ClusterWalk(const PagedDecodeArgs& a_, const uint8_t* hs, int len, int b_, int k_, int rank,
+                                         int lg_ctas)
+      : a(a_), heads_s(hs), b(b_), k(k_) {
+    q = make_seq<LG>(a, len);
+    tiles = streaming() ? q.ts : q.tr;
+    const int per = (tiles + (1 << lg_ctas) - 1) >> lg_ctas;
+    lo = min(tiles, rank * per);
+    hi = min(tiles, lo + per);
+    left = lo < hi;
+  }
+  __device__ __forceinline__ bool streaming() const { return k >= a.geom.n_r; }
+  __device__ __forceinline__ int kvh() const { return heads_s[k]; }
+  __device__ __forceinline__ int page_of_slot(int slot) const { return !streaming() || slot < q.gslot ? slot : slot + q.gap; }
+  __device__ __forceinline__ int slots() const {
+    return (int)(((unsigned)q.len + a.pool.ps - 1) >> a.pool.lg_ps) - (streaming() ? q.gap : 0);
+  }
+  __device__ __forceinline__ bool next() {
+    const bool r = left;
+    left = false;
+    return r;
+  }
+};
+
 // A state of an item that CTAs share: O [G][D], then the maxima and sums [G] each. Slots of
 // a CTA: 0, 1 the state of its first and of its last item, 2, 3 the states joined by the group
 // that it heads.
@@ -213,24 +256,26 @@ __device__ __forceinline__ float* state_slot(const PagedDecodeArgs& a, int cta, 
 }
 
 // Adds up n <= kGroup states and stores the outputs (out) or the sum (dst); 4 warps. State 0
-// is at `first`, state j > 0 at rest + j * stride. A lane owns four values at a time, and
+// is at `first`, state j > 0 at rest + j * STRIDE. A lane owns four values at a time, and
 // the lanes of a head hold the states' maxima and sums between them.
-template <int D>
-__device__ __forceinline__ void join(int n, const float* first, const float* rest, int stride, int G, bf16* out, float* dst) {
+template <int D, int STRIDE>
+__device__ __forceinline__ void join(int n, const float* first, const float* rest, int G, bf16* out, float* dst) {
   constexpr int U = 8;
   const int lane = threadIdx.x & 31, src = lane & 16;
-  auto part = [&](int j) { return j == 0 ? first : rest + (size_t)j * stride; };
 #pragma unroll 1
   for (int v = threadIdx.x & 127; v < (G * (D / 4) + 31) / 32 * 32; v += 128) {
     const bool mine = v < G * (D / 4);  // d_head 64, odd G: the last half-warp has no head
     const int h = mine ? v / (D / 4) : 0, vv = mine ? v : 0;
     float4 x[U];
+    const float4* from = reinterpret_cast<const float4*>(rest) + vv;
     auto load = [&](int j0) {
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (j0 + u < n) x[u] = __ldcg(reinterpret_cast<const float4*>(part(j0 + u)) + vv);
+        if (j0 + u < n) x[u] = __ldcg(u == 0 && j0 == 0 ? reinterpret_cast<const float4*>(first) + vv : from + u * (STRIDE / 4));
+      from += U * (STRIDE / 4);
     };
-    const float* p = part(min(lane & 15, n - 1)) + G * D + h;
+    const int js = min(lane & 15, n - 1);
+    const float* p = (js == 0 ? first : rest + js * STRIDE) + G * D + h;
     const float mj = (lane & 15) < n ? __ldcg(p) : -INFINITY, lj = __ldcg(p + G);
     load(0);
     float M = mj;
@@ -292,21 +337,21 @@ __device__ __forceinline__ void join_item(const PagedDecodeArgs& a, int p, int f
   constexpr int kCta = 4 * state_floats(D);
   const float *own = state_slot(a, p0, gslot, D), *own_rest = state_slot(a, p0, 0, D);
   if (groups == 1) {
-    join<D>(size, own, own_rest, kCta, G, out, nullptr);
+    join<D, kCta>(size, own, own_rest, G, out, nullptr);
     return;
   }
-  join<D>(size, own, own_rest, kCta, G, nullptr, state_slot(a, p0, 2 + gslot, D));
+  join<D, kCta>(size, own, own_rest, G, nullptr, state_slot(a, p0, 2 + gslot, D));
   if (!arrive(&a.counters[3 * f + 2], groups)) return;
-  join<D>(groups, state_slot(a, f, 3, D), state_slot(a, f, 2, D), kGroup * kCta, G, out, nullptr);
+  join<D, kGroup * kCta>(groups, state_slot(a, f, 3, D), state_slot(a, f, 2, D), G, out, nullptr);
 }
 
 // Powers of two as floats.
 __device__ __forceinline__ float pow2i(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
 
-template <int D, bool F8, int GP>
+template <int D, bool F8, int GP, bool CL>
 __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
     paged_decode_kernel(const __grid_constant__ PagedDecodeArgs a) {
-  using C = Lay<D, F8, GP>;
+  using C = Lay<D, F8, GP, CL>;
   constexpr int NK = C::NK, NW = C::NW, KP = C::KP, LG = NK == 1 ? 7 : NK == 2 ? 8 : 9;
   static_assert(1 << LG == C::KEYS, "keys of a tile");
   constexpr int NT = C::THREADS;
@@ -340,6 +385,8 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
   int* wsum = reinterpret_cast<int*>(smem + C::OFF_MISC + 32);
   uint8_t* heads_s = smem + C::OFF_MISC + 32 + 128;
   int* lens_s = reinterpret_cast<int*>(smem + C::OFF_LENS);
+  float* recv = reinterpret_cast<float*>(smem + C::OFF_LENS);         // clusters
+  float2* recv_ml = reinterpret_cast<float2*>(recv + GP * D);
 
   const CacheGeom& g = a.geom;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -382,80 +429,87 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  if constexpr (CL) cluster_arrive();  // others write into this CTA's shared memory once it runs
   // everything earlier kernels wrote is visible from here on
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-  // ---- this CTA's run: a prefix sum of the sequences' tiles; up to 32 sequences every warp
-  // forms it for itself, a lane a sequence, without a barrier
-  auto seq_tiles = [&](int len) {
-    const Seq q = make_seq<LG>(a, len);
-    return g.n_r * q.tr + g.n_s * q.ts;
-  };
-  auto scan = [&](int x, int n) {  // over the first n lanes
-    for (int o = 1; o < n; o <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, x, o);
-      if (lane >= o) x += y;
-    }
-    return x;
-  };
   const int p = blockIdx.x;
   const bool few = a.n_seqs <= 32, mirrored = !few && a.n_seqs <= kLensCap;
   Deal deal;
-  int len_reg = 0, b_first = 0, seq_off = 0;
-  auto set_deal = [&](int total, int most) {  // most: at least the longest item's tiles
-    deal.total = total;
-    // an item on more than kGroup CTAs is joined in two levels, which a short step does not do
-    // for less: several tiles a CTA there
-    const int least = max(1, (most + kGroup - 1) / kGroup);
-    deal.P = min((int)gridDim.x, quotient(total + least - 1, least));
-    deal.per = quotient(total, max(deal.P, 1));
-    deal.rem = total - deal.per * deal.P;
-  };
-  if (few) {
-    if (lane < a.n_seqs) len_reg = seq_len(a, lane, p == 0 && warp == 0);
-    const int mine = lane < a.n_seqs ? seq_tiles(len_reg) : 0;
-    const Seq q = make_seq<LG>(a, len_reg);
-    const int most = lane >= a.n_seqs ? 0 : g.n_r > 0 ? q.tr : q.ts;
-    set_deal(__reduce_add_sync(0xffffffffu, mine), __reduce_max_sync(0xffffffffu, most));
-    const int inc = scan(mine, a.n_seqs);
-    const unsigned past = __ballot_sync(0xffffffffu, lane < a.n_seqs && inc > deal.first(p));
-    b_first = past ? __ffs(past) - 1 : 0;
-    seq_off = __shfl_sync(0xffffffffu, inc - mine, b_first);
-  } else {
-    const int per = (a.n_seqs + NT - 1) / NT;
-    const int b0 = min(a.n_seqs, (int)threadIdx.x * per), b1 = min(a.n_seqs, b0 + per);
-    int mine = 0;
-    for (int b = b0; b < b1; ++b) {
-      const int len = seq_len(a, b, p == 0);
-      if (mirrored) lens_s[b] = len;
-      mine += seq_tiles(len);
-    }
-    const int inc = scan(mine, 32);
-    if (lane == 31) wsum[warp] = inc;
-    __syncthreads();
-    const int part = lane < NT / 32 ? wsum[lane] : 0, upto = scan(part, 32);
-    set_deal(__shfl_sync(0xffffffffu, upto, 31), 1);
-    int before = __shfl_sync(0xffffffffu, upto - part, warp) + inc - mine;
-    const int start = deal.first(p);
-    if (p < deal.P && before <= start && start < before + mine) {
-      int b = b0;
-      while (true) {
-        const int n = seq_tiles(mirrored ? lens_s[b] : seq_len(a, b, false));
-        if (start < before + n) break;
-        before += n;
-        ++b;
+  int len_reg = 0;
+  const int lg_ctas = CL ? __ffs((int)cluster_ctas()) - 1 : 0, rank = CL ? (int)cluster_rank() : 0;
+  auto plan = [&]() {
+    if constexpr (CL) {
+      const int id = p >> lg_ctas, b = quotient(id, g.Hkv);
+      return ClusterWalk<LG>(a, heads_s, seq_len(a, b, rank == 0 && threadIdx.x == 0), b, id - b * g.Hkv, rank, lg_ctas);
+    } else {
+      // ---- this CTA's run: a prefix sum of the sequences' tiles; up to 32 sequences every warp
+      // forms it for itself, a lane a sequence, without a barrier
+      auto seq_tiles = [&](int len) {
+        const Seq q = make_seq<LG>(a, len);
+        return g.n_r * q.tr + g.n_s * q.ts;
+      };
+      auto scan = [&](int x, int n) {  // over the first n lanes
+        for (int o = 1; o < n; o <<= 1) {
+          const int y = __shfl_up_sync(0xffffffffu, x, o);
+          if (lane >= o) x += y;
+        }
+        return x;
+      };
+      int b_first = 0, seq_off = 0;
+      auto set_deal = [&](int total) {
+        deal.total = total;
+        deal.P = min((int)gridDim.x, total);
+        deal.per = quotient(total, max(deal.P, 1));
+        deal.rem = total - deal.per * deal.P;
+      };
+      if (few) {
+        if (lane < a.n_seqs) len_reg = seq_len(a, lane, p == 0 && warp == 0);
+        const int mine = lane < a.n_seqs ? seq_tiles(len_reg) : 0;
+        set_deal(__reduce_add_sync(0xffffffffu, mine));
+        const int inc = scan(mine, a.n_seqs);
+        const unsigned past = __ballot_sync(0xffffffffu, lane < a.n_seqs && inc > deal.first(p));
+        b_first = past ? __ffs(past) - 1 : 0;
+        seq_off = __shfl_sync(0xffffffffu, inc - mine, b_first);
+      } else {
+        const int per = (a.n_seqs + NT - 1) / NT;
+        const int b0 = min(a.n_seqs, (int)threadIdx.x * per), b1 = min(a.n_seqs, b0 + per);
+        int mine = 0;
+        for (int b = b0; b < b1; ++b) {
+          const int len = seq_len(a, b, p == 0);
+          if (mirrored) lens_s[b] = len;
+          mine += seq_tiles(len);
+        }
+        const int inc = scan(mine, 32);
+        if (lane == 31) wsum[warp] = inc;
+        __syncthreads();
+        const int part = lane < NT / 32 ? wsum[lane] : 0, upto = scan(part, 32);
+        set_deal(__shfl_sync(0xffffffffu, upto, 31));
+        int before = __shfl_sync(0xffffffffu, upto - part, warp) + inc - mine;
+        const int start = deal.first(p);
+        if (p < deal.P && before <= start && start < before + mine) {
+          int b = b0;
+          while (true) {
+            const int n = seq_tiles(mirrored ? lens_s[b] : seq_len(a, b, false));
+            if (start < before + n) break;
+            before += n;
+            ++b;
+          }
+          first_s[0] = b;
+          first_s[1] = before;
+        }
+        __syncthreads();
+        b_first = first_s[0];
+        seq_off = first_s[1];
       }
-      first_s[0] = b;
-      first_s[1] = before;
+      const bool any = p < deal.P;
+      return Walk<LG>(a, mirrored ? lens_s : nullptr, heads_s, len_reg, any ? deal.first(p) : deal.total,
+                      any ? deal.first(p + 1) : deal.total, b_first, any ? seq_off : deal.total);
     }
-    __syncthreads();
-    b_first = first_s[0];
-    seq_off = first_s[1];
-  }
-  const bool any = p < deal.P;
-  Walk<LG> walk(a, mirrored ? lens_s : nullptr, heads_s, len_reg, any ? deal.first(p) : deal.total,
-                any ? deal.first(p + 1) : deal.total, b_first, any ? seq_off : deal.total);
+  };
+  auto walk = plan();
+  if constexpr (CL) cluster_wait();
 
   if (warp == kLoadK || warp == kLoadV) {
     // ------------------------------------------------------------ producers
@@ -662,15 +716,34 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
     const int r = threadIdx.x & 127;  // row of O^T
     const uint32_t tl = tmem + ((uint32_t)((warp & 3) * 32) << 16);
     // sequences without a token
-    for (int b = p; b < a.n_seqs; b += gridDim.x)
+    for (int b = p; !CL && b < a.n_seqs; b += gridDim.x)
       if ((few ? __shfl_sync(0xffffffffu, len_reg, b) : mirrored ? lens_s[b] : seq_len(a, b, false)) == 0)
         for (int i = r; i < g.Hq * D / 8; i += 128)
           reinterpret_cast<uint4*>(static_cast<bf16*>(a.out) + (size_t)b * g.Hq * D)[i] = make_uint4(0, 0, 0, 0);
+    // clusters: row r's values to the CTA that finishes it, head r's state to all
+    const int lg_rows = CL ? (D == 128 ? 7 : 6) - lg_ctas : 0;
+    auto push = [&](const float (&o)[GP], float m, float l) {
+      if (r < D) {
+        const uint32_t dst = cluster_addr(recv + ((rank * G) << lg_rows) + (r & ((1 << lg_rows) - 1)), (uint32_t)(r >> lg_rows));
+#pragma unroll
+        for (int h = 0; h < GP; ++h)
+          if (h < G) cluster_st_f32(dst + (uint32_t)(h << lg_rows) * 4, o[h]);
+      }
+      if (r < G)
+        for (int c = 0; c < 1 << lg_ctas; ++c)
+          cluster_st2(cluster_addr(recv_ml + rank * 16 + r, (uint32_t)c), __float_as_uint(m), __float_as_uint(l));
+    };
+    if constexpr (CL) {
+      if (!walk.left) {
+        const float none[GP] = {};
+        push(none, -INFINITY, 0.f);
+      }
+    }
     int item = 0;
     bool ok = true;
     while (ok && walk.next()) {
       const int x = item & 1;
-      const int f = deal.cta_of(walk.off), last = deal.cta_of(walk.off + walk.tiles - 1);
+      const int f = CL ? 0 : deal.cta_of(walk.off), last = CL ? 0 : deal.cta_of(walk.off + walk.tiles - 1);
       bf16* out = static_cast<bf16*>(a.out) + ((size_t)walk.b * g.Hq + (size_t)walk.kvh() * G) * D;
       ok = wait_bar(&l_full[x], (item >> 1) & 1, a.err, abort_flag);
       ok = wait_bar(&o_full[x], (item >> 1) & 1, a.err, abort_flag) && ok;
@@ -707,7 +780,9 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
         }
         return L;
       };
-      if (f == last) {
+      if constexpr (CL) {
+        push(o, r < G ? mfin[x * 16 + r] : 0.f, r < G ? sum_of(r) : 0.f);
+      } else if (f == last) {
 #pragma unroll
         for (int h = 0; h < GP; ++h)
           if (r < D && h < G) out[h * D + r] = __float2bfloat16_rn(__fdividef(o[h], sum_of(h)));
@@ -934,40 +1009,80 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
   }
 
   tc_fence_before();
+  if constexpr (CL) {
+    // the states of all CTAs have arrived (the waits of one that gave up are bounded: it comes
+    // here too)
+    __syncwarp();
+    cluster_arrive();
+    cluster_wait();
+    if (warp >= kFinish && warp < kFinish + 4) {
+      const int lg_rows = (D == 128 ? 7 : 6) - lg_ctas, n = 1 << lg_ctas;
+      bf16* out = static_cast<bf16*>(a.out) + ((size_t)walk.b * g.Hq + (size_t)walk.kvh() * G) * D + (rank << lg_rows);
+      for (int i = threadIdx.x & 127; i < G << lg_rows; i += 128) {
+        const int h = i >> lg_rows;
+        float M = -INFINITY, L = 0.f, O = 0.f;
+#pragma unroll 4
+        for (int c = 0; c < n; ++c) M = fmaxf(M, recv_ml[c * 16 + h].x);
+#pragma unroll 4
+        for (int c = 0; c < n; ++c) {
+          const float2 ml = recv_ml[c * 16 + h];
+          const float w = ml.y == 0.f ? 0.f : fast_exp2(ml.x - M);
+          L += w * ml.y;
+          O += w * recv[((c * G) << lg_rows) + i];
+        }
+        // (a sequence without a token: zeros)
+        out[(size_t)h * D + (i & ((1 << lg_rows) - 1))] = __float2bfloat16_rn(walk.tiles == 0 ? 0.f : O / L);
+      }
+    }
+  }
   __syncthreads();
   tc_fence_after();
   if (warp == kMma) tmem_dealloc(tmem, C::TMEM_COLS);
 }
 
-template <int D, bool F8, int GP>
-cudaError_t launch(const PagedDecodeArgs& a, int num_sms, cudaStream_t s) {
-  using C = Lay<D, F8, GP>;
-  auto kernel = paged_decode_kernel<D, F8, GP>;
+// cluster: CTAs of a cluster, 0: no clusters.
+template <int D, bool F8, int GP, bool CL>
+cudaError_t launch(const PagedDecodeArgs& a, int ctas, int cluster, cudaStream_t s) {
+  using C = Lay<D, F8, GP, CL>;
+  auto kernel = paged_decode_kernel<D, F8, GP, CL>;
   static std::atomic<uint64_t> done{0};
-  const cudaError_t e = once_per_device(
-      done, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM); });
+  const cudaError_t e = once_per_device(done, [&] {
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+    if (e == cudaSuccess && CL) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    return e;
+  });
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)num_sms);
+  cfg.gridDim = dim3((unsigned)ctas);
   cfg.blockDim = dim3(C::THREADS);
   cfg.dynamicSmemBytes = C::SMEM;
   cfg.stream = s;
   // its start runs under the end of the kernel before it
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = CL ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
+template <int D, bool F8, int GP>
+cudaError_t launch_split(const PagedDecodeArgs& a, int num_sms, int cluster, cudaStream_t s) {
+  if constexpr (GP <= kClusterHeads)
+    if (cluster > 0) return launch<D, F8, GP, true>(a, a.n_seqs * a.geom.Hkv * cluster, cluster, s);
+  return launch<D, F8, GP, false>(a, num_sms, 0, s);
+}
+
 template <int D, bool F8>
-cudaError_t launch_heads(const PagedDecodeArgs& a, int num_sms, cudaStream_t s) {
+cudaError_t launch_heads(const PagedDecodeArgs& a, int num_sms, int cluster, cudaStream_t s) {
   const int G = a.geom.G;
-  if (G <= 2) return launch<D, F8, 2>(a, num_sms, s);
-  if (G <= 4) return launch<D, F8, 4>(a, num_sms, s);
-  if (G <= 8) return launch<D, F8, 8>(a, num_sms, s);
-  return launch<D, F8, 16>(a, num_sms, s);
+  if (G <= 2) return launch_split<D, F8, 2>(a, num_sms, cluster, s);
+  if (G <= 4) return launch_split<D, F8, 4>(a, num_sms, cluster, s);
+  if (G <= 8) return launch_split<D, F8, 8>(a, num_sms, cluster, s);
+  return launch_split<D, F8, 16>(a, num_sms, cluster, s);
 }
 
 }  // namespace pdec

@@ -1,7 +1,7 @@
 #include "paged_decode.cuh"
 
 namespace aoh {
-cudaError_t launch_paged_decode_bf16_128(const PagedDecodeArgs& a, int num_sms, cudaStream_t s) {
-  return pdec::launch_heads<128, false>(a, num_sms, s);
+cudaError_t launch_paged_decode_bf16_128(const PagedDecodeArgs& a, int num_sms, int cluster, cudaStream_t s) {
+  return pdec::launch_heads<128, false>(a, num_sms, cluster, s);
 }
 }  // namespace aoh

@@ -320,6 +320,24 @@ def test_decode(case, form):
 
 @pytest.mark.parametrize("form", ["bf16", "e4m3"])
 @pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hkv", [1, 4, 9])
+def test_decode_whatever_the_bound(form, d, hkv):
+    """Both splits of the work (max_len chooses) on the same step: long and short
+    sequences, one without a token, one of a single one."""
+    lens, hq, sink, window = [3000, 1, 0, 517, 130], 7 * hkv, 30, 200
+    labels = [i % 2 for i in range(hkv)]
+    p = Pages(lens, hq, hkv, d, 32, form, labels, sink, window)
+    held = p.fill(lens, seed=hkv)
+    q = randn((len(lens), hq, d), 3)
+    for max_len in (0, 1, 200, 100000):
+        out = torch.full_like(q, float("nan"))
+        p.cache.decode(q, ints(lens), p.table, out, max_len=max_len)
+        p.cache.check()
+        check_decode(out, q, held, labels, sink, window, f"bound {max_len}")
+
+
+@pytest.mark.parametrize("form", ["bf16", "e4m3"])
+@pytest.mark.parametrize("d", [64, 128])
 def test_decode_with_a_heavy_first_key(form, d):
     """An attention sink with a small value, far above the other keys: their sum still
     counts (its weight is e^6 to e^12 of each of theirs)."""

@@ -136,7 +136,7 @@ def test_calls_without_a_handle(lib):
     one = (ctypes.c_int32 * 1)(1)
     assert lib.aoh_paged_append(None, p, p, 128, 128, None, p, 1, 1, p, 1, None) == 1
     assert lib.aoh_paged_read(None, None, None, 1, 1, p, 1, p, p, None) == 1
-    assert lib.aoh_paged_decode(None, p, 512, p, 1, p, 1, p, None) == 1
+    assert lib.aoh_paged_decode(None, p, 512, p, 1, 0, p, 1, p, None) == 1
     assert lib.aoh_paged_prefill(None, p, p, p, 512, 128, 128, one, None, 1, p, None) == 1
     assert lib.aoh_paged_check(None, None) == 1
     lib.aoh_paged_destroy(None)

@@ -12,6 +12,7 @@ configuration; the handle-level functions (``aoh_prefill``,
 ``aoh_decode_step`` ...) pass the pointers on unchecked, as the C ABI does.
 """
 
+import array
 import ctypes
 import os
 
@@ -118,7 +119,7 @@ def load():
         "aoh_classify": (i32, [P, P, i32, i32, i32, i32, i32, i32, ctypes.POINTER(ctypes.c_double), u8p, P]),
         "aoh_paged_bytes": (ctypes.c_size_t, [pcfgp]),
         "aoh_paged_init": (i32, [pcfgp, u8p, P, ctypes.c_size_t, ctypes.POINTER(P)]),
-        "aoh_paged_prefill": (i32, [P, P, P, P, i64, i64, i64, i32p, i32p, i32, P, P]),
+        "aoh_paged_prefill": (i32, [P, P, P, P, i64, i64, i64, P, P, i32, P, P]),
         "aoh_paged_append": (i32, [P, P, P, i64, i64, P, P, i32, i32, P, i32, P]),
         "aoh_paged_read": (i32, [P, P, P, i32, i32, P, i32, P, P, P]),
         "aoh_paged_decode": (i32, [P, P, i64, P, i32, i32, P, i32, P, P]),
@@ -375,10 +376,6 @@ def aoh_paged_init(cfg, labels, pool):
     return h
 
 
-def _lens_arr(lens):
-    return (ctypes.c_int32 * max(1, len(lens)))(*lens)
-
-
 def aoh_paged_check(cache, stream=None):
     _check(load().aoh_paged_check(cache, _stream_ptr(stream)))
 
@@ -402,6 +399,8 @@ def _rows(t, name, heads, d):
     if t.dtype is not torch.bfloat16 or not t.is_cuda:
         raise ValueError(f"{name} must be a torch.bfloat16 CUDA tensor")
     n = shape[0]
+    if t.is_contiguous():
+        return t.data_ptr(), heads * d, n
     s0, s1, s2 = t.stride()
     if n <= 1:
         s0 = heads * d
@@ -563,8 +562,10 @@ class PagedCache:
             raise ValueError(f"q_lens and k_lens hold one length a sequence, at most {self.max_seqs}")
         if sum(q_lens) != nq or sum(q_lens if k_lens is None else k_lens) != nk or nk != nv:
             raise ValueError(f"q, k and v hold {nq}, {nk} and {nv} rows; q_lens and k_lens say otherwise")
-        st = _lib.aoh_paged_prefill(self.handle, qp, kp, vp, qs, ks, vs, _lens_arr(q_lens),
-                                    None if k_lens is None else _lens_arr(k_lens), n, op, self._stream(stream))
+        ql = array.array("i", q_lens)
+        kl = ql if k_lens is None else array.array("i", k_lens)
+        st = _lib.aoh_paged_prefill(self.handle, qp, kp, vp, qs, ks, vs, ql.buffer_info()[0], kl.buffer_info()[0], n, op,
+                                    self._stream(stream))
         if st:
             _check(st)
 

@@ -45,7 +45,6 @@ namespace aoh {
 namespace pdec {
 
 using bf16 = __nv_bfloat16;
-constexpr int kNS = 3;              // ring stages
 constexpr int kGroup = 16;          // states joined at a time
 constexpr int kLensCap = 1024;      // lengths mirrored in shared memory
 constexpr int kClusterMost = 16;    // CTAs of a cluster
@@ -64,6 +63,7 @@ struct Lay {
   // a tile's K, or V: 32 KB, but where the weights of 16 heads leave no room for three such tiles
   static constexpr int HALF = F8 && D == 64 && GP == 16 ? 16384 : 32768;
   static constexpr int STAGE = 2 * HALF;
+  static constexpr int NS = 3 * 32768 / HALF;              // ring stages
   static constexpr int NK = HALF / GRP;                    // groups of a tile
   static constexpr int KEYS = NK * 128;
   static constexpr int MB = 128 / D;                       // groups side by side in a P V MMA
@@ -83,18 +83,18 @@ struct Lay {
   static constexpr int PSET = PBLK * ES;
   static constexpr int PBUF = SETS * PSET;
   static constexpr int POWB = F8 ? 2 * KEYS : 0;           // a stage's powers
-  static constexpr int NBAR = 3 * kNS + 16 + 1;
+  static constexpr int NBAR = 3 * NS + 16 + 1;
   // behind the barriers, lengths; with clusters the others' states: [C][G][D / C] values, then
   // [C][16] (m, l)
   static constexpr int TAIL = CL ? GP * D * 4 + kClusterMost * 16 * 8 : kLensCap * 4;
   static constexpr int XBYTES = D == 64 ? GP * 64 * 4 : 0;
-  static constexpr int FIXED = kNS * STAGE + 2 * QBUF + kNS * POWB + 4 * GP * NW * 4 + 128 + XBYTES + 128 + NBAR * 8 + 32 +
+  static constexpr int FIXED = NS * STAGE + 2 * QBUF + NS * POWB + 4 * GP * NW * 4 + 128 + XBYTES + 128 + NBAR * 8 + 32 +
                                4 * 32 + kMaxKvHeads + TAIL + 1024;
   static constexpr int NPB = FIXED + 2 * PBUF <= 232448 ? 2 : 1;  // P buffers that fit
-  static constexpr int OFF_Q = kNS * STAGE;
+  static constexpr int OFF_Q = NS * STAGE;
   static constexpr int OFF_P = OFF_Q + 2 * QBUF;
   static constexpr int OFF_POW = OFF_P + NPB * PBUF;
-  static constexpr int OFF_RED = OFF_POW + kNS * POWB;     // [2][GP][NW] warp maxima
+  static constexpr int OFF_RED = OFF_POW + NS * POWB;     // [2][GP][NW] warp maxima
   static constexpr int OFF_SUM = OFF_RED + 2 * GP * NW * 4;  // [2][GP][NW] sums of an item, [2][16] maxima
   static constexpr int OFF_X = OFF_SUM + 2 * GP * NW * 4 + 128;  // [GP][64] the upper rows of O (d_head 64)
   static constexpr int OFF_QF = OFF_X + XBYTES;            // [2][16] factors of the scores
@@ -256,28 +256,27 @@ __device__ __forceinline__ float* state_slot(const PagedDecodeArgs& a, int cta, 
 }
 
 // Adds up n <= kGroup states and stores the outputs (out) or the sum (dst); 4 warps. State 0
-// is at `first`, state j > 0 at rest + j * STRIDE. A lane owns four values at a time, and
-// the lanes of a head hold the states' maxima and sums between them.
-template <int D, int STRIDE>
-__device__ __forceinline__ void join(int n, const float* first, const float* rest, int G, bf16* out, float* dst) {
-  constexpr int U = 8;
+// is at `first`, state j > 0 at rest + j * stride. A lane owns four values at a time, all
+// states' of them on their way at once, and the lanes of a head hold the states' maxima and
+// sums between them.
+template <int D>
+__device__ __forceinline__ void join(int n, const float* first, const float* rest, int stride, int G, bf16* out, float* dst) {
   const int lane = threadIdx.x & 31, src = lane & 16;
 #pragma unroll 1
   for (int v = threadIdx.x & 127; v < (G * (D / 4) + 31) / 32 * 32; v += 128) {
     const bool mine = v < G * (D / 4);  // d_head 64, odd G: the last half-warp has no head
     const int h = mine ? v / (D / 4) : 0, vv = mine ? v : 0;
-    float4 x[U];
-    const float4* from = reinterpret_cast<const float4*>(rest) + vv;
-    auto load = [&](int j0) {
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (j0 + u < n) x[u] = __ldcg(u == 0 && j0 == 0 ? reinterpret_cast<const float4*>(first) + vv : from + u * (STRIDE / 4));
-      from += U * (STRIDE / 4);
-    };
     const int js = min(lane & 15, n - 1);
-    const float* p = (js == 0 ? first : rest + js * STRIDE) + G * D + h;
+    const float* p = (js == 0 ? first : rest + (size_t)js * stride) + G * D + h;
     const float mj = (lane & 15) < n ? __ldcg(p) : -INFINITY, lj = __ldcg(p + G);
-    load(0);
+    float4 x[kGroup];
+    const float* from = rest + vv * 4;
+    x[0] = __ldcg(reinterpret_cast<const float4*>(first) + vv);
+#pragma unroll
+    for (int j = 1; j < kGroup; ++j) {
+      from += stride;
+      if (j < n) x[j] = __ldcg(reinterpret_cast<const float4*>(from));
+    }
     float M = mj;
 #pragma unroll
     for (int o = 8; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
@@ -286,18 +285,14 @@ __device__ __forceinline__ void join(int n, const float* first, const float* res
 #pragma unroll
     for (int o = 8; o >= 1; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
     float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 1
-    for (int j0 = 0; j0 < n; j0 += U) {
-      if (j0 > 0) load(j0);
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const float f = __shfl_sync(0xffffffffu, w, src | (j0 + u));
-        if (j0 + u < n) {
-          O.x += f * x[u].x;
-          O.y += f * x[u].y;
-          O.z += f * x[u].z;
-          O.w += f * x[u].w;
-        }
+    for (int j = 0; j < kGroup; ++j) {
+      const float f = __shfl_sync(0xffffffffu, w, src | j);
+      if (j < n) {
+        O.x += f * x[j].x;
+        O.y += f * x[j].y;
+        O.z += f * x[j].z;
+        O.w += f * x[j].w;
       }
     }
     if (!mine) continue;
@@ -320,29 +315,32 @@ __device__ __forceinline__ void join(int n, const float* first, const float* res
 template <int D>
 __device__ __forceinline__ void join_item(const PagedDecodeArgs& a, int p, int f, int last, int G, bf16* out,
                                           volatile int* flag) {
-  const int p0 = f + (p - f) / kGroup * kGroup;
-  const int size = min(kGroup, last - p0 + 1), groups = (last - f) / kGroup + 1;
-  const int gslot = p0 == f ? 1 : 0;
-  auto arrive = [&](uint32_t* counter, int of) {
+  constexpr int kCta = 4 * state_floats(D);
+  const int groups = (last - f) / kGroup + 1, p0 = f + (p - f) / kGroup * kGroup;
+  // what is joined: CTA p0's slot `slot`, then slot `slot_rest` of every step-th CTA from there
+  int first = p0, slot = p0 == f ? 1 : 0, slot_rest = 0, step = 1, n = min(kGroup, last - p0 + 1);
+  uint32_t* counter = &a.counters[3 * p0 + slot];
+#pragma unroll 1
+  while (true) {
     named_barrier_sync(2, 128);
     if ((threadIdx.x & 127) == 0) {
-      const bool done = atom_add_acq_rel_gpu(counter, 1u) == (uint32_t)(of - 1);
+      const bool done = atom_add_acq_rel_gpu(counter, 1u) == (uint32_t)(n - 1);
       if (done) *counter = 0u;
       *flag = done;
     }
     named_barrier_sync(2, 128);
-    return *flag != 0;
-  };
-  if (!arrive(&a.counters[3 * p0 + gslot], size)) return;
-  constexpr int kCta = 4 * state_floats(D);
-  const float *own = state_slot(a, p0, gslot, D), *own_rest = state_slot(a, p0, 0, D);
-  if (groups == 1) {
-    join<D, kCta>(size, own, own_rest, G, out, nullptr);
-    return;
+    if (!*flag) return;
+    const bool whole = step > 1 || groups == 1;
+    join<D>(n, state_slot(a, first, slot, D), state_slot(a, first, slot_rest, D), step * kCta, G, whole ? out : nullptr,
+            state_slot(a, p0, p0 == f ? 3 : 2, D));
+    if (whole) return;
+    first = f;
+    slot = 3;
+    slot_rest = 2;
+    step = kGroup;
+    n = groups;
+    counter = &a.counters[3 * f + 2];
   }
-  join<D, kCta>(size, own, own_rest, G, nullptr, state_slot(a, p0, 2 + gslot, D));
-  if (!arrive(&a.counters[3 * f + 2], groups)) return;
-  join<D, kGroup * kCta>(groups, state_slot(a, f, 3, D), state_slot(a, f, 2, D), G, out, nullptr);
 }
 
 // Powers of two as floats.
@@ -367,9 +365,9 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
   float* upper = reinterpret_cast<float*>(smem + C::OFF_X);
   float* qfac = reinterpret_cast<float*>(smem + C::OFF_QF);
   uint64_t* k_full = reinterpret_cast<uint64_t*>(smem + C::OFF_BAR);  // K and powers of a stage landed
-  uint64_t* v_full = k_full + kNS;
-  uint64_t* empty = v_full + kNS;
-  uint64_t* s_full = empty + kNS;  // [2] S(j) in TMEM
+  uint64_t* v_full = k_full + C::NS;
+  uint64_t* empty = v_full + C::NS;
+  uint64_t* s_full = empty + C::NS;  // [2] S(j) in TMEM
   uint64_t* s_free = s_full + 2;   // [2] S(j) read by the softmax
   uint64_t* p_full = s_free + 2;   // [2] P(j) written
   uint64_t* p_free = p_full + 2;   // [2] O += P(j) V(j) done
@@ -400,7 +398,7 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
   if (threadIdx.x < g.Hkv)
     heads_s[threadIdx.x] = (int)threadIdx.x < g.n_r ? g.r_head[threadIdx.x] : g.s_head[threadIdx.x - g.n_r];
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kNS; ++s) {
+    for (int s = 0; s < C::NS; ++s) {
       mbar_init(&k_full[s], 1);
       mbar_init(&v_full[s], 1);
       mbar_init(&empty[s], 1);
@@ -526,13 +524,13 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
       const int32_t* row = a.table + (size_t)walk.b * a.table_stride;
       const int slots = walk.slots(), kvh = walk.kvh();
       for (int j = walk.lo; j < walk.hi; ++j, ++it) {
-        const int st = it % kNS;
+        const int st = it % C::NS;
         const int n = min(spt, slots - j * spt);
         int page = 0;
         if (lane < n) page = __ldg(row + walk.page_of_slot(j * spt + lane));
         const bool bad = (unsigned)page >= (unsigned)a.pool.n_pages;
         if (bad && !is_v) atomicOr(a.err, kErrPages);
-        if (it >= kNS) ok = __all_sync(0xffffffffu, wait_bar(&empty[st], ((it / kNS) & 1) ^ 1, a.err, abort_flag));
+        if (it >= C::NS) ok = __all_sync(0xffffffffu, wait_bar(&empty[st], ((it / C::NS) & 1) ^ 1, a.err, abort_flag));
         if (!ok) break;
         if constexpr (F8) {
           if (!is_v) {
@@ -565,7 +563,7 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
     // every issued copy lands before the CTA can exit
     if (F8) asm volatile("cp.async.wait_all;" ::: "memory");
     if (lane == 0)
-      for (int j = it > kNS ? it - kNS : 0; j < it; ++j) drain_wait(&full[j % kNS], (j / kNS) & 1, a.err);
+      for (int j = it > C::NS ? it - C::NS : 0; j < it; ++j) drain_wait(&full[j % C::NS], (j / C::NS) & 1, a.err);
     __syncwarp();
   } else if (warp == kMma) {
     // ------------------------------------------------------------ MMA issuer
@@ -588,13 +586,13 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
     auto issue_pv = [&]() {
       const int j = pend;
       pend = -1;
-      wait_warp(&v_full[j % kNS], (j / kNS) & 1);
+      wait_warp(&v_full[j % C::NS], (j / C::NS) & 1);
       wait_warp(&p_full[j & 1], (j >> 1) & 1);
       if (!ok) return;
       if (elect_one()) {
         tc_fence_after();
         const uint32_t o = tmem + C::OCOL + (pend_item & 1) * C::NPV;
-        const uint64_t v_desc = v_desc0 + (uint32_t)((j % kNS) * sdesc_step(C::STAGE));
+        const uint64_t v_desc = v_desc0 + (uint32_t)((j % C::NS) * sdesc_step(C::STAGE));
         const uint64_t p_desc = p_desc0 + (uint32_t)((j % C::NPB) * sdesc_step(C::PBUF));
 #pragma unroll
         for (int z = 0; z < C::SETS; ++z)
@@ -604,7 +602,7 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
                            p_desc + sdesc_step(z * C::PSET + (kk >> 2) * C::PBLK + (kk & 3) * 32), C::IDESC_PV,
                            pend_first && z == 0 && kk == 0 ? 0u : 1u);
         tc_commit(&p_free[j & 1]);
-        tc_commit(&empty[j % kNS]);
+        tc_commit(&empty[j % C::NS]);
         if (pend_last) tc_commit(&o_full[pend_item & 1]);
       }
       __syncwarp();
@@ -678,10 +676,10 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
       more = walk.next();
       if (more) fetch(walk.b, walk.kvh());
       for (int j = lo; j < hi; ++j, ++it) {
-        const int st = it % kNS;
+        const int st = it % C::NS;
         // (a P V does not wait behind a tile that is still on its way)
-        if (pend >= 0 && !__all_sync(0xffffffffu, mbar_test(&k_full[st], (it / kNS) & 1))) issue_pv();
-        wait_warp(&k_full[st], (it / kNS) & 1);
+        if (pend >= 0 && !__all_sync(0xffffffffu, mbar_test(&k_full[st], (it / C::NS) & 1))) issue_pv();
+        wait_warp(&k_full[st], (it / C::NS) & 1);
         if (it >= 2) wait_warp(&s_free[it & 1], ((it >> 1) - 1) & 1);
         if (!ok) break;
         if (elect_one()) {
@@ -823,11 +821,11 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
         l[h] = 0.f;
       }
       for (int j = walk.lo; j < walk.hi; ++j, ++it) {
-        const int x = it & 1, st = it % kNS;
+        const int x = it & 1, st = it % C::NS;
         const bool first = j == walk.lo;
         bool see[KP];
         int ek[KP], ev[KP];
-        if (F8) local_ok = wait_bar(&k_full[st], (it / kNS) & 1, a.err, abort_flag) && local_ok;
+        if (F8) local_ok = wait_bar(&k_full[st], (it / C::NS) & 1, a.err, abort_flag) && local_ok;
 #pragma unroll
         for (int c = 0; c < KP; ++c) {
           const int key = t + c * C::SOFT, y = key >> 7;
@@ -844,7 +842,7 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
           if (hidden) {
             // V rows that no weight may meet (0 times a NaN is NaN), while S is formed
             constexpr int CH = C::ROWB / 16;
-            local_ok = wait_bar(&v_full[st], (it / kNS) & 1, a.err, abort_flag) && local_ok;
+            local_ok = wait_bar(&v_full[st], (it / C::NS) & 1, a.err, abort_flag) && local_ok;
 #pragma unroll
             for (int db = 0; db < C::DBLK; ++db) {
               uint4* v4 = reinterpret_cast<uint4*>(smem + st * C::STAGE + C::HALF + y * C::GRP + db * C::BOX +

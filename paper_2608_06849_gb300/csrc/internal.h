@@ -165,7 +165,7 @@ struct PackedSeqs {
 };
 
 // Arguments of the prefill kernels on packed prompts: tensor maps over q / k / v (rows of
-// [heads][D], box 128 rows x 64 columns, 128-byte swizzle). Work items travel by value.
+// [heads][D], 64 columns of 128 rows of a head, 128-byte swizzle). Work items travel by value.
 struct PackedArgs {
   CUtensorMap tq, tk, tv;
   CacheGeom geom;  // heads, S and W (no cache)
@@ -174,7 +174,12 @@ struct PackedArgs {
   const uint64_t* work;  // unused
   uint32_t* err;
   float scale_log2;
+  int follows;     // another launch of the same call comes before this one
+  int span;        // folded items: tokens of a query tile, 128 / G
+  int rcp;         // folded items: (r * rcp) >> 16 = r / G for r < 128, G <= 16
 };
+// The same with folded items, whose box of q is `span` rows of G heads.
+struct FoldedArgs : PackedArgs {};
 
 // Sequences that travel to the device as a kernel's arguments: unlike a copy from
 // pageable memory it waits for nothing and may be captured.
@@ -297,14 +302,17 @@ cudaError_t launch_prefill_tc(const PrefillTcArgs& a, const std::vector<uint64_t
 cudaError_t launch_prefill_short(const PrefillTcArgs& a, const std::vector<uint64_t>& items, int num_sms,
                                  cudaStream_t s);
 // 4D map over a [B][T][H][D] bf16 tensor whose rows lie `stride` elements apart (0: H * D),
-// box [1][128][1][64], 128-byte swizzle.
-bool make_rows_map(CUtensorMap* map, const void* base, int B, long long T, int H, int D, long long stride);
+// box [1][rows][heads][64], 128-byte swizzle.
+bool make_rows_map(CUtensorMap* map, const void* base, int B, long long T, int H, int D, long long stride, int rows = 128,
+                   int heads = 1);
 // Fills the first seqs.size() entries of the device table.
 cudaError_t launch_packed_seqs(int4* table, const std::vector<int4>& seqs, cudaStream_t s);
-// The items of packed prompts: `pairs` as in launch_prefill_tc; is_short: one CTA an SM
-// through all items.
+// The items of packed prompts, plain or folded. pairs: as in launch_prefill_tc; split: CTAs
+// that share each item (1, 2, 4 or 8); is_short: one CTA an SM through all items.
 cudaError_t launch_prefill_packed(const PackedArgs& a, const std::vector<uint64_t>& items,
                                   const std::vector<uint64_t>& pairs, bool is_short, int num_sms, cudaStream_t s);
+cudaError_t launch_prefill_folded(const FoldedArgs& a, const std::vector<uint64_t>& items, int split, bool is_short,
+                                  int num_sms, cudaStream_t s);
 cudaError_t launch_paged_append(const PagedAppendArgs& a, int num_sms, cudaStream_t s);
 cudaError_t launch_paged_read(const PagedReadArgs& a, int num_sms, cudaStream_t s);
 bool make_pages_map(CUtensorMap* map, const PagePool& p);

@@ -322,21 +322,21 @@ aoh_status aoh_paged_prefill(aoh_paged* cache, const void* q, const void* k, con
   if (st == AOH_OK && n_k > 0) st = check_rows("v", v, v_stride, c.n_kv_heads, c.d_head);
   if (st != AOH_OK) return st;
 
-  PackedArgs a;
+  FoldedArgs a;
   memset(&a, 0, sizeof(a));
   a.geom = cache->geom;
   a.out = out;
   a.err = cache->d_err;
   a.scale_log2 = (float)(1.4426950408889634 / sqrt((double)c.d_head));
+  a.span = 128 / a.geom.G;
+  a.rcp = 65536 / a.geom.G + 1;
+  const bool folds = packed_folds(a.geom, seqs, a.span, cache->num_sms);
   // without any key there is nothing to load, and the maps stand for the queries
   const bool keys = n_k > 0;
-  if (!make_rows_map(&a.tq, q, 1, n_q, c.n_q_heads, c.d_head, q_stride) ||
+  if (!make_rows_map(&a.tq, q, 1, n_q, c.n_q_heads, c.d_head, q_stride, folds ? a.span : 128, folds ? a.geom.G : 1) ||
       !make_rows_map(&a.tk, keys ? k : q, 1, keys ? n_k : n_q, c.n_kv_heads, c.d_head, keys ? k_stride : q_stride) ||
       !make_rows_map(&a.tv, keys ? v : q, 1, keys ? n_k : n_q, c.n_kv_heads, c.d_head, keys ? v_stride : q_stride))
     return fail(AOH_ERR_CUDA, "cuTensorMapEncodeTiled failed for q/k/v");
-  std::vector<int> costs;
-  const std::vector<uint64_t> items = packed_schedule(a.geom, seqs, &costs);
-  const std::vector<uint64_t> pairs = prefill_pairs(items, costs, cache->num_sms);
   cudaStream_t s = (cudaStream_t)stream;
   if (seqs.size() <= (size_t)PackedSeqs::kMost) {
     std::copy(seqs.begin(), seqs.end(), a.seqs.by_value);
@@ -345,9 +345,19 @@ aoh_status aoh_paged_prefill(aoh_paged* cache, const void* q, const void* k, con
     const cudaError_t e = launch_packed_seqs(cache->d_seqs, seqs, s);
     if (e != cudaSuccess) return cuda_fail(e, "sequence upload launch");
   }
+  std::vector<int> costs;
   // the pipeline over short items takes no item without a tile
-  const bool is_short = pairs.empty() && costs.back() > 0 && prefill_is_short(costs, cache->num_sms);
-  const cudaError_t e = launch_prefill_packed(a, items, pairs, is_short, cache->num_sms, s);
+  auto is_short = [&] { return costs.back() > 0 && prefill_is_short(costs, cache->num_sms); };
+  cudaError_t e;
+  if (folds) {
+    const std::vector<uint64_t> items = folded_schedule(a.geom, seqs, a.span, &costs);
+    const int split = folded_split(costs, cache->num_sms);
+    e = launch_prefill_folded(a, items, split, split == 1 && is_short(), cache->num_sms, s);
+  } else {
+    const std::vector<uint64_t> items = packed_schedule(a.geom, seqs, &costs);
+    const std::vector<uint64_t> pairs = prefill_pairs(items, costs, cache->num_sms);
+    e = launch_prefill_packed(a, items, pairs, pairs.empty() && is_short(), cache->num_sms, s);
+  }
   return e == cudaSuccess ? AOH_OK : cuda_fail(e, "packed prefill launch");
 } catch (const std::exception& x) {
   return fail(AOH_ERR_CUDA, "packed prefill: %s", x.what());

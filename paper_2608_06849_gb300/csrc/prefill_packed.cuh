@@ -5,6 +5,9 @@
 // sequence from its first key on, whatever row of the tensor that is, so a tile's first
 // key is always the tile's first row. Rows past a sequence's last key belong to the
 // next one; they are hidden by the mask and, as V rows, zeroed.
+//
+// Two kinds of items (packed_folds chooses): 128 rows of two heads, or 256 of one, as in a
+// cache's prefill (PackedArgs); or a few rows of all heads of a KV head (FoldedArgs).
 #pragma once
 
 #include "prefill_tile.cuh"
@@ -40,24 +43,19 @@ struct PackedItem {
       c_end = max(c_begin, tiles);
     }
   }
+  static constexpr int span = kBM;  // tokens of a query tile
   __device__ __forceinline__ int row0(int x) const { return two_heads ? q0 : q0 + x * kBM; }
   __device__ __forceinline__ int head(int x) const { return two_heads ? h + x : h; }
   __device__ __forceinline__ int tiles() const { return a_end + (c_end - c_begin); }
   __device__ __forceinline__ int chunk_tile(int i) const { return i < a_end ? i : c_begin + (i - a_end); }
   __device__ __forceinline__ int valid(const CacheGeom&, int i) const { return klen - chunk_tile(i) * kBN; }
-  __device__ __forceinline__ size_t out_row0(const PackedArgs&) const { return (size_t)qrow; }
+  __device__ __forceinline__ int row(int x, int r) const { return row0(x) + r; }
+  __device__ __forceinline__ bool has_row(int x, int r) const { return row(x, r) < len; }
+  __device__ __forceinline__ size_t out_row(const PackedArgs& a, int x, int r) const {
+    return (size_t)(qrow + row(x, r)) * a.geom.Hq + head(x);
+  }
   __device__ __forceinline__ int rot(const CacheGeom&) const { return 0; }
 };
-
-template <int D>
-__device__ __forceinline__ void load_kv(const PackedArgs& a, const PackedItem& t, int i, int sel, uint8_t* dst,
-                                        uint64_t* bar) {
-  using C = PfCfg<D>;
-  mbar_arrive_expect_tx(bar, C::KVBYTES);
-  const CUtensorMap* map = sel ? &a.tv : &a.tk;
-  for (int db = 0; db < C::DBLK; ++db)
-    tma_load_4d(dst + db * C::BOX, map, db * 64, t.kvh, t.krow + t.chunk_tile(i) * kBN, 0, bar);
-}
 
 template <int D>
 __device__ __forceinline__ void load_q(const PackedArgs& a, const PackedItem& t, int x, uint8_t* dst, uint64_t* bar) {
@@ -67,15 +65,92 @@ __device__ __forceinline__ void load_q(const PackedArgs& a, const PackedItem& t,
     tma_load_4d(dst + db * C::BOX, &a.tq, db * 64, t.head(x), t.qrow + t.row0(x), 0, bar);
 }
 
-// The keys of tile ja that row i (position off + i) sees, as in Mask.
+// A folded item is two query tiles, each of all G heads of a KV head at 128 / G neighbouring
+// tokens: row r of a tile is head r % G at its token r / G, the order in which a token's heads
+// lie in memory, so that a tile is one box of the queries' tensor (where G does not divide
+// 128 the last one or two rows of a tile are not used). Short rows thus fill their tiles with
+// heads, and the keys of a KV head are read once for all of its query heads.
+struct FoldedItem {
+  static constexpr int n_c = 0;  // no cached tiles
+  int G, span, rcp, kvh, q0, len, qrow, krow, klen, off, a_end, c_begin, c_end;
+  bool streaming;
+  __device__ __forceinline__ FoldedItem(const FoldedArgs& a, uint64_t code) {
+    const CacheGeom& g = a.geom;
+    G = g.G;
+    span = a.span;
+    rcp = a.rcp;
+    kvh = (int)(code >> 24) & 1023;
+    q0 = (int)(code & 0xffffffu) * (2 * span);
+    streaming = g.kind[kvh] != 0;
+    const int4 s = a.seqs.of((int)(code >> 34));
+    qrow = s.x;
+    len = s.y;
+    krow = s.z;
+    klen = s.w;
+    off = klen - len;
+    const int end = max(off + min(q0 + 2 * span, len), 0);
+    const int tiles = (end + kBN - 1) / kBN;
+    if (!streaming) {
+      a_end = c_begin = c_end = tiles;
+    } else {
+      a_end = (min(g.S, end) + kBN - 1) / kBN;
+      c_begin = max(a_end, max(0, g.wstart(off + q0)) / kBN);
+      c_end = max(c_begin, tiles);
+    }
+  }
+  // query tile x: its first token; row r of it: its token, whether there is one, and its place
+  // among the output's rows of D
+  __device__ __forceinline__ int row0(int x) const { return q0 + x * span; }
+  __device__ __forceinline__ int token(int r) const { return (r * rcp) >> 16; }  // r / G
+  __device__ __forceinline__ int row(int x, int r) const { return row0(x) + token(r); }
+  __device__ __forceinline__ bool has_row(int x, int r) const { return r < span * G && row(x, r) < len; }
+  __device__ __forceinline__ size_t out_row(const FoldedArgs& a, int x, int r) const {
+    return (size_t)(qrow + row0(x) + token(r)) * a.geom.Hq + kvh * G + (r - token(r) * G);
+  }
+  __device__ __forceinline__ int tiles() const { return a_end + (c_end - c_begin); }
+  __device__ __forceinline__ int chunk_tile(int i) const { return i < a_end ? i : c_begin + (i - a_end); }
+  __device__ __forceinline__ int valid(const CacheGeom&, int i) const { return klen - chunk_tile(i) * kBN; }
+  __device__ __forceinline__ int rot(const CacheGeom&) const { return 0; }
+};
+
+template <int D>
+__device__ __forceinline__ void load_q(const FoldedArgs& a, const FoldedItem& t, int x, uint8_t* dst, uint64_t* bar) {
+  using C = PfCfg<D>;
+  mbar_arrive_expect_tx(bar, C::DBLK * t.span * t.G * 128);
+  for (int db = 0; db < C::DBLK; ++db)
+    tma_load_4d(dst + db * C::BOX, &a.tq, db * 64, t.kvh * t.G, t.qrow + t.row0(x), 0, bar);
+}
+
+template <int D, class T>
+__device__ __forceinline__ void load_packed_kv(const PackedArgs& a, const T& t, int i, int sel, uint8_t* dst, uint64_t* bar) {
+  using C = PfCfg<D>;
+  mbar_arrive_expect_tx(bar, C::KVBYTES);
+  const CUtensorMap* map = sel ? &a.tv : &a.tk;
+  for (int db = 0; db < C::DBLK; ++db)
+    tma_load_4d(dst + db * C::BOX, map, db * 64, t.kvh, t.krow + t.chunk_tile(i) * kBN, 0, bar);
+}
+template <int D>
+__device__ __forceinline__ void load_kv(const PackedArgs& a, const PackedItem& t, int i, int sel, uint8_t* dst,
+                                        uint64_t* bar) {
+  load_packed_kv<D>(a, t, i, sel, dst, bar);
+}
+template <int D>
+__device__ __forceinline__ void load_kv(const FoldedArgs& a, const FoldedItem& t, int i, int sel, uint8_t* dst,
+                                        uint64_t* bar) {
+  load_packed_kv<D>(a, t, i, sel, dst, bar);
+}
+
+// The keys of tile ja that token i (position off + i) of a query tile from token qx0 on sees,
+// as in Mask.
 struct PackedMask {
   bool need;
   int e_hi, a0 = 0, a1 = 0;
   static constexpr int b0 = 0, b1 = 0;
-  __device__ __forceinline__ PackedMask(const CacheGeom& g, const PackedItem& t, int ja, int i, int qx0, int) {
+  template <class T>
+  __device__ __forceinline__ PackedMask(const CacheGeom& g, const T& t, int ja, int i, int qx0, int) {
     const int j0 = t.chunk_tile(ja) * kBN, jl = j0 + kBN - 1, pos = t.off + i;
     need = !(jl <= t.off + qx0 && jl < t.klen &&
-             (!t.streaming || jl < g.S || j0 >= g.wstart(t.off + qx0 + kBM - 1)));
+             (!t.streaming || jl < g.S || j0 >= g.wstart(t.off + qx0 + t.span - 1)));
     const int kmax = min(pos, t.klen - 1) - j0;
     e_hi = kmax + 1;
     if (t.streaming) {
@@ -91,6 +166,13 @@ struct CallOf<PackedArgs> {
   using ItemT = PackedItem;
   using MaskT = PackedMask;
   static constexpr bool kEmptyRows = true;  // fewer keys than rows
+  static constexpr bool kChained = true;
+};
+template <>
+struct CallOf<FoldedArgs> {
+  using ItemT = FoldedItem;
+  using MaskT = PackedMask;
+  static constexpr bool kEmptyRows = true;
   static constexpr bool kChained = true;
 };
 

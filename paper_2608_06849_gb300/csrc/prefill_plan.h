@@ -81,20 +81,118 @@ inline std::vector<uint64_t> prefill_schedule(const CacheGeom& g, const std::vec
 }
 
 // Packed prompts (PackedSeqs): row i of a sequence is the last but q_len - 1 - i of its
-// k_len positions. No tiles where every row lies before the first key.
-inline std::vector<uint64_t> packed_schedule(const CacheGeom& g, const std::vector<int4>& seqs, std::vector<int>* costs) {
+// k_len positions. The KV tiles that rows q0 .. q_end - 1 visit; none where every row lies before
+// the first key.
+inline int packed_tiles(const CacheGeom& g, const int4& seq, int q0, int q_end, bool streaming) {
   constexpr int BN = 128;
+  const int off = seq.w - seq.y, tiles = (std::max(off + q_end, 0) + BN - 1) / BN;
+  if (!streaming) return tiles;
+  const int a_end = std::min((g.S + BN - 1) / BN, tiles);
+  return a_end + std::max(0, tiles - std::max(a_end, std::max(0, g.wstart(off + q0)) / BN));
+}
+
+inline std::vector<uint64_t> packed_schedule(const CacheGeom& g, const std::vector<int4>& seqs, std::vector<int>* costs) {
   return prefill_items(
       g, (int)seqs.size(), [&](int b) { return seqs[b].y; },
-      [&](int b, int q0, int q_end, bool streaming) {
-        const int off = seqs[b].w - seqs[b].y;
-        const int end = std::max(off + q_end, 0);
-        if (!streaming) return (end + BN - 1) / BN;
-        const int a_end = (std::min(g.S, end) + BN - 1) / BN;
-        const int c_begin = std::max(a_end, std::max(0, g.wstart(off + q0)) / BN);
-        return a_end + std::max(0, (end + BN - 1) / BN - c_begin);
-      },
-      costs);
+      [&](int b, int q0, int q_end, bool streaming) { return packed_tiles(g, seqs[b], q0, q_end, streaming); }, costs);
+}
+
+// Folded items: 2 * span rows of all heads of a KV head, heaviest first.
+inline std::vector<uint64_t> folded_schedule(const CacheGeom& g, const std::vector<int4>& seqs, int span,
+                                             std::vector<int>* costs) {
+  struct Entry {
+    int cost, b, index;
+    bool streaming;
+  };
+  std::vector<Entry> entries;
+  size_t most = 0;
+  for (int b = 0; b < (int)seqs.size(); ++b)
+    for (int streaming = 0; streaming < 2; ++streaming) {
+      if ((streaming ? g.n_s : g.n_r) == 0) continue;
+      for (int q0 = 0; q0 < seqs[b].y; q0 += 2 * span) {
+        entries.push_back({packed_tiles(g, seqs[b], q0, std::min(q0 + 2 * span, seqs[b].y), streaming != 0), b,
+                           q0 / (2 * span), streaming != 0});
+        most += streaming ? g.n_s : g.n_r;
+      }
+    }
+  std::stable_sort(entries.begin(), entries.end(), [](const Entry& x, const Entry& y) { return x.cost > y.cost; });
+  std::vector<uint64_t> items;
+  items.reserve(most);
+  costs->reserve(most);
+  for (const Entry& e : entries)
+    for (int i = 0; i < (e.streaming ? g.n_s : g.n_r); ++i) {
+      items.push_back(prefill_item(e.b, e.streaming ? g.s_head[i] : g.r_head[i], e.index));
+      costs->push_back(e.cost);
+    }
+  return items;
+}
+
+// Whether folded items end well before plain ones, by the work that each leaves an SM and the
+// longest item, in visited tiles, with 4 tiles' time added to an item and 8 to a part of one.
+// Rows of more than a few hundred tokens fill plain items, which waste no row where G does not
+// divide 128 and are some percent faster then. Measured, us of a call in plain / folded items:
+// 33 x 7-34 tokens, 40/8 heads of 128: 28.4 / 14.9; 4 x 17 rows after 20,000, 32/8 heads of 64:
+// 100 / 56; 100 rows after 100,000, 28/4 heads of 128: 557 / 151; 4,000 tokens of 32/8 heads 94 /
+// 93, of 40/8 heads 122 / 132, of 24/8 heads 77 / 81; 16 x 101-2,999, 32/8 heads, half
+// streaming: 236 / 243.
+inline bool packed_folds(const CacheGeom& g, const std::vector<int4>& seqs, int span, int num_sms) {
+  if (g.G == 1) return false;  // the same items
+  struct Load {
+    long long work = 0, items = 0;
+    int longest = 0;
+  };
+  auto load_of = [&](auto parts) {  // parts(add): add(rows of an item, items a KV head and such rows)
+    Load l;
+    for (const int4& seq : seqs)
+      for (int streaming = 0; streaming < 2; ++streaming) {
+        const int heads = streaming ? g.n_s : g.n_r;
+        if (heads == 0) continue;
+        parts([&](int rows, int times) {
+          for (int q0 = 0; times > 0 && q0 < seq.y; q0 += rows) {
+            const int c = packed_tiles(g, seq, q0, std::min(q0 + rows, seq.y), streaming != 0);
+            l.work += (long long)heads * times * c;
+            l.items += heads * times;
+            l.longest = std::max(l.longest, c);
+          }
+        });
+      }
+    return l;
+  };
+  // tiles' time to the end on clusters of c CTAs an item
+  auto end_of = [&](const Load& l, int c) {
+    const long long extra = c == 1 ? 4 : 8;
+    return std::max((double)(l.work + l.items * c * extra) / num_sms, (double)((l.longest + c - 1) / c + extra));
+  };
+  const Load plain = load_of([&](auto add) { add(128, g.G / 2), add(256, g.G % 2); });
+  const Load folded = load_of([&](auto add) { add(2 * span, 1); });
+  double p = end_of(plain, 1), f = end_of(folded, 1);
+  if (plain.longest >= 7 && plain.items <= num_sms / 2) p = std::min(p, end_of(plain, 2));
+  for (int c = 2; c <= 8 && folded.longest >= 7 && folded.items <= num_sms; c *= 2) f = std::min(f, end_of(folded, c));
+  return f < 0.9 * p;
+}
+
+// CTAs that share each folded item (clusters of 1, 2, 4 or 8), by the end of
+// longest-first schedules in visited tiles, with 4 tiles' time added to an item and 8 to a
+// part of one.
+inline int folded_split(const std::vector<int>& costs, int num_sms) {
+  const int n = (int)costs.size();
+  if (n > kPrefillSplitMost || n > 4 * num_sms || costs[0] < 7) return 1;
+  std::vector<int> free_at;  // a min-heap
+  int best = 0, pick = 1;
+  for (int c = 1; c <= 8; c *= 2) {
+    free_at.assign(std::max(1, num_sms / c), 0);
+    int end = 0;
+    for (int cost : costs) {
+      std::pop_heap(free_at.begin(), free_at.end(), std::greater<int>());
+      end = std::max(end, free_at.back() += c == 1 ? cost + 4 : (cost + c - 1) / c + 8);
+      std::push_heap(free_at.begin(), free_at.end(), std::greater<int>());
+    }
+    if (c == 1 || end < best) {
+      best = end;
+      pick = c;
+    }
+  }
+  return pick;
 }
 
 // The work of clusters of two CTAs, two entries a cluster: two items, or one item

@@ -62,6 +62,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const CacheGeom& g = a.geom;
   const int P = gridDim.x, cta = blockIdx.x;
+  if constexpr (Call::kChained) wait_to_start(a);
   // this CTA's k-th item
   auto item_index = [&](int k) { return k * P + ((k & 1) ? P - 1 - cta : cta); };
   auto item_code = [&](int i) { return CAP > 0 ? wl.item[i] : a.work[i]; };
@@ -234,7 +235,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int ii = item_index(k);
       if (ii >= n_items) break;
       const typename Call::ItemT t(a, item_code(ii));
-      const int qx0 = t.row0(x), i = qx0 + r, n = t.tiles();
+      const int qx0 = t.row0(x), i = t.row(x, r), n = t.tiles();
       const int rot = t.rot(g);
       float m = -INFINITY, l = 0.f;
       for (int jj = 0; jj < n && ok; ++jj, ++kt) {
@@ -249,7 +250,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       ok = __all_sync(0xffffffffu, wait_bar(&pv_done[x], (kt - 1) & 1, a.err, abort_flag));
       if (!ok) break;
       tc_fence_after();
-      store_o<D, X::COLS>(a, t, x, qx0 + q4 * 32, tl + o_col, l, stage, lane);
+      store_o<D, X::COLS>(a, t, x, q4 * 32, tl + o_col, l, stage, lane);
       tc_fence_before();
     }
   }
@@ -258,7 +259,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncthreads();
   tc_fence_after();
   if (warp == 1) tmem_dealloc(tmem, kTmemCols);
-  if constexpr (Call::kChained) asm volatile("griddepcontrol.wait;" ::: "memory");
+  if constexpr (Call::kChained) wait_to_end(a);
 }
 
 }  // namespace pf

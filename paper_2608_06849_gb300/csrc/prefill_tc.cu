@@ -18,13 +18,14 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
   return fn;
 }
 
-bool make_rows_map(CUtensorMap* map, const void* base, int B, long long T, int H, int D, long long stride) {
+bool make_rows_map(CUtensorMap* map, const void* base, int B, long long T, int H, int D, long long stride, int rows,
+                   int heads) {
   auto fn = encode_fn();
   if (!fn) return false;
   if (stride == 0) stride = (long long)H * D;
   cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)H, (cuuint64_t)T, (cuuint64_t)B};
   cuuint64_t strides[3] = {(cuuint64_t)D * 2, (cuuint64_t)stride * 2, (cuuint64_t)T * stride * 2};
-  cuuint32_t box[4] = {64, 1, 128, 1};
+  cuuint32_t box[4] = {64, (cuuint32_t)heads, (cuuint32_t)rows, 1};
   cuuint32_t estr[4] = {1, 1, 1, 1};
   CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr,
                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
@@ -36,12 +37,12 @@ namespace {
 
 constexpr int kSmall = 640;  // items of a launch that copies 5 KB of arguments instead of 30
 
-template <int D, bool PAIRS, int CAP>
+template <int D, int MODE, int CAP>
 cudaError_t launch_cfg(const PrefillTcArgs& a, const std::vector<uint64_t>& items, cudaStream_t s) {
   using C = PfCfg<D>;
   static std::atomic<uint64_t> done{0};
   const cudaError_t e = once_per_device(done, [] {
-    return cudaFuncSetAttribute(prefill_tc_kernel<PrefillTcArgs, D, PAIRS, CAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+    return cudaFuncSetAttribute(prefill_tc_kernel<PrefillTcArgs, D, MODE, CAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
   });
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
@@ -54,19 +55,19 @@ cudaError_t launch_cfg(const PrefillTcArgs& a, const std::vector<uint64_t>& item
   attr[0].val.clusterDim.x = 2;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = PAIRS ? 1 : 0;
+  cfg.numAttrs = MODE == kPairs ? 1 : 0;
   WorkList<CAP> wl;
   if (CAP > 0) memcpy(wl.item, items.data(), items.size() * sizeof(uint64_t));
-  return cudaLaunchKernelEx(&cfg, prefill_tc_kernel<PrefillTcArgs, D, PAIRS, CAP>, a, wl);
+  return cudaLaunchKernelEx(&cfg, prefill_tc_kernel<PrefillTcArgs, D, MODE, CAP>, a, wl);
 }
 
 template <int D>
 cudaError_t launch_d(const PrefillTcArgs& a, const std::vector<uint64_t>& items, const std::vector<uint64_t>& pairs,
                      cudaStream_t s) {
-  if (!pairs.empty()) return launch_cfg<D, true, 2 * kPrefillSplitMost>(a, pairs, s);
-  if (items.size() <= kSmall) return launch_cfg<D, false, kSmall>(a, items, s);
-  if (items.size() <= kPrefillByValue) return launch_cfg<D, false, kPrefillByValue>(a, items, s);
-  return launch_cfg<D, false, 0>(a, items, s);
+  if (!pairs.empty()) return launch_cfg<D, kPairs, 2 * kPrefillSplitMost>(a, pairs, s);
+  if (items.size() <= kSmall) return launch_cfg<D, kWhole, kSmall>(a, items, s);
+  if (items.size() <= kPrefillByValue) return launch_cfg<D, kWhole, kPrefillByValue>(a, items, s);
+  return launch_cfg<D, kWhole, 0>(a, items, s);
 }
 
 }  // namespace

@@ -48,12 +48,15 @@
 namespace aoh {
 namespace pf {
 
-// PAIRS: clusters of two CTAs, each with its entry of the list. Where both have the
+// kPairs: clusters of two CTAs, each with its entry of the list. Where both have the
 // same item's halves, each visits half of its KV tiles; then each finishes one of
 // the two query tiles: it receives the other
 // CTA's state of that tile (O, running max and sum) in shared memory that the
 // main loop no longer needs, adds its own and writes the rows.
-template <class A, int D, bool PAIRS, int CAP>
+// kSplit: clusters of C = 2, 4 or 8 CTAs, an item each: every CTA visits a C-th of its KV tiles
+// and finishes a C-th of its 256 rows, whose states it receives from all (its own among them).
+constexpr int kWhole = 0, kPairs = 1, kSplit = 2;
+template <class A, int D, int MODE, int CAP>
 __global__ void __launch_bounds__(kThreads, 1)
     prefill_tc_kernel(const __grid_constant__ A a, const __grid_constant__ WorkList<CAP> wl) {
   using C = PfCfg<D>;
@@ -80,16 +83,21 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   // the append may start once the last CTAs of this grid run (append.cu)
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const uint64_t code = CAP > 0 ? wl.item[blockIdx.x] : a.work[blockIdx.x];
+  if constexpr (Call::kChained) wait_to_start(a);
+  constexpr bool PAIRS = MODE == kPairs, SPLIT = MODE == kSplit;
+  const int lg_ctas = SPLIT ? __ffs((int)cluster_ctas()) - 1 : 1;
+  const int entry = SPLIT ? blockIdx.x >> lg_ctas : blockIdx.x;
+  const uint64_t code = CAP > 0 ? wl.item[entry] : a.work[entry];
   if (PAIRS && code == kPrefillNone) return;
-  const bool half = PAIRS && code >= kPrefillHalf;  // alike in both CTAs of a cluster
+  const bool half = SPLIT || (PAIRS && code >= kPrefillHalf);  // alike in all CTAs of a cluster
   const typename Call::ItemT t(a, code & ~kPrefillHalf);
   const CacheGeom& g = a.geom;
   const int n_all = t.tiles();
   // this CTA visits tiles t0 .. t0 + n_tiles - 1 of the item's n_all
   const int rank = half ? (int)cluster_rank() : 0;
-  const int t0 = rank * ((n_all + 1) / 2);
-  const int n_tiles = !half ? n_all : rank == 0 ? (n_all + 1) / 2 : n_all / 2;
+  const int per = SPLIT ? (n_all + (1 << lg_ctas) - 1) >> lg_ctas : (n_all + 1) / 2;
+  const int t0 = rank * per;
+  const int n_tiles = !half ? n_all : SPLIT ? max(0, min(per, n_all - t0)) : rank == 0 ? (n_all + 1) / 2 : n_all / 2;
   if (threadIdx.x == 0) {
     mbar_init(q_full, 2);
     for (int s = 0; s < kNS; ++s) {
@@ -247,7 +255,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int q4 = warp & 3;              // TMEM lane quarter this warp may access
     const int r = q4 * 32 + lane;
     const int qx0 = t.row0(x);            // first row of this query tile
-    const int i = qx0 + r;
+    const int i = t.row(x, r);            // of the sequence
     const uint32_t tl = tmem + ((uint32_t)(q4 * 32) << 16);
     const uint32_t s_col = x * 128, o_col = 256 + x * D;
     const int rot = t.rot(g);
@@ -270,14 +278,82 @@ __global__ void __launch_bounds__(kThreads, 1)
                       __all_sync(0xffffffffu, wait_bar(&pv_done[x], (n_tiles - 1) & 1, a.err, abort_flag)))) {
       tc_fence_after();
       // Q_X is free: the last S_X was done before the last P V
-      store_o<D, D>(a, t, x, qx0 + q4 * 32, tl + o_col, l, sQ + x * C::QBYTES + q4 * (C::QBYTES / 4), lane);
+      store_o<D, D>(a, t, x, q4 * 32, tl + o_col, l, sQ + x * C::QBYTES + q4 * (C::QBYTES / 4), lane);
     }
   }
 
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (half) {
+  if constexpr (SPLIT) {
+    // all CTAs' copies and MMAs are done with their shared memory
+    cluster_arrive();
+    cluster_wait();
+    // receive buffer: [C][D / 4][256 / C rows] float4, then [C][256 / C rows] (m, l)
+    const int C2 = 1 << lg_ctas, lg_rows = 8 - lg_ctas, rows = 1 << lg_rows;
+    float4* recv = reinterpret_cast<float4*>(smem);
+    float2* recv_ml = reinterpret_cast<float2*>(recv + D / 4 * 256);
+    const int x = (warp - 2) >> 2, q4 = warp & 3, r = q4 * 32 + lane;
+    if (warp >= 2) {
+      const int row = x * 128 + r, dst = row >> lg_rows, at = row & (rows - 1);
+      const uint32_t tl = tmem + ((uint32_t)(q4 * 32) << 16) + 256 + x * D;
+      const uint32_t to = cluster_addr(recv + ((rank * (D / 4)) << lg_rows) + at, (uint32_t)dst);
+      cluster_st2(cluster_addr(recv_ml + (rank << lg_rows) + at, (uint32_t)dst), __float_as_uint(end_m),
+                  __float_as_uint(end_l));
+      if (n_tiles > 0) {
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t v[32];
+          tmem_ld32(tl + c * 32, v);
+          tmem_ld_wait();
+#pragma unroll
+          for (int e = 0; e < 32; e += 4)
+            cluster_st4(to + (uint32_t)(((c * 8 + e / 4) << lg_rows) * 16), v[e], v[e + 1], v[e + 2], v[e + 3]);
+        }
+      }
+      tc_fence_before();
+    }
+    cluster_arrive();
+    cluster_wait();
+    // the eight warps: rows in groups of 32 (8 / C of them), columns in C groups; a lane a row
+    if (warp >= 2) {
+      const int w = warp - 2, groups = 8 >> lg_ctas, rg = w & (groups - 1), cg = w >> (3 - lg_ctas);
+      const int at = rg * 32 + lane, row = (rank << lg_rows) + at, ox = row >> 7, orow = row & 127;
+      float M = -INFINITY;
+      for (int c = 0; c < C2; ++c) M = fmaxf(M, recv_ml[(c << lg_rows) + at].x);
+      // a state of -inf saw no key (its CTA may have had no tile: unwritten values); any other
+      // state counts
+      float wt[8], L = 0.f;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        wt[c] = 0.f;
+        if (c >= C2) continue;
+        const float2 ml = recv_ml[(c << lg_rows) + at];
+        wt[c] = ml.x == -INFINITY ? -1.f : fast_exp2(ml.x - M);
+        if (ml.x != -INFINITY) L += wt[c] * ml.y;
+      }
+      const float inv = L == 0.f ? 0.f : 1.f / L;
+      if (end_ok && t.has_row(ox, orow)) {
+        bf16* out = static_cast<bf16*>(a.out) + t.out_row(a, ox, orow) * D;
+        for (int k = cg * (D / 4) >> lg_ctas; k < (cg + 1) * (D / 4) >> lg_ctas; ++k) {
+          float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+          for (int c = 0; c < 8; ++c) {
+            if (c >= C2 || wt[c] < 0.f) continue;
+            const float4 z = recv[((c * (D / 4) + k) << lg_rows) + at];
+            const float f = wt[c] * inv;
+            o.x += f * z.x;
+            o.y += f * z.y;
+            o.z += f * z.z;
+            o.w += f * z.w;
+          }
+          *reinterpret_cast<uint2*>(out + k * 4) = make_uint2(float2_to_bf16x2(o.x, o.y), float2_to_bf16x2(o.z, o.w));
+        }
+      }
+    }
+    __syncthreads();
+    tc_fence_after();
+  } else if (half) {
     // both CTAs' copies and MMAs are done with their shared memory
     cluster_arrive();
     cluster_wait();
@@ -333,15 +409,14 @@ __global__ void __launch_bounds__(kThreads, 1)
           put_row<D>(stage, lane, c * 4 + e / 8, y);
         }
       }
-      write_rows<D, D>(a, t, x, t.row0(x) + q4 * 32, 0, stage, lane);
+      write_rows<D, D>(a, t, x, q4 * 32, 0, stage, lane);
       tc_fence_before();
     }
     __syncthreads();
     tc_fence_after();
   }
   if (warp == 1) tmem_dealloc(tmem, kTmemCols);
-  // a launch that started under the one before it ends after it
-  if constexpr (Call::kChained) asm volatile("griddepcontrol.wait;" ::: "memory");
+  if constexpr (Call::kChained) wait_to_end(a);
 }
 
 }  // namespace pf

@@ -91,8 +91,13 @@ struct Item {
   __device__ __forceinline__ int row0(int x) const { return two_heads ? q0 : q0 + x * kBM; }
   __device__ __forceinline__ int head(int x) const { return two_heads ? h + x : h; }
   __device__ __forceinline__ int tiles() const { return n_c + a_end + (c_end - c_begin); }
-  // row 0 of the sequence among the output's rows
-  __device__ __forceinline__ size_t out_row0(const PrefillTcArgs& a) const { return (size_t)b * a.T; }
+  // row r of query tile x: its row of the chunk, whether there is one, and its place among the
+  // output's rows of D
+  __device__ __forceinline__ int row(int x, int r) const { return row0(x) + r; }
+  __device__ __forceinline__ bool has_row(int x, int r) const { return row(x, r) < len; }
+  __device__ __forceinline__ size_t out_row(const PrefillTcArgs& a, int x, int r) const {
+    return ((size_t)b * a.T + row(x, r)) * a.geom.Hq + head(x);
+  }
   // oldest ring slot of a wrapped cached ring
   __device__ __forceinline__ int rot(const CacheGeom& g) const { return (streaming && Lb > g.S + g.W) ? (Lb - g.S) % g.W : 0; }
   // visited tile i: the chunk tile, for i >= n_c
@@ -231,8 +236,20 @@ struct CallOf<PrefillTcArgs> {
   using ItemT = Item;
   using MaskT = Mask;
   static constexpr bool kEmptyRows = false;
-  static constexpr bool kChained = false;  // launches that follow one another without a wait between
+  static constexpr bool kChained = false;  // launches overlap the one before (wait_to_start, wait_to_end)
 };
+
+// A call's first launch waits for the kernel before it once it runs; one that follows
+// another of the same call (a.follows) starts under it, the two being independent, and ends
+// after it.
+template <class A>
+__device__ __forceinline__ void wait_to_start(const A& a) {
+  if (!a.follows) asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+template <class A>
+__device__ __forceinline__ void wait_to_end(const A& a) {
+  if (a.follows) asm volatile("griddepcontrol.wait;" ::: "memory");
+}
 
 // The softmax of one landed S tile, one row (TMEM lane) a thread: reads the row,
 // hides keys, moves the running max m (rescaling O in TMEM when it grew by more
@@ -380,28 +397,28 @@ __device__ __forceinline__ void put_row(uint8_t* stage, int lane, int chunk, con
   *reinterpret_cast<uint4*>(stage + lane * (D * 2) + ((chunk ^ (lane % CH)) << 4)) = w;
 }
 
-// COLS columns, from col0 on, of rows i0 .. i0 + 31 of the chunk (those below len), query
-// tile x's head, from the warp's `stage`.
+// COLS columns, from col0 on, of rows row0 .. row0 + 31 of query tile x (those there are), from
+// the warp's `stage`.
 template <int D, int COLS, class A, class T>
-__device__ __forceinline__ void write_rows(const A& a, const T& t, int x, int i0, int col0,
+__device__ __forceinline__ void write_rows(const A& a, const T& t, int x, int row0, int col0,
                                            const uint8_t* stage, int lane) {
   constexpr int CH = COLS / 8, RPI = 32 / CH;  // chunks a row, rows a step
   __syncwarp();
   const int c = lane % CH;
-  bf16* out = static_cast<bf16*>(a.out) + (t.out_row0(a) * a.geom.Hq + t.head(x)) * D + col0 + c * 8;
+  bf16* out = static_cast<bf16*>(a.out) + col0 + c * 8;
 #pragma unroll
   for (int r0 = 0; r0 < 32; r0 += RPI) {
     const int r = r0 + lane / CH;
     const uint4 w = *reinterpret_cast<const uint4*>(stage + r * (COLS * 2) + ((c ^ (r % CH)) << 4));
-    if (i0 + r < t.len) *reinterpret_cast<uint4*>(out + (size_t)(i0 + r) * a.geom.Hq * D) = w;
+    if (t.has_row(x, row0 + r)) *reinterpret_cast<uint4*>(out + t.out_row(a, x, row0 + r) * D) = w;
   }
 }
 
-// Write a warp's 32 finished rows of query tile x's O (each lane's times its inv), the
-// first of them row i0 of the chunk, COLS columns at a time. taddr: O's first
+// Write a warp's 32 finished rows of query tile x's O (each lane's divided by its l), the
+// first of them row row0 of the tile, COLS columns at a time. taddr: O's first
 // column, stage: 32 * COLS * 2 bytes, l: the row's sum (0: it saw no key).
 template <int D, int COLS, class A, class T>
-__device__ __forceinline__ void store_o(const A& a, const T& t, int x, int i0, uint32_t taddr, float l,
+__device__ __forceinline__ void store_o(const A& a, const T& t, int x, int row0, uint32_t taddr, float l,
                                         uint8_t* stage, int lane) {
   const float inv = 1.f / l;
   const bool none = CallOf<A>::kEmptyRows && l == 0.f;
@@ -418,7 +435,7 @@ __device__ __forceinline__ void store_o(const A& a, const T& t, int x, int i0, u
       put_row<COLS>(stage, lane, c % (COLS / 32) * 4 + e / 8, y);
     }
     if ((c + 1) * 32 % COLS == 0) {
-      write_rows<D, COLS>(a, t, x, i0, (c + 1) * 32 - COLS, stage, lane);
+      write_rows<D, COLS>(a, t, x, row0, (c + 1) * 32 - COLS, stage, lane);
       __syncwarp();
     }
   }

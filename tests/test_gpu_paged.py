@@ -55,6 +55,15 @@ PROMPTS = [
     ([3 + 5 * (i % 7) for i in range(70)], None, 4, 2, 64, [0, 1], 8, 9),
     ([140 + 31 * (i % 5) for i in range(40)], None, 24, 8, 128, [0, 1] * 4, 8, 100),
     ([40] * 130, [60] * 130, 32, 8, 64, [0] * 8, 0, 1),
+    # few rows of many heads: heads fold into the tiles; after long prefixes the keys are split
+    ([17, 3, 1], [3000, 2999, 1], 32, 8, 64, [0, 1] * 4, 10, 500),
+    ([33, 20], [2500, 900], 7, 1, 128, [0], 0, 1),
+    ([5, 100, 26], [2049, 10, 1500], 10, 2, 128, [0, 1], 100, 300),
+    ([16, 9], [1900, 1281], 16, 1, 128, [0], 0, 1),
+    ([9] * 30, [9 + 50 * (i % 4) for i in range(30)], 24, 2, 64, [1, 0], 3, 70),
+    ([30 - i % 25 for i in range(70)], None, 40, 8, 128, [0, 1] * 4, 2, 11),
+    ([70], [1111], 6, 2, 128, [0, 1], 128, 129),
+    ([1, 1, 1, 1], [5000, 100, 1, 640], 8, 1, 128, [0], 0, 1),
 ]
 
 
@@ -124,6 +133,28 @@ def test_prompts_do_not_see_their_neighbours():
     pc.check()
     keep = list(range(70)) + list(range(270, 303))
     assert torch.equal(out[keep], again[keep])
+
+
+@pytest.mark.parametrize("case", [2, 6, 10, 13])
+def test_prompts_in_a_graph(case):
+    """A captured call, by-value sequences and uploaded ones, replays with new inputs."""
+    q_lens, k_lens, hq, hkv, d, labels, sink, window = PROMPTS[case]
+    q, k, v = prompt_inputs(q_lens, k_lens, hq, hkv, d, seed=1)
+    pc = aoh.PagedCache(1, 16, hq, hkv, d, sink, window, labels, max_seqs=len(q_lens))
+    out = torch.empty_like(q)
+    pc.prefill(q, k, v, q_lens, out, k_lens=k_lens)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        pc.prefill(q, k, v, q_lens, out, k_lens=k_lens)
+    q2, k2, v2 = prompt_inputs(q_lens, k_lens, hq, hkv, d, seed=7)
+    want = torch.empty_like(q)
+    pc.prefill(q2, k2, v2, q_lens, want, k_lens=k_lens)
+    for x, y in ((q, q2), (k, k2), (v, v2)):
+        x.copy_(y)
+    out.fill_(float("nan"))
+    graph.replay()
+    pc.check()
+    assert torch.equal(out, want)
 
 
 # ------------------------------------------------------------------ pages
@@ -451,6 +482,28 @@ def test_a_prompt_continued_from_its_pages(form):
     p.cache.check()
     assert np.array_equal(f64(k_held), p.held(f64(k)))
     check_prompts(out, q, k_held, v_held, rows, total, labels, sink, window, "continued")
+
+
+@pytest.mark.parametrize("form", ["bf16", "e4m3"])
+def test_offsets_past_32_bits(form):
+    """Pages at the end of a pool of more than 2^32 elements."""
+    hq, hkv, d, page, lens = 8, 8, 128, 128, [300, 5]
+    n_pages = 2 ** 32 // (2 * hkv * page * d) + 700
+    pc = aoh.PagedCache(n_pages, page, hq, hkv, d, 0, 1, [0] * hkv, form=form, max_seqs=2)
+    assert pc.nbytes > 2 ** 32
+    table = ints([[n_pages - 1, n_pages - 3, n_pages - 2], [n_pages - 600, 0, 1]])
+    k, v, q = randn((sum(lens), hkv, d), 1), randn((sum(lens), hkv, d), 2), randn((2, hq, d), 3)
+    at = sums(lens)
+    pc.append(k, v, ints(lens), table, cu_rows=ints(at))
+    held = [torch.empty_like(k), torch.empty_like(v)]
+    pc.read(table, ints(at), *held)
+    out = torch.empty_like(q)
+    pc.decode(q, ints(lens), table, out)
+    pc.check()
+    want = [f64(k), f64(v)] if form == "bf16" else [opaged.decode(*opaged.encode(f64(x))) for x in (k, v)]
+    for x, w in zip(held, want):
+        assert np.array_equal(f64(x), w)
+    check_decode(out, q, [tuple(w[a:b] for w in want) for a, b in zip(at, at[1:])], [0] * hkv, 0, 1, "far pages")
 
 
 def test_out_of_range_tables_are_reported():

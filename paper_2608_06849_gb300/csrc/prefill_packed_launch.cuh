@@ -10,7 +10,8 @@
 namespace aoh {
 namespace pf {
 
-constexpr int kSmall = 640;  // items of a launch that copies 7 KB of arguments instead of 32
+// items of a launch that copies 2 or 7 KB of arguments instead of 32
+constexpr int kTiny = 64, kSmall = 640;
 
 // The launch overlaps the kernel before it.
 template <class A, class K, int CAP, class... More>
@@ -64,6 +65,7 @@ cudaError_t launch_short(const A& a, const uint64_t* items, int n, int num_sms, 
 template <class A, int D>
 cudaError_t launch_all(A a, const std::vector<uint64_t>& items, bool is_short, int num_sms, cudaStream_t s) {
   const size_t n = items.size();
+  if (n <= kTiny && !is_short) return launch_items<A, D, kWhole, kTiny>(a, items.data(), (int)n, 1, s);
   if (n <= kSmall && !is_short) return launch_items<A, D, kWhole, kSmall>(a, items.data(), (int)n, 1, s);
   for (size_t i = 0; i < n; i += kPrefillByValue) {
     const int m = (int)(n - i < (size_t)kPrefillByValue ? n - i : (size_t)kPrefillByValue);

@@ -62,7 +62,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const CacheGeom& g = a.geom;
   const int P = gridDim.x, cta = blockIdx.x;
-  if constexpr (Call::kChained) wait_to_start(a);
+  if constexpr (Call::kChained)
+    if (threadIdx.x == 0) prefetch_maps(a);
   // this CTA's k-th item
   auto item_index = [&](int k) { return k * P + ((k & 1) ? P - 1 - cta : cta); };
   auto item_code = [&](int i) { return CAP > 0 ? wl.item[i] : a.work[i]; };
@@ -92,6 +93,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  if constexpr (Call::kChained) wait_to_start(a);
 
   if (warp == 0) {
     // ------------------------------------------------------------ producer

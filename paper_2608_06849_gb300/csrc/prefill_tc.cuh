@@ -83,7 +83,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   // the append may start once the last CTAs of this grid run (append.cu)
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  if constexpr (Call::kChained) wait_to_start(a);
+  if constexpr (Call::kChained) {
+    if (threadIdx.x == 0) prefetch_maps(a);
+    if (a.seqs.table != nullptr) wait_to_start(a);  // the item is read from device memory
+  }
   constexpr bool PAIRS = MODE == kPairs, SPLIT = MODE == kSplit;
   const int lg_ctas = SPLIT ? __ffs((int)cluster_ctas()) - 1 : 1;
   const int entry = SPLIT ? blockIdx.x >> lg_ctas : blockIdx.x;
@@ -116,6 +119,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     *abort_flag = 0;
     fence_mbar_init();
     fence_proxy_async_smem();
+    if constexpr (Call::kChained) wait_to_start(a);
     // the first loads need no other warp
     load_q<D>(a, t, 0, sQ, q_full);
     load_q<D>(a, t, 1, sQ + C::QBYTES, q_full);
@@ -129,6 +133,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  if constexpr (Call::kChained) wait_to_start(a);
 
   // a half: a row's final softmax state (softmax warps)
   float end_m = -INFINITY, end_l = 0.f;

@@ -239,6 +239,13 @@ struct CallOf<PrefillTcArgs> {
   static constexpr bool kChained = false;  // launches overlap the one before (wait_to_start, wait_to_end)
 };
 
+template <class A>
+__device__ __forceinline__ void prefetch_maps(const A& a) {
+  prefetch_tmap(&a.tq);
+  prefetch_tmap(&a.tk);
+  prefetch_tmap(&a.tv);
+}
+
 // A call's first launch waits for the kernel before it once it runs; one that follows
 // another of the same call (a.follows) starts under it, the two being independent, and ends
 // after it.

@@ -351,7 +351,9 @@ aoh_status aoh_paged_prefill(aoh_paged* cache, const void* q, const void* k, con
   cudaError_t e;
   if (folds) {
     const std::vector<uint64_t> items = folded_schedule(a.geom, seqs, a.span, &costs);
-    const int split = folded_split(costs, cache->num_sms);
+    bool lone = true;
+    for (const int4& b : seqs) lone = lone && b.y <= a.span;
+    const int split = folded_split(costs, lone, decode_tc_max_clusters(16), cache->num_sms);
     e = launch_prefill_folded(a, items, split, split == 1 && is_short(), cache->num_sms, s);
   } else {
     const std::vector<uint64_t> items = packed_schedule(a.geom, seqs, &costs);

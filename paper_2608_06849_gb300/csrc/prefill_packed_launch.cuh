@@ -43,8 +43,12 @@ template <class A, int D, int MODE, int CAP>
 cudaError_t launch_items(const A& a, const uint64_t* items, int n, int each, cudaStream_t s) {
   auto kernel = prefill_tc_kernel<A, D, MODE, CAP>;
   static std::atomic<uint64_t> done{0};
-  const cudaError_t e = once_per_device(
-      done, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, PfCfg<D>::SMEM); });
+  const cudaError_t e = once_per_device(done, [&] {
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, PfCfg<D>::SMEM);
+    if (e == cudaSuccess && MODE == kSplit)
+      e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    return e;
+  });
   if (e != cudaSuccess) return e;
   return launch<A, decltype(kernel), CAP>(kernel, PfCfg<D>::SMEM, n * each, MODE == kPairs ? 2 : each, a, items, n, s);
 }

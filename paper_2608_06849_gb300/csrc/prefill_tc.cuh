@@ -53,8 +53,11 @@ namespace pf {
 // the two query tiles: it receives the other
 // CTA's state of that tile (O, running max and sum) in shared memory that the
 // main loop no longer needs, adds its own and writes the rows.
-// kSplit: clusters of C = 2, 4 or 8 CTAs, an item each: every CTA visits a C-th of its KV tiles
-// and finishes a C-th of its 256 rows, whose states it receives from all (its own among them).
+// kSplit: clusters of C = 2, 4, 8 or 16 CTAs, an item each: every CTA visits a C-th of its KV
+// tiles and finishes a C-th of its 256 rows, whose states it receives from all (its own among
+// them). An item whose second query tile has no row is a lone one: both halves of the
+// pipeline work on its first tile, A on the even KV tiles and B on the odd ones, and their states
+// count as those of two CTAs.
 constexpr int kWhole = 0, kPairs = 1, kSplit = 2;
 template <class A, int D, int MODE, int CAP>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -101,6 +104,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int per = SPLIT ? (n_all + (1 << lg_ctas) - 1) >> lg_ctas : (n_all + 1) / 2;
   const int t0 = rank * per;
   const int n_tiles = !half ? n_all : SPLIT ? max(0, min(per, n_all - t0)) : rank == 0 ? (n_all + 1) / 2 : n_all / 2;
+  const bool lone = SPLIT && !t.has_row(1, 0);
   if (threadIdx.x == 0) {
     mbar_init(q_full, 2);
     for (int s = 0; s < kNS; ++s) {
@@ -187,7 +191,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     auto s_of = [&](int x, int jj) {
       const uint64_t k_desc = k_desc0 + (uint32_t)(((2 * jj) % kNS) * sdesc_step(C::KVBYTES));
       if (elect_one()) {
-        issue_s<D>(tmem, q_desc + sdesc_step(x * C::QBYTES), k_desc, x);
+        issue_s<D>(tmem, q_desc + (lone ? 0u : sdesc_step(x * C::QBYTES)), k_desc, x);
         tc_commit(&s_full[x]);
       }
     };
@@ -199,21 +203,22 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (ok) ok = __all_sync(0xffffffffu, wait_bar(bar, parity, a.err, abort_flag));
       return ok;
     };
-    // O_X += P_X(jj) V_jj: the first half of the keys while the softmax forms the
+    // O_X += P_X(step) V_jj: the first half of the keys while the softmax forms the
     // second half's weights
-    auto pv_of = [&](int x, int jj) {
+    auto pv_at = [&](int x, int step, int jj) {
       const uint64_t v_desc = v_desc0 + (uint32_t)(((2 * jj + 1) % kNS) * sdesc_step(C::KVBYTES));
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        if (!wait(&p_full[2 * x + half], jj & 1)) return false;
+        if (!wait(&p_full[2 * x + half], step & 1)) return false;
         tc_fence_after();
         if (elect_one()) {
-          issue_pv<D>(tmem, v_desc, x, half, jj == 0);
+          issue_pv<D>(tmem, v_desc, x, half, step == 0);
           if (half) tc_commit(&pv_done[x]);
         }
       }
       return true;
     };
+    auto pv_of = [&](int x, int jj) { return pv_at(x, jj, jj); };
     auto wait_k = [&](int jj) { return wait(&kv_full[(2 * jj) % kNS], ((2 * jj) / kNS) & 1); };
     // only the last cached tile and the last chunk tile can be partial
     int n_partial = 0;  // partial V tiles seen so far (index into v_zeroed)
@@ -227,13 +232,30 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       return true;
     };
-    if (wait(q_full, 0) && wait_k(0)) {
+    if (SPLIT && lone) {
+      // S_X of tile j, whose K is then free
+      auto lone_s = [&](int x, int j) {
+        if (j >= n_tiles) return true;
+        if (!wait_k(j)) return false;
+        tc_fence_after();
+        s_of(x, j);
+        commit(&kv_empty[(2 * j) % kNS]);
+        return true;
+      };
+      if (wait(q_full, 0) && lone_s(0, 0)) lone_s(1, 1);
+      for (int j = 0; j < n_tiles && ok; ++j) {
+        const int x = j & 1;
+        if (!wait_v(j) || !pv_at(x, j >> 1, j)) break;
+        commit(&kv_empty[(2 * j + 1) % kNS]);
+        if (!lone_s(x, j + 2)) break;
+      }
+    } else if (wait(q_full, 0) && wait_k(0)) {
       tc_fence_after();
       s_of(0, 0);
       s_of(1, 0);
       commit(&kv_empty[0]);
     }
-    for (int jj = 0; jj < n_tiles && ok; ++jj) {
+    for (int jj = 0; jj < n_tiles && ok && !lone; ++jj) {
       const bool more = jj + 1 < n_tiles;
       // tile A: P_A(jj) sits in S_A's columns; S_A(jj+1) may overwrite them
       // only after O_A += P_A(jj) V_jj is issued (same-thread MMAs run in order)
@@ -259,15 +281,17 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int x = (warp - 2) >> 2;        // 0: tile A (warps 2-5), 1: tile B (warps 6-9)
     const int q4 = warp & 3;              // TMEM lane quarter this warp may access
     const int r = q4 * 32 + lane;
-    const int qx0 = t.row0(x);            // first row of this query tile
-    const int i = t.row(x, r);            // of the sequence
+    const int qt = lone ? 0 : x;          // the query tile
+    const int qx0 = t.row0(qt);           // its first row
+    const int i = t.row(qt, r);           // of the sequence
+    const int steps = lone ? (n_tiles + 1 - x) >> 1 : n_tiles;
     const uint32_t tl = tmem + ((uint32_t)(q4 * 32) << 16);
     const uint32_t s_col = x * 128, o_col = 256 + x * D;
     const int rot = t.rot(g);
     float m = -INFINITY, l = 0.f;
     bool ok = true;
-    for (int jj = 0; jj < n_tiles && ok; ++jj) {
-      const typename Call::MaskT mask(g, t, t0 + jj, i, qx0, rot);
+    for (int jj = 0; jj < steps && ok; ++jj) {
+      const typename Call::MaskT mask(g, t, t0 + (lone ? 2 * jj + x : jj), i, qx0, rot);
       ok = __all_sync(0xffffffffu, wait_bar(&s_full[x], jj & 1, a.err, abort_flag));
       if (!ok) break;
       tc_fence_after();
@@ -277,8 +301,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (half) {
       end_m = m;
       end_l = l;
-      end_ok = ok && (n_tiles == 0 ||
-                      __all_sync(0xffffffffu, wait_bar(&pv_done[x], (n_tiles - 1) & 1, a.err, abort_flag)));
+      end_ok = ok && (steps == 0 ||
+                      __all_sync(0xffffffffu, wait_bar(&pv_done[x], (steps - 1) & 1, a.err, abort_flag)));
     } else if (ok && ((Call::kEmptyRows && n_tiles == 0) ||
                       __all_sync(0xffffffffu, wait_bar(&pv_done[x], (n_tiles - 1) & 1, a.err, abort_flag)))) {
       tc_fence_after();
@@ -294,18 +318,20 @@ __global__ void __launch_bounds__(kThreads, 1)
     // all CTAs' copies and MMAs are done with their shared memory
     cluster_arrive();
     cluster_wait();
-    // receive buffer: [C][D / 4][256 / C rows] float4, then [C][256 / C rows] (m, l)
-    const int C2 = 1 << lg_ctas, lg_rows = 8 - lg_ctas, rows = 1 << lg_rows;
+    // n states of each of this CTA's rows. Receive buffer: [n][D / 4][rows] float4, then [n][rows]
+    // (m, l)
+    const int lg_rows = (lone ? 7 : 8) - lg_ctas, rows = 1 << lg_rows, n = lone ? 2 << lg_ctas : 1 << lg_ctas;
     float4* recv = reinterpret_cast<float4*>(smem);
     float2* recv_ml = reinterpret_cast<float2*>(recv + D / 4 * 256);
     const int x = (warp - 2) >> 2, q4 = warp & 3, r = q4 * 32 + lane;
     if (warp >= 2) {
-      const int row = x * 128 + r, dst = row >> lg_rows, at = row & (rows - 1);
+      const int row = lone ? r : x * 128 + r, from = lone ? 2 * rank + x : rank;
+      const int dst = row >> lg_rows, at = row & (rows - 1);
       const uint32_t tl = tmem + ((uint32_t)(q4 * 32) << 16) + 256 + x * D;
-      const uint32_t to = cluster_addr(recv + ((rank * (D / 4)) << lg_rows) + at, (uint32_t)dst);
-      cluster_st2(cluster_addr(recv_ml + (rank << lg_rows) + at, (uint32_t)dst), __float_as_uint(end_m),
+      const uint32_t to = cluster_addr(recv + ((from * (D / 4)) << lg_rows) + at, (uint32_t)dst);
+      cluster_st2(cluster_addr(recv_ml + (from << lg_rows) + at, (uint32_t)dst), __float_as_uint(end_m),
                   __float_as_uint(end_l));
-      if (n_tiles > 0) {
+      if (n_tiles > (lone ? x : 0)) {
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) {
           uint32_t v[32];
@@ -320,40 +346,40 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     cluster_arrive();
     cluster_wait();
-    // the eight warps: rows in groups of 32 (8 / C of them), columns in C groups; a lane a row
     if (warp >= 2) {
-      const int w = warp - 2, groups = 8 >> lg_ctas, rg = w & (groups - 1), cg = w >> (3 - lg_ctas);
-      const int at = rg * 32 + lane, row = (rank << lg_rows) + at, ox = row >> 7, orow = row & 127;
-      float M = -INFINITY;
-      for (int c = 0; c < C2; ++c) M = fmaxf(M, recv_ml[(c << lg_rows) + at].x);
-      // a state of -inf saw no key (its CTA may have had no tile: unwritten values); any other
-      // state counts
-      float wt[8], L = 0.f;
-#pragma unroll
-      for (int c = 0; c < 8; ++c) {
-        wt[c] = 0.f;
-        if (c >= C2) continue;
-        const float2 ml = recv_ml[(c << lg_rows) + at];
-        wt[c] = ml.x == -INFINITY ? -1.f : fast_exp2(ml.x - M);
-        if (ml.x != -INFINITY) L += wt[c] * ml.y;
-      }
-      const float inv = L == 0.f ? 0.f : 1.f / L;
-      if (end_ok && t.has_row(ox, orow)) {
-        bf16* out = static_cast<bf16*>(a.out) + t.out_row(a, ox, orow) * D;
-        for (int k = cg * (D / 4) >> lg_ctas; k < (cg + 1) * (D / 4) >> lg_ctas; ++k) {
-          float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-          for (int c = 0; c < 8; ++c) {
-            if (c >= C2 || wt[c] < 0.f) continue;
-            const float4 z = recv[((c * (D / 4) + k) << lg_rows) + at];
-            const float f = wt[c] * inv;
-            o.x += f * z.x;
-            o.y += f * z.y;
-            o.z += f * z.z;
-            o.w += f * z.w;
-          }
-          *reinterpret_cast<uint2*>(out + k * 4) = make_uint2(float2_to_bf16x2(o.x, o.y), float2_to_bf16x2(o.z, o.w));
+      const int tid = threadIdx.x - 64;  // of the 256 softmax threads
+      // (m, l) -> the state's weight, negative for a state of -inf: it saw no key (and its CTA may
+      // have had no tile: unwritten values); any other counts
+      if (tid < rows) {
+        float M = -INFINITY, L = 0.f;
+        for (int c = 0; c < n; ++c) M = fmaxf(M, recv_ml[(c << lg_rows) + tid].x);
+        for (int c = 0; c < n; ++c) {
+          const float2 ml = recv_ml[(c << lg_rows) + tid];
+          if (ml.x != -INFINITY) L += fast_exp2(ml.x - M) * ml.y;
         }
+        const float inv = L == 0.f ? 0.f : 1.f / L;
+        for (int c = 0; c < n; ++c) {
+          const float m = recv_ml[(c << lg_rows) + tid].x;
+          recv_ml[(c << lg_rows) + tid].x = m == -INFINITY ? -1.f : fast_exp2(m - M) * inv;
+        }
+      }
+      named_barrier_sync(3, 256);
+      for (int u = tid; u < D / 4 << lg_rows; u += 256) {
+        const int at = u & (rows - 1), k = u >> lg_rows, row = (rank << lg_rows) + at, ox = row >> 7, orow = row & 127;
+        if (!end_ok || !t.has_row(ox, orow)) continue;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int c = 0; c < n; ++c) {
+          const float f = recv_ml[(c << lg_rows) + at].x;
+          const float4 z = recv[((c * (D / 4) + k) << lg_rows) + at];
+          if (f < 0.f) continue;
+          o.x += f * z.x;
+          o.y += f * z.y;
+          o.z += f * z.z;
+          o.w += f * z.w;
+        }
+        *reinterpret_cast<uint2*>(static_cast<bf16*>(a.out) + t.out_row(a, ox, orow) * D + k * 4) =
+            make_uint2(float2_to_bf16x2(o.x, o.y), float2_to_bf16x2(o.z, o.w));
       }
     }
     __syncthreads();

@@ -64,6 +64,12 @@ PROMPTS = [
     ([30 - i % 25 for i in range(70)], None, 40, 8, 128, [0, 1] * 4, 2, 11),
     ([70], [1111], 6, 2, 128, [0, 1], 128, 129),
     ([1, 1, 1, 1], [5000, 100, 1, 640], 8, 1, 128, [0], 0, 1),
+    # one query tile an item, its keys shared by both halves of the pipeline: small clusters, ...
+    ([1 + i % 16 for i in range(60)], [1500 + 64 * i for i in range(60)], 24, 3, 64, [0, 1, 0], 5, 1100),
+    # ... and clusters of 16, with one query tile an item and with two
+    ([3, 1], [9000, 257], 4, 1, 128, [0], 0, 1),
+    ([100], [7003], 4, 2, 128, [0, 0], 0, 1),
+    ([2, 11], [6300, 1], 16, 2, 64, [0, 1], 300, 3000),
 ]
 
 

@@ -25,10 +25,13 @@ Modules
                section): anchor-group importance and top-k selection,
                sparse attention at borrowed positions, the Eq. sim head
                similarity and the group mapping.
+  paged        the paged cache: attention over packed prompts with a causal
+               offset, the 8-bit rows with their powers of two, and one
+               token's attention over them.
 
 Parity status: every function here is pinned by ``tests/test_oracle_*.py``
 against closed forms, brute force, a textbook library routine or values the
 paper prints. None is "parity unpinned".
 """
 
-from . import attention, effective_rank, h2share, kv_memory  # noqa: F401
+from . import attention, effective_rank, h2share, kv_memory, paged  # noqa: F401

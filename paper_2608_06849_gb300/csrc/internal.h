@@ -170,6 +170,8 @@ struct PackedArgs {
   CUtensorMap tq, tk, tv;
   CacheGeom geom;  // heads, S and W (no cache)
   void* out;       // [rows][Hq][D]
+  const void *q, *k, *v;  // as the maps have them: a row every stride elements
+  long long q_stride, k_stride, v_stride;
   PackedSeqs seqs;
   const uint64_t* work;  // unused
   uint32_t* err;

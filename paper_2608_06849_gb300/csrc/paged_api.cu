@@ -326,6 +326,12 @@ aoh_status aoh_paged_prefill(aoh_paged* cache, const void* q, const void* k, con
   memset(&a, 0, sizeof(a));
   a.geom = cache->geom;
   a.out = out;
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
   a.err = cache->d_err;
   a.scale_log2 = (float)(1.4426950408889634 / sqrt((double)c.d_head));
   a.span = 128 / a.geom.G;

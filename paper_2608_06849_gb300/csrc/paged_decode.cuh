@@ -28,6 +28,16 @@
 // add up their states through distributed shared memory, each finishing D / C values of every
 // head.
 //
+// What bounds it: the bytes of the visible rows. A tile is 64 KB because a smaller one leaves the
+// chain S -> weights -> P V above its transfer time (64 KB: 0.95 us a tile on an SM alone, 1.47 with
+// all SMs reading), and three tiles are what shared memory holds: 96 KB in flight an SM
+// behind the tile that is worked on. 16 sequences of 32,768 tokens, 32/8 heads, pages of 64, us
+// (floor: bytes at the 6.8 TB/s of a copy): 8-bit d_head 128 162 (159), 64 92 (80); bf16 128 310
+// (316), 64 160 (158). Pages of 16 cost 5% (8-bit, 128) to 20% (8-bit, 64): eight copies a
+// block. 16 query heads a KV head: 177 and 151, the softmax of 16 columns takes longer than the
+// tile's transfer. A step in equal runs pays 8-9 us besides (launch, plan, first tile, last tile's
+// chain, arrival, joins), one on clusters 5: 1 x 4096 5.9 us, 4 x 8192 11.5.
+//
 // Warps: 4 or 8 of softmax (a thread one or two keys of the tile), 4 that finish items, two
 // producers, one MMA issuer. O and the sums have two buffers, so that a CTA's next item goes
 // on while its last one is finished, stored and joined.

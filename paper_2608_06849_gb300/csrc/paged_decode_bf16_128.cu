@@ -1,3 +1,4 @@
+// Instances of the paged decode for bf16 pages and d_head 128; a unit of its own, compiled beside the others.
 #include "paged_decode.cuh"
 
 namespace aoh {

@@ -1,3 +1,4 @@
+// Instances of the paged decode for 8-bit pages and d_head 128; a unit of its own, compiled beside the others.
 #include "paged_decode.cuh"
 
 namespace aoh {

@@ -161,11 +161,85 @@ struct PackedMask {
   }
 };
 
+// The rows of an item's query tile x whose bits are set (bit 0: row row0) once more, by the
+// warp, where a hidden key's V made their outputs wrong: in a matrix product a weight of zero
+// times a NaN or an infinity is a NaN, so that such a V row reaches rows that share a tile with it
+// and do not see it. Rows with an output that is not finite come here. One whose tiles hide no such V row
+// from it keeps its output; any other is computed from the keys that it sees alone, the
+// newest first (a sequence that went bad at some token ends there), a lane D / 32 of the numbers.
+// Calls without such values pay for the look at their outputs alone: 16 x 101-2,999 tokens 230 ->
+// 233 us, 32,768 tokens the same.
+template <int D, class A>
+__device__ void repair_rows(const A& a, uint64_t code, int x, int row0, uint32_t rows) {
+  constexpr int N = D / 32;
+  const typename CallOf<A>::ItemT t(a, code);
+  const CacheGeom& g = a.geom;
+  const int lane = threadIdx.x & 31;
+  auto load = [&](const void* base, long long stride, long long row, int head, float (&to)[N]) {
+    const bf16* p = static_cast<const bf16*>(base) + row * stride + head * D + lane * N;
+#pragma unroll
+    for (int n = 0; n < N; n += 2) {
+      const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(p + n));
+      to[n] = f.x;
+      to[n + 1] = f.y;
+    }
+  };
+  __syncwarp();  // the rows' first writes come before
+  for (; rows; rows &= rows - 1) {
+    const int r = row0 + __ffs((int)rows) - 1;
+    if (!t.has_row(x, r)) continue;
+    const int pos = t.off + t.row(x, r);
+    const int w0 = t.streaming ? max(0, g.wstart(pos)) : 0, sinks = t.streaming ? min(g.S, w0) : 0;
+    float v[N], o[N] = {};
+    bool hit = false;
+    for (int i = 0; i < t.tiles() && !hit; ++i) {
+      const int j0 = t.chunk_tile(i) * kBN, j1 = min(j0 + kBN, t.klen);
+      float bad = 0.f;
+      for (int j = j0; j < j1; ++j) {
+        if (j <= pos && (j >= w0 || j < sinks)) continue;
+        load(a.v, a.v_stride, t.krow + j, t.kvh, v);
+#pragma unroll
+        for (int n = 0; n < N; ++n) bad = fmaf(v[n], 0.f, bad);
+      }
+      hit = __any_sync(0xffffffffu, !(bad == 0.f));
+    }
+    if (!hit) continue;
+    const size_t at = t.out_row(a, x, r);
+    float q[N], k[N], m = -INFINITY, l = 0.f;
+    load(a.q, a.q_stride, at / g.Hq, (int)(at % g.Hq), q);
+    for (int j = pos; j >= 0; --j) {
+      if (j < w0) j = min(j, sinks - 1);
+      if (j < 0) break;
+      load(a.k, a.k_stride, t.krow + j, t.kvh, k);
+      load(a.v, a.v_stride, t.krow + j, t.kvh, v);
+      float s = 0.f;
+#pragma unroll
+      for (int n = 0; n < N; ++n) s = fmaf(q[n], k[n], s);
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+      s *= a.scale_log2;
+      const float top = fmaxf(m, s), base = top == -INFINITY ? 0.f : top;
+      const float f = fast_exp2(m - base), p = fast_exp2(s - base);
+      m = top;
+      l = l * f + p;
+#pragma unroll
+      for (int n = 0; n < N; ++n) o[n] = o[n] * f + p * v[n];
+      if (isnan(l)) break;
+    }
+    bf16* out = static_cast<bf16*>(a.out) + at * D + lane * N;
+#pragma unroll
+    for (int n = 0; n < N; n += 2)
+      *reinterpret_cast<uint32_t*>(out + n) =
+          l == 0.f ? 0u : isnan(l) ? 0x7fc07fc0u : float2_to_bf16x2(o[n] / l, o[n + 1] / l);
+  }
+}
+
 template <>
 struct CallOf<PackedArgs> {
   using ItemT = PackedItem;
   using MaskT = PackedMask;
   static constexpr bool kEmptyRows = true;  // fewer keys than rows
+  static constexpr bool kRepairs = true;
   static constexpr bool kChained = true;
 };
 template <>
@@ -173,6 +247,7 @@ struct CallOf<FoldedArgs> {
   using ItemT = FoldedItem;
   using MaskT = PackedMask;
   static constexpr bool kEmptyRows = true;
+  static constexpr bool kRepairs = true;
   static constexpr bool kChained = true;
 };
 

@@ -58,6 +58,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* drain = v_zeroed + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  uint32_t* spoilt = tmem_slot + 2;  // this CTA's items with a value that is not finite: bit k mod 32
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const CacheGeom& g = a.geom;
@@ -83,6 +84,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     mbar_init(drain, 1);
     *abort_flag = 0;
+    *spoilt = 0;
     fence_mbar_init();
   }
   if (warp == 1) {
@@ -252,8 +254,16 @@ __global__ void __launch_bounds__(kThreads, 1)
       ok = __all_sync(0xffffffffu, wait_bar(&pv_done[x], (kt - 1) & 1, a.err, abort_flag));
       if (!ok) break;
       tc_fence_after();
-      store_o<D, X::COLS>(a, t, x, q4 * 32, tl + o_col, l, stage, lane);
+      if (store_o<D, X::COLS>(a, t, x, q4 * 32, tl + o_col, l, stage, lane) && lane == 0)
+        atomicOr(spoilt, 1u << (k & 31));
       tc_fence_before();
+    }
+    // after the loop, which a call would slow down; rows that need none come out the same
+    if constexpr (Call::kRepairs) {
+      __syncwarp();
+      const uint32_t which = *spoilt;
+      for (int k = 0; which && item_index(k) < n_items; ++k)
+        if (which >> (k & 31) & 1) repair_rows<D>(a, item_code(item_index(k)), x, q4 * 32, ~0u);
     }
   }
 

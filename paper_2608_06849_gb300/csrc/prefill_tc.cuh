@@ -307,7 +307,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                       __all_sync(0xffffffffu, wait_bar(&pv_done[x], (n_tiles - 1) & 1, a.err, abort_flag)))) {
       tc_fence_after();
       // Q_X is free: the last S_X was done before the last P V
-      store_o<D, D>(a, t, x, q4 * 32, tl + o_col, l, sQ + x * C::QBYTES + q4 * (C::QBYTES / 4), lane);
+      const uint32_t spoilt =
+          store_o<D, D>(a, t, x, q4 * 32, tl + o_col, l, sQ + x * C::QBYTES + q4 * (C::QBYTES / 4), lane);
+      if constexpr (Call::kRepairs)
+        if (spoilt) repair_rows<D>(a, code, x, q4 * 32, spoilt);
     }
   }
 
@@ -323,6 +326,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int lg_rows = (lone ? 7 : 8) - lg_ctas, rows = 1 << lg_rows, n = lone ? 2 << lg_ctas : 1 << lg_ctas;
     float4* recv = reinterpret_cast<float4*>(smem);
     float2* recv_ml = reinterpret_cast<float2*>(recv + D / 4 * 256);
+    uint32_t* spoilt = reinterpret_cast<uint32_t*>(recv_ml + 256);  // [4]: rows with a value that is not finite
     const int x = (warp - 2) >> 2, q4 = warp & 3, r = q4 * 32 + lane;
     if (warp >= 2) {
       const int row = lone ? r : x * 128 + r, from = lone ? 2 * rank + x : rank;
@@ -350,6 +354,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int tid = threadIdx.x - 64;  // of the 256 softmax threads
       // (m, l) -> the state's weight, negative for a state of -inf: it saw no key (and its CTA may
       // have had no tile: unwritten values); any other counts
+      if (tid < 4) spoilt[tid] = 0;
       if (tid < rows) {
         float M = -INFINITY, L = 0.f;
         for (int c = 0; c < n; ++c) M = fmaxf(M, recv_ml[(c << lg_rows) + tid].x);
@@ -380,7 +385,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         *reinterpret_cast<uint2*>(static_cast<bf16*>(a.out) + t.out_row(a, ox, orow) * D + k * 4) =
             make_uint2(float2_to_bf16x2(o.x, o.y), float2_to_bf16x2(o.z, o.w));
+        if (!(o.x * 0.f + o.y * 0.f + o.z * 0.f + o.w * 0.f == 0.f)) atomicOr(spoilt + (at >> 5), 1u << (at & 31));
       }
+      named_barrier_sync(3, 256);
+      const int first = (rank << lg_rows) + (warp - 2) * 32;  // rows of the item
+      if (warp < 6 && spoilt[warp - 2]) repair_rows<D>(a, code, first >> 7, first & 127, spoilt[warp - 2]);
     }
     __syncthreads();
     tc_fence_after();
@@ -421,6 +430,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const float inv = 1.f / (end_l * w0 + o_ml.y * w1);
       const float f0 = w0 * inv, f1 = w1 * inv;
       uint8_t* stage = smem + C::OFF_BAR - C::QBYTES + q4 * (C::QBYTES / 4);  // past the receive buffer
+      Spoilt spoilt;
 #pragma unroll
       for (int c = 0; c < D / 32; ++c) {
         uint32_t v[32];
@@ -437,10 +447,15 @@ __global__ void __launch_bounds__(kThreads, 1)
             y[k + 2] = (mine ? __uint_as_float(v[e + k + 2]) * f0 : 0.f) + (other ? z.z * f1 : 0.f);
             y[k + 3] = (mine ? __uint_as_float(v[e + k + 3]) * f0 : 0.f) + (other ? z.w * f1 : 0.f);
           }
-          put_row<D>(stage, lane, c * 4 + e / 8, y);
+          const uint4 w = put_row<D>(stage, lane, c * 4 + e / 8, y);
+          if (Call::kRepairs) spoilt.add(w);
         }
       }
       write_rows<D, D>(a, t, x, q4 * 32, 0, stage, lane);
+      if constexpr (Call::kRepairs) {
+        const uint32_t rows = spoilt.rows();
+        if (rows) repair_rows<D>(a, code & ~kPrefillHalf, x, q4 * 32, rows);
+      }
       tc_fence_before();
     }
     __syncthreads();

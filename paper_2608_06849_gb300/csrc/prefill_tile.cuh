@@ -236,6 +236,7 @@ struct CallOf<PrefillTcArgs> {
   using ItemT = Item;
   using MaskT = Mask;
   static constexpr bool kEmptyRows = false;
+  static constexpr bool kRepairs = false;  // rows that a hidden V row's NaN reached are gone over again (repair_rows)
   static constexpr bool kChained = false;  // launches overlap the one before (wait_to_start, wait_to_end)
 };
 
@@ -394,7 +395,7 @@ __device__ __forceinline__ bool softmax_tile(const A& a, const M& mask,
 // lanes. 8 ragged sequences of up to 2,999 tokens: 313 -> 298 us; 32K tokens with
 // streaming heads alone (S = 128, W = 1024) 570 -> 517 us.
 template <int D>
-__device__ __forceinline__ void put_row(uint8_t* stage, int lane, int chunk, const float (&y)[8]) {
+__device__ __forceinline__ uint4 put_row(uint8_t* stage, int lane, int chunk, const float (&y)[8]) {
   constexpr int CH = D / 8;
   uint4 w;
   w.x = float2_to_bf16x2(y[0], y[1]);
@@ -402,7 +403,25 @@ __device__ __forceinline__ void put_row(uint8_t* stage, int lane, int chunk, con
   w.z = float2_to_bf16x2(y[4], y[5]);
   w.w = float2_to_bf16x2(y[6], y[7]);
   *reinterpret_cast<uint4*>(stage + lane * (D * 2) + ((chunk ^ (lane % CH)) << 4)) = w;
+  return w;
 }
+
+// Whether a row has a value that is not finite: zero times it is a NaN, which stays in the sums.
+struct Spoilt {
+  __nv_bfloat162 z[4] = {};
+  __device__ __forceinline__ void add(const uint4& w) {
+    const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      z[i] = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&v[i]), __float2bfloat162_rn(0.f), z[i]);
+  }
+  __device__ __forceinline__ uint32_t rows() const {  // of the warp, a lane a row
+    const float2 f = __bfloat1622float2(__hadd2(__hadd2(z[0], z[1]), __hadd2(z[2], z[3])));
+    return __ballot_sync(0xffffffffu, !(f.x + f.y == 0.f));
+  }
+};
+template <int D, class A>
+__device__ __noinline__ void repair_rows(const A& a, uint64_t code, int x, int row0, uint32_t rows);
 
 // COLS columns, from col0 on, of rows row0 .. row0 + 31 of query tile x (those there are), from
 // the warp's `stage`.
@@ -425,10 +444,11 @@ __device__ __forceinline__ void write_rows(const A& a, const T& t, int x, int ro
 // first of them row row0 of the tile, COLS columns at a time. taddr: O's first
 // column, stage: 32 * COLS * 2 bytes, l: the row's sum (0: it saw no key).
 template <int D, int COLS, class A, class T>
-__device__ __forceinline__ void store_o(const A& a, const T& t, int x, int row0, uint32_t taddr, float l,
+__device__ __forceinline__ uint32_t store_o(const A& a, const T& t, int x, int row0, uint32_t taddr, float l,
                                         uint8_t* stage, int lane) {
   const float inv = 1.f / l;
   const bool none = CallOf<A>::kEmptyRows && l == 0.f;
+  Spoilt spoilt;
 #pragma unroll
   for (int c = 0; c < D / 32; ++c) {
     uint32_t v[32];
@@ -439,13 +459,15 @@ __device__ __forceinline__ void store_o(const A& a, const T& t, int x, int row0,
       float y[8];
 #pragma unroll
       for (int k = 0; k < 8; ++k) y[k] = none ? 0.f : __uint_as_float(v[e + k]) * inv;
-      put_row<COLS>(stage, lane, c % (COLS / 32) * 4 + e / 8, y);
+      const uint4 w = put_row<COLS>(stage, lane, c % (COLS / 32) * 4 + e / 8, y);
+      if (CallOf<A>::kRepairs) spoilt.add(w);
     }
     if ((c + 1) * 32 % COLS == 0) {
       write_rows<D, COLS>(a, t, x, row0, (c + 1) * 32 - COLS, stage, lane);
       __syncwarp();
     }
   }
+  return CallOf<A>::kRepairs ? spoilt.rows() : 0u;
 }
 
 }  // namespace pf

@@ -141,6 +141,73 @@ def test_prompts_do_not_see_their_neighbours():
     assert torch.equal(out[keep], again[keep])
 
 
+SPOILT = [PROMPTS[i] for i in (2, 3, 5, 6, 10, 11, 13, 14, 18, 20, 21, 23)]
+SPOILT.append(([1100, 3], None, 4, 4, 128, [0, 1, 0, 1], 3, 50))  # items that two CTAs share
+
+
+@pytest.mark.parametrize("what", ["nan in k and v", "inf in v"])
+@pytest.mark.parametrize("case", range(len(SPOILT)))
+def test_prompts_do_not_see_hidden_keys(case, what):
+    """A NaN or an infinity in a key reaches the rows that see the key, and no other: neither
+    rows before it nor those whose window it has left."""
+    q_lens, k_lens, hq, hkv, d, labels, sink, window = SPOILT[case]
+    q, k, v = prompt_inputs(q_lens, k_lens, hq, hkv, d, seed=3)
+    clean = (k.clone(), v.clone())
+    k_lens = q_lens if k_lens is None else k_lens
+    ks, spoilt = sums(k_lens), []
+    for b, m in enumerate(k_lens):
+        first = max(m - q_lens[b], 0)
+        # among a sequence's rows, and at its end
+        spoilt.append(sorted({first + (m - first) // 2, m - 1}) if m > first + 1 else [])
+        for j in spoilt[b]:
+            at = ks[b] + j
+            if what == "inf in v":
+                v[at, :, 5] = float("inf")
+                clean[1][at, :, 5] = 0
+            else:
+                k[at, :, 2] = float("nan")
+                v[at, :, 1::2] = float("nan")
+                clean[0][at], clean[1][at] = 0, 0
+    pc = aoh.PagedCache(1, 16, hq, hkv, d, sink, window, labels, max_seqs=len(q_lens))
+    out = torch.zeros((sum(q_lens), hq, d), dtype=torch.bfloat16, device="cuda")
+    pc.prefill(q, k, v, q_lens, out, k_lens=k_lens)
+    pc.check()
+    # what sees a spoilt key is not finite, and left out of the comparison
+    want_bad = torch.zeros_like(out, dtype=torch.bool)
+    row = 0
+    for b, n in enumerate(q_lens):
+        pos = torch.arange(k_lens[b] - n, k_lens[b], device="cuda")
+        for j in spoilt[b]:
+            for h in range(hkv):
+                sees = (j <= pos) & ((labels[h] == 0) | (j < sink) | (pos - j < window))
+                heads = slice(h * (hq // hkv), (h + 1) * (hq // hkv))
+                if what == "inf in v":
+                    want_bad[row:row + n, heads, 5] |= sees[:, None]
+                else:
+                    want_bad[row:row + n, heads] |= sees[:, None, None]
+        row += n
+    assert torch.equal(~torch.isfinite(out), want_bad)
+    if what == "inf in v":  # infinite weights do not mix signs here
+        assert (out[want_bad] == float("inf")).all()
+    again = torch.zeros_like(out)
+    pc.prefill(q, *clean, q_lens, again, k_lens=k_lens)
+    pc.check()
+    rows = ~want_bad.any(-1).any(-1)
+    out[want_bad] = 0
+    again[want_bad] = 0
+    ref, got = f64(again[rows]), f64(out[rows])
+    # the same sums, once with weights rounded to bf16 and once not
+    assert np.abs(ref - got).max(initial=0) <= 2.0 ** -6 * max(1.0, np.abs(ref).max(initial=0))
+    for b, r in [(b, r) for b, n in enumerate(q_lens) for r in range(0, n, max(1, n // 5))][:40]:
+        at, m = sums(q_lens)[b] + r, k_lens[b] - q_lens[b] + r + 1
+        if rows[at] and m > 0:
+            keys = slice(ks[b], ks[b] + m)
+            args, vb = (f64(q[at:at + 1]), f64(clean[0][keys])), f64(clean[1][keys])
+            want = opaged.attend(*args, vb, labels, sink, window)
+            mag = opaged.attend(*args, np.abs(vb), labels, sink, window)
+            assert_matches(f64(out[at:at + 1]), want, f"row {r} of sequence {b}", mag=mag, abs_bounds=False)
+
+
 @pytest.mark.parametrize("case", [2, 6, 10, 13])
 def test_prompts_in_a_graph(case):
     """A captured call, by-value sequences and uploaded ones, replays with new inputs."""

@@ -34,10 +34,9 @@ size_t paged_state_floats(int num_sms, int D) { return (size_t)num_sms * 4 * pde
 // an item's states through global memory 3.3 us, 5.5 in two levels. Measured, us a step in
 // equal runs / on clusters (8-bit, 32/8 heads of 128): 1 x 4096 9.4 / 6.0, 4 x 8192 15.7 /
 // 11.5, 8 streaming heads (S = 64, W = 2048) of 8 x 20000 13.1 / 8.9; bf16, 28/4 heads, half
-// streaming, 1 x 4096 9.8 / 6.0.
+// streaming, 1 x 4096 9.8 / 6.0; 16/1 heads, 8 x 8000 19.3 / 12.1, bf16 21.4 / 11.7.
 static int cluster_size(const PagedDecodeArgs& a, int num_sms) {
   const CacheGeom& g = a.geom;
-  if (g.G > pdec::kClusterHeads) return 0;
   const long long items = (long long)a.n_seqs * g.Hkv;
   const long long keys = 32768 / (g.D * (a.pool.form ? 1 : 2)), ring = (long long)g.S + g.W + 2 * a.pool.ps;
   const long long tr = (a.max_len + keys - 1) / keys, ts = ((a.max_len < ring ? a.max_len : ring) + keys - 1) / keys;

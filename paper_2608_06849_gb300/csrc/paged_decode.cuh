@@ -58,7 +58,6 @@ using bf16 = __nv_bfloat16;
 constexpr int kGroup = 16;          // states joined at a time
 constexpr int kLensCap = 1024;      // lengths mirrored in shared memory
 constexpr int kClusterMost = 16;    // CTAs of a cluster
-constexpr int kClusterHeads = 8;    // query heads a KV head there: the states of 16 do not fit
 
 // Shapes of one head size, format and (padded) number of query heads a KV head.
 template <int D_, bool F8_, int GP_, bool CL = false>
@@ -89,6 +88,7 @@ struct Lay {
   static constexpr int NW = SOFT / 32;
   static constexpr int THREADS = SOFT + 128 + 96;
   static constexpr int QBLK = SN * ROWB, QBUF = DBLK * QBLK;
+  static constexpr int NQ = CL ? 1 : 2;                    // Q buffers: a cluster has one item
   static constexpr int PBLK = NPV * 128;                   // weights of 128 bytes of keys
   static constexpr int PSET = PBLK * ES;
   static constexpr int PBUF = SETS * PSET;
@@ -98,11 +98,11 @@ struct Lay {
   // [C][16] (m, l)
   static constexpr int TAIL = CL ? GP * D * 4 + kClusterMost * 16 * 8 : kLensCap * 4;
   static constexpr int XBYTES = D == 64 ? GP * 64 * 4 : 0;
-  static constexpr int FIXED = NS * STAGE + 2 * QBUF + NS * POWB + 4 * GP * NW * 4 + 128 + XBYTES + 128 + NBAR * 8 + 32 +
+  static constexpr int FIXED = NS * STAGE + NQ * QBUF + NS * POWB + 4 * GP * NW * 4 + 128 + XBYTES + 128 + NBAR * 8 + 32 +
                                4 * 32 + kMaxKvHeads + TAIL + 1024;
   static constexpr int NPB = FIXED + 2 * PBUF <= 232448 ? 2 : 1;  // P buffers that fit
   static constexpr int OFF_Q = NS * STAGE;
-  static constexpr int OFF_P = OFF_Q + 2 * QBUF;
+  static constexpr int OFF_P = OFF_Q + NQ * QBUF;
   static constexpr int OFF_POW = OFF_P + NPB * PBUF;
   static constexpr int OFF_RED = OFF_POW + NS * POWB;     // [2][GP][NW] warp maxima
   static constexpr int OFF_SUM = OFF_RED + 2 * GP * NW * 4;  // [2][GP][NW] sums of an item, [2][16] maxima
@@ -401,7 +401,7 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
   const int G = g.G, lg = a.pool.lg_ps;
 
   // rows of Q and P that no head fills stay zero for the whole launch
-  for (int i = threadIdx.x; i < (2 * C::QBUF + C::NPB * C::PBUF) / 16; i += NT)
+  for (int i = threadIdx.x; i < (C::NQ * C::QBUF + C::NPB * C::PBUF) / 16; i += NT)
     reinterpret_cast<uint4*>(sQ)[i] = make_uint4(0, 0, 0, 0);
   fence_proxy_async_smem();
   if (threadIdx.x < 32) qfac[threadIdx.x] = 0.f;
@@ -637,7 +637,7 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
       // Q's buffer and O's were last in use by item - 2
       if (item >= 2) wait_warp(&o_free[item & 1], ((item >> 1) - 1) & 1);
       if (!ok) break;
-      uint8_t* qs = sQ + (item & 1) * C::QBUF;
+      uint8_t* qs = sQ + item % C::NQ * C::QBUF;
 #pragma unroll
       for (int i = 0; i < QV; ++i) {
         const int c = lane + 32 * i, h = c / CPR, cc = c % CPR;
@@ -695,7 +695,7 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
         if (elect_one()) {
           tc_fence_after();
           const uint64_t k_desc = k_desc0 + (uint32_t)(st * sdesc_step(C::STAGE));
-          const uint64_t q_desc = q_desc0 + (uint32_t)((item & 1) * sdesc_step(C::QBUF));
+          const uint64_t q_desc = q_desc0 + (uint32_t)((item % C::NQ) * sdesc_step(C::QBUF));
 #pragma unroll
           for (int y = 0; y < NK; ++y)
 #pragma unroll
@@ -1079,8 +1079,7 @@ cudaError_t launch(const PagedDecodeArgs& a, int ctas, int cluster, cudaStream_t
 
 template <int D, bool F8, int GP>
 cudaError_t launch_split(const PagedDecodeArgs& a, int num_sms, int cluster, cudaStream_t s) {
-  if constexpr (GP <= kClusterHeads)
-    if (cluster > 0) return launch<D, F8, GP, true>(a, a.n_seqs * a.geom.Hkv * cluster, cluster, s);
+  if (cluster > 0) return launch<D, F8, GP, true>(a, a.n_seqs * a.geom.Hkv * cluster, cluster, s);
   return launch<D, F8, GP, false>(a, num_sms, 0, s);
 }
 

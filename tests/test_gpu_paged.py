@@ -442,6 +442,23 @@ def test_decode_whatever_the_bound(form, d, hkv):
 
 @pytest.mark.parametrize("form", ["bf16", "e4m3"])
 @pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("g", [9, 16])
+def test_decode_with_many_heads_whatever_the_bound(form, d, g):
+    """As above, with as many query heads a KV head as there can be."""
+    lens, hkv, sink, window = [2900, 0, 1, 700], 2, 30, 200
+    labels = [0, 1]
+    p = Pages(lens, g * hkv, hkv, d, 16, form, labels, sink, window)
+    held = p.fill(lens, seed=g)
+    q = randn((len(lens), g * hkv, d), 4)
+    for max_len in (0, 1, 200, 100000):
+        out = torch.full_like(q, float("nan"))
+        p.cache.decode(q, ints(lens), p.table, out, max_len=max_len)
+        p.cache.check()
+        check_decode(out, q, held, labels, sink, window, f"bound {max_len}")
+
+
+@pytest.mark.parametrize("form", ["bf16", "e4m3"])
+@pytest.mark.parametrize("d", [64, 128])
 def test_decode_with_a_heavy_first_key(form, d):
     """An attention sink with a small value, far above the other keys: their sum still
     counts (its weight is e^6 to e^12 of each of theirs)."""

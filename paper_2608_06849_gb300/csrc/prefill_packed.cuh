@@ -161,8 +161,7 @@ struct PackedMask {
   }
 };
 
-// The rows of an item's query tile x whose bits are set (bit 0: row row0) once more, by the
-// warp, where a hidden key's V made their outputs wrong: in a matrix product a weight of zero
+// Rows row0, row0 + 1, ... of an item's 256 whose bits are set once more, by the warp, where a hidden key's V made their outputs wrong: in a matrix product a weight of zero
 // times a NaN or an infinity is a NaN, so that such a V row reaches rows that share a tile with it
 // and do not see it. Rows with an output that is not finite come here. One whose tiles hide no such V row
 // from it keeps its output; any other is computed from the keys that it sees alone, the
@@ -170,7 +169,7 @@ struct PackedMask {
 // Calls without such values pay for the look at their outputs alone: 16 x 101-2,999 tokens 230 ->
 // 233 us, 32,768 tokens the same.
 template <int D, class A>
-__device__ void repair_rows(const A& a, uint64_t code, int x, int row0, uint32_t rows) {
+__device__ void repair_rows(const A& a, uint64_t code, int row0, uint32_t rows) {
   constexpr int N = D / 32;
   const typename CallOf<A>::ItemT t(a, code);
   const CacheGeom& g = a.geom;
@@ -186,7 +185,7 @@ __device__ void repair_rows(const A& a, uint64_t code, int x, int row0, uint32_t
   };
   __syncwarp();  // the rows' first writes come before
   for (; rows; rows &= rows - 1) {
-    const int r = row0 + __ffs((int)rows) - 1;
+    const int row = row0 + __ffs((int)rows) - 1, x = row >> 7, r = row & 127;
     if (!t.has_row(x, r)) continue;
     const int pos = t.off + t.row(x, r);
     const int w0 = t.streaming ? max(0, g.wstart(pos)) : 0, sinks = t.streaming ? min(g.S, w0) : 0;

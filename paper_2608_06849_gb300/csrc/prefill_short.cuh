@@ -263,7 +263,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
       const uint32_t which = *spoilt;
       for (int k = 0; which && item_index(k) < n_items; ++k)
-        if (which >> (k & 31) & 1) repair_rows<D>(a, item_code(item_index(k)), x, q4 * 32, ~0u);
+        if (which >> (k & 31) & 1) repair_rows<D>(a, item_code(item_index(k)), x * 128 + q4 * 32, ~0u);
     }
   }
 

@@ -310,7 +310,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint32_t spoilt =
           store_o<D, D>(a, t, x, q4 * 32, tl + o_col, l, sQ + x * C::QBYTES + q4 * (C::QBYTES / 4), lane);
       if constexpr (Call::kRepairs)
-        if (spoilt) repair_rows<D>(a, code, x, q4 * 32, spoilt);
+        if (spoilt) repair_rows<D>(a, code, x * 128 + q4 * 32, spoilt);
     }
   }
 
@@ -321,21 +321,24 @@ __global__ void __launch_bounds__(kThreads, 1)
     // all CTAs' copies and MMAs are done with their shared memory
     cluster_arrive();
     cluster_wait();
+    // The rows that there are, rounded up, are dealt to the CTAs in runs, and only those travel.
     // n states of each of this CTA's rows. Receive buffer: [n][D / 4][rows] float4, then [n][rows]
     // (m, l)
-    const int lg_rows = (lone ? 7 : 8) - lg_ctas, rows = 1 << lg_rows, n = lone ? 2 << lg_ctas : 1 << lg_ctas;
+    const int lg_all = !lone ? 8 : t.has_row(0, 64) ? 7 : t.has_row(0, 32) ? 6 : 5;
+    const int lg_rows = lg_all - lg_ctas, rows = 1 << lg_rows, n = lone ? 2 << lg_ctas : 1 << lg_ctas;
     float4* recv = reinterpret_cast<float4*>(smem);
     float2* recv_ml = reinterpret_cast<float2*>(recv + D / 4 * 256);
     uint32_t* spoilt = reinterpret_cast<uint32_t*>(recv_ml + 256);  // [4]: rows with a value that is not finite
     const int x = (warp - 2) >> 2, q4 = warp & 3, r = q4 * 32 + lane;
     if (warp >= 2) {
       const int row = lone ? r : x * 128 + r, from = lone ? 2 * rank + x : rank;
-      const int dst = row >> lg_rows, at = row & (rows - 1);
+      const int dst = (row >> lg_rows) & ((1 << lg_ctas) - 1), at = row & (rows - 1);
       const uint32_t tl = tmem + ((uint32_t)(q4 * 32) << 16) + 256 + x * D;
       const uint32_t to = cluster_addr(recv + ((from * (D / 4)) << lg_rows) + at, (uint32_t)dst);
-      cluster_st2(cluster_addr(recv_ml + (from << lg_rows) + at, (uint32_t)dst), __float_as_uint(end_m),
-                  __float_as_uint(end_l));
-      if (n_tiles > (lone ? x : 0)) {
+      if (row < 1 << lg_all)
+        cluster_st2(cluster_addr(recv_ml + (from << lg_rows) + at, (uint32_t)dst), __float_as_uint(end_m),
+                    __float_as_uint(end_l));
+      if (n_tiles > (lone ? x : 0) && t.has_row(lone ? 0 : x, q4 * 32)) {
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) {
           uint32_t v[32];
@@ -388,8 +391,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!(o.x * 0.f + o.y * 0.f + o.z * 0.f + o.w * 0.f == 0.f)) atomicOr(spoilt + (at >> 5), 1u << (at & 31));
       }
       named_barrier_sync(3, 256);
-      const int first = (rank << lg_rows) + (warp - 2) * 32;  // rows of the item
-      if (warp < 6 && spoilt[warp - 2]) repair_rows<D>(a, code, first >> 7, first & 127, spoilt[warp - 2]);
+      if (warp < 6 && spoilt[warp - 2])
+        repair_rows<D>(a, code, (rank << lg_rows) + (warp - 2) * 32, spoilt[warp - 2]);
     }
     __syncthreads();
     tc_fence_after();
@@ -454,7 +457,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       write_rows<D, D>(a, t, x, q4 * 32, 0, stage, lane);
       if constexpr (Call::kRepairs) {
         const uint32_t rows = spoilt.rows();
-        if (rows) repair_rows<D>(a, code & ~kPrefillHalf, x, q4 * 32, rows);
+        if (rows) repair_rows<D>(a, code & ~kPrefillHalf, x * 128 + q4 * 32, rows);
       }
       tc_fence_before();
     }

@@ -421,7 +421,7 @@ struct Spoilt {
   }
 };
 template <int D, class A>
-__device__ __noinline__ void repair_rows(const A& a, uint64_t code, int x, int row0, uint32_t rows);
+__device__ __noinline__ void repair_rows(const A& a, uint64_t code, int row0, uint32_t rows);
 
 // COLS columns, from col0 on, of rows row0 .. row0 + 31 of query tile x (those there are), from
 // the warp's `stage`.

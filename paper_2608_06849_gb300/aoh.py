@@ -389,6 +389,9 @@ def aoh_paged_destroy(cache):
 # Grace core and the 13 arguments of a call 1 us: an append of four tensors through
 # layers of checks took 7.2 us where the library's own part is 1.8.
 
+_BF16, _I32 = torch.bfloat16, torch.int32
+
+
 def _rows(t, name, heads, d):
     """Pointer, token stride and rows of a [rows, heads, d] bf16 CUDA tensor
     whose rows are dense and may lie any distance apart (a slice of a fused
@@ -396,7 +399,7 @@ def _rows(t, name, heads, d):
     shape = t.shape
     if len(shape) != 3 or shape[1] != heads or shape[2] != d:
         raise ValueError(f"{name} has shape {tuple(shape)}; expected [rows, {heads}, {d}]")
-    if t.dtype is not torch.bfloat16 or not t.is_cuda:
+    if t.dtype is not _BF16 or not t.is_cuda:
         raise ValueError(f"{name} must be a torch.bfloat16 CUDA tensor")
     n = shape[0]
     if t.is_contiguous():
@@ -415,6 +418,15 @@ def _dense(t, name, shape, dtype):
         raise ValueError(f"{name} has shape {tuple(t.shape)}; expected {list(shape)}")
     if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} CUDA tensor")
+    return t.data_ptr()
+
+
+def _ints(t, name, n):
+    """Pointer of a contiguous int32 CUDA tensor of n numbers."""
+    if t.shape != (n,):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}; expected [{n}]")
+    if t.dtype is not _I32 or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous torch.int32 CUDA tensor")
     return t.data_ptr()
 
 
@@ -545,7 +557,9 @@ class PagedCache:
         shape = table.shape
         if len(shape) != 2 or shape[0] > self.max_seqs:
             raise ValueError(f"table has shape {tuple(shape)}; expected [sequences <= {self.max_seqs}, pages]")
-        return _dense(table, "table", shape, torch.int32), shape[0], shape[1]
+        if table.dtype is not _I32 or not table.is_cuda or not table.is_contiguous():
+            raise ValueError("table must be a contiguous torch.int32 CUDA tensor")
+        return table.data_ptr(), shape[0], shape[1]
 
     def prefill(self, q, k, v, q_lens, out, k_lens=None, stream=None):
         """Causal attention over packed prompts: q, out [rows, Hq, d], k, v [keys, Hkv, d]
@@ -556,7 +570,7 @@ class PagedCache:
         qp, qs, nq = _rows(q, "q", hq, d)
         kp, ks, nk = _rows(k, "k", hkv, d)
         vp, vs, nv = _rows(v, "v", hkv, d)
-        op = _dense(out, "out", (nq, hq, d), torch.bfloat16)
+        op = _dense(out, "out", (nq, hq, d), _BF16)
         n = len(q_lens)
         if n > self.max_seqs or (k_lens is not None and len(k_lens) != n):
             raise ValueError(f"q_lens and k_lens hold one length a sequence, at most {self.max_seqs}")
@@ -578,8 +592,8 @@ class PagedCache:
         tp, n, width = self._table(table)
         if rows != rows_v or (cu_rows is None and rows != n):
             raise ValueError(f"k and v hold {rows} and {rows_v} rows for {n} sequences")
-        cp = None if cu_rows is None else _dense(cu_rows, "cu_rows", (n + 1,), torch.int32)
-        st = _lib.aoh_paged_append(self.handle, kp, vp, ks, vs, cp, _dense(lens, "lens", (n,), torch.int32), n, rows, tp,
+        cp = None if cu_rows is None else _ints(cu_rows, "cu_rows", n + 1)
+        st = _lib.aoh_paged_append(self.handle, kp, vp, ks, vs, cp, _ints(lens, "lens", n), n, rows, tp,
                                    width, self._stream(stream))
         if st:
             _check(st)
@@ -590,11 +604,11 @@ class PagedCache:
         tp, n, width = self._table(table)
         rows = k_out.shape[0]
         shape = (rows, self.n_kv_heads, self.d_head)
-        kp, vp = _dense(k_out, "k_out", shape, torch.bfloat16), _dense(v_out, "v_out", shape, torch.bfloat16)
+        kp, vp = _dense(k_out, "k_out", shape, _BF16), _dense(v_out, "v_out", shape, _BF16)
         if cu_rows is None and rows != n:
             raise ValueError(f"k_out and v_out hold {rows} rows for {n} sequences")
-        cp = None if cu_rows is None else _dense(cu_rows, "cu_rows", (n + 1,), torch.int32)
-        fp = None if first is None else _dense(first, "first", (n,), torch.int32)
+        cp = None if cu_rows is None else _ints(cu_rows, "cu_rows", n + 1)
+        fp = None if first is None else _ints(first, "first", n)
         st = _lib.aoh_paged_read(self.handle, cp, fp, n, rows, tp, width, kp, vp, self._stream(stream))
         if st:
             _check(st)
@@ -609,8 +623,8 @@ class PagedCache:
         tp, n, width = self._table(table)
         if rows != n:
             raise ValueError(f"q holds {rows} rows for {n} sequences")
-        st = _lib.aoh_paged_decode(self.handle, qp, qs, _dense(lens, "lens", (n,), torch.int32), n, max_len, tp,
-                                   width, _dense(out, "out", (n, self.n_q_heads, self.d_head), torch.bfloat16),
+        st = _lib.aoh_paged_decode(self.handle, qp, qs, _ints(lens, "lens", n), n, max_len, tp,
+                                   width, _dense(out, "out", (n, self.n_q_heads, self.d_head), _BF16),
                                    self._stream(stream))
         if st:
             _check(st)

@@ -310,7 +310,7 @@ bool make_rows_map(CUtensorMap* map, const void* base, int B, long long T, int H
 // Fills the first seqs.size() entries of the device table.
 cudaError_t launch_packed_seqs(int4* table, const std::vector<int4>& seqs, cudaStream_t s);
 // The items of packed prompts, plain or folded. pairs: as in launch_prefill_tc; split: CTAs
-// that share each item (1, 2, 4, 8 or 16); is_short: one CTA an SM through all items.
+// that share each item (1 .. 16); is_short: one CTA an SM through all items.
 cudaError_t launch_prefill_packed(const PackedArgs& a, const std::vector<uint64_t>& items,
                                   const std::vector<uint64_t>& pairs, bool is_short, int num_sms, cudaStream_t s);
 cudaError_t launch_prefill_folded(const FoldedArgs& a, const std::vector<uint64_t>& items, int split, bool is_short,

@@ -355,14 +355,23 @@ aoh_status aoh_paged_prefill(aoh_paged* cache, const void* q, const void* k, con
   // the pipeline over short items takes no item without a tile
   auto is_short = [&] { return costs.back() > 0 && prefill_is_short(costs, cache->num_sms); };
   cudaError_t e;
-  if (folds) {
-    const std::vector<uint64_t> items = folded_schedule(a.geom, seqs, a.span, &costs);
-    bool lone = true;
+  std::vector<uint64_t> items;
+  int split = 1;
+  bool lone = true;
+  if (folds || a.geom.G == 1) {
+    items = folded_schedule(a.geom, seqs, a.span, &costs);
     for (const int4& b : seqs) lone = lone && b.y <= a.span;
-    const int split = folded_split(costs, lone, decode_tc_max_clusters(16), cache->num_sms);
+    split = folded_split(costs, lone, decode_tc_max_clusters, cache->num_sms);
+  }
+  // With one query head a KV head both kinds are the same items, and two CTAs share a plain one at
+  // less cost; more than two share folded ones alone, which is worth it from some tiles on. 8/8 heads,
+  // plain / folded: 1,100 rows (9 tiles) 14.7 / 16.4 us, 300 after 5,000 (42) 36.5 / 22.2, 17 after
+  // 2,000 18.7 / 8.8, after 20,000 110 / 23.
+  if (folds || (lone ? split > 1 : split > 2 && costs[0] >= 16)) {
     e = launch_prefill_folded(a, items, split, split == 1 && is_short(), cache->num_sms, s);
   } else {
-    const std::vector<uint64_t> items = packed_schedule(a.geom, seqs, &costs);
+    costs.clear();
+    items = packed_schedule(a.geom, seqs, &costs);
     const std::vector<uint64_t> pairs = prefill_pairs(items, costs, cache->num_sms);
     e = launch_prefill_packed(a, items, pairs, pairs.empty() && is_short(), cache->num_sms, s);
   }

@@ -132,15 +132,15 @@ inline std::vector<uint64_t> folded_schedule(const CacheGeom& g, const std::vect
 // Rows of more than a few hundred tokens fill plain items, which waste no row where G does not
 // divide 128 and are some percent faster then. Measured, us of a call in plain / folded items:
 // 33 x 7-34 tokens, 40/8 heads of 128: 28.4 / 14.9; 4 x 17 rows after 20,000, 32/8 heads of 64:
-// 100 / 48; 100 rows after 100,000, 28/4 heads of 128: 557 / 148; 4,000 tokens of 32/8 heads 94 /
+// 100 / 48; 100 rows after 100,000, 28/4 heads of 128: 557 / 124; 4,000 tokens of 32/8 heads 94 /
 // 93, of 40/8 heads 122 / 132, of 24/8 heads 77 / 81; 16 x 101-2,999, 32/8 heads, half
 // streaming: 236 / 243.
 inline bool packed_folds(const CacheGeom& g, const std::vector<int4>& seqs, int span, int num_sms) {
-  if (g.G == 1) return false;  // the same items
   struct Load {
     long long work = 0, items = 0;
     int longest = 0;
   };
+  if (g.G == 1) return false;  // the same items: folded_split alone decides
   auto load_of = [&](auto parts) {  // parts(add): add(rows of an item, items a KV head and such rows)
     Load l;
     for (const int4& seq : seqs)
@@ -167,21 +167,23 @@ inline bool packed_folds(const CacheGeom& g, const std::vector<int4>& seqs, int 
   const Load folded = load_of([&](auto add) { add(2 * span, 1); });
   double p = end_of(plain, 1), f = end_of(folded, 1);
   if (plain.longest >= 7 && plain.items <= num_sms / 2) p = std::min(p, end_of(plain, 2));
-  for (int c = 2; c <= 16 && folded.longest >= 7 && folded.items * c <= 2 * num_sms; c *= 2)
+  for (int c = 2; c <= 16 && folded.longest >= 7 && folded.items * c <= 2 * num_sms; ++c)
     f = std::min(f, end_of(folded, c));
   return f < 0.9 * p;
 }
 
-// CTAs that share each folded item (clusters of 2, 4, 8 or 16), or 1, by the end of
-// longest-first schedules in visited tiles, with 4 tiles' time added to an item and 8 to a part
-// of one. lone: every item has one query tile alone, whose KV tiles the two halves of a split
-// item's pipeline share (a pair of tiles takes 1.3 times one; in several waves the reads take as
-// long either way). most16: clusters of 16 that run at once. Measured, 16 rows, us of a call with clusters of 8 whose second query tile is empty / of 16
-// whose halves share the tiles: after 50,000, 7/1 heads of 128 78 / 35, 8/1 heads of 64 64 /
-// 26; 32/8 heads of 128 after 20,000 37 / 31, after 100,000 142 / 120; in four waves, 32
-// sequences' rows after 8,000, unshared / shared 192 / 206. The same pipeline in single CTAs
-// gained 4% there and lost 7% on 16 sequences' rows after 4,000: not used.
-inline int folded_split(const std::vector<int>& costs, bool lone, int most16, int num_sms) {
+// CTAs that share each folded item (clusters of 2 to 16), or 1, by the end of longest-first
+// schedules in visited tiles, with 4 tiles' time added to an item and 8 to a part of one. lone:
+// every item has one query tile alone, whose KV tiles the two halves of a split item's pipeline
+// share (a pair of tiles takes 1.3 times one; in several waves the reads take as long either
+// way). most(c): clusters of c CTAs that run at once. Measured, 16 rows, us of a call with clusters of 8 whose second query tile is empty / of 16
+// whose halves share the tiles: after 50,000, 7/1 heads of 128 78 / 35, 8/1 heads of 64 64 / 26; in
+// four waves, 32 sequences' rows after 8,000, unshared / shared 192 / 206. The same pipeline in
+// single CTAs gained 4% there and lost 7% on 16 sequences' rows after 4,000: not used. With powers of two
+// alone / these sizes: 300 rows of 32/8 heads after 20,000 111 / 83, 256 of 16/2 after 5,000 34 / 22,
+// 100 of 28/4 after 100,000 148 / 124.
+template <class F>
+int folded_split(const std::vector<int>& costs, bool lone, F most, int num_sms) {
   const int n = (int)costs.size();
   if (n > kPrefillSplitMost || n > 4 * num_sms || costs[0] < 7) return 1;
   std::vector<double> free_at;  // a min-heap
@@ -197,10 +199,14 @@ inline int folded_split(const std::vector<int>& costs, bool lone, int most16, in
   };
   double best = end_of(num_sms, [](int cost) { return cost + 4.0; });
   int pick = 1;
-  for (int c = 2; c <= 16; c *= 2) {
-    if (c == 16 && n > most16) break;
-    const double pace = lone && n * c <= num_sms ? 0.65 : 1.0;
-    const double end = end_of(num_sms / c, [&](int cost) { return (cost + c - 1) / c * pace + 8.0; });
+  double work = 0;
+  for (int cost : costs) work += cost;
+  for (int c : {2, 3, 4, 5, 6, 8, 10, 12, 16}) {
+    const int slots = most(c);
+    // what the parts cost together, and a longest one, may be too much already
+    const double pace = lone && n <= slots ? 0.65 : 1.0;
+    if (slots < 1 || best <= std::max((work * pace + 8.0 * n * c) / (slots * c), (costs[0] + c - 1) / c * pace + 8.0)) continue;
+    const double end = end_of(slots, [&](int cost) { return (cost + c - 1) / c * pace + 8.0; });
     if (end < best) {
       best = end;
       pick = c;

@@ -53,7 +53,7 @@ namespace pf {
 // the two query tiles: it receives the other
 // CTA's state of that tile (O, running max and sum) in shared memory that the
 // main loop no longer needs, adds its own and writes the rows.
-// kSplit: clusters of C = 2, 4, 8 or 16 CTAs, an item each: every CTA visits a C-th of its KV
+// kSplit: clusters of C = 2 .. 16 CTAs, an item each: every CTA visits a C-th of its KV
 // tiles and finishes a C-th of its 256 rows, whose states it receives from all (its own among
 // them). An item whose second query tile has no row is a lone one: both halves of the
 // pipeline work on its first tile, A on the even KV tiles and B on the odd ones, and their states
@@ -91,8 +91,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (a.seqs.table != nullptr) wait_to_start(a);  // the item is read from device memory
   }
   constexpr bool PAIRS = MODE == kPairs, SPLIT = MODE == kSplit;
-  const int lg_ctas = SPLIT ? __ffs((int)cluster_ctas()) - 1 : 1;
-  const int entry = SPLIT ? blockIdx.x >> lg_ctas : blockIdx.x;
+  const int ctas = SPLIT ? (int)cluster_ctas() : 2;
+  const int entry = SPLIT ? (int)blockIdx.x / ctas : blockIdx.x;
   const uint64_t code = CAP > 0 ? wl.item[entry] : a.work[entry];
   if (PAIRS && code == kPrefillNone) return;
   const bool half = SPLIT || (PAIRS && code >= kPrefillHalf);  // alike in all CTAs of a cluster
@@ -101,7 +101,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int n_all = t.tiles();
   // this CTA visits tiles t0 .. t0 + n_tiles - 1 of the item's n_all
   const int rank = half ? (int)cluster_rank() : 0;
-  const int per = SPLIT ? (n_all + (1 << lg_ctas) - 1) >> lg_ctas : (n_all + 1) / 2;
+  const int per = SPLIT ? (n_all + ctas - 1) / ctas : (n_all + 1) / 2;
   const int t0 = rank * per;
   const int n_tiles = !half ? n_all : SPLIT ? max(0, min(per, n_all - t0)) : rank == 0 ? (n_all + 1) / 2 : n_all / 2;
   const bool lone = SPLIT && !t.has_row(1, 0);
@@ -324,19 +324,20 @@ __global__ void __launch_bounds__(kThreads, 1)
     // The rows that there are, rounded up, are dealt to the CTAs in runs, and only those travel.
     // n states of each of this CTA's rows. Receive buffer: [n][D / 4][rows] float4, then [n][rows]
     // (m, l)
-    const int lg_all = !lone ? 8 : t.has_row(0, 64) ? 7 : t.has_row(0, 32) ? 6 : 5;
-    const int lg_rows = lg_all - lg_ctas, rows = 1 << lg_rows, n = lone ? 2 << lg_ctas : 1 << lg_ctas;
+    const int all = !lone ? 256 : t.has_row(0, 64) ? 128 : t.has_row(0, 32) ? 64 : 32;
+    const int rows = (all + ctas - 1) / ctas, n = lone ? 2 * ctas : ctas;
+    constexpr int kMostStates = 288;  // n * rows at any C
     float4* recv = reinterpret_cast<float4*>(smem);
-    float2* recv_ml = reinterpret_cast<float2*>(recv + D / 4 * 256);
-    uint32_t* spoilt = reinterpret_cast<uint32_t*>(recv_ml + 256);  // [4]: rows with a value that is not finite
+    float2* recv_ml = reinterpret_cast<float2*>(recv + D / 4 * kMostStates);
+    uint32_t* spoilt = reinterpret_cast<uint32_t*>(recv_ml + kMostStates);  // [4]: rows with a value that is not finite
     const int x = (warp - 2) >> 2, q4 = warp & 3, r = q4 * 32 + lane;
     if (warp >= 2) {
       const int row = lone ? r : x * 128 + r, from = lone ? 2 * rank + x : rank;
-      const int dst = (row >> lg_rows) & ((1 << lg_ctas) - 1), at = row & (rows - 1);
+      const int dst = min(row / rows, ctas - 1), at = row - dst * rows;
       const uint32_t tl = tmem + ((uint32_t)(q4 * 32) << 16) + 256 + x * D;
-      const uint32_t to = cluster_addr(recv + ((from * (D / 4)) << lg_rows) + at, (uint32_t)dst);
-      if (row < 1 << lg_all)
-        cluster_st2(cluster_addr(recv_ml + (from << lg_rows) + at, (uint32_t)dst), __float_as_uint(end_m),
+      const uint32_t to = cluster_addr(recv + from * (D / 4) * rows + at, (uint32_t)dst);
+      if (row < all)
+        cluster_st2(cluster_addr(recv_ml + from * rows + at, (uint32_t)dst), __float_as_uint(end_m),
                     __float_as_uint(end_l));
       if (n_tiles > (lone ? x : 0) && t.has_row(lone ? 0 : x, q4 * 32)) {
 #pragma unroll
@@ -346,7 +347,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           tmem_ld_wait();
 #pragma unroll
           for (int e = 0; e < 32; e += 4)
-            cluster_st4(to + (uint32_t)(((c * 8 + e / 4) << lg_rows) * 16), v[e], v[e + 1], v[e + 2], v[e + 3]);
+            cluster_st4(to + (uint32_t)((c * 8 + e / 4) * rows * 16), v[e], v[e + 1], v[e + 2], v[e + 3]);
         }
       }
       tc_fence_before();
@@ -360,26 +361,26 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (tid < 4) spoilt[tid] = 0;
       if (tid < rows) {
         float M = -INFINITY, L = 0.f;
-        for (int c = 0; c < n; ++c) M = fmaxf(M, recv_ml[(c << lg_rows) + tid].x);
+        for (int c = 0; c < n; ++c) M = fmaxf(M, recv_ml[c * rows + tid].x);
         for (int c = 0; c < n; ++c) {
-          const float2 ml = recv_ml[(c << lg_rows) + tid];
+          const float2 ml = recv_ml[c * rows + tid];
           if (ml.x != -INFINITY) L += fast_exp2(ml.x - M) * ml.y;
         }
         const float inv = L == 0.f ? 0.f : 1.f / L;
         for (int c = 0; c < n; ++c) {
-          const float m = recv_ml[(c << lg_rows) + tid].x;
-          recv_ml[(c << lg_rows) + tid].x = m == -INFINITY ? -1.f : fast_exp2(m - M) * inv;
+          const float m = recv_ml[c * rows + tid].x;
+          recv_ml[c * rows + tid].x = m == -INFINITY ? -1.f : fast_exp2(m - M) * inv;
         }
       }
       named_barrier_sync(3, 256);
-      for (int u = tid; u < D / 4 << lg_rows; u += 256) {
-        const int at = u & (rows - 1), k = u >> lg_rows, row = (rank << lg_rows) + at, ox = row >> 7, orow = row & 127;
-        if (!end_ok || !t.has_row(ox, orow)) continue;
+      for (int u = tid; u < D / 4 * rows; u += 256) {
+        const int k = u / rows, at = u - k * rows, row = rank * rows + at, ox = row >> 7, orow = row & 127;
+        if (!end_ok || row >= all || !t.has_row(ox, orow)) continue;
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
         for (int c = 0; c < n; ++c) {
-          const float f = recv_ml[(c << lg_rows) + at].x;
-          const float4 z = recv[((c * (D / 4) + k) << lg_rows) + at];
+          const float f = recv_ml[c * rows + at].x;
+          const float4 z = recv[(c * (D / 4) + k) * rows + at];
           if (f < 0.f) continue;
           o.x += f * z.x;
           o.y += f * z.y;
@@ -392,7 +393,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       named_barrier_sync(3, 256);
       if (warp < 6 && spoilt[warp - 2])
-        repair_rows<D>(a, code, (rank << lg_rows) + (warp - 2) * 32, spoilt[warp - 2]);
+        repair_rows<D>(a, code, rank * rows + (warp - 2) * 32, spoilt[warp - 2]);
     }
     __syncthreads();
     tc_fence_after();

@@ -70,6 +70,13 @@ PROMPTS = [
     ([3, 1], [9000, 257], 4, 1, 128, [0], 0, 1),
     ([100], [7003], 4, 2, 128, [0, 0], 0, 1),
     ([2, 11], [6300, 1], 16, 2, 64, [0, 1], 300, 3000),
+    # a query head a KV head: few rows and long ones after long prefixes
+    ([5], [4000], 2, 2, 64, [0, 1], 7, 90),
+    ([300, 40], [3333, 2600], 3, 3, 128, [0, 1, 0], 0, 1000),
+    # clusters whose size is no power of two
+    ([300], [3000], 32, 8, 64, [0] * 8, 0, 1),
+    ([311], [2900], 16, 4, 128, [0, 0, 1, 0], 5, 900),
+    ([140, 150], [2000, 1700], 5, 5, 128, [0, 1, 0, 0, 0], 5, 900),
 ]
 
 

@@ -457,7 +457,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       write_rows<D, D>(a, t, x, q4 * 32, 0, stage, lane);
       if constexpr (Call::kRepairs) {
-        const uint32_t rows = spoilt.rows();
+        const uint32_t rows = spoilt.rows(t.has_row(x, r));
         if (rows) repair_rows<D>(a, code & ~kPrefillHalf, x * 128 + q4 * 32, rows);
       }
       tc_fence_before();

@@ -415,9 +415,10 @@ struct Spoilt {
     for (int i = 0; i < 4; ++i)
       z[i] = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&v[i]), __float2bfloat162_rn(0.f), z[i]);
   }
-  __device__ __forceinline__ uint32_t rows() const {  // of the warp, a lane a row
+  // of the warp, a lane a row; there: whether there is one (what stands in for a row may be anything)
+  __device__ __forceinline__ uint32_t rows(bool there) const {
     const float2 f = __bfloat1622float2(__hadd2(__hadd2(z[0], z[1]), __hadd2(z[2], z[3])));
-    return __ballot_sync(0xffffffffu, !(f.x + f.y == 0.f));
+    return __ballot_sync(0xffffffffu, there && !(f.x + f.y == 0.f));
   }
 };
 template <int D, class A>
@@ -467,7 +468,7 @@ __device__ __forceinline__ uint32_t store_o(const A& a, const T& t, int x, int r
       __syncwarp();
     }
   }
-  return CallOf<A>::kRepairs ? spoilt.rows() : 0u;
+  return CallOf<A>::kRepairs ? spoilt.rows(t.has_row(x, row0 + lane)) : 0u;
 }
 
 }  // namespace pf

@@ -215,6 +215,39 @@ def test_prompts_do_not_see_hidden_keys(case, what):
             assert_matches(f64(out[at:at + 1]), want, f"row {r} of sequence {b}", mag=mag, abs_bounds=False)
 
 
+@pytest.mark.parametrize("g,hkv", [(3, 8), (7, 4)])
+def test_short_prompts_after_nans_in_shared_memory(g, hkv):
+    """Rows of a tile that are nobody's, whose contents are whatever lay there, cost
+    nothing: the call takes as long after one whose tensors are all NaN."""
+    d, q_lens = 64, [15 + i % 20 for i in range(100)]
+    q, k, v = prompt_inputs(q_lens, None, g * hkv, hkv, d)
+    pc = aoh.PagedCache(1, 16, g * hkv, hkv, d, 8, 30, [i % 2 for i in range(hkv)], max_seqs=len(q_lens))
+    out = torch.empty_like(q)
+
+    def timed():
+        best = float("inf")
+        for _ in range(5):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            torch.cuda._sleep(1000000)
+            a.record()
+            pc.prefill(q, k, v, q_lens, out)
+            b.record()
+            torch.cuda.synchronize()
+            best = min(best, a.elapsed_time(b))
+        return best
+
+    timed()
+    before = timed()
+    want = out.clone()
+    n = 1500
+    bad = torch.full((n, g * hkv, d), float("nan"), dtype=torch.bfloat16, device="cuda")
+    pc.prefill(bad, bad[:, :hkv], bad[:, :hkv], [n], torch.empty_like(bad))
+    after = timed()
+    pc.check()
+    assert torch.equal(out, want)
+    assert after < 3 * before + 0.02, (before, after)
+
+
 @pytest.mark.parametrize("case", [2, 6, 10, 13])
 def test_prompts_in_a_graph(case):
     """A captured call, by-value sequences and uploaded ones, replays with new inputs."""

@@ -239,6 +239,7 @@ struct CallOf<PackedArgs> {
   using MaskT = PackedMask;
   static constexpr bool kEmptyRows = true;  // fewer keys than rows
   static constexpr bool kRepairs = true;
+  static constexpr bool kThirdS = true;
   static constexpr bool kChained = true;
 };
 template <>
@@ -247,6 +248,7 @@ struct CallOf<FoldedArgs> {
   using MaskT = PackedMask;
   static constexpr bool kEmptyRows = true;
   static constexpr bool kRepairs = true;
+  static constexpr bool kThirdS = true;
   static constexpr bool kChained = true;
 };
 

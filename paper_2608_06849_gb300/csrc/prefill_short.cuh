@@ -32,7 +32,7 @@ struct ShortCfg {
   static constexpr int STAGE = 32 * COLS * 2;    // a warp's
   static constexpr int OFF_STAGE = C::OFF_BAR;   // 8 warps
   static constexpr int OFF_BAR = OFF_STAGE + 8 * STAGE;
-  static constexpr int NBAR = 2 + 2 * kNS + 2 + 4 + 2 + 2 + 1;
+  static constexpr int NBAR = 2 + 2 * kNS + 4 + 8 + 2 + 2 + 1;
   static constexpr int SMEM = OFF_BAR + NBAR * 8 + 16 + 1024;
   static_assert(SMEM <= 232448, "shared memory");
 };
@@ -43,6 +43,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   using C = PfCfg<D>;
   using X = ShortCfg<D>;
   using Call = CallOf<A>;
+  using SB = SBuf<A, D>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
   uint8_t* sQ = smem + C::OFF_Q;
@@ -51,9 +52,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* q_empty = q_full + 1;
   uint64_t* kv_full = q_empty + 1;
   uint64_t* kv_empty = kv_full + kNS;
-  uint64_t* s_full = kv_empty + kNS;   // [2]: S_A, S_B ready
-  uint64_t* p_full = s_full + 2;       // [2][2]: P_A, P_B written, keys 0-63 and 64-127
-  uint64_t* pv_done = p_full + 4;      // [2]: O_A, O_B updated
+  uint64_t* s_full = kv_empty + kNS;   // [SB::bar]: S_A, S_B ready
+  uint64_t* p_full = s_full + 4;       // [SB::bar][2]: P_A, P_B written, keys 0-63 and 64-127
+  uint64_t* pv_done = p_full + 8;      // [2]: O_A, O_B updated
   uint64_t* v_zeroed = pv_done + 2;    // [2]: padding rows of every other partial V tile are zeroed
   uint64_t* drain = v_zeroed + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
@@ -75,10 +76,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&kv_full[s], 1);
       mbar_init(&kv_empty[s], 1);
     }
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(&s_full[i], 1);
+      mbar_init(&p_full[2 * i], 4);
+      mbar_init(&p_full[2 * i + 1], 4);
+    }
     for (int x = 0; x < 2; ++x) {
-      mbar_init(&s_full[x], 1);
-      mbar_init(&p_full[2 * x], 4);
-      mbar_init(&p_full[2 * x + 1], 4);
       mbar_init(&pv_done[x], 1);
       mbar_init(&v_zeroed[x], 1);
     }
@@ -165,26 +168,29 @@ __global__ void __launch_bounds__(kThreads, 1)
     auto commit = [&](uint64_t* bar) {
       if (elect_one()) tc_commit(bar);
     };
-    auto s_of = [&](int x, int kt) {
+    auto s_at = [&](int x, int kt, int b) {
       const uint64_t k_desc = k_desc0 + (uint32_t)(((2 * kt) % kNS) * sdesc_step(C::KVBYTES));
       if (elect_one()) {
-        issue_s<D>(tmem, q_desc + sdesc_step(x * C::QBYTES), k_desc, x);
-        tc_commit(&s_full[x]);
+        issue_s<D>(tmem + b * 128, q_desc + sdesc_step(x * C::QBYTES), k_desc);
+        tc_commit(&s_full[SB::bar(x, kt)]);
       }
     };
-    auto pv_of = [&](int x, bool first) {
+    auto s_of = [&](int x, int kt) { s_at(x, kt, x); };
+    auto pv_at = [&](int x, bool first, int b) {
       const uint64_t v_desc = v_desc0 + (uint32_t)(((2 * kt + 1) % kNS) * sdesc_step(C::KVBYTES));
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        if (!wait(&p_full[2 * x + half], kt & 1)) return false;
+        if (!wait(&p_full[2 * SB::bar(x, kt) + half], SB::phase(kt))) return false;
         tc_fence_after();
         if (elect_one()) {
-          issue_pv<D>(tmem, v_desc, x, half, first);
+          issue_pv<D>(tmem + SB::O + x * D, tmem + b * 128, v_desc, half, first);
           if (half) tc_commit(&pv_done[x]);
         }
       }
       return true;
     };
+    auto pv_of = [&](int x, bool first) { return pv_at(x, first, x); };
+    int b = 0;  // three buffers: that of tile kt's S_A
     auto wait_k = [&](int kt) { return wait(&kv_full[(2 * kt) % kNS], ((2 * kt) / kNS) & 1); };
     for (int k = 0; ok; ++k) {
       const int ii = item_index(k);
@@ -195,6 +201,43 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int part1 = t.valid(g, n - 1) < kBN ? n - 1 : -1;
       if (!wait(q_full, k & 1) || !wait_k(kt)) break;
       tc_fence_after();
+      if constexpr (SB::N == 3) {
+        auto on = [](int b) { return b == 2 ? 0 : b + 1; };
+        s_at(0, kt, b);
+        s_at(1, kt, on(b));
+        commit(&kv_empty[(2 * kt) % kNS]);
+        if (n == 1) {
+          commit(q_empty);
+        } else {
+          if (!wait_k(kt + 1)) break;
+          tc_fence_after();
+          s_at(0, kt + 1, on(on(b)));
+        }
+        // after the P V of an S comes the third S after it
+        for (int jj = 0; jj < n && ok; ++jj, ++kt) {
+          if (!wait(&kv_full[(2 * kt + 1) % kNS], ((2 * kt + 1) / kNS) & 1)) break;
+          if (jj == part0 || jj == part1) {
+            if (!wait(&v_zeroed[n_partial & 1], (n_partial >> 1) & 1)) break;
+            ++n_partial;
+          }
+          if (!pv_at(0, jj == 0, b)) break;
+          if (jj + 1 < n) {
+            s_at(1, kt + 1, b);
+            commit(&kv_empty[(2 * (kt + 1)) % kNS]);
+            if (jj + 2 == n) commit(q_empty);
+          }
+          b = on(b);
+          if (!pv_at(1, jj == 0, b)) break;
+          commit(&kv_empty[(2 * kt + 1) % kNS]);
+          if (jj + 2 < n) {
+            if (!wait_k(kt + 2)) break;
+            tc_fence_after();
+            s_at(0, kt + 2, b);
+          }
+          b = on(b);
+        }
+        continue;
+      }
       s_of(0, kt);
       s_of(1, kt);
       commit(&kv_empty[(2 * kt) % kNS]);
@@ -231,7 +274,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int q4 = warp & 3;        // TMEM lane quarter this warp may access
     const int r = q4 * 32 + lane;
     const uint32_t tl = tmem + ((uint32_t)(q4 * 32) << 16);
-    const uint32_t s_col = x * 128, o_col = 256 + x * D;
+    const uint32_t o_col = SB::O + x * D;
+    uint32_t s_col = x * 128;
     uint8_t* stage = smem + X::OFF_STAGE + (warp - 2) * X::STAGE;
     uint32_t kt = 0;  // KV tiles so far, over all items
     bool ok = true;
@@ -244,11 +288,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       float m = -INFINITY, l = 0.f;
       for (int jj = 0; jj < n && ok; ++jj, ++kt) {
         const typename Call::MaskT mask(g, t, jj, i, qx0, rot);
-        ok = __all_sync(0xffffffffu, wait_bar(&s_full[x], kt & 1, a.err, abort_flag));
+        ok = __all_sync(0xffffffffu, wait_bar(&s_full[SB::bar(x, kt)], SB::phase(kt), a.err, abort_flag));
         if (!ok) break;
         tc_fence_after();
-        ok = softmax_tile<D>(a, mask, tl, s_col, o_col, jj == 0, m, l, &pv_done[x], (kt - 1) & 1, &p_full[2 * x],
-                             abort_flag);
+        ok = softmax_tile<D>(a, mask, tl, s_col, o_col, jj == 0, m, l, &pv_done[x], (kt - 1) & 1,
+                             &p_full[2 * SB::bar(x, kt)], abort_flag);
+        if (SB::N == 3) s_col = s_col >= 128 ? s_col - 128 : 256;  // two buffers on
       }
       if (!ok) break;
       ok = __all_sync(0xffffffffu, wait_bar(&pv_done[x], (kt - 1) & 1, a.err, abort_flag));

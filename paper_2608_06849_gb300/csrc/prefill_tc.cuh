@@ -64,6 +64,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     prefill_tc_kernel(const __grid_constant__ A a, const __grid_constant__ WorkList<CAP> wl) {
   using C = PfCfg<D>;
   using Call = CallOf<A>;
+  using SB = SBuf<A, D>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
   uint8_t* sQ = smem + C::OFF_Q;
@@ -72,9 +73,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* q_full = bars;
   uint64_t* kv_full = bars + 1;
   uint64_t* kv_empty = kv_full + kNS;
-  uint64_t* s_full = kv_empty + kNS;  // [2]: S_A, S_B ready
-  uint64_t* p_full = s_full + 2;      // [2][2]: P_A, P_B written, keys 0-63 and 64-127
-  uint64_t* pv_done = p_full + 4;     // [2]: O_A, O_B updated (P buffer free)
+  uint64_t* s_full = kv_empty + kNS;  // [SB::bar]: S_A, S_B ready
+  uint64_t* p_full = s_full + 4;      // [SB::bar][2]: P_A, P_B written, keys 0-63 and 64-127
+  uint64_t* pv_done = p_full + 8;     // [2]: O_A, O_B updated (P buffer free)
   uint64_t* drain = pv_done + 2;
   // [2]: padding rows of the item's first / second partial V tile are zeroed.
   // Only the last cache tile and the chunk tile holding row len - 1 can be
@@ -111,10 +112,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&kv_full[s], 1);
       mbar_init(&kv_empty[s], 1);
     }
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(&s_full[i], 1);
+      mbar_init(&p_full[2 * i], 4);
+      mbar_init(&p_full[2 * i + 1], 4);
+    }
     for (int x = 0; x < 2; ++x) {
-      mbar_init(&s_full[x], 1);
-      mbar_init(&p_full[2 * x], 4);
-      mbar_init(&p_full[2 * x + 1], 4);
       mbar_init(&pv_done[x], 1);
     }
     mbar_init(drain, 1);
@@ -188,13 +191,15 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint64_t q_desc = sdesc_sw128(smem_u32(sQ), 16, 1024);
     const uint64_t k_desc0 = sdesc_sw128(smem_u32(sKV), 16, 1024);
     const uint64_t v_desc0 = sdesc_sw128(smem_u32(sKV), C::BOX, 1024);
-    auto s_of = [&](int x, int jj) {
+    // S_X of the step, against K_jj, to buffer b
+    auto s_at = [&](int x, int step, int jj, int b) {
       const uint64_t k_desc = k_desc0 + (uint32_t)(((2 * jj) % kNS) * sdesc_step(C::KVBYTES));
       if (elect_one()) {
-        issue_s<D>(tmem, q_desc + (lone ? 0u : sdesc_step(x * C::QBYTES)), k_desc, x);
-        tc_commit(&s_full[x]);
+        issue_s<D>(tmem + b * 128, q_desc + (lone ? 0u : sdesc_step(x * C::QBYTES)), k_desc);
+        tc_commit(&s_full[SB::bar(x, step)]);
       }
     };
+    auto s_of = [&](int x, int jj) { s_at(x, jj, jj, x); };
     auto commit = [&](uint64_t* bar) {
       if (elect_one()) tc_commit(bar);
     };
@@ -203,22 +208,22 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (ok) ok = __all_sync(0xffffffffu, wait_bar(bar, parity, a.err, abort_flag));
       return ok;
     };
-    // O_X += P_X(step) V_jj: the first half of the keys while the softmax forms the
+    // O_X += P_X(step) V_jj, P in buffer b: the first half of the keys while the softmax forms the
     // second half's weights
-    auto pv_at = [&](int x, int step, int jj) {
+    auto pv_at = [&](int x, int step, int jj, int b) {
       const uint64_t v_desc = v_desc0 + (uint32_t)(((2 * jj + 1) % kNS) * sdesc_step(C::KVBYTES));
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        if (!wait(&p_full[2 * x + half], step & 1)) return false;
+        if (!wait(&p_full[2 * SB::bar(x, step) + half], SB::phase(step))) return false;
         tc_fence_after();
         if (elect_one()) {
-          issue_pv<D>(tmem, v_desc, x, half, step == 0);
+          issue_pv<D>(tmem + SB::O + x * D, tmem + b * 128, v_desc, half, step == 0);
           if (half) tc_commit(&pv_done[x]);
         }
       }
       return true;
     };
-    auto pv_of = [&](int x, int jj) { return pv_at(x, jj, jj); };
+    auto pv_of = [&](int x, int jj) { return pv_at(x, jj, jj, x); };
     auto wait_k = [&](int jj) { return wait(&kv_full[(2 * jj) % kNS], ((2 * jj) / kNS) & 1); };
     // only the last cached tile and the last chunk tile can be partial
     int n_partial = 0;  // partial V tiles seen so far (index into v_zeroed)
@@ -238,16 +243,45 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (j >= n_tiles) return true;
         if (!wait_k(j)) return false;
         tc_fence_after();
-        s_of(x, j);
+        s_at(x, j >> 1, j, j % SB::N);
         commit(&kv_empty[(2 * j) % kNS]);
         return true;
       };
       if (wait(q_full, 0) && lone_s(0, 0)) lone_s(1, 1);
       for (int j = 0; j < n_tiles && ok; ++j) {
         const int x = j & 1;
-        if (!wait_v(j) || !pv_at(x, j >> 1, j)) break;
+        if (!wait_v(j) || !pv_at(x, j >> 1, j, j % SB::N)) break;
         commit(&kv_empty[(2 * j + 1) % kNS]);
         if (!lone_s(x, j + 2)) break;
+      }
+    } else if (SB::N == 3) {
+      if (wait(q_full, 0) && wait_k(0)) {
+        tc_fence_after();
+        s_at(0, 0, 0, 0);
+        s_at(1, 0, 0, 1);
+        commit(&kv_empty[0]);
+        if (n_tiles > 1 && wait_k(1)) {
+          tc_fence_after();
+          s_at(0, 1, 1, 2);
+        }
+      }
+      // after the P V of the n-th S comes the n + 3rd S
+      int b = 0;
+      for (int jj = 0; jj < n_tiles && ok; ++jj) {
+        if (!wait_v(jj) || !pv_at(0, jj, jj, b)) break;
+        if (jj + 1 < n_tiles) {
+          s_at(1, jj + 1, jj + 1, b);
+          commit(&kv_empty[(2 * (jj + 1)) % kNS]);
+        }
+        b = b == 2 ? 0 : b + 1;
+        if (!pv_at(1, jj, jj, b)) break;
+        commit(&kv_empty[(2 * jj + 1) % kNS]);
+        if (jj + 2 < n_tiles) {
+          if (!wait_k(jj + 2)) break;
+          tc_fence_after();
+          s_at(0, jj + 2, jj + 2, b);
+        }
+        b = b == 2 ? 0 : b + 1;
       }
     } else if (wait(q_full, 0) && wait_k(0)) {
       tc_fence_after();
@@ -255,7 +289,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       s_of(1, 0);
       commit(&kv_empty[0]);
     }
-    for (int jj = 0; jj < n_tiles && ok && !lone; ++jj) {
+    for (int jj = 0; SB::N == 2 && jj < n_tiles && ok && !lone; ++jj) {
       const bool more = jj + 1 < n_tiles;
       // tile A: P_A(jj) sits in S_A's columns; S_A(jj+1) may overwrite them
       // only after O_A += P_A(jj) V_jj is issued (same-thread MMAs run in order)
@@ -286,17 +320,19 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int i = t.row(qt, r);           // of the sequence
     const int steps = lone ? (n_tiles + 1 - x) >> 1 : n_tiles;
     const uint32_t tl = tmem + ((uint32_t)(q4 * 32) << 16);
-    const uint32_t s_col = x * 128, o_col = 256 + x * D;
+    const uint32_t o_col = SB::O + x * D;
+    uint32_t s_col = x * 128;
     const int rot = t.rot(g);
     float m = -INFINITY, l = 0.f;
     bool ok = true;
     for (int jj = 0; jj < steps && ok; ++jj) {
       const typename Call::MaskT mask(g, t, t0 + (lone ? 2 * jj + x : jj), i, qx0, rot);
-      ok = __all_sync(0xffffffffu, wait_bar(&s_full[x], jj & 1, a.err, abort_flag));
+      ok = __all_sync(0xffffffffu, wait_bar(&s_full[SB::bar(x, jj)], SB::phase(jj), a.err, abort_flag));
       if (!ok) break;
       tc_fence_after();
       ok = softmax_tile<D>(a, mask, tl, s_col, o_col, jj == 0, m, l, &pv_done[x], (jj - 1) & 1,
-                           &p_full[2 * x], abort_flag);
+                           &p_full[2 * SB::bar(x, jj)], abort_flag);
+      if (SB::N == 3) s_col = s_col >= 128 ? s_col - 128 : 256;  // two buffers on
     }
     if (half) {
       end_m = m;
@@ -334,7 +370,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (warp >= 2) {
       const int row = lone ? r : x * 128 + r, from = lone ? 2 * rank + x : rank;
       const int dst = min(row / rows, ctas - 1), at = row - dst * rows;
-      const uint32_t tl = tmem + ((uint32_t)(q4 * 32) << 16) + 256 + x * D;
+      const uint32_t tl = tmem + ((uint32_t)(q4 * 32) << 16) + SB::O + x * D;
       const uint32_t to = cluster_addr(recv + from * (D / 4) * rows + at, (uint32_t)dst);
       if (row < all)
         cluster_st2(cluster_addr(recv_ml + from * rows + at, (uint32_t)dst), __float_as_uint(end_m),
@@ -402,7 +438,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     cluster_arrive();
     cluster_wait();
     const int x = (warp - 2) >> 2, q4 = warp & 3, r = q4 * 32 + lane;
-    const uint32_t tl = tmem + ((uint32_t)(q4 * 32) << 16) + 256 + x * D;
+    const uint32_t tl = tmem + ((uint32_t)(q4 * 32) << 16) + SB::O + x * D;
     float4* recv = reinterpret_cast<float4*>(smem);  // [D / 4][128 rows], then (m, l) per row
     float2* recv_ml = reinterpret_cast<float2*>(recv + D / 4 * 128);
     if (warp >= 2 && x != rank) {

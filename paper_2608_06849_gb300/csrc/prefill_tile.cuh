@@ -32,7 +32,7 @@ struct PfCfg {
   static constexpr int OFF_Q = 0;                // Q_A, Q_B
   static constexpr int OFF_KV = OFF_Q + 2 * QBYTES;
   static constexpr int OFF_BAR = OFF_KV + kNS * KVBYTES;
-  static constexpr int NBAR = 1 + 2 * kNS + 2 + 4 + 2 + 1 + 2;
+  static constexpr int NBAR = 1 + 2 * kNS + 4 + 8 + 2 + 1 + 2;
   static constexpr int SMEM = OFF_BAR + NBAR * 8 + 16 + 1024;
   static constexpr uint32_t IDESC_S = idesc_bf16(kBM, kBN, false);
   static constexpr uint32_t IDESC_PV = idesc_bf16(kBM, D, true);
@@ -154,24 +154,24 @@ __device__ __forceinline__ void zero_tail(uint8_t* vt, int valid, int lane) {
 // S_X = Q_X K^T; one thread. q_desc, k_desc: descriptors of the query tile and of
 // the K tile.
 template <int D>
-__device__ __forceinline__ void issue_s(uint32_t tmem, uint64_t q_desc, uint64_t k_desc, int x) {
+__device__ __forceinline__ void issue_s(uint32_t s_tmem, uint64_t q_desc, uint64_t k_desc) {
   using C = PfCfg<D>;
 #pragma unroll
   for (int kk = 0; kk < D / 16; ++kk) {
     const uint32_t off = sdesc_step((kk >> 2) * C::BOX + (kk & 3) * 32);
-    tc_mma(tmem + x * 128, q_desc + off, k_desc + off, C::IDESC_S, kk > 0 ? 1u : 0u);
+    tc_mma(s_tmem, q_desc + off, k_desc + off, C::IDESC_S, kk > 0 ? 1u : 0u);
   }
 }
 
 // O_X (+)= P_X V over half of the tile's keys (0-63 or 64-127); one thread.
 // v_desc: descriptor of the V tile.
 template <int D>
-__device__ __forceinline__ void issue_pv(uint32_t tmem, uint64_t v_desc, int x, int half, bool first) {
+__device__ __forceinline__ void issue_pv(uint32_t o_tmem, uint32_t p_tmem, uint64_t v_desc, int half, bool first) {
   using C = PfCfg<D>;
 #pragma unroll
   for (int k = 0; k < kBN / 32; ++k) {
     const int kk = half * (kBN / 32) + k;
-    tc_mma_ts(tmem + 256 + x * D, tmem + x * 128 + kk * 8, v_desc + sdesc_step(kk * 16 * 128), C::IDESC_PV,
+    tc_mma_ts(o_tmem, p_tmem + kk * 8, v_desc + sdesc_step(kk * 16 * 128), C::IDESC_PV,
               (kk > 0 || !first) ? 1u : 0u);
   }
 }
@@ -231,11 +231,26 @@ struct Mask {
 // whether rows may see no key at all (their outputs are zeros).
 template <class A>
 struct CallOf;
+
+// The columns of S. With two buffers, one a query tile, S_X(j + 1) waits for O_X += P_X(j) V, and
+// a tile's softmax for both. d_head 64 leaves room for a third, in which the n-th S (of tile n & 1, KV
+// tile n >> 1) goes to buffer n % 3 as soon as the n - 3rd P V is issued, so that a softmax finds its
+// next S ready. Barriers are then two a query tile, taken in turns, each completed again only when its last phase
+// has been waited for.
+template <class A, int D>
+struct SBuf {
+  static constexpr int N = D == 64 && CallOf<A>::kThirdS ? 3 : 2;
+  static constexpr int O = N * 128;  // first column of O
+  // barrier and phase of query tile x's j-th S, and of its P
+  __device__ __forceinline__ static int bar(int x, int j) { return N == 3 ? 2 * x + (j & 1) : x; }
+  __device__ __forceinline__ static uint32_t phase(int j) { return N == 3 ? (j >> 1) & 1 : j & 1; }
+};
 template <>
 struct CallOf<PrefillTcArgs> {
   using ItemT = Item;
   using MaskT = Mask;
   static constexpr bool kEmptyRows = false;
+  static constexpr bool kThirdS = false;
   static constexpr bool kRepairs = false;  // rows that a hidden V row's NaN reached are gone over again (repair_rows)
   static constexpr bool kChained = false;  // launches overlap the one before (wait_to_start, wait_to_end)
 };

@@ -37,7 +37,7 @@
 //               tcgen05.st (key k in column k/2, even k in the low half),
 //               announced in two halves of 64 keys.
 // TMEM columns: S_A / P_A [0,128), S_B / P_B [128,256), O_A [256, 256+D),
-// O_B [256+D, 256+2D).
+// O_B [256+D, 256+2D); with three buffers for S (SBuf) O comes 128 columns later.
 #pragma once
 
 #include <string.h>

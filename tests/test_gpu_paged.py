@@ -77,6 +77,10 @@ PROMPTS = [
     ([300], [3000], 32, 8, 64, [0] * 8, 0, 1),
     ([311], [2900], 16, 4, 128, [0, 0, 1, 0], 5, 900),
     ([140, 150], [2000, 1700], 5, 5, 128, [0, 1, 0, 0, 0], 5, 900),
+    # heads of 64: items that two CTAs share, long ones, and many with several tiles
+    ([1200], None, 4, 4, 64, [0, 1, 0, 0], 3, 700),
+    ([1700, 900], [1900, 900], 16, 8, 64, [0, 1] * 4, 3, 700),
+    ([200 + 37 * (i % 9) for i in range(24)], None, 32, 8, 64, [0, 1] * 4, 9, 150),
 ]
 
 

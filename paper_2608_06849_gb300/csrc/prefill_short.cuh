@@ -32,7 +32,7 @@ struct ShortCfg {
   static constexpr int STAGE = 32 * COLS * 2;    // a warp's
   static constexpr int OFF_STAGE = C::OFF_BAR;   // 8 warps
   static constexpr int OFF_BAR = OFF_STAGE + 8 * STAGE;
-  static constexpr int NBAR = 2 + 2 * kNS + 4 + 8 + 2 + 2 + 1;
+  static constexpr int NBAR = 2 + 2 * kNS + 4 + 8 + 4 + 2 + 1;
   static constexpr int SMEM = OFF_BAR + NBAR * 8 + 16 + 1024;
   static_assert(SMEM <= 232448, "shared memory");
 };
@@ -54,8 +54,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* kv_empty = kv_full + kNS;
   uint64_t* s_full = kv_empty + kNS;   // [SB::bar]: S_A, S_B ready
   uint64_t* p_full = s_full + 4;       // [SB::bar][2]: P_A, P_B written, keys 0-63 and 64-127
-  uint64_t* pv_done = p_full + 8;      // [2]: O_A, O_B updated
-  uint64_t* v_zeroed = pv_done + 2;    // [2]: padding rows of every other partial V tile are zeroed
+  uint64_t* pv_done = p_full + 8;      // [SB::bar]: O_A, O_B updated
+  uint64_t* v_zeroed = pv_done + 4;    // [2]: padding rows of every other partial V tile are zeroed
   uint64_t* drain = v_zeroed + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
@@ -80,9 +80,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&s_full[i], 1);
       mbar_init(&p_full[2 * i], 4);
       mbar_init(&p_full[2 * i + 1], 4);
+      mbar_init(&pv_done[i], 1);
     }
     for (int x = 0; x < 2; ++x) {
-      mbar_init(&pv_done[x], 1);
       mbar_init(&v_zeroed[x], 1);
     }
     mbar_init(drain, 1);
@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc_fence_after();
         if (elect_one()) {
           issue_pv<D>(tmem + SB::O + x * D, tmem + b * 128, v_desc, half, first);
-          if (half) tc_commit(&pv_done[x]);
+          if (half) tc_commit(&pv_done[SB::bar(x, kt)]);
         }
       }
       return true;
@@ -291,12 +291,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         ok = __all_sync(0xffffffffu, wait_bar(&s_full[SB::bar(x, kt)], SB::phase(kt), a.err, abort_flag));
         if (!ok) break;
         tc_fence_after();
-        ok = softmax_tile<D>(a, mask, tl, s_col, o_col, jj == 0, m, l, &pv_done[x], (kt - 1) & 1,
+        ok = softmax_tile<D>(a, mask, tl, s_col, o_col, jj == 0, m, l, &pv_done[SB::bar(x, kt - 1)], SB::phase(kt - 1),
                              &p_full[2 * SB::bar(x, kt)], abort_flag);
         if (SB::N == 3) s_col = s_col >= 128 ? s_col - 128 : 256;  // two buffers on
       }
       if (!ok) break;
-      ok = __all_sync(0xffffffffu, wait_bar(&pv_done[x], (kt - 1) & 1, a.err, abort_flag));
+      ok = __all_sync(0xffffffffu, wait_bar(&pv_done[SB::bar(x, kt - 1)], SB::phase(kt - 1), a.err, abort_flag));
       if (!ok) break;
       tc_fence_after();
       if (store_o<D, X::COLS>(a, t, x, q4 * 32, tl + o_col, l, stage, lane) && lane == 0)

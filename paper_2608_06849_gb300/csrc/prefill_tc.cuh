@@ -75,8 +75,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* kv_empty = kv_full + kNS;
   uint64_t* s_full = kv_empty + kNS;  // [SB::bar]: S_A, S_B ready
   uint64_t* p_full = s_full + 4;      // [SB::bar][2]: P_A, P_B written, keys 0-63 and 64-127
-  uint64_t* pv_done = p_full + 8;     // [2]: O_A, O_B updated (P buffer free)
-  uint64_t* drain = pv_done + 2;
+  uint64_t* pv_done = p_full + 8;     // [SB::bar]: O_A, O_B updated (P buffer free)
+  uint64_t* drain = pv_done + 4;
   // [2]: padding rows of the item's first / second partial V tile are zeroed.
   // Only the last cache tile and the chunk tile holding row len - 1 can be
   // partial, so each barrier completes at most once per item.
@@ -116,9 +116,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&s_full[i], 1);
       mbar_init(&p_full[2 * i], 4);
       mbar_init(&p_full[2 * i + 1], 4);
-    }
-    for (int x = 0; x < 2; ++x) {
-      mbar_init(&pv_done[x], 1);
+      mbar_init(&pv_done[i], 1);
     }
     mbar_init(drain, 1);
     mbar_init(&v_zeroed[0], 1);
@@ -218,7 +216,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc_fence_after();
         if (elect_one()) {
           issue_pv<D>(tmem + SB::O + x * D, tmem + b * 128, v_desc, half, step == 0);
-          if (half) tc_commit(&pv_done[x]);
+          if (half) tc_commit(&pv_done[SB::bar(x, step)]);
         }
       }
       return true;
@@ -330,7 +328,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       ok = __all_sync(0xffffffffu, wait_bar(&s_full[SB::bar(x, jj)], SB::phase(jj), a.err, abort_flag));
       if (!ok) break;
       tc_fence_after();
-      ok = softmax_tile<D>(a, mask, tl, s_col, o_col, jj == 0, m, l, &pv_done[x], (jj - 1) & 1,
+      ok = softmax_tile<D>(a, mask, tl, s_col, o_col, jj == 0, m, l, &pv_done[SB::bar(x, jj - 1)], SB::phase(jj - 1),
                            &p_full[2 * SB::bar(x, jj)], abort_flag);
       if (SB::N == 3) s_col = s_col >= 128 ? s_col - 128 : 256;  // two buffers on
     }
@@ -338,9 +336,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       end_m = m;
       end_l = l;
       end_ok = ok && (steps == 0 ||
-                      __all_sync(0xffffffffu, wait_bar(&pv_done[x], (steps - 1) & 1, a.err, abort_flag)));
+                      __all_sync(0xffffffffu, wait_bar(&pv_done[SB::bar(x, steps - 1)], SB::phase(steps - 1), a.err, abort_flag)));
     } else if (ok && ((Call::kEmptyRows && n_tiles == 0) ||
-                      __all_sync(0xffffffffu, wait_bar(&pv_done[x], (n_tiles - 1) & 1, a.err, abort_flag)))) {
+                      __all_sync(0xffffffffu, wait_bar(&pv_done[SB::bar(x, n_tiles - 1)], SB::phase(n_tiles - 1), a.err, abort_flag)))) {
       tc_fence_after();
       // Q_X is free: the last S_X was done before the last P V
       const uint32_t spoilt =

@@ -32,7 +32,7 @@ struct PfCfg {
   static constexpr int OFF_Q = 0;                // Q_A, Q_B
   static constexpr int OFF_KV = OFF_Q + 2 * QBYTES;
   static constexpr int OFF_BAR = OFF_KV + kNS * KVBYTES;
-  static constexpr int NBAR = 1 + 2 * kNS + 4 + 8 + 2 + 1 + 2;
+  static constexpr int NBAR = 1 + 2 * kNS + 4 + 8 + 4 + 1 + 2;
   static constexpr int SMEM = OFF_BAR + NBAR * 8 + 16 + 1024;
   static constexpr uint32_t IDESC_S = idesc_bf16(kBM, kBN, false);
   static constexpr uint32_t IDESC_PV = idesc_bf16(kBM, D, true);
@@ -237,13 +237,14 @@ struct CallOf;
 // tile n >> 1) goes to buffer n % 3 as soon as the n - 3rd P V is issued, so that a softmax finds its
 // next S ready: 16,384 tokens of 32/8 heads 1055 -> 1012 us, 512 rows after 30,000 154 -> 145, 2,048 of 8/8
 // heads 16.9 -> 15.6. (What is left is the softmax itself: half of the issue slots, its chains the rest.)
-// Barriers are then two a query tile, taken in turns, each completed again only when its last
-// phase has been waited for.
+// Barriers are then two a query tile, taken in turns: by the time that a phase is waited for, the
+// one before it on the same barrier is complete, also that of a P V, which may be two behind its
+// tile's last S.
 template <class A, int D>
 struct SBuf {
   static constexpr int N = D == 64 && CallOf<A>::kThirdS ? 3 : 2;
   static constexpr int O = N * 128;  // first column of O
-  // barrier and phase of query tile x's j-th S, and of its P
+  // barrier and phase of query tile x's j-th S, of its P and of its P V
   __device__ __forceinline__ static int bar(int x, int j) { return N == 3 ? 2 * x + (j & 1) : x; }
   __device__ __forceinline__ static uint32_t phase(int j) { return N == 3 ? (j >> 1) & 1 : j & 1; }
 };

@@ -219,6 +219,29 @@ def test_prompts_do_not_see_hidden_keys(case, what):
             assert_matches(f64(out[at:at + 1]), want, f"row {r} of sequence {b}", mag=mag, abs_bounds=False)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("kind", ["many", "long", "split"])
+def test_prompts_come_out_alike_every_time(d, kind):
+    """The same call with its tensors in and out of the cache: bit for bit the same."""
+    hq, hkv = 32, 8
+    q_lens, k_lens = {"many": ([200 + 37 * (i % 9) for i in range(24)], None), "long": ([2500], None),
+                      "split": ([40], [6000])}[kind]
+    q, k, v = prompt_inputs(q_lens, k_lens, hq, hkv, d, seed=9)
+    pc = aoh.PagedCache(1, 16, hq, hkv, d, 9, 150, [0, 1] * 4, max_seqs=len(q_lens))
+    want = torch.empty_like(q)
+    pc.prefill(q, k, v, q_lens, want, k_lens=k_lens)
+    flush = torch.empty(256 << 20, dtype=torch.uint8, device="cuda")
+    bad = torch.zeros((), dtype=torch.int64, device="cuda")
+    for i in range(60):
+        if i % 2:
+            flush.fill_(i)
+        out = torch.full_like(q, float("nan"))
+        pc.prefill(q, k, v, q_lens, out, k_lens=k_lens)
+        bad += (out != want).any().long()
+    pc.check()
+    assert bad.item() == 0
+
+
 @pytest.mark.parametrize("g,hkv", [(3, 8), (7, 4)])
 def test_short_prompts_after_nans_in_shared_memory(g, hkv):
     """Rows of a tile that are nobody's, whose contents are whatever lay there, cost

@@ -240,6 +240,8 @@ struct CallOf<PackedArgs> {
   static constexpr bool kEmptyRows = true;  // fewer keys than rows
   static constexpr bool kRepairs = true;
   static constexpr bool kThirdS = true;
+  template <int D>
+  static constexpr bool kLaneRows = D == 64;
   static constexpr bool kChained = true;
 };
 template <>
@@ -249,6 +251,8 @@ struct CallOf<FoldedArgs> {
   static constexpr bool kEmptyRows = true;
   static constexpr bool kRepairs = true;
   static constexpr bool kThirdS = true;
+  template <int D>
+  static constexpr bool kLaneRows = true;
   static constexpr bool kChained = true;
 };
 

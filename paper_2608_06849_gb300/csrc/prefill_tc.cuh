@@ -59,6 +59,11 @@ namespace pf {
 // pipeline work on its first tile, A on the even KV tiles and B on the odd ones, and their states
 // count as those of two CTAs.
 constexpr int kWhole = 0, kPairs = 1, kSplit = 2;
+
+// Whether a part of an item saw no key of a row. A part whose visible scores are all NaN has a
+// maximum of -inf as well, no NaN being the greater of two numbers, but its sum is NaN.
+__device__ __forceinline__ bool empty_state(float m, float l) { return m == -INFINITY && l == 0.f; }
+
 template <class A, int D, int MODE, int CAP>
 __global__ void __launch_bounds__(kThreads, 1)
     prefill_tc_kernel(const __grid_constant__ A a, const __grid_constant__ WorkList<CAP> wl) {
@@ -390,20 +395,20 @@ __global__ void __launch_bounds__(kThreads, 1)
     cluster_wait();
     if (warp >= 2) {
       const int tid = threadIdx.x - 64;  // of the 256 softmax threads
-      // (m, l) -> the state's weight, negative for a state of -inf: it saw no key (and its CTA may
-      // have had no tile: unwritten values); any other counts
+      // (m, l) -> the state's weight, negative for an empty state, whose CTA may have had no tile
+      // (unwritten values); any other counts
       if (tid < 4) spoilt[tid] = 0;
       if (tid < rows) {
         float M = -INFINITY, L = 0.f;
         for (int c = 0; c < n; ++c) M = fmaxf(M, recv_ml[c * rows + tid].x);
         for (int c = 0; c < n; ++c) {
           const float2 ml = recv_ml[c * rows + tid];
-          if (ml.x != -INFINITY) L += fast_exp2(ml.x - M) * ml.y;
+          if (!empty_state(ml.x, ml.y)) L += fast_exp2(ml.x - M) * ml.y;
         }
         const float inv = L == 0.f ? 0.f : 1.f / L;
         for (int c = 0; c < n; ++c) {
-          const float m = recv_ml[c * rows + tid].x;
-          recv_ml[c * rows + tid].x = m == -INFINITY ? -1.f : fast_exp2(m - M) * inv;
+          const float2 ml = recv_ml[c * rows + tid];
+          recv_ml[c * rows + tid].x = empty_state(ml.x, ml.y) ? -1.f : fast_exp2(ml.x - M) * inv;
         }
       }
       named_barrier_sync(3, 256);
@@ -460,10 +465,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (warp >= 2 && x == rank && end_ok) {
       const float2 o_ml = recv_ml[r];
       const float M = fmaxf(end_m, o_ml.x);
-      // a state of -inf saw no key of this row, and its CTA may have had no tile at all
-      // (unwritten values); any other state counts, also with a weight that rounds to
-      // zero, whose NaN is one in a single CTA as well
-      const bool mine = end_m != -INFINITY, other = o_ml.x != -INFINITY;
+      // an empty state's CTA may have had no tile at all (unwritten values); any other state
+      // counts, also with a weight that rounds to zero, whose NaN is one in a single CTA as well
+      const bool mine = !empty_state(end_m, end_l), other = !empty_state(o_ml.x, o_ml.y);
       const float w0 = mine ? fast_exp2(end_m - M) : 0.f, w1 = other ? fast_exp2(o_ml.x - M) : 0.f;
       const float inv = 1.f / (end_l * w0 + o_ml.y * w1);
       const float f0 = w0 * inv, f1 = w1 * inv;

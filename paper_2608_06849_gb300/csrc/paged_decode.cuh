@@ -12,7 +12,8 @@
 // 8-bit pages. The codes are multiplied as they are (kind::f8f6f4); a row's power of two
 // is applied to its score, and its V power to its weight:
 //   s_j = 2^ek_j (q . K8_j) c,  w_j = 2^(s_j + ev_j - m),  o = sum_j w_j V8_j / sum_j w_j 2^-ev_j
-// with m the running maximum of s_j + ev_j, so that w_j is the size of key j's contribution. q
+// with m the running maximum of s_j + ev_j, so that w_j is the size of key j's contribution (a key
+// whose w_j is zero as a float adds nothing to the numerator, but may to the sum below it). q
 // (8 significant bits) is the sum of two e4m3 numbers (4 bits each): exactly, down to 2^-17 of the
 // row's largest. A weight is the sum of three e5m2 numbers (3 bits each, rounded to
 // nearest: 2^-9 of it, as good as bf16, at 2^-16 .. 2^15.8, so a key counts down to 2^-28 of
@@ -86,6 +87,7 @@ struct Lay {
   static constexpr int KP = NK == 4 ? 2 : 1;               // keys of a softmax thread
   static constexpr int SOFT = 128 * NK / KP;               // softmax threads
   static constexpr int NW = SOFT / 32;
+  static constexpr int REDH = GP + (F8 ? 1 : 0);           // maxima that warps exchange: the heads', and of the V powers
   static constexpr int THREADS = SOFT + 128 + 96;
   static constexpr int QBLK = SN * ROWB, QBUF = DBLK * QBLK;
   static constexpr int NQ = CL ? 1 : 2;                    // Q buffers: a cluster has one item
@@ -98,14 +100,14 @@ struct Lay {
   // [C][16] (m, l)
   static constexpr int TAIL = CL ? GP * D * 4 + kClusterMost * 16 * 8 : kLensCap * 4;
   static constexpr int XBYTES = D == 64 ? GP * 64 * 4 : 0;
-  static constexpr int FIXED = NS * STAGE + NQ * QBUF + NS * POWB + 4 * GP * NW * 4 + 128 + XBYTES + 128 + NBAR * 8 + 32 +
+  static constexpr int FIXED = NS * STAGE + NQ * QBUF + NS * POWB + 2 * (REDH + GP) * NW * 4 + 128 + XBYTES + 128 + NBAR * 8 + 32 +
                                4 * 32 + kMaxKvHeads + TAIL + 1024;
   static constexpr int NPB = FIXED + 2 * PBUF <= 232448 ? 2 : 1;  // P buffers that fit
   static constexpr int OFF_Q = NS * STAGE;
   static constexpr int OFF_P = OFF_Q + NQ * QBUF;
   static constexpr int OFF_POW = OFF_P + NPB * PBUF;
-  static constexpr int OFF_RED = OFF_POW + NS * POWB;     // [2][GP][NW] warp maxima
-  static constexpr int OFF_SUM = OFF_RED + 2 * GP * NW * 4;  // [2][GP][NW] sums of an item, [2][16] maxima
+  static constexpr int OFF_RED = OFF_POW + NS * POWB;     // [2][REDH][NW] warp maxima
+  static constexpr int OFF_SUM = OFF_RED + 2 * REDH * NW * 4;  // [2][GP][NW] sums of an item, [2][16] maxima
   static constexpr int OFF_X = OFF_SUM + 2 * GP * NW * 4 + 128;  // [GP][64] the upper rows of O (d_head 64)
   static constexpr int OFF_QF = OFF_X + XBYTES;            // [2][16] factors of the scores
   static constexpr int OFF_BAR = OFF_QF + 128;
@@ -265,6 +267,13 @@ __device__ __forceinline__ float* state_slot(const PagedDecodeArgs& a, int cta, 
   return a.states + ((size_t)cta * 4 + slot) * state_floats(D);
 }
 
+// l * 2^d of a state's sum, d <= 0. With 8-bit pages 2^d alone may round to zero where the product does
+// not: a part whose V rows are 2^-120 of the others' has a sum that much greater than its weights.
+__device__ __forceinline__ float scaled(float l, float d) {
+  const float half = fast_exp2(0.5f * d);
+  return l * half * half;
+}
+
 // Adds up n <= kGroup states and stores the outputs (out) or the sum (dst); 4 warps. State 0
 // is at `first`, state j > 0 at rest + j * stride. A lane owns four values at a time, all
 // states' of them on their way at once, and the lanes of a head hold the states' maxima and
@@ -291,7 +300,7 @@ __device__ __forceinline__ void join(int n, const float* first, const float* res
 #pragma unroll
     for (int o = 8; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
     const float w = mj == -INFINITY ? 0.f : fast_exp2(mj - M);
-    float L = mj == -INFINITY ? 0.f : w * lj;
+    float L = mj == -INFINITY ? 0.f : scaled(lj, mj - M);
 #pragma unroll
     for (int o = 8; o >= 1; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
     float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -825,6 +834,9 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
       const Seq& w = walk.q;
       const bool strm = walk.streaming();
       float m[GP], l[GP];
+      // V powers below this, 90 below the largest of the tiles that moved a maximum: a key of any other whose
+      // weight is zero as a float has less than 2^-48 of the weight of the one that is the maximum
+      float ev_far = -INFINITY;
 #pragma unroll
       for (int h = 0; h < GP; ++h) {
         m[h] = -INFINITY;
@@ -898,7 +910,7 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
           for (int h = 0; h < GP; ++h) below = below && wm[h] <= m[h] + C::kLag;
         }
         if (first || !named_barrier_and(1, C::SOFT, below)) {
-          float* rx = red + x * (GP * NW);
+          float* rx = red + x * (C::REDH * NW);
           {
             float wm[GP];
 #pragma unroll
@@ -907,26 +919,35 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
 #pragma unroll
               for (int h = 0; h < GP; ++h) rx[h * NW + warp] = wm[h];
             }
+            if constexpr (F8) {
+              const float top = warp_max((float)max(ev[0], ev[KP - 1]));
+              if (lane == 0) rx[GP * NW + warp] = top;
+            }
           }
           ok = named_barrier_and(1, C::SOFT, local_ok);
           if (!ok) break;
-          bool resc = false;
-          float alpha[GP];
-#pragma unroll
-          for (int h = 0; h < GP; ++h) {
+          auto top_in = [&](int h) {
             float top = -INFINITY;
 #pragma unroll
             for (int u = 0; u < NW; u += 4) {
               const float4 f = *reinterpret_cast<const float4*>(rx + h * NW + u);
               top = fmaxf(top, fmaxf(fmax3f(f.x, f.y, f.z), f.w));
             }
+            return top;
+          };
+          if (F8) ev_far = fmaxf(ev_far, top_in(GP) - 90.f);
+          bool resc = false;
+          float alpha[GP];
+#pragma unroll
+          for (int h = 0; h < GP; ++h) {
+            const float top = top_in(h);
             alpha[h] = 1.f;
             if (first) {
               m[h] = top;
             } else if (top > m[h] + C::kLag) {
               alpha[h] = m[h] == -INFINITY ? 0.f : fast_exp2(m[h] - top);
+              l[h] = F8 ? scaled(l[h], m[h] - top) : l[h] * alpha[h];
               m[h] = top;
-              l[h] *= alpha[h];
               resc = true;
             }
           }
@@ -946,6 +967,18 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
             }
             tmem_st_wait();
           }
+        }
+        if (F8 && fminf((float)ev[0], (float)ev[KP - 1]) < ev_far) {  // a weight that is zero may not be so times 2^-ev
+#pragma unroll
+          for (int c = 0; c < KP; ++c)
+#pragma unroll
+            for (int h = 0; h < GP; ++h) {
+              const float low = s[c][h] - m[h] + C::kRaise;
+              if (see[c] && low < -126.f) {
+                l[h] += fast_exp2(low - (float)ev[c]);
+                s[c][h] = -INFINITY;
+              }
+            }
         }
         // the P buffer is free once O += P(it - NPB) V is done
         if (it >= C::NPB)
@@ -1035,7 +1068,7 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
         for (int c = 0; c < n; ++c) {
           const float2 ml = recv_ml[c * 16 + h];
           const float w = ml.y == 0.f ? 0.f : fast_exp2(ml.x - M);
-          L += w * ml.y;
+          L += ml.y == 0.f ? 0.f : scaled(ml.y, ml.x - M);
           O += w * recv[((c * G) << lg_rows) + i];
         }
         // (a sequence without a token: zeros)

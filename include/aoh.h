@@ -514,7 +514,8 @@ aoh_status aoh_paged_prefill(aoh_paged* cache, const void* q, const void* k, con
  *   k, v     rows of [n_kv_heads][d_head], k_stride and v_stride elements apart
  *   cu_rows  device [n_seqs + 1], cu_rows[0] = 0, or NULL: one row a sequence
  *   lens     device [n_seqs]
- *   n_rows   rows in all (cu_rows[n_seqs])
+ *   n_rows   rows in all: cu_rows[n_seqs]. A row that cu_rows gives to no sequence (where
+ *            n_rows is more, or cu_rows[0] is not 0) is not written, and reported as out of range
  *   table    device [n_seqs][table_stride]
  * No two rows may name the same place. Errors: INVALID, CUDA.
  */
@@ -526,7 +527,8 @@ aoh_status aoh_paged_append(aoh_paged* cache, const void* k, const void* v, int6
  * Read positions first[b] .. first[b] + (cu_rows[b + 1] - cu_rows[b]) - 1 of every
  * sequence as rows cu_rows[b] .. of k_out and v_out, dense bf16
  * [n_rows][n_kv_heads][d_head]. first: device [n_seqs], or NULL: from position 0. The
- * other arguments as for aoh_paged_append. Errors: INVALID, CUDA.
+ * other arguments as for aoh_paged_append; a row of no sequence is reported likewise, and what
+ * stands there afterwards is unspecified. Errors: INVALID, CUDA.
  */
 aoh_status aoh_paged_read(aoh_paged* cache, const int32_t* cu_rows, const int32_t* first, int32_t n_seqs,
                           int32_t n_rows, const int32_t* table, int32_t table_stride, void* k_out, void* v_out,

@@ -49,6 +49,18 @@ __device__ __forceinline__ int seq_of(const PageRows& rows, int r0, int r) {
   return lo;
 }
 
+// The sequence of row r of the call, and where its rows begin and end; a row that cu gives to
+// no sequence (before its first number or behind its last) lies outside of them.
+struct Owner {
+  int b, begin, end;
+  __device__ __forceinline__ bool has(int r) const { return begin <= r && r < end; }
+};
+__device__ __forceinline__ Owner owner_of(const PageRows& rows, int r0, int r) {
+  const int b = seq_of(rows, r0, r);
+  return rows.cu ? Owner{b, __ldg(rows.cu + b), __ldg(rows.cu + b + 1)} : Owner{b, r, r + 1};
+}
+
+// The place of position pos of sequence b; an error where there is none.
 __device__ __forceinline__ Place place_of(const PagePool& pool, const PageRows& rows, int b, long long pos, uint32_t* err) {
   Place p{-1, (int)(pos & (pool.ps - 1))};
   const long long slot = pos >> pool.lg_ps;
@@ -230,10 +242,10 @@ __global__ void __launch_bounds__(kThreads, 4) append_kernel(const __grid_consta
   int vec = t.vec, i0 = t.sub;
   if (vec < per_row) load(vec, i0);
   if (threadIdx.x < 32) {
-    const int r = r0 + min((int)threadIdx.x, n - 1), b = seq_of(a.rows, r0, r);
-    const int end = a.rows.cu ? __ldg(a.rows.cu + b + 1) : r + 1;
-    if ((int)threadIdx.x < n)
-      place[threadIdx.x] = place_of(a.pool, a.rows, b, (long long)__ldg(a.lens + b) - (end - r), a.err);
+    const int r = r0 + min((int)threadIdx.x, n - 1);
+    const Owner o = owner_of(a.rows, r0, r);
+    const long long pos = (long long)__ldg(a.lens + o.b) - (o.end - r);
+    if ((int)threadIdx.x < n) place[threadIdx.x] = place_of(a.pool, a.rows, o.b, o.has(r) ? pos : -1, a.err);
   }
   __syncthreads();
   while (vec < per_row) {
@@ -262,9 +274,10 @@ __global__ void __launch_bounds__(kThreads, 4) read_kernel(const __grid_constant
   const int r0 = blockIdx.x * rows_per_block, n = min(rows_per_block, a.rows.n_rows - r0);
   after_the_last_kernel();
   if (threadIdx.x < 32) {
-    const int r = r0 + min((int)threadIdx.x, n - 1), b = seq_of(a.rows, r0, r);
-    const long long pos = (a.first ? __ldg(a.first + b) : 0) + (long long)(a.rows.cu ? r - __ldg(a.rows.cu + b) : 0);
-    if ((int)threadIdx.x < n) place[threadIdx.x] = place_of(a.pool, a.rows, b, pos, a.err);
+    const int r = r0 + min((int)threadIdx.x, n - 1);
+    const Owner o = owner_of(a.rows, r0, r);
+    const long long pos = (a.first ? __ldg(a.first + o.b) : 0) + (long long)(r - o.begin);
+    if ((int)threadIdx.x < n) place[threadIdx.x] = place_of(a.pool, a.rows, o.b, o.has(r) ? pos : -1, a.err);
   }
   __syncthreads();
   const int per_row = 2 * a.pool.Hkv;

@@ -1,0 +1,46 @@
+"""Rows of a call that no sequence has (buffers padded to a captured call's size)."""
+
+import pytest
+import torch
+
+from gpu_cases import ensure_lib
+from paper_2608_06849_gb300 import aoh
+from test_gpu_paged import Pages, ints, randn
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True, scope="module")
+def _lib():
+    ensure_lib()
+
+
+@pytest.mark.parametrize("form", ["bf16", "e4m3"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("cu", [[0, 20, 37], [0, 37, 37], [3, 20, 37]])
+def test_rows_behind_the_last_sequence(form, d, cu):
+    """More rows than cu_rows gives out (and fewer than from its first on): what is nobody's is
+    not written, although the last sequence's table goes on, and reported."""
+    hkv, page, extra = 3, 16, 40
+    lens = [30, 25] if cu[1] != 37 else [50, 25]
+    p = Pages([n + 64 for n in lens], hkv, hkv, d, page, form, [0] * hkv, seed=d)
+    n = cu[-1]
+    k, v = randn((n + extra, hkv, d), 1), randn((n + extra, hkv, d), 2)
+    outs = [torch.zeros((n + extra, hkv, d), dtype=torch.bfloat16, device="cuda") for _ in range(4)]
+    first = ints([a - (cu[b + 1] - cu[b]) for b, a in enumerate(lens)])
+    # the rows of the sequences alone
+    p.cache.append(k[cu[0]:n], v[cu[0]:n], ints(lens), p.table, cu_rows=ints([c - cu[0] for c in cu]))
+    p.cache.read(p.table, ints([c - cu[0] for c in cu]), outs[0][cu[0]:n], outs[1][cu[0]:n], first=first)
+    p.cache.check()
+    want = p.pool.clone()
+    p.pool.fill_(255)
+    for call in (lambda: p.cache.append(k, v, ints(lens), p.table, cu_rows=ints(cu)),
+                 lambda: p.cache.read(p.table, ints(cu), outs[2], outs[3], first=first)):
+        call()
+        with pytest.raises(aoh.AohError) as e:
+            p.cache.check()
+        assert e.value.status == 1
+        p.cache.check()
+    assert torch.equal(p.pool, want)
+    for a, b in ((0, 2), (1, 3)):
+        assert torch.equal(outs[a][cu[0]:n], outs[b][cu[0]:n])

@@ -512,7 +512,8 @@ aoh_status aoh_paged_prefill(aoh_paged* cache, const void* q, const void* k, con
  * of k and v, and become the last ones of its lens[b] tokens (lens counts them
  * already).
  *   k, v     rows of [n_kv_heads][d_head], k_stride and v_stride elements apart
- *   cu_rows  device [n_seqs + 1], cu_rows[0] = 0, or NULL: one row a sequence
+ *   cu_rows  device [n_seqs + 1], cu_rows[0] = 0, or NULL: one row a sequence, and none where
+ *            lens[b] = 0 (its row of k and v is passed over, as a decode gives zeros there)
  *   lens     device [n_seqs]
  *   n_rows   rows in all: cu_rows[n_seqs]. A row that cu_rows gives to no sequence (where
  *            n_rows is more, or cu_rows[0] is not 0) is not written, and reported as out of range

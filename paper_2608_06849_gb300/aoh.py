@@ -585,8 +585,8 @@ class PagedCache:
 
     def append(self, k, v, lens, table, cu_rows=None, stream=None):
         """Write k, v [rows, Hkv, d] (any distance between tokens): rows cu_rows[b] ..
-        cu_rows[b + 1] - 1 (without cu_rows: row b) become the last of sequence b's
-        lens[b] tokens."""
+        cu_rows[b + 1] - 1 (without cu_rows: row b, or none where lens[b] is 0) become the
+        last of sequence b's lens[b] tokens."""
         kp, ks, rows = _rows(k, "k", self.n_kv_heads, self.d_head)
         vp, vs, rows_v = _rows(v, "v", self.n_kv_heads, self.d_head)
         tp, n, width = self._table(table)

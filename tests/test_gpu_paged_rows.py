@@ -1,4 +1,5 @@
-"""Rows of a call that no sequence has (buffers padded to a captured call's size)."""
+"""Rows of a call that no sequence has (buffers padded to a captured call's size, slots
+of a step without a request)."""
 
 import pytest
 import torch
@@ -44,3 +45,41 @@ def test_rows_behind_the_last_sequence(form, d, cu):
     assert torch.equal(p.pool, want)
     for a, b in ((0, 2), (1, 3)):
         assert torch.equal(outs[a][cu[0]:n], outs[b][cu[0]:n])
+
+
+@pytest.mark.parametrize("form", ["bf16", "e4m3"])
+def test_a_captured_step_with_idle_slots(form):
+    """A slot without a request has length 0: nothing of it is written, its output is zeros,
+    and no error is reported."""
+    hq, hkv, d, page = 8, 2, 128, 16
+    lens = [31, 15, 200, 5]
+    p = Pages([n + 8 for n in lens], hq, hkv, d, page, form, [0, 1], 5, 40)
+    p.fill(lens)
+    k, v, q = randn((4, hkv, d), 1), randn((4, hkv, d), 2), randn((4, hq, d), 3)
+    t, out = ints([n + 1 for n in lens]), torch.empty_like(q)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        p.cache.append(k, v, t, p.table)
+        p.cache.decode(q, t, p.table, out)
+    torch.cuda.current_stream().wait_stream(side)
+    p.cache.check()
+    want, pool = out.clone(), p.pool.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        p.cache.append(k, v, t, p.table)
+        p.cache.decode(q, t, p.table, out)
+    for idle in (0, 3):
+        t[idle] = 0
+        out.fill_(float("nan"))
+        graph.replay()
+        p.cache.check()
+        assert (out[idle] == 0).all()
+        rest = [b for b in range(4) if t[b] > 0]
+        assert torch.equal(out[rest], want[rest])
+        assert torch.equal(p.pool, pool)
+    # a negative length is an error all the same
+    t[0] = -1
+    graph.replay()
+    with pytest.raises(aoh.AohError):
+        p.cache.check()

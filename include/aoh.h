@@ -446,8 +446,8 @@ aoh_status aoh_classify(const void* w_q, const void* w_k, int32_t n_layers, int3
  * [n_pages][n_kv_heads][K, V][page_size]: code c of a row with power e stands for
  * c * 2^e. e is the least power for which the row's largest finite magnitude is at
  * most 448 * 2^e, within [-80, 120]; a code is the nearest one (ties to even) to the
- * number * 2^-e; an infinity or NaN is stored as NaN. What was never written may
- * hold anything.
+ * number * 2^-e, with e = 120 of at most 240 (more would stand for no bf16 number); an
+ * infinity or NaN is stored as NaN. What was never written may hold anything.
  *
  * Tables and lengths are device arrays, read when the kernels run: a captured graph
  * sees their contents at replay. Entries of a table past a sequence's pages are not read. A page

@@ -45,7 +45,8 @@ def e4m3_values():
 def encode(x):
     """Codes and powers of rows x [..., d]: for each row the least power e in [E_MIN,
     E_MAX] with max |x| <= 448 * 2^e over its finite numbers, and for each number the
-    code nearest to x * 2^-e (ties to the even code; NaN for what is not finite)."""
+    code nearest to x * 2^-e (ties to the even code; with the power E_MAX at most 240, as
+    256 * 2^120 is no bf16 number; NaN for what is not finite)."""
     x = np.asarray(x, dtype=np.float64)
     finite = np.isfinite(x)
     most = np.where(finite, np.abs(x), 0).max(-1)
@@ -59,6 +60,7 @@ def encode(x):
     lo = hi - 1
     up = (a - val[lo] > val[hi] - a) | ((a - val[lo] == val[hi] - a) & (hi % 2 == 0))
     code = np.where(up, hi, lo)
+    code = np.where(e[..., None] == E_MAX, np.minimum(code, np.searchsorted(val, 240.0)), code)
     code = np.where(np.signbit(y), code | 128, code)
     return np.where(finite, code, 127).astype(np.uint8), e.astype(np.int8)
 

@@ -7,7 +7,8 @@
 // floating-point numbers, whose relative precision does not depend on where in their
 // range the row lies, x 2^-e is exact in fp32, so that each code is the nearest one to
 // the exact quotient, and c 2^e is exact in bf16, so that a row read back is the stored
-// one. NaN and infinities become the NaN code and do not count for e.
+// one. At e = 120 codes end at 240: 256 * 2^120 and above are no bf16 numbers, and a finite number
+// stays finite. NaN and infinities become the NaN code and do not count for e.
 //
 // Both kernels only move bytes: a lane holds 16 numbers (32 bytes of bf16) and D / 16
 // neighbouring lanes one row of one head, the heads of a token next to each other, so that a
@@ -141,11 +142,13 @@ __device__ __forceinline__ uint4 encode(const Sixteen& x, int* e) {
   // most = 1.f * 2^(E - 127): 448 = 1.75 * 2^8
   *e = min(max((int)(most >> 7) - ((most & 0x7fu) <= 0x60u ? 135 : 134), -80), 120);
   const float scale = __uint_as_float((uint32_t)(127 - *e) << 23);
+  const bool largest = *e == 120;
   uint32_t c[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     float2 f = __fmul2_rn(bf16x2_to_float2(x.w[i]), make_float2(scale, scale));
-    if (odd) {  // infinities: NaN
+    if (odd || largest) {  // codes end at 240; infinities: NaN
+      if (largest) f = make_float2(fminf(fmaxf(f.x, -240.f), 240.f), fminf(fmaxf(f.y, -240.f), 240.f));
       if ((x.w[i] & 0x7f80u) == 0x7f80u) f.x = __uint_as_float(0x7fffffffu);
       if ((x.w[i] & 0x7f800000u) == 0x7f800000u) f.y = __uint_as_float(0x7fffffffu);
     }

@@ -430,6 +430,16 @@ def _ints(t, name, n):
     return t.data_ptr()
 
 
+def _device_index(device, pool=None):
+    """Index of the GPU of a new object's memory: a handle belongs to the current
+    device, so memory anywhere else is refused."""
+    current = torch.cuda.current_device()
+    where = pool.device if pool is not None else torch.device("cuda" if device is None else device)
+    if where.type != "cuda" or (where.index is not None and where.index != current):
+        raise ValueError(f"the memory is on {where}, the handle would be on the current device, cuda:{current}")
+    return current
+
+
 # ------------------------------------------------------------- convenience
 
 def _need(t, name, n):
@@ -450,6 +460,7 @@ class Cache:
         self.cfg = make_config(batch, n_q_heads, n_kv_heads, d_head, max_seq, sink, window, chunk)
         self.labels = [int(x) for x in labels]
         self.nbytes = aoh_cache_bytes(self.cfg, self.labels)
+        _device_index(device)
         self.buffer = torch.empty(self.nbytes, dtype=torch.uint8, device=device or "cuda")
         self.handle = aoh_cache_init(self.cfg, self.labels, self.buffer)
         self.batch, self.n_q_heads, self.n_kv_heads, self.d_head = batch, n_q_heads, n_kv_heads, d_head
@@ -542,9 +553,10 @@ class PagedCache:
         self.cfg = make_paged_config(n_q_heads, n_kv_heads, d_head, page_size, n_pages, form, max_seqs, sink, window)
         self.labels = [int(x) for x in labels]
         self.nbytes = aoh_paged_bytes(self.cfg)
+        self.device = _device_index(device, pool)
+        self.several_devices = torch.cuda.device_count() > 1
         self.pool = torch.empty(self.nbytes, dtype=torch.uint8, device=device or "cuda") if pool is None else pool
         self.handle = aoh_paged_init(self.cfg, self.labels, self.pool)
-        self.device = self.pool.device.index
         self.n_pages, self.page_size, self.form, self.max_seqs = n_pages, page_size, form, max_seqs
         self.n_q_heads, self.n_kv_heads, self.d_head = n_q_heads, n_kv_heads, d_head
         self.sink, self.window = sink, window
@@ -552,6 +564,12 @@ class PagedCache:
     def _stream(self, stream):
         """As _stream_ptr, of the pool's device (which has to be the current one)."""
         return torch._C._cuda_getCurrentRawStream(self.device) if stream is None else stream.cuda_stream
+
+    def _on_device(self, *tensors):
+        """Called where the process sees several GPUs (with one, every CUDA tensor is on it)."""
+        for t in tensors:
+            if t is not None and t.get_device() != self.device:
+                raise ValueError(f"a tensor is on cuda:{t.get_device()}, the pool on cuda:{self.device}")
 
     def _table(self, table):
         shape = table.shape
@@ -576,6 +594,8 @@ class PagedCache:
             raise ValueError(f"q_lens and k_lens hold one length a sequence, at most {self.max_seqs}")
         if sum(q_lens) != nq or sum(q_lens if k_lens is None else k_lens) != nk or nk != nv:
             raise ValueError(f"q, k and v hold {nq}, {nk} and {nv} rows; q_lens and k_lens say otherwise")
+        if self.several_devices:
+            self._on_device(q, k, v, out)
         ql = array.array("i", q_lens)
         kl = ql if k_lens is None else array.array("i", k_lens)
         st = _lib.aoh_paged_prefill(self.handle, qp, kp, vp, qs, ks, vs, ql.buffer_info()[0], kl.buffer_info()[0], n, op,
@@ -593,8 +613,10 @@ class PagedCache:
         if rows != rows_v or (cu_rows is None and rows != n):
             raise ValueError(f"k and v hold {rows} and {rows_v} rows for {n} sequences")
         cp = None if cu_rows is None else _ints(cu_rows, "cu_rows", n + 1)
-        st = _lib.aoh_paged_append(self.handle, kp, vp, ks, vs, cp, _ints(lens, "lens", n), n, rows, tp,
-                                   width, self._stream(stream))
+        lp = _ints(lens, "lens", n)
+        if self.several_devices:
+            self._on_device(k, v, lens, table, cu_rows)
+        st = _lib.aoh_paged_append(self.handle, kp, vp, ks, vs, cp, lp, n, rows, tp, width, self._stream(stream))
         if st:
             _check(st)
 
@@ -609,6 +631,8 @@ class PagedCache:
             raise ValueError(f"k_out and v_out hold {rows} rows for {n} sequences")
         cp = None if cu_rows is None else _ints(cu_rows, "cu_rows", n + 1)
         fp = None if first is None else _ints(first, "first", n)
+        if self.several_devices:
+            self._on_device(table, cu_rows, k_out, v_out, first)
         st = _lib.aoh_paged_read(self.handle, cp, fp, n, rows, tp, width, kp, vp, self._stream(stream))
         if st:
             _check(st)
@@ -623,9 +647,10 @@ class PagedCache:
         tp, n, width = self._table(table)
         if rows != n:
             raise ValueError(f"q holds {rows} rows for {n} sequences")
-        st = _lib.aoh_paged_decode(self.handle, qp, qs, _ints(lens, "lens", n), n, max_len, tp,
-                                   width, _dense(out, "out", (n, self.n_q_heads, self.d_head), _BF16),
-                                   self._stream(stream))
+        lp, op = _ints(lens, "lens", n), _dense(out, "out", (n, self.n_q_heads, self.d_head), _BF16)
+        if self.several_devices:
+            self._on_device(q, lens, table, out)
+        st = _lib.aoh_paged_decode(self.handle, qp, qs, lp, n, max_len, tp, width, op, self._stream(stream))
         if st:
             _check(st)
 

@@ -494,7 +494,9 @@ aoh_status aoh_paged_init(const aoh_paged_config* cfg, const uint8_t* head_label
  * the sequence's keys and sees keys by the rule above; with k_lens equal to q_lens
  * that is a whole prompt, with more keys the rows continue a prompt whose earlier
  * keys come first in k and v. A row that sees no key gives zeros. A NaN or an infinity in a key
- * or a value reaches the rows that see it, and no other (rows near it take longer).
+ * or a value reaches the rows that see it, and no other. Rows take longer that have such a value among
+ * the hidden ones of their tiles of 128 keys: rows near it and, where it shares its tile with
+ * the last sinks, all later rows of a streaming head.
  *   q            rows of [n_q_heads][d_head], q_stride elements apart (a multiple of 8,
  *                at least n_q_heads * d_head: slices of a fused projection will do)
  *   k, v         rows of [n_kv_heads][d_head], k_stride and v_stride apart

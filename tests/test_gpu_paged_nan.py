@@ -162,3 +162,32 @@ def test_nan_keys_in_pages(form, d, lens, hq, hkv):
             assert torch.isfinite(out[0, hq // hkv:]).all() and torch.isfinite(out[1:]).all(), (j0, j1)
 
 
+@pytest.mark.parametrize("what,most", [("all values", 100), ("the first value", 35)])
+def test_what_spoilt_values_cost(what, most):
+    """Rows that are gone over again look at the keys that their tiles hide from them, and no
+    longer than until all their numbers are NaN: with every V row NaN a call takes ten times as
+    long as a clean one (a thousand times with every key gone over), with one that hides from
+    nobody a dozen times (eighty)."""
+    case = ([8192], None, 8, 2, 128, [0, 1], 4, 300)
+    q, k, v = prompt_inputs(case[0], None, 8, 2, 128, seed=61)
+    pc = aoh.PagedCache(1, 16, 8, 2, 128, 4, 300, case[5])
+    out = torch.empty_like(q)
+
+    def took(v):
+        times = []
+        for _ in range(4):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            torch.cuda.synchronize()
+            a.record()
+            pc.prefill(q, k, v, case[0], out)
+            b.record()
+            torch.cuda.synchronize()
+            times.append(a.elapsed_time(b))
+        return min(times)
+
+    clean = took(v)
+    assert torch.isfinite(out).all()
+    spoilt = v.clone()
+    spoilt[slice(None) if what == "all values" else 0] = float("nan") if what == "all values" else float("inf")
+    assert took(spoilt) < most * clean
+    pc.check()

@@ -248,10 +248,10 @@ __global__ void __launch_bounds__(kThreads, 4) append_kernel(const __grid_consta
     const int r = r0 + min((int)threadIdx.x, n - 1);
     const Owner o = owner_of(a.rows, r0, r);
     const int len = __ldg(a.lens + o.b);
-    const long long pos = (long long)len - (o.end - r);
+    const bool fits = len <= a.rows.table_stride << a.pool.lg_ps;
+    const long long pos = o.has(r) && fits ? (long long)len - (o.end - r) : -1;
     if ((int)threadIdx.x < n)  // a step's slot without a request has no row
-      place[threadIdx.x] = a.rows.cu == nullptr && len == 0 ? Place{-1, 0}
-                                                            : place_of(a.pool, a.rows, o.b, o.has(r) ? pos : -1, a.err);
+      place[threadIdx.x] = a.rows.cu == nullptr && len == 0 ? Place{-1, 0} : place_of(a.pool, a.rows, o.b, pos, a.err);
   }
   __syncthreads();
   while (vec < per_row) {

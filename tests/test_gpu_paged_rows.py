@@ -83,3 +83,26 @@ def test_a_captured_step_with_idle_slots(form):
     graph.replay()
     with pytest.raises(aoh.AohError):
         p.cache.check()
+
+
+@pytest.mark.parametrize("form", ["bf16", "e4m3"])
+def test_a_length_past_the_table(form):
+    """Of a sequence whose length is past what its table holds no row is written, also not those
+    that would still lie within; the other sequences' are."""
+    hkv, d, page = 2, 64, 16
+    lens, cu = [40, 20], ints([0, 5, 8])
+    p = Pages([n + 16 for n in lens], hkv, hkv, d, page, form, [0] * hkv)
+    table = ints([list(range(3)), [3, 4, 0]])
+    k, v = randn((8, hkv, d), 1), randn((8, hkv, d), 2)
+    p.cache.append(k[5:], v[5:], ints([20]), table[1:], cu_rows=ints([0, 3]))
+    p.cache.check()
+    want = p.pool.clone()
+    p.pool.fill_(255)
+    for past in (49, 51, 2 ** 31 - 1):
+        p.cache.append(k, v, ints([past, 20]), table, cu_rows=cu)
+        with pytest.raises(aoh.AohError):
+            p.cache.check()
+        assert torch.equal(p.pool, want)
+    p.cache.append(k, v, ints([48, 20]), table, cu_rows=cu)  # to the last row of its table
+    p.cache.check()
+    assert not torch.equal(p.pool, want)

@@ -449,6 +449,9 @@ aoh_status aoh_classify(const void* w_q, const void* w_k, int32_t n_layers, int3
  * number * 2^-e, with e = 120 of at most 240 (more would stand for no bf16 number); an
  * infinity or NaN is stored as NaN. What was never written may hold anything.
  *
+ * A page holds every KV head, so streaming heads keep all their positions here (the
+ * cache above keeps their sinks and window alone); they read the sinks and the window.
+ *
  * Tables and lengths are device arrays, read when the kernels run: a captured graph
  * sees their contents at replay. Entries of a table past a sequence's pages are not read. A page
  * outside [0, n_pages) or a length outside [0, table_stride * page_size] is out
@@ -544,7 +547,8 @@ aoh_status aoh_paged_read(aoh_paged* cache, const int32_t* cu_rows, const int32_
  *   q        rows of [n_q_heads][d_head], q_stride elements apart
  *   lens     device [n_seqs];  table  device [n_seqs][table_stride]
  *   max_len  the host's upper bound of lens, or 0: what the table holds. It decides how the
- *            work is split; with a bound that is too low the outputs are still right.
+ *            work is split; with a bound that is too low the outputs are still right, with
+ *            none, or one far too high, a short step takes longer.
  *   out      [n_seqs][n_q_heads][d_head]
  * Errors: INVALID, CUDA.
  */

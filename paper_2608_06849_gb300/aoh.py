@@ -387,7 +387,7 @@ def aoh_paged_destroy(cache):
 # The other aoh_paged_* calls take sizes and strides, which PagedCache reads off its
 # tensors, checks and passes on. An attribute of a tensor costs 0.05 - 0.11 us on a
 # Grace core and the 13 arguments of a call 1 us: an append of four tensors through
-# layers of checks took 7.2 us where the library's own part is 1.8.
+# layers of checks took 7.2 us, of which the library's call is 2.7 (5.3 so).
 
 _BF16, _I32 = torch.bfloat16, torch.int32
 

@@ -33,11 +33,11 @@
 // chain S -> weights -> P V above its transfer time (64 KB: 0.95 us a tile on an SM alone, 1.47 with
 // all SMs reading), and three tiles are what shared memory holds: 96 KB in flight an SM
 // behind the tile that is worked on. 16 sequences of 32,768 tokens, 32/8 heads, pages of 64, us
-// (floor: bytes at the 6.8 TB/s of a copy): 8-bit d_head 128 162 (159), 64 92 (80); bf16 128 310
-// (316), 64 160 (158). Pages of 16 cost 5% (8-bit, 128) to 20% (8-bit, 64): eight copies a
-// block. 16 query heads a KV head: 177 and 151, the softmax of 16 columns takes longer than the
+// (floor: bytes at the 6.8 TB/s of a copy): 8-bit d_head 128 159 (159), 64 90 (80); bf16 128 315
+// (316), 64 159 (158). Pages of 16 cost 5% (8-bit, 128) to 20% (8-bit, 64): eight copies a
+// block. 16 query heads a KV head: 176 and 156, the softmax of 16 columns takes longer than the
 // tile's transfer. A step in equal runs pays 8-9 us besides (launch, plan, first tile, last tile's
-// chain, arrival, joins), one on clusters 5: 1 x 4096 5.9 us, 4 x 8192 11.5.
+// chain, arrival, joins), one on clusters 5: 1 x 4096 5.9 us, 4 x 8192 11.2.
 //
 // Warps: 4 or 8 of softmax (a thread one or two keys of the tile), 4 that finish items, two
 // producers, one MMA issuer. O and the sums have two buffers, so that a CTA's next item goes
@@ -835,7 +835,8 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
       const bool strm = walk.streaming();
       float m[GP], l[GP];
       // V powers below this, 90 below the largest of the tiles that moved a maximum: a key of any other whose
-      // weight is zero as a float has less than 2^-48 of the weight of the one that is the maximum
+      // weight is zero as a float has less than 2^-48 of the weight of the one that is the maximum. (Asking
+      // every weight instead costs 2 to 7%, asking so 1 to 4, and 6 on 128 x 1,000 tokens of 64-wide heads.)
       float ev_far = -INFINITY;
 #pragma unroll
       for (int h = 0; h < GP; ++h) {

@@ -13,10 +13,10 @@
 // Both kernels only move bytes: a lane holds 16 numbers (32 bytes of bf16) and D / 16
 // neighbouring lanes one row of one head, the heads of a token next to each other, so that a
 // token's K (or V) is read as one run of Hkv * D * 2 bytes, while each head's row goes to its
-// own page block. Bound by HBM: 22,490 rows of 8 heads of 128 to 8-bit pages 29.8 us, back 25.1
-// (138 MB, 4.6 and 5.5 TB/s); 65,536 rows 71.9 and 64.3 (5.6 and 6.3); 32,768 rows of 8 heads of 64,
-// bf16, 20.4 and 20.6 (6.6). A step's 64 rows written and read
-// back 5.3 us, two launches. With 8 numbers a lane the 8-bit append was bound by its integer
+// own page block. Bound by HBM: 22,490 rows of 8 heads of 128 to 8-bit pages 27.7 us, back 24.9
+// (139 MB, 5.0 and 5.6 TB/s); 65,536 rows 65.6 and 62.4 (6.2 and 6.5); 32,768 rows of 8 heads of 64,
+// bf16, 20.5 and 20.6 (6.5). A step's 64 rows written and read back 5.3 us in a graph, two launches
+// (10.9 us as calls, the host's time). With 8 numbers a lane the 8-bit append was bound by its integer
 // instructions (132 for 8 numbers, 61% of their rate).
 #include <cuda_fp8.h>
 

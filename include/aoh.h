@@ -422,6 +422,62 @@ aoh_status aoh_classify(const void* w_q, const void* w_k, int32_t n_layers, int3
                         int32_t n_kv_heads, int32_t d_head, int32_t d_model, int32_t sparsity_pct,
                         double* er_out, uint8_t* labels_out, void* stream);
 
+/* --------------------------------------------------- norms and rotation
+ *
+ * What lies between a projection and the calls that attend: queries and keys are normalised
+ * for each head and rotated by their positions. (The paper has no counterpart.) A row x of
+ * d_head numbers of one head becomes
+ *   y = x * w / sqrt(mean(x^2) + eps)        with norm weights w; without, y = x
+ * and of its first 2 * n_pairs numbers each pair (a, b), y_i and y_{i + n_pairs}, or, where
+ * interleaved, y_{2 i} and y_{2 i + 1}, becomes
+ *   scale * (a cos t - b sin t, a sin t + b cos t),   t = position * inv_freq[i].
+ * The other numbers stay y. All of it is computed in 32 bits (angles exactly, to 2^-24 of a
+ * half-turn, whatever the position) and rounded once. The squares are summed in 32 bits too: a row
+ * with numbers above 2^60 has no norm.
+ */
+typedef struct aoh_rope {
+  int32_t n_pairs;     /* pairs that turn: a multiple of 8, at most d_head / 2; 0: none      */
+  int32_t interleaved; /* 1: pairs of neighbouring numbers                                  */
+  float scale;         /* factor of what was turned, within [-1e30, 1e30]                    */
+  uint64_t turns[64];  /* fraction of a turn that a position makes, in 2^-64                 */
+} aoh_rope;
+
+/*
+ * Fill `out` for frequencies inv_freq [n_pairs] (host; radians a position, within
+ * [-1e6, 1e6]; e.g. base^(-2 i / (2 n_pairs)), or any scaled ones), with scale 1, which the
+ * caller may change. The struct is the caller's and may be copied; a captured call keeps its
+ * contents. Host only. Errors: INVALID.
+ */
+aoh_status aoh_rope_init(const double* inv_freq, int32_t n_pairs, int32_t interleaved, aoh_rope* out);
+
+/* Norm weights of queries and keys (a host struct of device pointers). */
+#define AOH_NORM_BF16 0
+#define AOH_NORM_F32 1
+typedef struct aoh_norms {
+  const void* q; /* device [d_head] of `type`, or NULL: queries are not normalised */
+  const void* k; /* likewise, of keys                                              */
+  int32_t type;  /* AOH_NORM_BF16 or AOH_NORM_F32                                   */
+  float eps;     /* >= 0                                                           */
+} aoh_norms;
+
+/*
+ * Norms and rotation of dense rows, e.g. before aoh_prefill, aoh_decode_step or
+ * aoh_paged_prefill.
+ *   q, k      rows of [n_q_heads][d_head], [n_kv_heads][d_head], q_stride and k_stride
+ *             elements apart (multiples of 8: slices of a fused projection will do). 0 heads:
+ *             no such rows (their pointers are not looked at)
+ *   norms     or NULL: none
+ *   positions device int32 [n_rows], of any sign
+ *   q_out, k_out  likewise rows, q_out_stride and k_out_stride apart; may be q and k
+ *             themselves with the same strides, and must not overlap them otherwise
+ *   d_head    64 or 128; at most 1024 heads a side
+ * Needs no handle; runs on the current device. Errors: INVALID, UNSUPPORTED, CUDA.
+ */
+aoh_status aoh_norm_rotate(const aoh_rope* rope, const aoh_norms* norms, const void* q, const void* k, int64_t q_stride,
+                           int64_t k_stride, const int32_t* positions, int32_t n_rows, int32_t n_q_heads,
+                           int32_t n_kv_heads, int32_t d_head, void* q_out, void* k_out, int64_t q_out_stride,
+                           int64_t k_out_stride, void* stream);
+
 /* ------------------------------------------------------------ paged cache
  *
  * Serving many requests at once: their keys and values lie in pages of a fixed
@@ -430,7 +486,8 @@ aoh_status aoh_classify(const void* w_q, const void* w_k, int32_t n_layers, int3
  * window rule and the grouping of heads are those of the calls above.)
  *
  *   aoh_paged_prefill  attention over packed prompts
- *   aoh_paged_append   new keys and values written to the pages
+ *   aoh_paged_append   new keys and values written to the pages; aoh_paged_append_rotated:
+ *                      normalised and rotated on the way
  *   aoh_paged_decode   attention of one new token of every sequence
  *   aoh_paged_read     cached keys and values back as dense bf16 rows, e.g. the
  *                      prefix of a prompt that aoh_paged_prefill continues
@@ -528,6 +585,24 @@ aoh_status aoh_paged_prefill(aoh_paged* cache, const void* q, const void* k, con
 aoh_status aoh_paged_append(aoh_paged* cache, const void* k, const void* v, int64_t k_stride, int64_t v_stride,
                             const int32_t* cu_rows, const int32_t* lens, int32_t n_seqs, int32_t n_rows,
                             const int32_t* table, int32_t table_stride, void* stream);
+
+/*
+ * aoh_paged_append with the norms and the rotation of aoh_norm_rotate on the way: one pass takes
+ * a projection's rows q, k and v, writes q, normalised and rotated, to q_out, and k, likewise,
+ * with v as it is, to the pages. 8-bit rows are encoded from the rotated numbers in 32 bits.
+ *   q, q_out   rows of [n_q_heads][d_head], q_stride and q_out_stride elements apart; q_out may
+ *              be q with the same stride, and must not overlap q, k or v otherwise
+ *   rope, norms  as for aoh_norm_rotate
+ *   positions  device int32 [n_rows], or NULL: a row's place in its sequence
+ *   others     as for aoh_paged_append
+ * Of a row that is of no sequence, or lies outside its sequence's table, nothing is written, q_out
+ * included. (Where a page is out of range q_out is written.) Errors: INVALID, CUDA.
+ */
+aoh_status aoh_paged_append_rotated(aoh_paged* cache, const aoh_rope* rope, const aoh_norms* norms, const void* q,
+                                    const void* k, const void* v, int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                                    const int32_t* positions, const int32_t* cu_rows, const int32_t* lens, int32_t n_seqs,
+                                    int32_t n_rows, const int32_t* table, int32_t table_stride, void* q_out,
+                                    int64_t q_out_stride, void* stream);
 
 /*
  * Read positions first[b] .. first[b] + (cu_rows[b + 1] - cu_rows[b]) - 1 of every

@@ -50,7 +50,10 @@ EXPORTS = [
     "aoh_paged_bytes",
     "aoh_paged_init",
     "aoh_paged_prefill",
+    "aoh_rope_init",
+    "aoh_norm_rotate",
     "aoh_paged_append",
+    "aoh_paged_append_rotated",
     "aoh_paged_read",
     "aoh_paged_decode",
     "aoh_paged_check",
@@ -72,6 +75,15 @@ class aoh_config(ctypes.Structure):
 class aoh_paged_config(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in
                 ("n_q_heads", "n_kv_heads", "d_head", "page_size", "n_pages", "form", "max_seqs", "sink", "window")]
+
+
+class aoh_rope(ctypes.Structure):
+    _fields_ = [("n_pairs", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("turns", ctypes.c_uint64 * 64)]
+
+
+class aoh_norms(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("type", ctypes.c_int32), ("eps", ctypes.c_float)]
 
 
 PAGE_FORMS = {"bf16": 0, "e4m3": 1}
@@ -121,6 +133,9 @@ def load():
         "aoh_paged_init": (i32, [pcfgp, u8p, P, ctypes.c_size_t, ctypes.POINTER(P)]),
         "aoh_paged_prefill": (i32, [P, P, P, P, i64, i64, i64, P, P, i32, P, P]),
         "aoh_paged_append": (i32, [P, P, P, i64, i64, P, P, i32, i32, P, i32, P]),
+        "aoh_rope_init": (i32, [ctypes.POINTER(ctypes.c_double), i32, i32, ctypes.POINTER(aoh_rope)]),
+        "aoh_norm_rotate": (i32, [P, P, P, P, i64, i64, P, i32, i32, i32, i32, P, P, i64, i64, P]),
+        "aoh_paged_append_rotated": (i32, [P, P, P, P, P, P, i64, i64, i64, P, P, P, i32, i32, P, i32, P, i64, P]),
         "aoh_paged_read": (i32, [P, P, P, i32, i32, P, i32, P, P, P]),
         "aoh_paged_decode": (i32, [P, P, i64, P, i32, i32, P, i32, P, P]),
         "aoh_paged_check": (i32, [P, P]),
@@ -430,6 +445,87 @@ def _ints(t, name, n):
     return t.data_ptr()
 
 
+class Rope:
+    """The frequencies of a position rotation (aoh_rope of include/aoh.h): host numbers, for calls
+    on any device. ``rotated`` numbers of each head turn (a multiple of 16), pair i by base^(-2 i /
+    rotated) radians a position; ``inv_freq`` gives the rotated / 2 frequencies themselves
+    instead. The pairs are numbers i and i + rotated / 2, or, ``interleaved``, 2 i and 2 i + 1;
+    what turns is multiplied by ``scale``. ``Rope(0)`` turns nothing."""
+
+    def __init__(self, rotated=None, base=10000.0, inv_freq=None, interleaved=False, scale=1.0):
+        if (rotated is None) == (inv_freq is None):
+            raise ValueError("a rope takes either rotated or inv_freq")
+        if inv_freq is None:
+            if rotated < 0 or rotated % 2:
+                raise ValueError(f"rotated = {rotated} must be a multiple of 16")
+            inv_freq = [float(base) ** (-2.0 * i / rotated) for i in range(rotated // 2)]
+        inv_freq = [float(f) for f in inv_freq]
+        self.c = aoh_rope()
+        _check(load().aoh_rope_init((ctypes.c_double * max(1, len(inv_freq)))(*inv_freq), len(inv_freq),
+                                    1 if interleaved else 0, ctypes.byref(self.c)))
+        if not abs(scale) <= 1e30:
+            raise ValueError(f"scale = {scale} must be within [-1e30, 1e30]")
+        self.c.scale = scale
+        self.address = ctypes.addressof(self.c)
+
+
+def _norm(w, name, d):
+    """Pointer and type number of norm weights [d] (None: no norm)."""
+    if w is None:
+        return None, None
+    if w.shape != (d,):
+        raise ValueError(f"{name} has shape {tuple(w.shape)}; expected [{d}]")
+    if w.dtype not in (_BF16, torch.float32) or not w.is_cuda or not w.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous torch.bfloat16 or torch.float32 CUDA tensor")
+    return w.data_ptr(), 0 if w.dtype is _BF16 else 1
+
+
+def _norms(q_norm, k_norm, eps, d):
+    """The aoh_norms of both sides' weights, or None."""
+    if q_norm is None and k_norm is None:
+        return None
+    qp, qt = _norm(q_norm, "q_norm", d)
+    kp, kt = _norm(k_norm, "k_norm", d)
+    if qt is not None and kt is not None and qt != kt:
+        raise ValueError(f"q_norm and k_norm must be of one type, not {q_norm.dtype} and {k_norm.dtype}")
+    return ctypes.byref(aoh_norms(qp, kp, kt if qt is None else qt, eps))
+
+
+def aoh_norm_rotate(rope, q, k, positions, q_out, k_out, q_norm=None, k_norm=None, eps=1e-6, stream=None):
+    """Norms of queries and keys for each head and their rotation by position (``rope``: a Rope),
+    in one pass: q, q_out [rows, Hq, d], k, k_out [rows, Hkv, d] (bf16, with any distance between
+    tokens; the outputs may be the inputs themselves; q and q_out, or k and k_out, may be None),
+    positions int32 [rows], norm weights [d] in bf16 or fp32 (None: no norm on that side)."""
+    some = q if q is not None else k
+    if some is None or (q is None) != (q_out is None) or (k is None) != (k_out is None):
+        raise ValueError("q with q_out, or k with k_out, or both")
+    if some.dim() != 3:
+        raise ValueError(f"rows have shape {tuple(some.shape)}; expected [rows, heads, d]")
+    n, _, d = some.shape
+    side = []
+    for x, out, name in ((q, q_out, "q"), (k, k_out, "k")):
+        if x is None:
+            side.append((None, 0, 0, None, 0))
+            continue
+        heads = x.shape[1] if x.dim() == 3 else 0
+        p, s, rows = _rows(x, name, heads, d)
+        op, os_, orows = _rows(out, name + "_out", heads, d)
+        if rows != n or orows != n:
+            raise ValueError(f"{name} and {name}_out hold {rows} and {orows} rows; expected {n}")
+        side.append((p, s, heads, op, os_))
+    norms = _norms(q_norm, k_norm, eps, d)
+    pp = _ints(positions, "positions", n)
+    if torch.cuda.device_count() > 1:
+        here = torch.cuda.current_device()
+        for t in (q, k, positions, q_out, k_out, q_norm, k_norm):
+            if t is not None and t.get_device() != here:
+                raise ValueError(f"a tensor is on cuda:{t.get_device()}, the current device is cuda:{here}")
+    (qp, qs, hq, qo, qos), (kp, ks, hkv, ko, kos) = side
+    st = load().aoh_norm_rotate(rope.address, norms, qp, kp, qs, ks, pp, n, hq, hkv, d, qo, ko, qos, kos, _stream_ptr(stream))
+    if st:
+        _check(st)
+
+
 def _device_index(device, pool=None):
     """Index of the GPU of a new object's memory: a handle belongs to the current
     device, so memory anywhere else is refused."""
@@ -617,6 +713,30 @@ class PagedCache:
         if self.several_devices:
             self._on_device(k, v, lens, table, cu_rows)
         st = _lib.aoh_paged_append(self.handle, kp, vp, ks, vs, cp, lp, n, rows, tp, width, self._stream(stream))
+        if st:
+            _check(st)
+
+    def append_rotated(self, rope, q, k, v, lens, table, q_out, cu_rows=None, positions=None, q_norm=None, k_norm=None,
+                       eps=1e-6, stream=None):
+        """As append, with q, k [rows, Hq / Hkv, d] normalised (weights [d] in bf16 or fp32; None: not)
+        and rotated (``rope``: a Rope) on the way: q into q_out (which may be q itself), k, with v as
+        it is, into the pages. positions: int32 [rows], or None: each row's place in its sequence."""
+        hq, hkv, d = self.n_q_heads, self.n_kv_heads, self.d_head
+        qp, qs, nq = _rows(q, "q", hq, d)
+        kp, ks, rows = _rows(k, "k", hkv, d)
+        vp, vs, nv = _rows(v, "v", hkv, d)
+        op, os_, no = _rows(q_out, "q_out", hq, d)
+        tp, n, width = self._table(table)
+        if not nq == rows == nv == no or (cu_rows is None and rows != n):
+            raise ValueError(f"q, k, v and q_out hold {nq}, {rows}, {nv} and {no} rows for {n} sequences")
+        cp = None if cu_rows is None else _ints(cu_rows, "cu_rows", n + 1)
+        pp = None if positions is None else _ints(positions, "positions", rows)
+        lp = _ints(lens, "lens", n)
+        norms = _norms(q_norm, k_norm, eps, d)
+        if self.several_devices:
+            self._on_device(q, k, v, lens, table, q_out, cu_rows, positions, q_norm, k_norm)
+        st = _lib.aoh_paged_append_rotated(self.handle, rope.address, norms, qp, kp, vp, qs, ks, vs, pp, cp, lp, n, rows, tp,
+                                           width, op, os_, self._stream(stream))
         if st:
             _check(st)
 

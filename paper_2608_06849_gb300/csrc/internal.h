@@ -230,6 +230,33 @@ struct PagedReadArgs {
   uint32_t* err;
 };
 
+// Frequencies of the position rotation (aoh_rope of include/aoh.h).
+struct RopeTurns {
+  int n_pairs, interleaved;
+  float scale;
+  uint64_t turns[64];
+};
+
+// Norms and rotation of rows q, k ([Hq][D], [Hkv][D] at token strides of so many elements):
+// into dense rows q_out, k_out, or, with rows.table, q into q_out and k, with v as it is, into
+// the pages, as PagedAppendArgs has them.
+struct RotateArgs {
+  RopeTurns rope;
+  int Hq, Hkv;  // 0: no such rows
+  const void *q, *k, *v;
+  long long q_stride, k_stride, v_stride;
+  void *q_out, *k_out;
+  long long q_out_stride, k_out_stride;
+  const void *q_norm, *k_norm;  // [D], or null: no norm
+  int norm_f32;                 // the weights' type: 0 bf16, 1 fp32
+  float eps;
+  const int32_t* positions;  // device [rows.n_rows]; null (pages alone): each row's place in its sequence
+  PageRows rows;
+  PagePool pool;
+  const int32_t* lens;
+  uint32_t* err;
+};
+
 struct PagedDecodeArgs {
   CUtensorMap pages;  // the pool as [page, K or V, head][row][D]
   PagePool pool;
@@ -317,6 +344,7 @@ cudaError_t launch_prefill_folded(const FoldedArgs& a, const std::vector<uint64_
                                   int num_sms, cudaStream_t s);
 cudaError_t launch_paged_append(const PagedAppendArgs& a, int num_sms, cudaStream_t s);
 cudaError_t launch_paged_read(const PagedReadArgs& a, int num_sms, cudaStream_t s);
+cudaError_t launch_rotate(const RotateArgs& a, int d_head, int num_sms, cudaStream_t s);
 bool make_pages_map(CUtensorMap* map, const PagePool& p);
 // Floats of PagedDecodeArgs::states.
 size_t paged_state_floats(int num_sms, int D);

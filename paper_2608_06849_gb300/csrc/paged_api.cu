@@ -118,6 +118,57 @@ PageRows page_rows(const int32_t* cu, int32_t n_seqs, int32_t n_rows, const int3
   return r;
 }
 
+// The rope and the norms of a rotation of heads of d numbers.
+aoh_status check_rotation(const aoh_rope* rope, const aoh_norms* norms, int d) {
+  if (!rope) return fail(AOH_ERR_INVALID, "rope is NULL");
+  if (rope->n_pairs < 0 || rope->n_pairs % 8 || 2 * rope->n_pairs > d || (rope->interleaved != 0 && rope->interleaved != 1))
+    return fail(AOH_ERR_INVALID, "rope turns %d pairs; heads of %d take a multiple of 8, at most %d (aoh_rope_init fills it)",
+                rope->n_pairs, d, d / 2);
+  if (!(rope->scale >= -1e30f && rope->scale <= 1e30f))
+    return fail(AOH_ERR_INVALID, "the rope's scale must be within [-1e30, 1e30]");
+  if (!norms || (!norms->q && !norms->k)) return AOH_OK;
+  if (norms->type != AOH_NORM_BF16 && norms->type != AOH_NORM_F32)
+    return fail(AOH_ERR_INVALID, "norm type %d is neither bf16 (0) nor fp32 (1)", norms->type);
+  const size_t align = norms->type == AOH_NORM_F32 ? 4 : 2;
+  if (!aligned(norms->q, align) || !aligned(norms->k, align))
+    return fail(AOH_ERR_INVALID, "norm weights must be aligned to their numbers");
+  if (!(norms->eps >= 0.f && norms->eps <= 1e30f)) return fail(AOH_ERR_INVALID, "eps must be a number >= 0");
+  return AOH_OK;
+}
+
+// Rows written where others are read: in place alone, with the same stride.
+aoh_status check_in_place(const char* name, const void* in, int64_t in_stride, const void* out, int64_t out_stride) {
+  if (in == out && in_stride != out_stride)
+    return fail(AOH_ERR_INVALID, "%s in place must keep its token stride", name);
+  return AOH_OK;
+}
+
+void set_rotation(RotateArgs* a, const aoh_rope* rope, const aoh_norms* norms) {
+  memset(a, 0, sizeof(*a));
+  a->rope.n_pairs = rope->n_pairs;
+  a->rope.interleaved = rope->interleaved;
+  a->rope.scale = rope->scale;
+  memcpy(a->rope.turns, rope->turns, sizeof(a->rope.turns));
+  if (!norms) return;
+  a->q_norm = norms->q;
+  a->k_norm = norms->k;
+  a->norm_f32 = norms->type;
+  a->eps = norms->eps;
+}
+
+// SMs of the current device.
+cudaError_t sm_count(int* n) {
+  static std::atomic<int> known[64];
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  *n = dev < 64 ? known[dev].load(std::memory_order_relaxed) : 0;
+  if (*n > 0) return cudaSuccess;
+  e = cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev);
+  if (e == cudaSuccess && dev < 64) known[dev].store(*n, std::memory_order_relaxed);
+  return e;
+}
+
 aoh_status check_cu(const int32_t* cu, int32_t n_seqs, int32_t n_rows) {
   if (n_rows < 0) return fail(AOH_ERR_INVALID, "n_rows must be >= 0");
   if (!cu && n_rows != n_seqs) return fail(AOH_ERR_INVALID, "without cu_rows, n_rows must be n_seqs");
@@ -233,6 +284,112 @@ aoh_status aoh_paged_append(aoh_paged* cache, const void* k, const void* v, int6
   a.err = cache->d_err;
   const cudaError_t e = launch_paged_append(a, cache->num_sms, (cudaStream_t)stream);
   return e == cudaSuccess ? AOH_OK : cuda_fail(e, "paged append launch");
+}
+
+aoh_status aoh_rope_init(const double* inv_freq, int32_t n_pairs, int32_t interleaved, aoh_rope* out) {
+  if (!out) return fail(AOH_ERR_INVALID, "out is NULL");
+  memset(out, 0, sizeof(*out));
+  if (n_pairs < 0 || n_pairs > 64 || n_pairs % 8)
+    return fail(AOH_ERR_INVALID, "n_pairs = %d must be a multiple of 8 in [0, 64]", n_pairs);
+  if (interleaved != 0 && interleaved != 1) return fail(AOH_ERR_INVALID, "interleaved must be 0 or 1");
+  if (n_pairs > 0 && !inv_freq) return fail(AOH_ERR_INVALID, "inv_freq is NULL");
+  for (int i = 0; i < n_pairs; ++i)
+    if (!(inv_freq[i] >= -1e6 && inv_freq[i] <= 1e6))
+      return fail(AOH_ERR_INVALID, "inv_freq[%d] = %g must be a number within [-1e6, 1e6]", i, inv_freq[i]);
+  out->n_pairs = n_pairs;
+  out->interleaved = interleaved;
+  out->scale = 1.f;
+  // inv_freq / 2 pi in two doubles, its whole turns dropped: whole + part, part in [-1/2, 1/2]
+  constexpr double kHi = 0.15915494309189535, kLo = -9.839338337591243e-18;  // 1 / (2 pi)
+  for (int i = 0; i < n_pairs; ++i) {
+    const double f = inv_freq[i], p = f * kHi, rest = fma(f, kHi, -p) + f * kLo, part = p - rint(p);
+    const uint64_t head = part >= 0.5 ? 1ull << 63 : (uint64_t)llrint(ldexp(part, 64));
+    out->turns[i] = head + (uint64_t)llrint(ldexp(rest, 64));
+  }
+  return AOH_OK;
+}
+
+aoh_status aoh_norm_rotate(const aoh_rope* rope, const aoh_norms* norms, const void* q, const void* k, int64_t q_stride,
+                           int64_t k_stride, const int32_t* positions, int32_t n_rows, int32_t n_q_heads,
+                           int32_t n_kv_heads, int32_t d_head, void* q_out, void* k_out, int64_t q_out_stride,
+                           int64_t k_out_stride, void* stream) {
+  if (d_head != 64 && d_head != 128) return fail(AOH_ERR_UNSUPPORTED, "d_head must be 64 or 128");
+  if (n_rows < 0) return fail(AOH_ERR_INVALID, "n_rows must be >= 0");
+  if (n_q_heads < 0 || n_kv_heads < 0 || n_q_heads > 1024 || n_kv_heads > 1024)
+    return fail(AOH_ERR_INVALID, "n_q_heads and n_kv_heads must be in [0, 1024]");
+  aoh_status st = check_rotation(rope, norms, d_head);
+  if (st != AOH_OK || n_rows == 0 || n_q_heads + n_kv_heads == 0) return st;
+  if (n_q_heads > 0) {
+    st = check_rows("q", q, q_stride, n_q_heads, d_head);
+    if (st == AOH_OK) st = check_rows("q_out", q_out, q_out_stride, n_q_heads, d_head);
+    if (st == AOH_OK) st = check_in_place("q", q, q_stride, q_out, q_out_stride);
+  }
+  if (st == AOH_OK && n_kv_heads > 0) {
+    st = check_rows("k", k, k_stride, n_kv_heads, d_head);
+    if (st == AOH_OK) st = check_rows("k_out", k_out, k_out_stride, n_kv_heads, d_head);
+    if (st == AOH_OK) st = check_in_place("k", k, k_stride, k_out, k_out_stride);
+  }
+  if (st != AOH_OK) return st;
+  if (!positions || !aligned(positions, 4)) return fail(AOH_ERR_INVALID, "positions must be a 4-byte aligned device pointer");
+  RotateArgs a;
+  set_rotation(&a, rope, norms);
+  a.Hq = n_q_heads;
+  a.Hkv = n_kv_heads;
+  a.q = q;
+  a.k = k;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.q_out = q_out;
+  a.k_out = k_out;
+  a.q_out_stride = q_out_stride;
+  a.k_out_stride = k_out_stride;
+  a.positions = positions;
+  a.rows.n_rows = n_rows;
+  int sms = 0;
+  cudaError_t e = sm_count(&sms);
+  if (e != cudaSuccess) return cuda_fail(e, "cudaDeviceGetAttribute");
+  e = launch_rotate(a, d_head, sms, (cudaStream_t)stream);
+  return e == cudaSuccess ? AOH_OK : cuda_fail(e, "rotation launch");
+}
+
+aoh_status aoh_paged_append_rotated(aoh_paged* cache, const aoh_rope* rope, const aoh_norms* norms, const void* q,
+                                    const void* k, const void* v, int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                                    const int32_t* positions, const int32_t* cu_rows, const int32_t* lens, int32_t n_seqs,
+                                    int32_t n_rows, const int32_t* table, int32_t table_stride, void* q_out,
+                                    int64_t q_out_stride, void* stream) {
+  aoh_status st = check_handle(cache);
+  if (st == AOH_OK) st = check_rotation(rope, norms, cache->cfg.d_head);
+  if (st == AOH_OK) st = check_seqs(cache, n_seqs);
+  if (st == AOH_OK) st = check_cu(cu_rows, n_seqs, n_rows);
+  if (st != AOH_OK || n_rows == 0) return st;
+  const aoh_paged_config& c = cache->cfg;
+  st = check_rows("q", q, q_stride, c.n_q_heads, c.d_head);
+  if (st == AOH_OK) st = check_rows("k", k, k_stride, c.n_kv_heads, c.d_head);
+  if (st == AOH_OK) st = check_rows("v", v, v_stride, c.n_kv_heads, c.d_head);
+  if (st == AOH_OK) st = check_rows("q_out", q_out, q_out_stride, c.n_q_heads, c.d_head);
+  if (st == AOH_OK) st = check_in_place("q", q, q_stride, q_out, q_out_stride);
+  if (st == AOH_OK) st = check_table(cache, table, table_stride);
+  if (st != AOH_OK) return st;
+  if (!lens) return fail(AOH_ERR_INVALID, "lens must not be NULL");
+  RotateArgs a;
+  set_rotation(&a, rope, norms);
+  a.Hq = c.n_q_heads;
+  a.Hkv = c.n_kv_heads;
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.q_out = q_out;
+  a.q_out_stride = q_out_stride;
+  a.positions = positions;
+  a.rows = page_rows(cu_rows, n_seqs, n_rows, table, table_stride);
+  a.pool = cache->pool;
+  a.lens = lens;
+  a.err = cache->d_err;
+  const cudaError_t e = launch_rotate(a, c.d_head, cache->num_sms, (cudaStream_t)stream);
+  return e == cudaSuccess ? AOH_OK : cuda_fail(e, "rotated append launch");
 }
 
 aoh_status aoh_paged_read(aoh_paged* cache, const int32_t* cu_rows, const int32_t* first, int32_t n_seqs,

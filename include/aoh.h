@@ -489,6 +489,7 @@ aoh_status aoh_norm_rotate(const aoh_rope* rope, const aoh_norms* norms, const v
  *   aoh_paged_append   new keys and values written to the pages; aoh_paged_append_rotated:
  *                      normalised and rotated on the way
  *   aoh_paged_decode   attention of one new token of every sequence
+ *   aoh_paged_attend   attention of a chunk of new tokens of every sequence over the pages
  *   aoh_paged_read     cached keys and values back as dense bf16 rows, e.g. the
  *                      prefix of a prompt that aoh_paged_prefill continues
  *
@@ -629,6 +630,27 @@ aoh_status aoh_paged_read(aoh_paged* cache, const int32_t* cu_rows, const int32_
  */
 aoh_status aoh_paged_decode(aoh_paged* cache, const void* q, int64_t q_stride, const int32_t* lens, int32_t n_seqs,
                             int32_t max_len, const int32_t* table, int32_t table_stride, void* out, void* stream);
+
+/*
+ * Attention of a chunk of new tokens of every sequence over its cached positions: a chunk of a
+ * long prompt, drafted tokens to be verified, single tokens, or all of them in one call. The rows of
+ * sequence b, q_lens[b] of them, follow those of sequence b - 1 in q and out, and are the last of its
+ * lens[b] positions, whose keys and values lie in the pages already (append them first): row
+ * i sits at position lens[b] - q_lens[b] + i and sees the positions up to its own by the rule
+ * above. A row that sees none (its position is below zero) gives zeros. A NaN or an infinity in a key or a value reaches the
+ * rows that see it, and no other, as in aoh_paged_prefill.
+ *   q        rows of [n_q_heads][d_head], q_stride elements apart
+ *   q_lens   host [n_seqs], >= 0; a captured call replays with the same ones
+ *   lens     device [n_seqs]
+ *   k_lens   host [n_seqs], or NULL: what the host takes lens to be (NULL: what the table holds). By
+ *            them the work is split; the outputs are right whatever they are
+ *   table    device [n_seqs][table_stride], of at most 2^30 tokens a row
+ *   out      [rows][n_q_heads][d_head]
+ * Errors: INVALID, CUDA.
+ */
+aoh_status aoh_paged_attend(aoh_paged* cache, const void* q, int64_t q_stride, const int32_t* q_lens,
+                            const int32_t* lens, const int32_t* k_lens, int32_t n_seqs, const int32_t* table,
+                            int32_t table_stride, void* out, void* stream);
 
 /*
  * Synchronise `stream` and read the device error word of the handle's calls: AOH_OK,

@@ -56,6 +56,7 @@ EXPORTS = [
     "aoh_paged_append_rotated",
     "aoh_paged_read",
     "aoh_paged_decode",
+    "aoh_paged_attend",
     "aoh_paged_check",
     "aoh_paged_destroy",
 ]
@@ -138,6 +139,7 @@ def load():
         "aoh_paged_append_rotated": (i32, [P, P, P, P, P, P, i64, i64, i64, P, P, P, i32, i32, P, i32, P, i64, P]),
         "aoh_paged_read": (i32, [P, P, P, i32, i32, P, i32, P, P, P]),
         "aoh_paged_decode": (i32, [P, P, i64, P, i32, i32, P, i32, P, P]),
+        "aoh_paged_attend": (i32, [P, P, i64, P, P, P, i32, P, i32, P, P]),
         "aoh_paged_check": (i32, [P, P]),
         "aoh_paged_destroy": (None, [P]),
     }
@@ -771,6 +773,28 @@ class PagedCache:
         if self.several_devices:
             self._on_device(q, lens, table, out)
         st = _lib.aoh_paged_decode(self.handle, qp, qs, lp, n, max_len, tp, width, op, self._stream(stream))
+        if st:
+            _check(st)
+
+    def attend(self, q, q_lens, lens, table, out, k_lens=None, stream=None):
+        """Attention of a chunk of new tokens of every sequence over its cached positions: q, out
+        [rows, Hq, d] (q with any distance between tokens), q_lens[b] rows of sequence b (a host list),
+        the last of its lens[b] positions (their own keys among them: append them first). k_lens: what the host
+        takes the lengths to be (None: what the table holds), by which the work is split."""
+        qp, qs, rows = _rows(q, "q", self.n_q_heads, self.d_head)
+        op = _dense(out, "out", (rows, self.n_q_heads, self.d_head), _BF16)
+        tp, n, width = self._table(table)
+        if len(q_lens) != n or (k_lens is not None and len(k_lens) != n):
+            raise ValueError(f"q_lens and k_lens hold one length for each of {n} sequences")
+        if sum(q_lens) != rows:
+            raise ValueError(f"q holds {rows} rows; q_lens say {sum(q_lens)}")
+        lp = _ints(lens, "lens", n)
+        if self.several_devices:
+            self._on_device(q, lens, table, out)
+        ql = array.array("i", q_lens)
+        kl = None if k_lens is None else array.array("i", k_lens)
+        st = _lib.aoh_paged_attend(self.handle, qp, qs, ql.buffer_info()[0], lp, kl.buffer_info()[0] if kl else None, n, tp,
+                                   width, op, self._stream(stream))
         if st:
             _check(st)
 

@@ -200,6 +200,16 @@ struct PagePool {
   int Hkv, D;
 };
 
+// Attention of chunks over a paged cache: folded items (seqs: {first query row, rows, the
+// sequence's number, -}) whose keys are those of the pages.
+struct PagedAttendArgs : FoldedArgs {
+  CUtensorMap pages;  // the pool as [page, K or V, head][row][D] (bf16 pages)
+  PagePool pool;
+  const int32_t* lens;   // device: tokens of each sequence
+  const int32_t* table;  // device [n_seqs][table_stride]
+  int table_stride;
+};
+
 // Rows of a call in a paged cache: sequence b's rows are cu[b] .. cu[b + 1] - 1 (cu
 // null: row b alone).
 struct PageRows {
@@ -342,6 +352,8 @@ cudaError_t launch_prefill_packed(const PackedArgs& a, const std::vector<uint64_
                                   const std::vector<uint64_t>& pairs, bool is_short, int num_sms, cudaStream_t s);
 cudaError_t launch_prefill_folded(const FoldedArgs& a, const std::vector<uint64_t>& items, int split, bool is_short,
                                   int num_sms, cudaStream_t s);
+// Chunks over pages, as launch_prefill_folded takes its items.
+cudaError_t launch_paged_attend(const PagedAttendArgs& a, const std::vector<uint64_t>& items, int split, cudaStream_t s);
 cudaError_t launch_paged_append(const PagedAppendArgs& a, int num_sms, cudaStream_t s);
 cudaError_t launch_paged_read(const PagedReadArgs& a, int num_sms, cudaStream_t s);
 cudaError_t launch_rotate(const RotateArgs& a, int d_head, int num_sms, cudaStream_t s);

@@ -537,6 +537,74 @@ aoh_status aoh_paged_prefill(aoh_paged* cache, const void* q, const void* k, con
   return fail(AOH_ERR_CUDA, "packed prefill: %s", x.what());
 }
 
+aoh_status aoh_paged_attend(aoh_paged* cache, const void* q, int64_t q_stride, const int32_t* q_lens, const int32_t* lens,
+                            const int32_t* k_lens, int32_t n_seqs, const int32_t* table, int32_t table_stride, void* out,
+                            void* stream) try {
+  aoh_status st = check_handle(cache);
+  if (st == AOH_OK) st = check_seqs(cache, n_seqs);
+  if (st != AOH_OK || n_seqs == 0) return st;
+  if (!q_lens) return fail(AOH_ERR_INVALID, "q_lens must not be NULL");
+  const aoh_paged_config& c = cache->cfg;
+  // what the kernel reads of the sequences that have rows, and what the plan takes them to be
+  std::vector<int4> seqs, planned;
+  seqs.reserve(n_seqs);
+  planned.reserve(n_seqs);
+  const long long holds = (long long)table_stride * c.page_size;
+  long long n_q = 0;
+  for (int b = 0; b < n_seqs; ++b) {
+    if (q_lens[b] < 0 || (k_lens && k_lens[b] < 0))
+      return fail(AOH_ERR_INVALID, "sequence %d has %d rows and %d keys", b, q_lens[b], k_lens ? k_lens[b] : 0);
+    if (q_lens[b] > 0) {
+      seqs.push_back(make_int4((int)n_q, q_lens[b], b, 0));
+      planned.push_back(make_int4((int)n_q, q_lens[b], 0, (int)std::min(k_lens ? (long long)k_lens[b] : holds, holds)));
+    }
+    n_q += q_lens[b];
+    if (n_q > (1 << 30)) return fail(AOH_ERR_INVALID, "more than 2^30 rows in one call");
+  }
+  if (n_q == 0) return AOH_OK;
+  st = check_rows("q", q, q_stride, c.n_q_heads, c.d_head);
+  if (st == AOH_OK) st = check_rows("out", out, (int64_t)c.n_q_heads * c.d_head, c.n_q_heads, c.d_head);
+  if (st == AOH_OK) st = check_table(cache, table, table_stride);
+  if (st != AOH_OK) return st;
+  if (!lens || !aligned(lens, 4)) return fail(AOH_ERR_INVALID, "lens must be a 4-byte aligned device pointer");
+  if (holds > (1 << 30)) return fail(AOH_ERR_INVALID, "a table's row must hold at most 2^30 tokens");
+
+  PagedAttendArgs a;
+  memset(&a, 0, sizeof(a));
+  a.geom = cache->geom;
+  a.out = out;
+  a.q = q;
+  a.q_stride = q_stride;
+  a.err = cache->d_err;
+  a.scale_log2 = (float)(1.4426950408889634 / sqrt((double)c.d_head));
+  a.span = 128 / a.geom.G;
+  a.rcp = 65536 / a.geom.G + 1;
+  a.pages = cache->pages;
+  a.pool = cache->pool;
+  a.lens = lens;
+  a.table = table;
+  a.table_stride = table_stride;
+  if (!make_rows_map(&a.tq, q, 1, n_q, c.n_q_heads, c.d_head, q_stride, a.span, a.geom.G))
+    return fail(AOH_ERR_CUDA, "cuTensorMapEncodeTiled failed for q");
+  cudaStream_t s = (cudaStream_t)stream;
+  if (seqs.size() <= (size_t)PackedSeqs::kMost) {
+    std::copy(seqs.begin(), seqs.end(), a.seqs.by_value);
+  } else {
+    a.seqs.table = cache->d_seqs;
+    const cudaError_t e = launch_packed_seqs(cache->d_seqs, seqs, s);
+    if (e != cudaSuccess) return cuda_fail(e, "sequence upload launch");
+  }
+  std::vector<int> costs;
+  const std::vector<uint64_t> items = folded_schedule(a.geom, planned, a.span, &costs);
+  bool lone = true;
+  for (const int4& b : seqs) lone = lone && b.y <= a.span;
+  const int split = folded_split(costs, lone, decode_tc_max_clusters, cache->num_sms);
+  const cudaError_t e = launch_paged_attend(a, items, split, s);
+  return e == cudaSuccess ? AOH_OK : cuda_fail(e, "paged attention launch");
+} catch (const std::exception& x) {
+  return fail(AOH_ERR_CUDA, "paged attention: %s", x.what());
+}
+
 aoh_status aoh_paged_check(aoh_paged* cache, void* stream) {
   const aoh_status st = check_handle(cache);
   if (st != AOH_OK) return st;

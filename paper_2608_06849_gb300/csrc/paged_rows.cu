@@ -75,20 +75,6 @@ __device__ __forceinline__ uint4 encode(const Sixteen& x, int* e) {
                     __byte_perm(c[6], c[7], 0x5410));
 }
 
-__device__ __forceinline__ Sixteen decode(const uint4& c, int e) {
-  const float scale = __uint_as_float((uint32_t)(127 + e) << 23);
-  const uint32_t w[4] = {c.x, c.y, c.z, c.w};
-  Sixteen x;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t two = w[i / 2] >> (16 * (i & 1));
-    const float2 f = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(two & 0xffffu), __NV_E4M3)));
-    const float2 y = __fmul2_rn(f, make_float2(scale, scale));
-    x.w[i] = float2_to_bf16x2(y.x, y.y);
-  }
-  return x;
-}
-
 // A block's threads as (row of several at a time, vector of a token, 16 numbers of it): the
 // vectors of a token side by side, up to as many as the block holds, and several tokens where
 // it holds more. Each thread has U rows on their way at once.

@@ -1,6 +1,8 @@
-// What the kernels over rows of a paged cache share (paged_rows.cu, rotate.cu): where a row of
-// a call lies, and loads and stores of 16 numbers.
+// What the kernels over rows of a paged cache share (paged_rows.cu, rotate.cu, paged_attend.cuh):
+// where a row of a call lies, and 16 numbers of it.
 #pragma once
+
+#include <cuda_fp8.h>
 
 #include "common.cuh"
 #include "internal.h"
@@ -90,6 +92,21 @@ __device__ __forceinline__ void store16(void* p, const Sixteen& x) {
     *static_cast<uint4*>(p) = make_uint4(x.w[0], x.w[1], x.w[2], x.w[3]);
     *(static_cast<uint4*>(p) + 1) = make_uint4(x.w[4], x.w[5], x.w[6], x.w[7]);
   }
+}
+
+// What 16 e4m3 codes of a row with power e stand for: exactly, in bf16.
+__device__ __forceinline__ Sixteen decode(const uint4& c, int e) {
+  const float scale = __uint_as_float((uint32_t)(127 + e) << 23);
+  const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+  Sixteen x;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t two = w[i / 2] >> (16 * (i & 1));
+    const float2 f = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(two & 0xffffu), __NV_E4M3)));
+    const float2 y = __fmul2_rn(f, make_float2(scale, scale));
+    x.w[i] = float2_to_bf16x2(y.x, y.y);
+  }
+  return x;
 }
 
 // What earlier kernels wrote is visible from here on; the next one may start its prologue.

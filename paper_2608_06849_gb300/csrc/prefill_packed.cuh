@@ -74,7 +74,9 @@ struct FoldedItem {
   static constexpr int n_c = 0;  // no cached tiles
   int G, span, rcp, kvh, q0, len, qrow, krow, klen, off, a_end, c_begin, c_end;
   bool streaming;
-  __device__ __forceinline__ FoldedItem(const FoldedArgs& a, uint64_t code) {
+  __device__ __forceinline__ FoldedItem(const FoldedArgs& a, uint64_t code)
+      : FoldedItem(a, code, a.seqs.of((int)(code >> 34))) {}
+  __device__ __forceinline__ FoldedItem(const FoldedArgs& a, uint64_t code, const int4& s) {
     const CacheGeom& g = a.geom;
     G = g.G;
     span = a.span;
@@ -82,7 +84,6 @@ struct FoldedItem {
     kvh = (int)(code >> 24) & 1023;
     q0 = (int)(code & 0xffffffu) * (2 * span);
     streaming = g.kind[kvh] != 0;
-    const int4 s = a.seqs.of((int)(code >> 34));
     qrow = s.x;
     len = s.y;
     krow = s.z;
@@ -172,21 +173,27 @@ struct PackedMask {
 // 1.1, one behind the sinks of every streaming row 4.2, one number of every V row infinite 90.
 // Calls without such values pay for the look at their outputs alone: 16 x 101-2,999 tokens 230 ->
 // 233 us, 32,768 tokens the same.
+template <int D>
+__device__ __forceinline__ void load_numbers(const bf16* p, float (&to)[D / 32]) {
+#pragma unroll
+  for (int n = 0; n < D / 32; n += 2) {
+    const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(p + n));
+    to[n] = f.x;
+    to[n + 1] = f.y;
+  }
+}
+// The lane's numbers of key j of an item's sequence, of K (sel 0) or V.
+template <int D, class T>
+__device__ __forceinline__ void load_key(const PackedArgs& a, const T& t, int j, int sel, int lane, float (&to)[D / 32]) {
+  load_numbers<D>(static_cast<const bf16*>(sel ? a.v : a.k) + (long long)(t.krow + j) * (sel ? a.v_stride : a.k_stride) +
+                      t.kvh * D + lane * (D / 32), to);
+}
 template <int D, class A>
 __device__ void repair_rows(const A& a, uint64_t code, int row0, uint32_t rows) {
   constexpr int N = D / 32;
   const typename CallOf<A>::ItemT t(a, code);
   const CacheGeom& g = a.geom;
   const int lane = threadIdx.x & 31;
-  auto load = [&](const void* base, long long stride, long long row, int head, float (&to)[N]) {
-    const bf16* p = static_cast<const bf16*>(base) + row * stride + head * D + lane * N;
-#pragma unroll
-    for (int n = 0; n < N; n += 2) {
-      const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(p + n));
-      to[n] = f.x;
-      to[n + 1] = f.y;
-    }
-  };
   __syncwarp();  // the rows' first writes come before
   for (; rows; rows &= rows - 1) {
     const int row = row0 + __ffs((int)rows) - 1, x = row >> 7, r = row & 127;
@@ -201,7 +208,7 @@ __device__ void repair_rows(const A& a, uint64_t code, int row0, uint32_t rows) 
       float bad = 0.f;
       auto look = [&](int from, int to) {
         for (int j = from; j < to; ++j) {
-          load(a.v, a.v_stride, t.krow + j, t.kvh, v);
+          load_key<D>(a, t, j, 1, lane, v);
 #pragma unroll
           for (int n = 0; n < N; ++n) bad = fmaf(v[n], 0.f, bad);
         }
@@ -213,12 +220,12 @@ __device__ void repair_rows(const A& a, uint64_t code, int row0, uint32_t rows) 
     if (!hit) continue;
     const size_t at = t.out_row(a, x, r);
     float q[N], k[N], m = -INFINITY, l = 0.f;
-    load(a.q, a.q_stride, at / g.Hq, (int)(at % g.Hq), q);
+    load_numbers<D>(static_cast<const bf16*>(a.q) + (long long)(at / g.Hq) * a.q_stride + (int)(at % g.Hq) * D + lane * N, q);
     for (int j = pos; j >= 0; --j) {
       if (j < w0) j = min(j, sinks - 1);
       if (j < 0) break;
-      load(a.k, a.k_stride, t.krow + j, t.kvh, k);
-      load(a.v, a.v_stride, t.krow + j, t.kvh, v);
+      load_key<D>(a, t, j, 0, lane, k);
+      load_key<D>(a, t, j, 1, lane, v);
       float s = 0.f;
 #pragma unroll
       for (int n = 0; n < N; ++n) s = fmaf(q[n], k[n], s);
@@ -255,6 +262,8 @@ struct CallOf<PackedArgs> {
   template <int D>
   static constexpr bool kLaneRows = D == 64;
   static constexpr bool kChained = true;
+  static constexpr bool kPaged = false, kF8 = false;
+  static constexpr int kThreads = pf::kThreads, kSoftmax = 2;
 };
 template <>
 struct CallOf<FoldedArgs> {
@@ -266,6 +275,8 @@ struct CallOf<FoldedArgs> {
   template <int D>
   static constexpr bool kLaneRows = true;
   static constexpr bool kChained = true;
+  static constexpr bool kPaged = false, kF8 = false;
+  static constexpr int kThreads = pf::kThreads, kSoftmax = 2;
 };
 
 }  // namespace pf

@@ -19,7 +19,7 @@ cudaError_t launch(K kernel, int smem, int grid, int cluster, const A& a, const 
                    More... more) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)grid);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(CallOf<A>::kThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
@@ -42,15 +42,22 @@ cudaError_t launch(K kernel, int smem, int grid, int cluster, const A& a, const 
 template <class A, int D, int MODE, int CAP>
 cudaError_t launch_items(const A& a, const uint64_t* items, int n, int each, cudaStream_t s) {
   auto kernel = prefill_tc_kernel<A, D, MODE, CAP>;
+  constexpr int smem = TcCfg<A, D>::SMEM;
   static std::atomic<uint64_t> done{0};
   const cudaError_t e = once_per_device(done, [&] {
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, PfCfg<D>::SMEM);
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e == cudaSuccess && CallOf<A>::kF8) {
+      // its warpgroups exchange registers: more than the block is launched with would wait forever
+      cudaFuncAttributes at;
+      e = cudaFuncGetAttributes(&at, kernel);
+      if (e == cudaSuccess && at.numRegs != kExchanged) e = cudaErrorInvalidConfiguration;
+    }
     if (e == cudaSuccess && MODE == kSplit)
       e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     return e;
   });
   if (e != cudaSuccess) return e;
-  return launch<A, decltype(kernel), CAP>(kernel, PfCfg<D>::SMEM, n * each, MODE == kPairs ? 2 : each, a, items, n, s);
+  return launch<A, decltype(kernel), CAP>(kernel, smem, n * each, MODE == kPairs ? 2 : each, a, items, n, s);
 }
 
 template <class A, int D>

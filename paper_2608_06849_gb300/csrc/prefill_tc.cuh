@@ -28,7 +28,8 @@
 //               and while one query tile's softmax runs the tensor pipe works
 //               on the other's MMAs, hiding the commit -> softmax -> issue
 //               latency of each tile.
-//   warps 2-5   softmax of tile A, warps 6-9 softmax of tile B: thread r owns
+//   warps 2-5   softmax of tile A, warps 6-9 softmax of tile B (of 8-bit pages warps 4-11,
+//               behind them four that turn codes into bf16 tiles: paged_attend.cuh): thread r owns
 //               row r (TMEM lane r). One tcgen05.ld pass reads its S row, a
 //               two-range integer mask hides keys, max and sum reduce in 8
 //               independent chains, p = 2^(s*scale - m) costs one FFMA and one
@@ -65,11 +66,13 @@ constexpr int kWhole = 0, kPairs = 1, kSplit = 2;
 __device__ __forceinline__ bool empty_state(float m, float l) { return m == -INFINITY && l == 0.f; }
 
 template <class A, int D, int MODE, int CAP>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(CallOf<A>::kThreads, 1)
     prefill_tc_kernel(const __grid_constant__ A a, const __grid_constant__ WorkList<CAP> wl) {
-  using C = PfCfg<D>;
+  using C = TcCfg<A, D>;
   using Call = CallOf<A>;
   using SB = SBuf<A, D>;
+  constexpr bool PAGED = Call::kPaged, F8 = Call::kF8;
+  constexpr int S0 = Call::kSoftmax;  // the first of the 8 softmax warps
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
   uint8_t* sQ = smem + C::OFF_Q;
@@ -94,7 +97,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if constexpr (Call::kChained) {
     if (threadIdx.x == 0) prefetch_maps(a);
-    if (a.seqs.table != nullptr) wait_to_start(a);  // the item is read from device memory
+    if (PAGED || a.seqs.table != nullptr) wait_to_start(a);  // the item is read from device memory
   }
   constexpr bool PAIRS = MODE == kPairs, SPLIT = MODE == kSplit;
   const int ctas = SPLIT ? (int)cluster_ctas() : 2;
@@ -111,10 +114,12 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int t0 = rank * per;
   const int n_tiles = !half ? n_all : SPLIT ? max(0, min(per, n_all - t0)) : rank == 0 ? (n_all + 1) / 2 : n_all / 2;
   const bool lone = SPLIT && !t.has_row(1, 0);
+  RawRing<A, D> ring(smem, lone);
+  PageWalk<A, D> pages(a, t, warp == 0 ? lane : -1);
   if (threadIdx.x == 0) {
-    mbar_init(q_full, 2);
+    mbar_init(q_full, lone && F8 ? 1 : 2);
     for (int s = 0; s < kNS; ++s) {
-      mbar_init(&kv_full[s], 1);
+      mbar_init(&kv_full[s], F8 ? kConvert : 1);
       mbar_init(&kv_empty[s], 1);
     }
     for (int i = 0; i < 4; ++i) {
@@ -127,13 +132,22 @@ __global__ void __launch_bounds__(kThreads, 1)
     mbar_init(&v_zeroed[0], 1);
     mbar_init(&v_zeroed[1], 1);
     *abort_flag = 0;
+    if constexpr (F8) ring.init();
     fence_mbar_init();
     fence_proxy_async_smem();
     if constexpr (Call::kChained) wait_to_start(a);
     // the first loads need no other warp
     load_q<D>(a, t, 0, sQ, q_full);
-    load_q<D>(a, t, 1, sQ + C::QBYTES, q_full);
-    if (n_tiles > 0) load_kv<D>(a, t, t0, 0, sKV, &kv_full[0]);
+    if (!(lone && F8)) load_q<D>(a, t, 1, sQ + C::QBYTES, q_full);  // (its place is the ring's)
+    if constexpr (!PAGED)
+      if (n_tiles > 0) load_kv<D>(a, t, t0, 0, sKV, &kv_full[0]);
+  }
+  if constexpr (PAGED && !F8) {
+    if (warp == 0 && n_tiles > 0) {
+      __syncwarp();
+      pages.look(a, t, t0);
+      pages.load(a, t, 0, sKV, &kv_full[0]);
+    }
   }
   if (warp == 1) {
     tmem_alloc(tmem_slot, kTmemCols);
@@ -148,174 +162,227 @@ __global__ void __launch_bounds__(kThreads, 1)
   // a half: a row's final softmax state (softmax warps)
   float end_m = -INFINITY, end_l = 0.f;
   bool end_ok = true;
-  if (warp == 0) {
-    // ------------------------------------------------------------ producer
-    // Lane 0 issues the copies. Rows of a V tile past its valid keys may hold
-    // anything (cache rows not yet written, chunk padding) and a zero weight
-    // times a NaN is still NaN, so for a partial V tile the whole warp waits
-    // for the copy, zeroes those rows and signals v_zeroed before the MMA
-    // issuer may read the tile.
-    int issued = min(n_tiles, 1), n_partial = 0;  // the first K tile is on its way
-    bool ok = true;
-    for (int jj = 0; jj < n_tiles && ok; ++jj) {
-      for (int sel = 0; sel < 2; ++sel) {
-        const int it = 2 * jj + sel;
-        const int st = it % kNS;
-        if (lane == 0) {
-          if (it >= kNS) ok = wait_bar(&kv_empty[st], ((it / kNS) & 1) ^ 1, a.err, abort_flag);
-          if (ok && it > 0) {
-            load_kv<D>(a, t, t0 + jj, sel, sKV + st * C::KVBYTES, &kv_full[st]);
-            issued = it + 1;
+  if (warp < S0 || warp >= S0 + 8) {
+    if constexpr (F8) {
+      // The softmax warps have their registers before any of these takes its own back below: a
+      // role may end at once, and then there would be none left for them to wait for.
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+      __syncthreads();
+    }
+    if (F8 && (warp == 0 || (warp > 1 && warp < S0) || warp >= S0 + 8)) {
+      if constexpr (F8) {
+        if (warp == 0) {
+          // -------------------------------------------------------- producer of codes
+          int n_units = 0;
+          bool ok = true;
+          for (int jj = 0; jj < n_tiles && ok; ++jj) {
+            pages.look(a, t, t0 + jj);
+            for (int u = 0; u < 4 && ok; ++u, ++n_units) ok = ring.fill(a, t, pages, n_units, u >> 1, u & 1, lane, abort_flag);
+          }
+          // every issued copy lands before the CTA can exit
+          if (lane == 0) drain_wait(q_full, 0, a.err);
+          ring.drain(a, n_units, lane);
+        } else if (warp >= S0 + 8) {
+          // -------------------------------------------------------- codes to bf16 tiles
+          bool ok = true;
+          for (int it = 0; it < 2 * n_tiles && ok; ++it) {
+            const int st = it % kNS, valid = t.valid(g, t0 + (it >> 1));
+            if (it >= kNS) ok = __all_sync(0xffffffffu, wait_bar(&kv_empty[st], ((it / kNS) & 1) ^ 1, a.err, abort_flag));
+            for (int u = 0; u < 2 && ok; ++u)
+              ok = ring.convert(a, 2 * it + u, sKV + st * C::KVBYTES, u, valid, warp - (S0 + 8), lane, abort_flag);
+            if (!ok) break;
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&kv_full[st]);
           }
         }
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-        const int valid = t.valid(g, t0 + jj);
-        if (sel == 1 && valid < kBN && n_partial < 2) {
-          ok = __all_sync(0xffffffffu, wait_bar(&kv_full[st], (it / kNS) & 1, a.err, abort_flag));
+        // (two warps fill up the producer's warpgroup)
+      }
+    } else if (warp == 0) {
+      // ------------------------------------------------------------ producer
+      // Lane 0 issues the copies. Rows of a V tile past its valid keys may hold
+      // anything (cache rows not yet written, chunk padding) and a zero weight
+      // times a NaN is still NaN, so for a partial V tile the whole warp waits
+      // for the copy, zeroes those rows and signals v_zeroed before the MMA
+      // issuer may read the tile.
+      int issued = min(n_tiles, 1), n_partial = 0;  // the first K tile is on its way
+      bool ok = true;
+      for (int jj = 0; jj < n_tiles && ok; ++jj) {
+        if constexpr (PAGED)
+          if (jj > 0) pages.look(a, t, t0 + jj);
+        for (int sel = 0; sel < 2; ++sel) {
+          const int it = 2 * jj + sel;
+          const int st = it % kNS;
+          if constexpr (PAGED) {
+            if (it >= kNS) ok = __all_sync(0xffffffffu, wait_bar(&kv_empty[st], ((it / kNS) & 1) ^ 1, a.err, abort_flag));
+            if (ok && it > 0) {
+              pages.load(a, t, sel, sKV + st * C::KVBYTES, &kv_full[st]);
+              issued = it + 1;
+            }
+          } else if (lane == 0) {
+            if (it >= kNS) ok = wait_bar(&kv_empty[st], ((it / kNS) & 1) ^ 1, a.err, abort_flag);
+            if (ok && it > 0) {
+              load_kv<D>(a, t, t0 + jj, sel, sKV + st * C::KVBYTES, &kv_full[st]);
+              issued = it + 1;
+            }
+          }
+          ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
-          zero_tail<D>(sKV + st * C::KVBYTES, valid, lane);
-          if (lane == 0) mbar_arrive(&v_zeroed[n_partial]);
-          ++n_partial;
+          const int valid = t.valid(g, t0 + jj);
+          if (sel == 1 && valid < kBN && n_partial < 2) {
+            ok = __all_sync(0xffffffffu, wait_bar(&kv_full[st], (it / kNS) & 1, a.err, abort_flag));
+            if (!ok) break;
+            zero_tail<D>(sKV + st * C::KVBYTES, valid, lane);
+            if (lane == 0) mbar_arrive(&v_zeroed[n_partial]);
+            ++n_partial;
+          }
         }
       }
-    }
-    // every issued copy lands before the CTA can exit
-    if (lane == 0) {
-      drain_wait(q_full, 0, a.err);
-      for (int it = issued > kNS ? issued - kNS : 0; it < issued; ++it)
-        drain_wait(&kv_full[it % kNS], (it / kNS) & 1, a.err);
-    }
-    __syncwarp();
-  } else if (warp == 1) {
-    // ------------------------------------------------------------ MMA issuer
-    // The whole warp runs the loop (its values stay warp-uniform); one elected
-    // lane, the same each time, issues.
-    const uint64_t q_desc = sdesc_sw128(smem_u32(sQ), 16, 1024);
-    const uint64_t k_desc0 = sdesc_sw128(smem_u32(sKV), 16, 1024);
-    const uint64_t v_desc0 = sdesc_sw128(smem_u32(sKV), C::BOX, 1024);
-    // S_X of the step, against K_jj, to buffer b
-    auto s_at = [&](int x, int step, int jj, int b) {
-      const uint64_t k_desc = k_desc0 + (uint32_t)(((2 * jj) % kNS) * sdesc_step(C::KVBYTES));
-      if (elect_one()) {
-        issue_s<D>(tmem + b * 128, q_desc + (lone ? 0u : sdesc_step(x * C::QBYTES)), k_desc);
-        tc_commit(&s_full[SB::bar(x, step)]);
+      // every issued copy lands before the CTA can exit
+      if (lane == 0) {
+        drain_wait(q_full, 0, a.err);
+        for (int it = issued > kNS ? issued - kNS : 0; it < issued; ++it)
+          drain_wait(&kv_full[it % kNS], (it / kNS) & 1, a.err);
       }
-    };
-    auto s_of = [&](int x, int jj) { s_at(x, jj, jj, x); };
-    auto commit = [&](uint64_t* bar) {
-      if (elect_one()) tc_commit(bar);
-    };
-    bool ok = n_tiles > 0;
-    auto wait = [&](uint64_t* bar, uint32_t parity) {
-      if (ok) ok = __all_sync(0xffffffffu, wait_bar(bar, parity, a.err, abort_flag));
-      return ok;
-    };
-    // O_X += P_X(step) V_jj, P in buffer b: the first half of the keys while the softmax forms the
-    // second half's weights
-    auto pv_at = [&](int x, int step, int jj, int b) {
-      const uint64_t v_desc = v_desc0 + (uint32_t)(((2 * jj + 1) % kNS) * sdesc_step(C::KVBYTES));
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        if (!wait(&p_full[2 * SB::bar(x, step) + half], SB::phase(step))) return false;
-        tc_fence_after();
+      __syncwarp();
+    } else {
+      // ------------------------------------------------------------ MMA issuer
+      // The whole warp runs the loop (its values stay warp-uniform); one elected
+      // lane, the same each time, issues.
+      const uint64_t q_desc = sdesc_sw128(smem_u32(sQ), 16, 1024);
+      const uint64_t k_desc0 = sdesc_sw128(smem_u32(sKV), 16, 1024);
+      const uint64_t v_desc0 = sdesc_sw128(smem_u32(sKV), C::BOX, 1024);
+      // S_X of the step, against K_jj, to buffer b
+      auto s_at = [&](int x, int step, int jj, int b) {
+        const uint64_t k_desc = k_desc0 + (uint32_t)(((2 * jj) % kNS) * sdesc_step(C::KVBYTES));
         if (elect_one()) {
-          issue_pv<D>(tmem + SB::O + x * D, tmem + b * 128, v_desc, half, step == 0);
-          if (half) tc_commit(&pv_done[SB::bar(x, step)]);
+          issue_s<D>(tmem + b * 128, q_desc + (lone ? 0u : sdesc_step(x * C::QBYTES)), k_desc);
+          tc_commit(&s_full[SB::bar(x, step)]);
         }
-      }
-      return true;
-    };
-    auto pv_of = [&](int x, int jj) { return pv_at(x, jj, jj, x); };
-    auto wait_k = [&](int jj) { return wait(&kv_full[(2 * jj) % kNS], ((2 * jj) / kNS) & 1); };
-    // only the last cached tile and the last chunk tile can be partial
-    int n_partial = 0;  // partial V tiles seen so far (index into v_zeroed)
-    const int part0 = t.n_c > 0 && t.valid(g, t.n_c - 1) < kBN ? t.n_c - 1 - t0 : -1;
-    const int part1 = t.valid(g, n_all - 1) < kBN ? n_all - 1 - t0 : -1;
-    auto wait_v = [&](int jj) {
-      if (!wait(&kv_full[(2 * jj + 1) % kNS], ((2 * jj + 1) / kNS) & 1)) return false;
-      if (jj == part0 || jj == part1) {
-        if (!wait(&v_zeroed[n_partial], 0)) return false;
-        ++n_partial;
-      }
-      return true;
-    };
-    if (SPLIT && lone) {
-      // S_X of tile j, whose K is then free
-      auto lone_s = [&](int x, int j) {
-        if (j >= n_tiles) return true;
-        if (!wait_k(j)) return false;
-        tc_fence_after();
-        s_at(x, j >> 1, j, j % SB::N);
-        commit(&kv_empty[(2 * j) % kNS]);
+      };
+      auto s_of = [&](int x, int jj) { s_at(x, jj, jj, x); };
+      auto commit = [&](uint64_t* bar) {
+        if (elect_one()) tc_commit(bar);
+      };
+      bool ok = n_tiles > 0;
+      auto wait = [&](uint64_t* bar, uint32_t parity) {
+        if (ok) ok = __all_sync(0xffffffffu, wait_bar(bar, parity, a.err, abort_flag));
+        return ok;
+      };
+      // O_X += P_X(step) V_jj, P in buffer b: the first half of the keys while the softmax forms the
+      // second half's weights
+      auto pv_at = [&](int x, int step, int jj, int b) {
+        const uint64_t v_desc = v_desc0 + (uint32_t)(((2 * jj + 1) % kNS) * sdesc_step(C::KVBYTES));
+  #pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          if (!wait(&p_full[2 * SB::bar(x, step) + half], SB::phase(step))) return false;
+          tc_fence_after();
+          if (elect_one()) {
+            issue_pv<D>(tmem + SB::O + x * D, tmem + b * 128, v_desc, half, step == 0);
+            if (half) tc_commit(&pv_done[SB::bar(x, step)]);
+          }
+        }
         return true;
       };
-      if (wait(q_full, 0) && lone_s(0, 0)) lone_s(1, 1);
-      for (int j = 0; j < n_tiles && ok; ++j) {
-        const int x = j & 1;
-        if (!wait_v(j) || !pv_at(x, j >> 1, j, j % SB::N)) break;
-        commit(&kv_empty[(2 * j + 1) % kNS]);
-        if (!lone_s(x, j + 2)) break;
-      }
-    } else if (SB::N == 3) {
-      if (wait(q_full, 0) && wait_k(0)) {
-        tc_fence_after();
-        s_at(0, 0, 0, 0);
-        s_at(1, 0, 0, 1);
-        commit(&kv_empty[0]);
-        if (n_tiles > 1 && wait_k(1)) {
-          tc_fence_after();
-          s_at(0, 1, 1, 2);
+      auto pv_of = [&](int x, int jj) { return pv_at(x, jj, jj, x); };
+      auto wait_k = [&](int jj) { return wait(&kv_full[(2 * jj) % kNS], ((2 * jj) / kNS) & 1); };
+      // only the last cached tile and the last chunk tile can be partial
+      int n_partial = 0;  // partial V tiles seen so far (index into v_zeroed)
+      const int part0 = t.n_c > 0 && t.valid(g, t.n_c - 1) < kBN ? t.n_c - 1 - t0 : -1;
+      const int part1 = t.valid(g, n_all - 1) < kBN ? n_all - 1 - t0 : -1;
+      auto wait_v = [&](int jj) {
+        if (!wait(&kv_full[(2 * jj + 1) % kNS], ((2 * jj + 1) / kNS) & 1)) return false;
+        if (!F8 && (jj == part0 || jj == part1)) {
+          if (!wait(&v_zeroed[n_partial], 0)) return false;
+          ++n_partial;
         }
+        return true;
+      };
+      if (SPLIT && lone) {
+        // S_X of tile j, whose K is then free
+        auto lone_s = [&](int x, int j) {
+          if (j >= n_tiles) return true;
+          if (!wait_k(j)) return false;
+          tc_fence_after();
+          s_at(x, j >> 1, j, j % SB::N);
+          commit(&kv_empty[(2 * j) % kNS]);
+          return true;
+        };
+        if (wait(q_full, 0) && lone_s(0, 0)) lone_s(1, 1);
+        for (int j = 0; j < n_tiles && ok; ++j) {
+          const int x = j & 1;
+          if (!wait_v(j) || !pv_at(x, j >> 1, j, j % SB::N)) break;
+          commit(&kv_empty[(2 * j + 1) % kNS]);
+          if (!lone_s(x, j + 2)) break;
+        }
+      } else if (SB::N == 3) {
+        if (wait(q_full, 0) && wait_k(0)) {
+          tc_fence_after();
+          s_at(0, 0, 0, 0);
+          s_at(1, 0, 0, 1);
+          commit(&kv_empty[0]);
+          if (n_tiles > 1 && wait_k(1)) {
+            tc_fence_after();
+            s_at(0, 1, 1, 2);
+          }
+        }
+        // after the P V of the n-th S comes the n + 3rd S
+        int b = 0;
+        for (int jj = 0; jj < n_tiles && ok; ++jj) {
+          if (!wait_v(jj) || !pv_at(0, jj, jj, b)) break;
+          if (jj + 1 < n_tiles) {
+            s_at(1, jj + 1, jj + 1, b);
+            commit(&kv_empty[(2 * (jj + 1)) % kNS]);
+          }
+          b = b == 2 ? 0 : b + 1;
+          if (!pv_at(1, jj, jj, b)) break;
+          commit(&kv_empty[(2 * jj + 1) % kNS]);
+          if (jj + 2 < n_tiles) {
+            if (!wait_k(jj + 2)) break;
+            tc_fence_after();
+            s_at(0, jj + 2, jj + 2, b);
+          }
+          b = b == 2 ? 0 : b + 1;
+        }
+      } else if (wait(q_full, 0) && wait_k(0)) {
+        tc_fence_after();
+        s_of(0, 0);
+        s_of(1, 0);
+        commit(&kv_empty[0]);
       }
-      // after the P V of the n-th S comes the n + 3rd S
-      int b = 0;
-      for (int jj = 0; jj < n_tiles && ok; ++jj) {
-        if (!wait_v(jj) || !pv_at(0, jj, jj, b)) break;
-        if (jj + 1 < n_tiles) {
-          s_at(1, jj + 1, jj + 1, b);
+      for (int jj = 0; SB::N == 2 && jj < n_tiles && ok && !lone; ++jj) {
+        const bool more = jj + 1 < n_tiles;
+        // tile A: P_A(jj) sits in S_A's columns; S_A(jj+1) may overwrite them
+        // only after O_A += P_A(jj) V_jj is issued (same-thread MMAs run in order)
+        if (!wait_v(jj) || !pv_of(0, jj)) break;
+        if (more) {
+          if (!wait_k(jj + 1)) break;
+          tc_fence_after();
+          s_of(0, jj + 1);
+        }
+        if (!pv_of(1, jj)) break;
+        commit(&kv_empty[(2 * jj + 1) % kNS]);
+        if (more) {
+          s_of(1, jj + 1);
           commit(&kv_empty[(2 * (jj + 1)) % kNS]);
         }
-        b = b == 2 ? 0 : b + 1;
-        if (!pv_at(1, jj, jj, b)) break;
-        commit(&kv_empty[(2 * jj + 1) % kNS]);
-        if (jj + 2 < n_tiles) {
-          if (!wait_k(jj + 2)) break;
-          tc_fence_after();
-          s_at(0, jj + 2, jj + 2, b);
-        }
-        b = b == 2 ? 0 : b + 1;
       }
-    } else if (wait(q_full, 0) && wait_k(0)) {
-      tc_fence_after();
-      s_of(0, 0);
-      s_of(1, 0);
-      commit(&kv_empty[0]);
+      commit(drain);
+      __syncwarp();
+      drain_wait(drain, 0, a.err);
+      __syncwarp();
     }
-    for (int jj = 0; SB::N == 2 && jj < n_tiles && ok && !lone; ++jj) {
-      const bool more = jj + 1 < n_tiles;
-      // tile A: P_A(jj) sits in S_A's columns; S_A(jj+1) may overwrite them
-      // only after O_A += P_A(jj) V_jj is issued (same-thread MMAs run in order)
-      if (!wait_v(jj) || !pv_of(0, jj)) break;
-      if (more) {
-        if (!wait_k(jj + 1)) break;
-        tc_fence_after();
-        s_of(0, jj + 1);
-      }
-      if (!pv_of(1, jj)) break;
-      commit(&kv_empty[(2 * jj + 1) % kNS]);
-      if (more) {
-        s_of(1, jj + 1);
-        commit(&kv_empty[(2 * (jj + 1)) % kNS]);
-      }
+    if constexpr (F8) {
+      __syncwarp();
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kExchanged));
     }
-    commit(drain);
-    __syncwarp();
-    drain_wait(drain, 0, a.err);
-    __syncwarp();
   } else {
+    if constexpr (F8) {
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+      __syncthreads();
+    }
     // ------------------------------------------------------------ softmax
-    const int x = (warp - 2) >> 2;        // 0: tile A (warps 2-5), 1: tile B (warps 6-9)
+    const int x = (warp - S0) >> 2;       // 0: tile A (the first four warps), 1: tile B
     const int q4 = warp & 3;              // TMEM lane quarter this warp may access
     const int r = q4 * 32 + lane;
     const int qt = lone ? 0 : x;          // the query tile
@@ -351,6 +418,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       if constexpr (Call::kRepairs)
         if (spoilt) repair_rows<D>(a, code, x * 128 + q4 * 32, spoilt);
     }
+    if constexpr (F8) {
+      __syncwarp();
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kExchanged));
+    }
   }
 
   tc_fence_before();
@@ -369,8 +440,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     float4* recv = reinterpret_cast<float4*>(smem);
     float2* recv_ml = reinterpret_cast<float2*>(recv + D / 4 * kMostStates);
     uint32_t* spoilt = reinterpret_cast<uint32_t*>(recv_ml + kMostStates);  // [4]: rows with a value that is not finite
-    const int x = (warp - 2) >> 2, q4 = warp & 3, r = q4 * 32 + lane;
-    if (warp >= 2) {
+    const int x = (warp - S0) >> 2, q4 = warp & 3, r = q4 * 32 + lane;
+    const bool soft = warp >= S0 && warp < S0 + 8;
+    if (soft) {
       const int row = lone ? r : x * 128 + r, from = lone ? 2 * rank + x : rank;
       const int dst = min(row / rows, ctas - 1), at = row - dst * rows;
       const uint32_t tl = tmem + ((uint32_t)(q4 * 32) << 16) + SB::O + x * D;
@@ -393,8 +465,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     cluster_arrive();
     cluster_wait();
-    if (warp >= 2) {
-      const int tid = threadIdx.x - 64;  // of the 256 softmax threads
+    if (soft) {
+      const int tid = threadIdx.x - S0 * 32;  // of the 256 softmax threads
       // (m, l) -> the state's weight, negative for an empty state, whose CTA may have had no tile
       // (unwritten values); any other counts
       if (tid < 4) spoilt[tid] = 0;
@@ -431,8 +503,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!(o.x * 0.f + o.y * 0.f + o.z * 0.f + o.w * 0.f == 0.f)) atomicOr(spoilt + (at >> 5), 1u << (at & 31));
       }
       named_barrier_sync(3, 256);
-      if (warp < 6 && spoilt[warp - 2])
-        repair_rows<D>(a, code, rank * rows + (warp - 2) * 32, spoilt[warp - 2]);
+      if (warp < S0 + 4 && spoilt[warp - S0])
+        repair_rows<D>(a, code, rank * rows + (warp - S0) * 32, spoilt[warp - S0]);
     }
     __syncthreads();
     tc_fence_after();
@@ -440,11 +512,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     // both CTAs' copies and MMAs are done with their shared memory
     cluster_arrive();
     cluster_wait();
-    const int x = (warp - 2) >> 2, q4 = warp & 3, r = q4 * 32 + lane;
+    const int x = (warp - S0) >> 2, q4 = warp & 3, r = q4 * 32 + lane;
+    const bool soft = warp >= S0 && warp < S0 + 8;
     const uint32_t tl = tmem + ((uint32_t)(q4 * 32) << 16) + SB::O + x * D;
     float4* recv = reinterpret_cast<float4*>(smem);  // [D / 4][128 rows], then (m, l) per row
     float2* recv_ml = reinterpret_cast<float2*>(recv + D / 4 * 128);
-    if (warp >= 2 && x != rank) {
+    if (soft && x != rank) {
       const uint32_t dst = cluster_addr(recv + r, (uint32_t)(rank ^ 1));
       cluster_st2(cluster_addr(recv_ml + r, (uint32_t)(rank ^ 1)), __float_as_uint(end_m), __float_as_uint(end_l));
       if (n_tiles > 0) {
@@ -462,7 +535,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     cluster_arrive();
     cluster_wait();
-    if (warp >= 2 && x == rank && end_ok) {
+    if (soft && x == rank && end_ok) {
       const float2 o_ml = recv_ml[r];
       const float M = fmaxf(end_m, o_ml.x);
       // an empty state's CTA may have had no tile at all (unwritten values); any other state

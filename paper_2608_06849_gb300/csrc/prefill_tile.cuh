@@ -41,6 +41,27 @@ struct PfCfg {
   static_assert(128 * (D * 4 + 8) <= OFF_BAR - QBYTES, "receive buffer of the split and its output rows");
 };
 
+// What prefill_tc_kernel's shared memory holds: the parts above, or, for calls whose K and V need
+// more of it, a layout of the call's own.
+template <class A, int D>
+struct TcCfg : PfCfg<D> {};
+// Calls over pages alone (paged_attend.cuh): the walk through a sequence's pages, and the ring of
+// 8-bit codes.
+template <class A, int D>
+struct PageWalk {
+  template <class T>
+  __device__ __forceinline__ PageWalk(const A&, const T&, int) {}
+};
+template <class A, int D>
+struct RawRing {
+  __device__ __forceinline__ RawRing(uint8_t*, bool) {}
+};
+constexpr int kConvert = 4;  // warps that turn codes into bf16
+// Registers a thread that such a kernel is launched with, and what its softmax warps and the others then
+// have: 256 threads each.
+constexpr int kExchanged = 128, kSoftmaxRegs = 168, kOtherRegs = 88;
+static_assert(kSoftmaxRegs + kOtherRegs == 2 * kExchanged, "registers are exchanged, not made");
+
 // Bits lo..hi-1 of a 32-bit word (lo, hi clamped to [0, 32]).
 __device__ __forceinline__ uint32_t range_bits(int lo, int hi) {
   lo = max(lo, 0);
@@ -258,13 +279,19 @@ struct CallOf<PrefillTcArgs> {
   static constexpr bool kLaneRows = false;  // output rows whose places take some work (write_rows)
   static constexpr bool kRepairs = false;  // rows that a hidden V row's NaN reached are gone over again (repair_rows)
   static constexpr bool kChained = false;  // launches overlap the one before (wait_to_start, wait_to_end)
+  static constexpr bool kPaged = false, kF8 = false;  // K and V in pages, and in 8 bits
+  static constexpr int kThreads = pf::kThreads, kSoftmax = 2;
 };
 
 template <class A>
 __device__ __forceinline__ void prefetch_maps(const A& a) {
   prefetch_tmap(&a.tq);
-  prefetch_tmap(&a.tk);
-  prefetch_tmap(&a.tv);
+  if constexpr (CallOf<A>::kPaged) {
+    if constexpr (!CallOf<A>::kF8) prefetch_tmap(&a.pages);
+  } else {
+    prefetch_tmap(&a.tk);
+    prefetch_tmap(&a.tv);
+  }
 }
 
 // A call's first launch waits for the kernel before it once it runs; one that follows

@@ -1,0 +1,299 @@
+"""Attention of chunks over pages against its 64-bit definition (oracle.paged) on what the
+pages hold.
+
+Tolerance: as for packed prompts (test_gpu_paged.py): rounding each softmax weight to 8 significant
+bits moves an output by at most 2^-9 * sum_j p_j |v_j| (``mag``, the definition run on |v|), storing it
+as bf16 by 2^-9 |o|; twice both plus 1e-4 is allowed (gpu_cases.assert_matches). Rows of 8 bits
+reach the tensor cores as the bf16 numbers that they stand for, so nothing else is added."""
+
+import numpy as np
+import pytest
+import torch
+
+from gpu_cases import assert_matches, ensure_lib, f64
+from oracle import paged as opaged
+from oracle import rotary as orot
+from paper_2608_06849_gb300 import aoh
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True, scope="module")
+def _lib():
+    ensure_lib()
+
+
+def randn(shape, seed, spread=0.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randn(shape, generator=g, device="cuda")
+    return (x * torch.exp2(spread * torch.randn(shape[:-1] + (1,), generator=g, device="cuda"))).bfloat16()
+
+
+def ints(xs):
+    return torch.tensor(xs, dtype=torch.int32, device="cuda")
+
+
+def sums(xs):
+    return np.concatenate([[0], np.cumsum(xs)]).tolist()
+
+
+def held(x, form):
+    return f64(x) if form == "bf16" else opaged.decode(*opaged.encode(f64(x)))
+
+
+class Case:
+    """Sequences of k_lens tokens in pages of a random order, and queries for their last q_lens."""
+
+    def __init__(self, q_lens, k_lens, hq, hkv, d, labels, sink, window, page, form, seed=0, fused=False, spread=0.0):
+        self.q_lens, self.k_lens, self.labels, self.sink, self.window, self.form = q_lens, k_lens, labels, sink, window, form
+        n, m = sum(q_lens), sum(k_lens)
+        self.q = randn((n, hq, d), seed)
+        if fused:
+            self.q = torch.cat([self.q, randn((n, 2 * hkv, d), seed + 5)], 1)[:, :hq]
+        self.k, self.v = randn((m, hkv, d), seed + 1, spread), randn((m, hkv, d), seed + 2, spread)
+        width = max(1, max(-(-x // page) for x in k_lens))
+        need = sum(-(-x // page) for x in k_lens)
+        order = np.random.default_rng(seed).permutation(need + 3)
+        table = np.full((len(k_lens), width), -7, dtype=np.int32)
+        at = 0
+        for b, x in enumerate(k_lens):
+            c = -(-x // page)
+            table[b, :c] = order[at:at + c]
+            at += c
+        self.c = aoh.PagedCache(need + 3, page, hq, hkv, d, sink, window, labels, form=form, max_seqs=len(q_lens))
+        self.c.pool.fill_(255)  # NaN wherever nothing is written
+        self.table, self.lens = ints(table), ints(k_lens)
+        if m:
+            self.c.append(self.k, self.v, self.lens, self.table, cu_rows=ints(sums(k_lens)))
+        self.c.check()
+        self.out = torch.full((n, hq, d), float("nan"), dtype=torch.bfloat16, device="cuda")
+
+    def attend(self, **kw):
+        self.c.attend(self.q, self.q_lens, self.lens, self.table, self.out, **kw)
+        self.c.check()
+        return self.out
+
+    def matches(self, what, sequences=None):
+        qs, ks = sums(self.q_lens), sums(self.k_lens)
+        q, out = f64(self.q), f64(self.out)
+        for b in range(len(self.q_lens)) if sequences is None else sequences:
+            if self.q_lens[b] == 0:
+                continue
+            rows, keys = slice(qs[b], qs[b + 1]), slice(ks[b], ks[b + 1])
+            k, v = held(self.k[keys], self.form), held(self.v[keys], self.form)
+            want = opaged.attend(q[rows], k, v, self.labels, self.sink, self.window)
+            mag = opaged.attend(q[rows], k, np.abs(v), self.labels, self.sink, self.window)
+            assert_matches(out[rows], want, f"{what}, sequence {b}", mag=mag, abs_bounds=False)
+
+
+CASES = [
+    # q_lens, k_lens, Hq, Hkv, d, labels, sink, window, page
+    ([1], [1], 2, 1, 64, [0], 0, 1, 16),
+    ([5], [5], 4, 4, 128, [0, 1, 0, 1], 0, 1, 64),
+    ([1, 128, 0, 129, 127, 300], [1, 128, 7, 129, 127, 300], 8, 2, 128, [0, 1], 4, 40, 32),
+    ([77, 1, 513, 64], [77, 900, 600, 64], 8, 2, 64, [1, 0], 0, 130, 16),
+    ([600, 257], [700, 258], 7, 1, 128, [1], 200, 30, 128),
+    ([1300], [1300], 14, 2, 128, [0, 1], 128, 256, 64),
+    ([90, 1, 200], [400, 1000, 200], 6, 2, 128, [0, 1], 16, 100, 16),
+    ([33, 5], [1290, 129], 16, 1, 64, [0], 0, 1, 32),
+    # fewer positions than rows, and none
+    ([300, 7, 130], [10, 0, 131], 4, 2, 128, [0, 1], 2, 3, 16),
+    ([9, 260], [0, 0], 4, 2, 64, [0, 1], 2, 3, 64),
+    # many sequences (lengths that travel by way of the device), and few rows of each
+    ([3 + 5 * (i % 7) for i in range(70)], [60 + 5 * (i % 7) for i in range(70)], 4, 2, 64, [0, 1], 8, 9, 16),
+    ([1 + i % 5 for i in range(90)], [1 + i % 5 + 37 * i for i in range(90)], 32, 8, 128, [0, 1] * 4, 20, 300, 64),
+    ([140 + 31 * (i % 5) for i in range(20)], [140 + 31 * (i % 5) + i for i in range(20)], 24, 8, 128, [0, 1] * 4, 8, 100, 32),
+    # few rows after long prefixes: shared by clusters
+    ([17, 3, 1], [3000, 2999, 1], 32, 8, 64, [0, 1] * 4, 10, 500, 64),
+    ([33, 20], [2500, 900], 7, 1, 128, [0], 0, 1, 16),
+    ([5, 100, 26], [2049, 10, 1500], 10, 2, 128, [0, 1], 100, 300, 128),
+    ([16, 9], [1900, 1281], 16, 1, 128, [0], 0, 1, 32),
+    ([1, 1, 1, 1], [5000, 100, 1, 640], 8, 1, 128, [0], 0, 1, 16),
+    ([3, 1], [9000, 257], 4, 1, 128, [0], 0, 1, 64),
+    ([100], [7003], 4, 2, 128, [0, 0], 0, 1, 16),
+    ([2, 11], [6300, 1], 16, 2, 64, [0, 1], 300, 3000, 16),
+    ([5], [4000], 2, 2, 64, [0, 1], 7, 90, 128),
+    ([300, 40], [3333, 2600], 3, 3, 128, [0, 1, 0], 0, 1000, 64),
+    ([311], [2900], 16, 4, 128, [0, 0, 1, 0], 5, 900, 32),
+    # a window that begins inside of the sinks' last tile, and behind a gap
+    ([70], [1111], 6, 2, 128, [1, 1], 128, 129, 16),
+    ([4], [2000], 40, 8, 64, [1] * 8, 130, 63, 16),
+    # several waves of items
+    ([1400, 900], [1700, 901], 16, 8, 64, [0, 1] * 4, 3, 700, 64),
+    ([2100], [2500], 32, 8, 128, [0, 1] * 4, 64, 600, 64),
+]
+
+
+@pytest.mark.parametrize("form", ["bf16", "e4m3"])
+@pytest.mark.parametrize("case", range(len(CASES)))
+def test_chunks(case, form):
+    c = Case(*CASES[case], form, seed=10 * case, fused=case % 2 == 1, spread=1.5 if case % 3 == 0 else 0.0)
+    # the host's idea of the lengths: right, none, too short, too long
+    hint = [c.k_lens, None, [x // 3 for x in c.k_lens], [x + 4000 for x in c.k_lens]][case % 4]
+    c.attend(k_lens=hint)
+    c.matches(f"chunks {case}")
+
+
+@pytest.mark.parametrize("form", ["bf16", "e4m3"])
+def test_many_items_in_several_launches(form):
+    c = Case([40] * 110, [50] * 110, 64, 64, 64, [0] * 64, 0, 1, 16, form)
+    c.attend()
+    c.matches("many items", [0, 48, 49, 50, 51, 99, 100, 101, 109])
+    assert torch.isfinite(c.out.float()).all()
+
+
+@pytest.mark.parametrize("form", ["bf16", "e4m3"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_as_a_single_token(form, d):
+    """One row a sequence is what the decode gives."""
+    lens = [1, 700, 33, 2048, 129]
+    c = Case([1] * 5, lens, 8, 2, d, [0, 1], 10, 100, 16, form, seed=3)
+    c.attend(k_lens=lens)
+    c.matches("single tokens")
+    other = torch.empty_like(c.out)
+    c.c.decode(c.q, c.lens, c.table, other)
+    c.c.check()
+    assert (f64(other) - f64(c.out)).max() < 0.02
+
+
+@pytest.mark.parametrize("form", ["bf16", "e4m3"])
+def test_neighbours_and_free_pages_are_not_seen(form):
+    """NaN in other sequences' pages, in free ones and behind a sequence's end changes nothing."""
+    c = Case([70, 200, 33], [75, 300, 633], 8, 2, 128, [0, 1], 4, 50, 64, form, seed=5)
+    first = c.attend(k_lens=c.k_lens).clone()
+    k = torch.full((300, 2, 128), float("nan"), dtype=torch.bfloat16, device="cuda")
+    c.c.append(k, k, ints([0, 300, 0]), c.table, cu_rows=ints([0, 0, 300, 300]))
+    c.out.fill_(float("nan"))
+    c.attend(k_lens=c.k_lens)
+    assert torch.equal(c.out[:70], first[:70]) and torch.equal(c.out[270:], first[270:])
+
+
+SPOILT = [CASES[i] for i in (2, 3, 5, 6, 13, 14, 17, 20, 22, 24)]
+
+
+@pytest.mark.parametrize("form", ["bf16", "e4m3"])
+@pytest.mark.parametrize("case", range(len(SPOILT)))
+def test_spoilt_keys_reach_the_rows_that_see_them(case, form):
+    """K and V of some positions NaN (or infinite, which 8 bits hold as NaN): the rows that see them
+    are NaN, the others as they would be without."""
+    c = Case(*SPOILT[case], form, seed=7 * case)
+    clean = c.attend(k_lens=c.k_lens).clone()
+    g = np.random.default_rng(case)
+    ks, bad = sums(c.k_lens), []
+    k, v = c.k.clone(), c.v.clone()
+    for b, m in enumerate(c.k_lens):
+        at = sorted(set(g.integers(max(0, m - c.q_lens[b] - 20), m, 2))) if m else []
+        bad.append(at)
+        for j in at:
+            k[ks[b] + j] = float("nan")
+            v[ks[b] + j] = float("inf") if case % 2 else float("nan")
+    c.c.append(k, v, c.lens, c.table, cu_rows=ints(ks))
+    c.out.fill_(0)
+    out = f64(c.attend(k_lens=c.k_lens))
+    qs, clean = sums(c.q_lens), f64(clean)
+    hq, hkv = c.q.shape[1], len(c.labels)
+    for b, (n, m) in enumerate(zip(c.q_lens, c.k_lens)):
+        pos = np.arange(m - n, m)[:, None]
+        j = np.array(bad[b], dtype=int)[None, :]
+        for h in range(hq):
+            see = j <= pos
+            if c.labels[h // (hq // hkv)]:
+                see &= (j < c.sink) | (pos - j < c.window)
+            hit = see.any(1)
+            rows = np.arange(qs[b], qs[b + 1])
+            assert np.isnan(out[rows[hit], h]).all(), (b, h)
+            # (rows that are gone over again are summed in another order)
+            d = np.abs(out[rows[~hit], h] - clean[rows[~hit], h])
+            assert (d <= 2.0 ** -6 * np.abs(clean[rows[~hit], h]) + 0.02).all(), (b, h, d.max())
+
+
+@pytest.mark.parametrize("form", ["bf16", "e4m3"])
+def test_out_of_range(form):
+    """Pages and lengths out of range are reported; other sequences are right all the same."""
+    c = Case([20, 30], [150, 600], 8, 2, 128, [0, 1], 4, 50, 32, form, seed=2)
+    good = c.table.clone()
+    for page in (-1, c.c.n_pages, 2 ** 31 - 1):
+        c.table.copy_(good)
+        c.table[0, 3] = page
+        c.c.attend(c.q, c.q_lens, c.lens, c.table, c.out, k_lens=c.k_lens)
+        with pytest.raises(aoh.AohError, match="out of range"):
+            c.c.check()
+        c.matches(f"page {page}", [1])
+    c.table.copy_(good)
+    for n in (-5, good.shape[1] * 32 + 1, 2 ** 31 - 1):
+        c.lens.copy_(ints([n, 600]))
+        c.table[0, :] = 0  # (of a length past the table all of it is read)
+        c.c.attend(c.q, c.q_lens, c.lens, c.table, c.out, k_lens=c.k_lens)
+        with pytest.raises(aoh.AohError, match="out of range"):
+            c.c.check()
+        c.matches(f"length {n}", [1])
+        if n < 0:
+            assert (c.out[:20] == 0).all()
+
+
+def test_large_and_tiny_rows():
+    """8-bit rows of any size: the scores of K rows of 2^-60 to 2^6, V rows of 2^-70 to 2^90."""
+    for d in (64, 128):
+        c = Case([1, 40], [300, 700], 4, 2, d, [0, 1], 3, 90, 16, "e4m3", seed=d)
+        e = torch.linspace(-70, 90, c.v.shape[0], device="cuda")[torch.randperm(c.v.shape[0], device="cuda")]
+        c.v = (c.v.float() * torch.exp2(e.round()).view(-1, 1, 1)).bfloat16()
+        e = torch.linspace(-60, 6, c.k.shape[0], device="cuda")
+        c.k = (c.k.float() * torch.exp2(e.round()).view(-1, 1, 1)).bfloat16()
+        c.c.append(c.k, c.v, c.lens, c.table, cu_rows=ints(sums(c.k_lens)))
+        c.attend(k_lens=c.k_lens)
+        c.matches(f"d {d}")
+
+
+def test_captured_over_growing_lengths():
+    """A graph of append and attend reads lengths and table at replay: two calls of one handle, three
+    drafted tokens a step, a slot whose request ends."""
+    hq, hkv, d, page, form = 8, 2, 128, 16, "e4m3"
+    rope = aoh.Rope(d)
+    c = aoh.PagedCache(40, page, hq, hkv, d, 4, 40, [0, 1], form=form, max_seqs=2)
+    table, lens, cu = ints(np.arange(40).reshape(2, 20)), ints([0, 0]), ints([0, 3, 6])
+    q, k, v = randn((6, hq, d), 0), randn((6, hkv, d), 1), randn((6, hkv, d), 2)
+    turned, out = torch.empty_like(q), torch.empty_like(q)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        lens.add_(3)
+        c.append_rotated(rope, q, k, v, lens, table, turned, cu_rows=cu)
+        c.attend(turned, [3, 3], lens, table, out)
+    freqs = orot.frequencies(d, 1e4)
+    past = [[np.zeros((0, hkv, d))] * 2 for _ in range(2)]
+    for step in range(30):
+        for i, x in enumerate((q, k, v)):
+            x.copy_(randn(tuple(x.shape), 100 * step + i))
+        graph.replay()
+        assert lens.tolist() == [3 * step + 3] * 2
+        for b in range(2):
+            rows, pos = slice(3 * b, 3 * b + 3), np.arange(3 * step, 3 * step + 3)
+            kk = opaged.decode(*opaged.encode(orot.rotate(f64(k[rows]), pos, freqs)))
+            past[b] = [np.concatenate([past[b][0], kk]), np.concatenate([past[b][1], held(v[rows], form)])]
+            if step % 7 == 6:
+                want = opaged.attend(f64(turned[rows]), past[b][0], past[b][1], [0, 1], 4, 40)
+                mag = opaged.attend(f64(turned[rows]), past[b][0], np.abs(past[b][1]), [0, 1], 4, 40)
+                # a K number whose 32-bit rotation falls on the other side of a border of its codes is a step
+                # off, 2^-4 of its row's largest at most: rarely, and in one number of a row
+                assert_matches(f64(out[rows]), want, f"step {step}", mag=mag, abs_bounds=False)
+    c.check()
+    lens.fill_(-3)  # the next step's lengths are 0: slots without a request
+    c.attend(turned, [3, 3], ints([0, 0]), table, out)
+    c.check()
+    assert (out == 0).all()
+
+
+def test_on_another_stream():
+    c = Case([40, 3], [400, 1000], 8, 2, 64, [0, 1], 4, 50, 64, "bf16", seed=1)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    c.c.attend(c.q, c.q_lens, c.lens, c.table, c.out, stream=s)
+    s.synchronize()
+    c.matches("another stream")
+
+
+def test_same_results_again():
+    c = Case([40, 3, 300], [4000, 9000, 2500], 8, 2, 128, [0, 1], 4, 2000, 64, "e4m3", seed=1)
+    first = c.attend(k_lens=c.k_lens).clone()
+    for _ in range(5):
+        c.out.fill_(float("nan"))
+        assert torch.equal(c.attend(k_lens=c.k_lens), first)

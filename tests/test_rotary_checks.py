@@ -156,3 +156,23 @@ def test_library_refuses_on_the_host(lib):
     assert lib.aoh_rope_init(None, 0, 0, None) == 1
     assert lib.aoh_rope_init(None, 8, 0, ctypes.byref(wrong)) == 1
     assert lib.aoh_rope_init((ctypes.c_double * 8)(), 8, 2, ctypes.byref(wrong)) == 1
+
+
+def test_attend_tensors():
+    c = cache()
+    q, lens, table, out = bf(9, 8, 64), ints(3), ints(3, 9), bf(9, 8, 64)
+    f = c.attend
+    refused("^q has shape", f, bf(9, 2, 64), [3, 3, 3], lens, table, out)
+    refused("^out has shape", f, q, [3, 3, 3], lens, table, bf(8, 8, 64))
+    refused("one length for each", f, q, [3, 6], lens, table, out)
+    refused("one length for each", f, q, [3, 3, 3], lens, table, out, k_lens=[1])
+    refused("q_lens say 8", f, q, [3, 3, 2], lens, table, out)
+    refused("^lens has shape", f, q, [3, 3, 3], ints(2), table, out)
+    refused("^table has shape", f, bf(5, 8, 64), [1] * 5, ints(5), ints(5, 9), bf(5, 8, 64))
+    refused("^table must be", f, q, [3, 3, 3], lens, Cuda(torch.zeros(9, 3, dtype=torch.int32).t()), out)
+    refused("contiguous", f, q, [3, 3, 3], lens, table, Cuda(torch.zeros(9, 16, 64, dtype=torch.bfloat16)[:, :8]))
+
+
+def test_attend_without_a_handle(lib):
+    p, one = ctypes.c_void_p(1 << 20), (ctypes.c_int32 * 1)(1)
+    assert lib.aoh_paged_attend(None, p, 512, one, p, None, 1, p, 1, p, None) == 1

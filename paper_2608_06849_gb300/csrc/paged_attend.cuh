@@ -3,10 +3,9 @@
 // query heads of a KV head at some neighbouring tokens, so that a KV head's pages are read once for
 // all of them; the tokens' own keys lie in the pages already. Lengths and tables are read on the device.
 //
-// bf16 pages go to the shared tiles by TMA, page by page. Codes of 8 bits come as they lie into a
-// ring of units of 64 keys, from which four warps write bf16 tiles (code * 2^power is one exactly, so
-// that everything behind is the computation on bf16 pages). With few rows the second query tile's
-// place is part of the ring.
+// bf16 pages go to the shared tiles by TMA, page by page. Codes of 8 bits are loaded into registers by seven
+// more warps, which write bf16 tiles (code * 2^power is one exactly, so that everything behind is
+// the computation on bf16 pages).
 #pragma once
 
 #include "paged_rows.cuh"
@@ -46,52 +45,41 @@ struct CallOf<PagedArgs<F8>> {
   static constexpr bool kLaneRows = true;
   static constexpr bool kChained = true;
   static constexpr bool kPaged = true, kF8 = F8;
-  // 8 bits: producer and MMA issuer (and two warps that fill up their group), two groups of softmax
-  // and one that converts
+  // 8 bits: MMA issuer (warp 1) and three warps that convert, two groups of softmax, four more that convert
   static constexpr int kThreads = F8 ? 512 : pf::kThreads, kSoftmax = F8 ? 4 : 2;
 };
 
-// Q_A, Q_B, units of codes, K and V tiles, powers of the units, barriers.
+// bf16: a tile's pages in the lanes of the producer.
 template <int D>
-struct TcCfg<PagedArgs<true>, D> : PfCfg<D> {
+struct PageWalk<PagedArgs<false>, D> {
   using C = PfCfg<D>;
-  static constexpr int UNIT = 64 * D;                    // codes of 64 keys
-  static constexpr int UNITS = 4, LONE = C::QBYTES / UNIT;  // in the ring, and in Q_B's place
-  static constexpr int MOST = UNITS + LONE;
-  static constexpr int OFF_RAW = C::OFF_Q + 2 * C::QBYTES;
-  static constexpr int OFF_KV = OFF_RAW + UNITS * UNIT;
-  static constexpr int OFF_POW = OFF_KV + kNS * C::KVBYTES;
-  static constexpr int OFF_BAR = OFF_POW + MOST * 64;
-  static constexpr int OFF_RING = OFF_BAR + C::NBAR * 8 + 16;  // barriers of the ring, rows without data
-  static constexpr int SMEM = OFF_RING + MOST * (8 + 8 + 4) + 1024;
-  static_assert(SMEM <= 232448, "shared memory");
-};
-
-// A tile's pages in the lanes of the producer: `rows` of a page (all of it, or 64 of 128) at key
-// lane * rows of the tile.
-template <bool F8, int D>
-struct PageWalk<PagedArgs<F8>, D> {
-  using C = PfCfg<D>;
-  int lane, rows, page, row;  // page: the lane's, or -1: out of range; row: the first in the page
-  bool has;                   // whether the lane has a page with keys
+  int lane, rows, page;  // page: the lane's, at key lane * rows, or -1: out of range
+  int ahead;             // the entry of the tile after it, which is on its way meanwhile
+  bool has;              // whether the lane has a page with keys
   __device__ __forceinline__ PageWalk(const PagedAttendArgs& a, const PagedItem&, int lane_)
-      : lane(lane_), rows(min(a.pool.ps, F8 ? 64 : 128)), page(-1), row(0), has(false) {}
+      : lane(lane_), rows(a.pool.ps), page(-1), ahead(-1), has(false) {}
   __device__ __forceinline__ int key() const { return lane * rows; }
-  // visited tile i of the item
-  __device__ __forceinline__ void look(const PagedAttendArgs& a, const PagedItem& t, int i) {
-    const int pos = t.chunk_tile(i) * kBN + key();
-    has = key() < kBN && pos < t.klen;
-    row = pos & (a.pool.ps - 1);
-    page = -1;
-    if (!has) return;
-    page = __ldg(a.table + (size_t)t.b * a.table_stride + (pos >> a.pool.lg_ps));
-    if ((unsigned)page >= (unsigned)a.pool.n_pages) {
+  __device__ __forceinline__ bool position(const PagedItem& t, int i, int* pos) const {
+    *pos = t.chunk_tile(i) * kBN + key();
+    return key() < kBN && *pos < t.klen;
+  }
+  // visited tile i of the item, the first that is looked up or the one after the last that was
+  __device__ __forceinline__ void fetch(const PagedAttendArgs& a, const PagedItem& t, int i) {
+    int pos;
+    ahead = position(t, i, &pos) ? __ldg(a.table + (size_t)t.b * a.table_stride + (pos >> a.pool.lg_ps)) : -1;
+  }
+  __device__ __forceinline__ void look(const PagedAttendArgs& a, const PagedItem& t, int i, bool more) {
+    int pos;
+    has = position(t, i, &pos);
+    page = ahead;
+    if (more) fetch(a, t, i + 1);
+    if (has && (unsigned)page >= (unsigned)a.pool.n_pages) {
       page = -1;
       atomicOr(a.err, kErrPages);
     }
   }
-  // K (sel 0) or V of the tile: the pages that hold keys; the warp (bf16 pages)
-  __device__ __forceinline__ void load(const PagedArgs<F8>& a, const PagedItem& t, int sel, uint8_t* dst, uint64_t* bar) const {
+  // K (sel 0) or V of the tile: the pages that hold keys; the warp
+  __device__ __forceinline__ void load(const PagedArgs<false>& a, const PagedItem& t, int sel, uint8_t* dst, uint64_t* bar) const {
     const int n = __popc(__ballot_sync(0xffffffffu, has));
     if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)(n * rows) * (D * 2));
     __syncwarp();
@@ -105,92 +93,103 @@ struct PageWalk<PagedArgs<F8>, D> {
   }
 };
 
-// The ring of codes: unit n (of the n-th half of a K or V tile) in place n % count.
+// 8 bits: a warp's way through the groups of 16 rows of an item's K and V tiles, eight of a tile, every
+// kConvert-th its own. A group lies in one page. kAhead groups are in registers or on their way, the entry
+// of the table for the one behind them too.
 template <int D>
-struct RawRing<PagedArgs<true>, D> {
+struct CodeWalk<PagedArgs<true>, D> {
   using A = PagedArgs<true>;
-  using L = TcCfg<A, D>;
-  uint8_t* data;
-  int8_t* powers;  // [MOST][64]
-  uint64_t *full, *empty;
-  uint32_t* bad;  // [MOST]: groups of 16 rows whose page is out of range
-  int count;
-  __device__ __forceinline__ RawRing(uint8_t* smem, bool lone)
-      : data(smem + (lone ? L::OFF_Q + L::QBYTES : L::OFF_RAW)),
-        powers(reinterpret_cast<int8_t*>(smem + L::OFF_POW)),
-        full(reinterpret_cast<uint64_t*>(smem + L::OFF_RING)),
-        empty(full + L::MOST),
-        bad(reinterpret_cast<uint32_t*>(empty + L::MOST)),
-        count(lone ? L::MOST : L::UNITS) {}
-  __device__ __forceinline__ void init() {
-    for (int i = 0; i < L::MOST; ++i) {
-      mbar_init(&full[i], 1);
-      mbar_init(&empty[i], kConvert);
-    }
+  using C = PfCfg<D>;
+  static constexpr int kAhead = 3;
+  struct Group {
+    uint2 x[4][D / 64];  // 8 codes of every fourth row, in both boxes
+    int power;           // of row lane % 16
+    int rows;            // rows that hold keys (others are zeros)
+  };
+  Group group[kAhead];
+  int page;  // of the next group to be loaded
+  // Group n: K or V of visited tile first + n / 16, rows 16 (n % 8) on.
+  __device__ __forceinline__ static int position(const PagedItem& t, int first, int n) {
+    return t.chunk_tile(first + (n >> 4)) * kBN + (n & 7) * 16;
   }
-  // Unit n: half of K (sel 0) or V of the tile that `pages` looked up; the producer's warp.
-  __device__ __forceinline__ bool fill(const A& a, const PagedItem& t, const PageWalk<A, D>& pages, int n, int sel, int half,
-                                       int lane, volatile int* abort_flag) {
-    const int r = n % count;
-    if (n >= count && !__all_sync(0xffffffffu, wait_bar(&empty[r], ((n / count) & 1) ^ 1, a.err, abort_flag))) return false;
-    const bool mine = pages.has && (pages.key() >> 6) == half, good = mine && pages.page >= 0;
-    const int at = pages.key() & 63, rows = pages.rows;
-    const uint32_t groups = mine && !good ? ((1u << (rows >> 4)) - 1u) << (at >> 4) : 0u;
-    const uint32_t all_bad = __reduce_or_sync(0xffffffffu, groups);
-    const int loads = __popc(__ballot_sync(0xffffffffu, good));
-    if (lane == 0) {
-      bad[r] = all_bad;
-      mbar_arrive_expect_tx(&full[r], (uint32_t)(loads * rows) * (D + 1));
-    }
-    __syncwarp();
-    if (good) {
-      const size_t block = ((size_t)pages.page * 2 + sel) * a.pool.Hkv + t.kvh;
-      bulk_g2s(data + r * L::UNIT + at * D, static_cast<const uint8_t*>(a.pool.data) + ((block << a.pool.lg_ps) + pages.row) * D,
-               (uint32_t)(rows * D), &full[r]);
-      const size_t power = (((size_t)pages.page * a.pool.Hkv + t.kvh) * 2 + sel) << a.pool.lg_ps;
-      bulk_g2s(powers + r * 64 + at, a.pool.powers + power + pages.row, (uint32_t)rows, &full[r]);
-    }
-    __syncwarp();
-    return true;
+  __device__ __forceinline__ void look(const A& a, const PagedItem& t, int first, int n, int all) {
+    page = -1;
+    if (n >= all) return;
+    const int pos = position(t, first, n);
+    if (pos < t.klen) page = __ldg(a.table + (size_t)t.b * a.table_stride + (pos >> a.pool.lg_ps));
   }
-  // Every issued copy has landed.
-  __device__ __forceinline__ void drain(const A& a, int n, int lane) {
-    if (lane == 0)
-      for (int u = n > count ? n - count : 0; u < n; ++u) drain_wait(&full[u % count], (u / count) & 1, a.err);
-    __syncwarp();
-  }
-  // Unit n as bf16 rows 64 * half .. of a tile (zeros from row `valid` on): warp w of kConvert writes 16 rows, a
-  // lane 16 numbers at a time, as two 16-byte pieces, the lanes of the second box the other one first: the
-  // lanes that store at a time touch every bank once.
-  __device__ __forceinline__ bool convert(const A& a, int n, uint8_t* tile, int half, int valid, int w, int lane,
-                                          volatile int* abort_flag) {
-    constexpr int LPR = D / 16, STEP = 32 / LPR;
-    const int r = n % count;
-    if (!__all_sync(0xffffffffu, wait_bar(&full[r], (n / count) & 1, a.err, abort_flag))) return false;
-    const uint32_t lost = bad[r];
-    const int c = lane % LPR, flip = (c >> 2) & 1;
-    uint4 x[16 / STEP];
-    int e[16 / STEP];
+  // A lane 8 codes of a row at a time, 8 lanes a row of a box, so that the lanes that store a row
+  // of a tile touch every bank once.
+  __device__ __forceinline__ void load(const A& a, const PagedItem& t, int first, int n, int all, int lane, Group& g) {
+    g.rows = 0;
+    if (n >= all) return;
+    const int pos = position(t, first, n), sel = n >> 3 & 1, lg = a.pool.lg_ps;
+    if (pos >= t.klen) return;
+    if ((unsigned)page >= (unsigned)a.pool.n_pages) {
+      if (lane == 0) atomicOr(a.err, kErrPages);
+      return;
+    }
+    g.rows = t.klen - pos;
+    const int row = pos & (a.pool.ps - 1);
+    const uint8_t* from = static_cast<const uint8_t*>(a.pool.data) +
+                          (((((size_t)page * 2 + sel) * a.pool.Hkv + t.kvh) << lg) + row + (lane >> 3)) * D + (lane & 7) * 8;
 #pragma unroll
-    for (int i = 0; i < 16 / STEP; ++i) {
-      const int row = w * 16 + i * STEP + lane / LPR;
-      x[i] = lds128(data + r * L::UNIT + row * D + c * 16);
-      e[i] = powers[r * 64 + row];
-    }
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int i = 0; i < 16 / STEP; ++i) {
-      const int row = w * 16 + i * STEP + lane / LPR, at = half * 64 + row;
-      rows::Sixteen y = rows::decode(x[i], e[i]);
-      if (at >= valid || (lost >> (row >> 4) & 1)) y = rows::Sixteen{};
-      const uint4 p0 = make_uint4(y.w[0], y.w[1], y.w[2], y.w[3]), p1 = make_uint4(y.w[4], y.w[5], y.w[6], y.w[7]);
-      uint8_t* to = tile + (c >> 2) * L::BOX + at * 128;
-      const int piece = 2 * c & 7;
-      *reinterpret_cast<uint4*>(to + (((piece + flip) ^ (at & 7)) << 4)) = flip ? p1 : p0;
-      *reinterpret_cast<uint4*>(to + (((piece + 1 - flip) ^ (at & 7)) << 4)) = flip ? p0 : p1;
+      for (int k = 0; k < D / 64; ++k) g.x[i][k] = __ldg(reinterpret_cast<const uint2*>(from + i * 4 * D + k * 64));
+    g.power = __ldg(a.pool.powers + (((((size_t)page * a.pool.Hkv + t.kvh) * 2 + sel) << lg) + row + (lane & 15)));
+  }
+  // Group n as bf16 rows of its tile.
+  __device__ __forceinline__ static void put(const Group& g, int n, uint8_t* tile, int lane) {
+    const int sub = lane >> 3, c = lane & 7, row0 = (n & 7) * 16;
+    // row at of the tile: its pieces c ^ (at & 7)
+    uint8_t* to = tile + (row0 + sub) * 128 + ((c ^ sub) << 4);
+    const int other = (c ^ sub ^ 4) * 16 - (c ^ sub) * 16;  // rows 4 on
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float scale = __uint_as_float((uint32_t)(127 + __shfl_sync(0xffffffffu, g.power, i * 4 + sub)) << 23);
+      const float2 f2 = make_float2(scale, scale);
+#pragma unroll
+      for (int k = 0; k < D / 64; ++k) {
+        uint32_t y[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const uint32_t word = u < 2 ? g.x[i][k].x : g.x[i][k].y, two = u & 1 ? word >> 16 : word & 0xffffu;
+          const float2 f = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3)));
+          const float2 z = __fmul2_rn(f, f2);
+          y[u] = float2_to_bf16x2(z.x, z.y);
+        }
+        if (g.rows < 16 && i * 4 + sub >= g.rows) y[0] = y[1] = y[2] = y[3] = 0;
+        *reinterpret_cast<uint4*>(to + i * 4 * 128 + (i & 1 ? other : 0) + k * C::BOX) = make_uint4(y[0], y[1], y[2], y[3]);
+      }
     }
-    __syncwarp();
-    if (lane == 0) mbar_arrive(&empty[r]);
-    return true;
+  }
+  // All groups of the warp, the w-th of kConvert, into the ring of tiles.
+  __device__ __forceinline__ void run(const A& a, const PagedItem& t, int first, int n_tiles, int w, uint8_t* ring,
+                                      uint64_t* kv_full, uint64_t* kv_empty, int lane, volatile int* abort_flag) {
+    const int all = 16 * n_tiles;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      look(a, t, first, w + k * kConvert, all);
+      load(a, t, first, w + k * kConvert, all, lane, group[k]);
+    }
+    look(a, t, first, w + kAhead * kConvert, all);
+    int n = w;
+    while (true) {
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        if (n >= all) return;
+        const int it = n >> 3, st = it % kNS;
+        if (it >= kNS && !__all_sync(0xffffffffu, wait_bar(&kv_empty[st], ((it / kNS) & 1) ^ 1, a.err, abort_flag))) return;
+        put(group[k], n, ring + st * C::KVBYTES, lane);
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&kv_full[st]);
+        load(a, t, first, n + kAhead * kConvert, all, lane, group[k]);
+        n += kConvert;
+        look(a, t, first, n + kAhead * kConvert, all);
+      }
+    }
   }
 };
 

@@ -42,7 +42,7 @@ cudaError_t launch(K kernel, int smem, int grid, int cluster, const A& a, const 
 template <class A, int D, int MODE, int CAP>
 cudaError_t launch_items(const A& a, const uint64_t* items, int n, int each, cudaStream_t s) {
   auto kernel = prefill_tc_kernel<A, D, MODE, CAP>;
-  constexpr int smem = TcCfg<A, D>::SMEM;
+  constexpr int smem = PfCfg<D>::SMEM;
   static std::atomic<uint64_t> done{0};
   const cudaError_t e = once_per_device(done, [&] {
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);

@@ -68,7 +68,7 @@ __device__ __forceinline__ bool empty_state(float m, float l) { return m == -INF
 template <class A, int D, int MODE, int CAP>
 __global__ void __launch_bounds__(CallOf<A>::kThreads, 1)
     prefill_tc_kernel(const __grid_constant__ A a, const __grid_constant__ WorkList<CAP> wl) {
-  using C = TcCfg<A, D>;
+  using C = PfCfg<D>;
   using Call = CallOf<A>;
   using SB = SBuf<A, D>;
   constexpr bool PAGED = Call::kPaged, F8 = Call::kF8;
@@ -114,12 +114,11 @@ __global__ void __launch_bounds__(CallOf<A>::kThreads, 1)
   const int t0 = rank * per;
   const int n_tiles = !half ? n_all : SPLIT ? max(0, min(per, n_all - t0)) : rank == 0 ? (n_all + 1) / 2 : n_all / 2;
   const bool lone = SPLIT && !t.has_row(1, 0);
-  RawRing<A, D> ring(smem, lone);
   PageWalk<A, D> pages(a, t, warp == 0 ? lane : -1);
   if (threadIdx.x == 0) {
-    mbar_init(q_full, lone && F8 ? 1 : 2);
+    mbar_init(q_full, 2);
     for (int s = 0; s < kNS; ++s) {
-      mbar_init(&kv_full[s], F8 ? kConvert : 1);
+      mbar_init(&kv_full[s], F8 ? 8 : 1);  // (eight groups of rows)
       mbar_init(&kv_empty[s], 1);
     }
     for (int i = 0; i < 4; ++i) {
@@ -132,20 +131,20 @@ __global__ void __launch_bounds__(CallOf<A>::kThreads, 1)
     mbar_init(&v_zeroed[0], 1);
     mbar_init(&v_zeroed[1], 1);
     *abort_flag = 0;
-    if constexpr (F8) ring.init();
     fence_mbar_init();
     fence_proxy_async_smem();
     if constexpr (Call::kChained) wait_to_start(a);
     // the first loads need no other warp
     load_q<D>(a, t, 0, sQ, q_full);
-    if (!(lone && F8)) load_q<D>(a, t, 1, sQ + C::QBYTES, q_full);  // (its place is the ring's)
+    load_q<D>(a, t, 1, sQ + C::QBYTES, q_full);
     if constexpr (!PAGED)
       if (n_tiles > 0) load_kv<D>(a, t, t0, 0, sKV, &kv_full[0]);
   }
   if constexpr (PAGED && !F8) {
     if (warp == 0 && n_tiles > 0) {
       __syncwarp();
-      pages.look(a, t, t0);
+      pages.fetch(a, t, t0);
+      pages.look(a, t, t0, n_tiles > 1);
       pages.load(a, t, 0, sKV, &kv_full[0]);
     }
   }
@@ -169,34 +168,16 @@ __global__ void __launch_bounds__(CallOf<A>::kThreads, 1)
       asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
       __syncthreads();
     }
-    if (F8 && (warp == 0 || (warp > 1 && warp < S0) || warp >= S0 + 8)) {
+    if (F8 && warp != 1) {
       if constexpr (F8) {
+        // ---------------------------------------------------------- codes to bf16 tiles
+        CodeWalk<A, D> walk;
+        walk.run(a, t, t0, n_tiles, warp == 0 ? 0 : warp < S0 ? warp - 1 : warp - (S0 + 8) + S0 - 1, sKV, kv_full, kv_empty,
+                 lane, abort_flag);
         if (warp == 0) {
-          // -------------------------------------------------------- producer of codes
-          int n_units = 0;
-          bool ok = true;
-          for (int jj = 0; jj < n_tiles && ok; ++jj) {
-            pages.look(a, t, t0 + jj);
-            for (int u = 0; u < 4 && ok; ++u, ++n_units) ok = ring.fill(a, t, pages, n_units, u >> 1, u & 1, lane, abort_flag);
-          }
-          // every issued copy lands before the CTA can exit
           if (lane == 0) drain_wait(q_full, 0, a.err);
-          ring.drain(a, n_units, lane);
-        } else if (warp >= S0 + 8) {
-          // -------------------------------------------------------- codes to bf16 tiles
-          bool ok = true;
-          for (int it = 0; it < 2 * n_tiles && ok; ++it) {
-            const int st = it % kNS, valid = t.valid(g, t0 + (it >> 1));
-            if (it >= kNS) ok = __all_sync(0xffffffffu, wait_bar(&kv_empty[st], ((it / kNS) & 1) ^ 1, a.err, abort_flag));
-            for (int u = 0; u < 2 && ok; ++u)
-              ok = ring.convert(a, 2 * it + u, sKV + st * C::KVBYTES, u, valid, warp - (S0 + 8), lane, abort_flag);
-            if (!ok) break;
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&kv_full[st]);
-          }
+          __syncwarp();
         }
-        // (two warps fill up the producer's warpgroup)
       }
     } else if (warp == 0) {
       // ------------------------------------------------------------ producer
@@ -208,12 +189,12 @@ __global__ void __launch_bounds__(CallOf<A>::kThreads, 1)
       int issued = min(n_tiles, 1), n_partial = 0;  // the first K tile is on its way
       bool ok = true;
       for (int jj = 0; jj < n_tiles && ok; ++jj) {
-        if constexpr (PAGED)
-          if (jj > 0) pages.look(a, t, t0 + jj);
+        if constexpr (PAGED && !F8)
+          if (jj > 0) pages.look(a, t, t0 + jj, jj + 1 < n_tiles);
         for (int sel = 0; sel < 2; ++sel) {
           const int it = 2 * jj + sel;
           const int st = it % kNS;
-          if constexpr (PAGED) {
+          if constexpr (PAGED && !F8) {
             if (it >= kNS) ok = __all_sync(0xffffffffu, wait_bar(&kv_empty[st], ((it / kNS) & 1) ^ 1, a.err, abort_flag));
             if (ok && it > 0) {
               pages.load(a, t, sel, sKV + st * C::KVBYTES, &kv_full[st]);

@@ -41,22 +41,15 @@ struct PfCfg {
   static_assert(128 * (D * 4 + 8) <= OFF_BAR - QBYTES, "receive buffer of the split and its output rows");
 };
 
-// What prefill_tc_kernel's shared memory holds: the parts above, or, for calls whose K and V need
-// more of it, a layout of the call's own.
-template <class A, int D>
-struct TcCfg : PfCfg<D> {};
-// Calls over pages alone (paged_attend.cuh): the walk through a sequence's pages, and the ring of
-// 8-bit codes.
+// Calls over pages alone (paged_attend.cuh): the walks through a sequence's pages of bf16, and of 8 bits.
 template <class A, int D>
 struct PageWalk {
   template <class T>
   __device__ __forceinline__ PageWalk(const A&, const T&, int) {}
 };
 template <class A, int D>
-struct RawRing {
-  __device__ __forceinline__ RawRing(uint8_t*, bool) {}
-};
-constexpr int kConvert = 4;  // warps that turn codes into bf16
+struct CodeWalk {};
+constexpr int kConvert = 7;  // warps that turn codes into bf16
 // Registers a thread that such a kernel is launched with, and what its softmax warps and the others then
 // have: 256 threads each.
 constexpr int kExchanged = 128, kSoftmaxRegs = 168, kOtherRegs = 88;

@@ -200,14 +200,35 @@ struct PagePool {
   int Hkv, D;
 };
 
+// Sequences whose 8-bit pages are first written out as bf16 ones (launch_paged_expand): those of the
+// i-th sequence with rows are pages first[i] .. first[i + 1] - 1 of the written ones, 128 tokens each.
+struct Expanded {
+  static constexpr int kMost = 64;
+  int n;  // 0: none
+  int first[kMost + 1];
+};
+
 // Attention of chunks over a paged cache: folded items (seqs: {first query row, rows, the
 // sequence's number, -}) whose keys are those of the pages.
 struct PagedAttendArgs : FoldedArgs {
   CUtensorMap pages;  // the pool as [page, K or V, head][row][D] (bf16 pages)
   PagePool pool;
   const int32_t* lens;   // device: tokens of each sequence
-  const int32_t* table;  // device [n_seqs][table_stride]
+  const int32_t* table;  // device [n_seqs][table_stride]; null: the pages of `expanded`
   int table_stride;
+  int holds;          // tokens that a row of the caller's table holds
+  Expanded expanded;  // with a table: sequences that fit there are left out
+};
+
+struct PagedExpandArgs {
+  PagePool from, to;
+  CacheGeom geom;
+  PackedSeqs seqs;  // as PagedAttendArgs has them, by value
+  Expanded expanded;
+  const int32_t* lens;
+  const int32_t* table;
+  int table_stride, holds;
+  uint32_t* err;
 };
 
 // Rows of a call in a paged cache: sequence b's rows are cu[b] .. cu[b + 1] - 1 (cu
@@ -354,6 +375,7 @@ cudaError_t launch_prefill_folded(const FoldedArgs& a, const std::vector<uint64_
                                   int num_sms, cudaStream_t s);
 // Chunks over pages, as launch_prefill_folded takes its items.
 cudaError_t launch_paged_attend(const PagedAttendArgs& a, const std::vector<uint64_t>& items, int split, cudaStream_t s);
+cudaError_t launch_paged_expand(const PagedExpandArgs& a, cudaStream_t s);
 cudaError_t launch_paged_append(const PagedAppendArgs& a, int num_sms, cudaStream_t s);
 cudaError_t launch_paged_read(const PagedReadArgs& a, int num_sms, cudaStream_t s);
 cudaError_t launch_rotate(const RotateArgs& a, int d_head, int num_sms, cudaStream_t s);

@@ -25,6 +25,7 @@ struct aoh_paged {
   uint32_t* d_counters = nullptr;  // decode: arrivals, zero between calls
   float* d_states = nullptr;       // decode: states of items that CTAs share
   CUtensorMap pages;               // of the pool, which does not move
+  cudaMemPool_t expand_pool = nullptr;  // pages written out as bf16, from call to call
 };
 
 namespace {
@@ -167,6 +168,59 @@ cudaError_t sm_count(int* n) {
   e = cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev);
   if (e == cudaSuccess && dev < 64) known[dev].store(*n, std::memory_order_relaxed);
   return e;
+}
+
+// Device memory of a call that is not captured, ordered on its stream; null if there is none to be had. The
+// handle's own pool keeps it from call to call.
+void* expand_memory(aoh_paged* h, size_t bytes, cudaStream_t s) {
+  cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+  void* p = nullptr;
+  if (cudaStreamIsCapturing(s, &capture) != cudaSuccess || capture != cudaStreamCaptureStatusNone) {
+    cudaGetLastError();
+    return nullptr;
+  }
+  if (!h->expand_pool) {
+    cudaMemPoolProps props;
+    memset(&props, 0, sizeof(props));
+    props.allocType = cudaMemAllocationTypePinned;
+    props.location.type = cudaMemLocationTypeDevice;
+    props.location.id = h->device;
+    uint64_t keep = UINT64_MAX;
+    if (cudaMemPoolCreate(&h->expand_pool, &props) != cudaSuccess) {
+      h->expand_pool = nullptr;
+      cudaGetLastError();
+      return nullptr;
+    }
+    cudaMemPoolSetAttribute(h->expand_pool, cudaMemPoolAttrReleaseThreshold, &keep);
+  }
+  if (cudaMallocFromPoolAsync(&p, bytes, h->expand_pool, s) != cudaSuccess) {
+    cudaGetLastError();
+    return nullptr;
+  }
+  return p;
+}
+
+// Which 8-bit pages of a call to write out as bf16 ones first: none, or those of all its sequences (seqs: as
+// the plan takes them), where its items visit the same tiles often enough. work: tiles that they visit in all.
+// An item's visit costs an SM 1.1 us more with codes (d_head 128; 2,824 us of 8,192 rows after 16,384 of
+// 32/8 heads, 1,626 over bf16 pages), a tile's writing 98 KB of traffic, and the two launches some 8 us.
+bool expand_plan(const aoh_paged* h, const std::vector<int4>& seqs, long long work, Expanded* x) {
+  x->n = 0;
+  if (h->cfg.form != AOH_PAGES_E4M3 || seqs.size() > (size_t)Expanded::kMost) return false;
+  const CacheGeom& g = h->geom;
+  long long pages = 0, tiles = 0;
+  for (size_t i = 0; i < seqs.size(); ++i) {
+    const int keys = seqs[i].w, all = (int)(((long long)keys + 127) / 128);
+    x->first[i] = (int)pages;
+    pages += all;
+    const long long seen = (long long)g.S + g.W + seqs[i].y + 256;
+    tiles += (long long)g.n_r * all + (long long)g.n_s * std::min<long long>(all, seen / 128);
+  }
+  x->first[seqs.size()] = (int)pages;
+  const double visit = 7.2 * g.D / 128, write = 16.4 * g.D / 128;
+  if (pages == 0 || pages * 2 * g.Hkv * 128 * g.D * 2 > (4ll << 30) || work * visit < tiles * write * 1.2 + 8000) return false;
+  x->n = (int)seqs.size();
+  return true;
 }
 
 aoh_status check_cu(const int32_t* cu, int32_t n_seqs, int32_t n_rows) {
@@ -584,6 +638,7 @@ aoh_status aoh_paged_attend(aoh_paged* cache, const void* q, int64_t q_stride, c
   a.lens = lens;
   a.table = table;
   a.table_stride = table_stride;
+  a.holds = (int)holds;
   if (!make_rows_map(&a.tq, q, 1, n_q, c.n_q_heads, c.d_head, q_stride, a.span, a.geom.G))
     return fail(AOH_ERR_CUDA, "cuTensorMapEncodeTiled failed for q");
   cudaStream_t s = (cudaStream_t)stream;
@@ -599,7 +654,50 @@ aoh_status aoh_paged_attend(aoh_paged* cache, const void* q, int64_t q_stride, c
   bool lone = true;
   for (const int4& b : seqs) lone = lone && b.y <= a.span;
   const int split = folded_split(costs, lone, decode_tc_max_clusters, cache->num_sms);
-  const cudaError_t e = launch_paged_attend(a, items, split, s);
+  long long work = 0;
+  for (int cost : costs) work += cost;
+  cudaError_t e = cudaSuccess;
+  Expanded expanded;
+  void* written = nullptr;
+  if (expand_plan(cache, planned, work, &expanded)) {
+    const size_t pages = (size_t)expanded.first[expanded.n];
+    written = expand_memory(cache, pages * 2 * c.n_kv_heads * 128 * c.d_head * 2, s);
+  }
+  bool covered = false;  // whether all sequences fit there, whatever their lengths
+  if (written) {
+    PagedAttendArgs w = a;
+    w.expanded = expanded;
+    w.table = nullptr;
+    w.pool.data = written;
+    w.pool.powers = nullptr;
+    w.pool.n_pages = expanded.first[expanded.n];
+    w.pool.ps = 128;
+    w.pool.lg_ps = 7;
+    w.pool.form = AOH_PAGES_BF16;
+    PagedExpandArgs x;
+    memset(&x, 0, sizeof(x));
+    x.from = cache->pool;
+    x.to = w.pool;
+    x.geom = cache->geom;
+    std::copy(seqs.begin(), seqs.end(), x.seqs.by_value);
+    x.expanded = expanded;
+    x.lens = lens;
+    x.table = table;
+    x.table_stride = table_stride;
+    x.holds = a.holds;
+    x.err = cache->d_err;
+    covered = true;
+    for (int i = 0; i < expanded.n; ++i) covered = covered && (expanded.first[i + 1] - expanded.first[i]) * 128ll >= holds;
+    if (!make_pages_map(&w.pages, w.pool)) e = cudaErrorInvalidValue;
+    if (e == cudaSuccess) e = launch_paged_expand(x, s);
+    if (e == cudaSuccess) e = launch_paged_attend(w, items, split, s);
+    a.expanded = expanded;
+  }
+  if (e == cudaSuccess && !covered) e = launch_paged_attend(a, items, split, s);
+  if (written) {
+    const cudaError_t f = cudaFreeAsync(written, s);
+    if (e == cudaSuccess) e = f;
+  }
   return e == cudaSuccess ? AOH_OK : cuda_fail(e, "paged attention launch");
 } catch (const std::exception& x) {
   return fail(AOH_ERR_CUDA, "paged attention: %s", x.what());
@@ -623,6 +721,7 @@ aoh_status aoh_paged_check(aoh_paged* cache, void* stream) {
 
 void aoh_paged_destroy(aoh_paged* cache) {
   if (!cache) return;
+  if (cache->expand_pool) cudaMemPoolDestroy(cache->expand_pool);
   if (cache->meta) cudaFree(cache->meta);
   delete cache;
 }

@@ -5,7 +5,9 @@
 //
 // bf16 pages go to the shared tiles by TMA, page by page. Codes of 8 bits are loaded into registers by seven
 // more warps, which write bf16 tiles (code * 2^power is one exactly, so that everything behind is
-// the computation on bf16 pages).
+// the computation on bf16 pages). That takes an item as many instructions as its softmax: where several
+// items visit the same tiles, paged_api.cu has them written out as bf16 pages once, for the bf16 kernel;
+// sequences that prove longer than the host took them to be are then left to this one.
 #pragma once
 
 #include "paged_rows.cuh"
@@ -20,18 +22,28 @@ struct PagedArgs : PagedAttendArgs {};
 
 // The tokens of sequence b, within what its table holds.
 __device__ __forceinline__ int attend_len(const PagedAttendArgs& a, int b) {
-  const int n = __ldcg(a.lens + b), most = a.table_stride << a.pool.lg_ps;
-  if (n >= 0 && n <= most) return n;
+  const int n = __ldcg(a.lens + b);
+  if (n >= 0 && n <= a.holds) return n;
   if (threadIdx.x == 0) atomicOr(a.err, kErrPages);
-  return n < 0 ? 0 : most;
+  return n < 0 ? 0 : a.holds;
 }
 
 struct PagedItem : FoldedItem {
-  int b;
+  int index, b;  // among the sequences with rows, and the sequence's number
   __device__ __forceinline__ PagedItem(const PagedAttendArgs& a, uint64_t code)
       : PagedItem(a, code, a.seqs.of((int)(code >> 34))) {}
   __device__ __forceinline__ PagedItem(const PagedAttendArgs& a, uint64_t code, const int4& s)
-      : FoldedItem(a, code, make_int4(s.x, s.y, 0, attend_len(a, s.z))), b(s.z) {}
+      : FoldedItem(a, code, make_int4(s.x, s.y, 0, attend_len(a, s.z))), index((int)(code >> 34)), b(s.z) {}
+  // whether another kernel of the call computes it
+  __device__ __forceinline__ bool elsewhere(const PagedAttendArgs& a) const {
+    if (a.expanded.n == 0) return false;
+    return (klen <= (a.expanded.first[index + 1] - a.expanded.first[index]) * kBN) == (a.table != nullptr);
+  }
+  // the page with position pos
+  __device__ __forceinline__ int page_of(const PagedAttendArgs& a, int pos) const {
+    const int slot = pos >> a.pool.lg_ps;
+    return a.table ? __ldg(a.table + (size_t)b * a.table_stride + slot) : a.expanded.first[index] + slot;
+  }
 };
 
 template <bool F8>
@@ -66,7 +78,7 @@ struct PageWalk<PagedArgs<false>, D> {
   // visited tile i of the item, the first that is looked up or the one after the last that was
   __device__ __forceinline__ void fetch(const PagedAttendArgs& a, const PagedItem& t, int i) {
     int pos;
-    ahead = position(t, i, &pos) ? __ldg(a.table + (size_t)t.b * a.table_stride + (pos >> a.pool.lg_ps)) : -1;
+    ahead = position(t, i, &pos) ? t.page_of(a, pos) : -1;
   }
   __device__ __forceinline__ void look(const PagedAttendArgs& a, const PagedItem& t, int i, bool more) {
     int pos;
@@ -116,7 +128,7 @@ struct CodeWalk<PagedArgs<true>, D> {
     page = -1;
     if (n >= all) return;
     const int pos = position(t, first, n);
-    if (pos < t.klen) page = __ldg(a.table + (size_t)t.b * a.table_stride + (pos >> a.pool.lg_ps));
+    if (pos < t.klen) page = t.page_of(a, pos);
   }
   // A lane 8 codes of a row at a time, 8 lanes a row of a box, so that the lanes that store a row
   // of a tile touch every bank once.
@@ -197,7 +209,7 @@ struct CodeWalk<PagedArgs<true>, D> {
 template <int D>
 __device__ __forceinline__ void load_key(const PagedAttendArgs& a, const PagedItem& t, int j, int sel, int lane,
                                          float (&to)[D / 32]) {
-  const int page = __ldg(a.table + (size_t)t.b * a.table_stride + (j >> a.pool.lg_ps)), row = j & (a.pool.ps - 1);
+  const int page = t.page_of(a, j), row = j & (a.pool.ps - 1);
   if ((unsigned)page >= (unsigned)a.pool.n_pages) {
 #pragma unroll
     for (int n = 0; n < D / 32; ++n) to[n] = 0.f;

@@ -224,6 +224,53 @@ __global__ void __launch_bounds__(kThreads, 4) read_kernel(const __grid_constant
   }
 }
 
+// 8-bit pages written out as bf16 ones of 128 tokens, for an attention whose items visit them several
+// times: a block one of those pages of one head, K and V. Only what the call's rows may see: of streaming
+// heads the sinks and the first row's window on.
+template <int D>
+__global__ void __launch_bounds__(kThreads, 4) expand_kernel(const __grid_constant__ PagedExpandArgs a) {
+  constexpr int LPR = D / 16, ROWS = kThreads / LPR, U = 128 / ROWS;
+  const int page_to = blockIdx.x, h = blockIdx.y, lane = threadIdx.x & 31;
+  // the sequence: the last one that begins at or before the page
+  int i = __popc(__ballot_sync(0xffffffffu, lane < a.expanded.n && a.expanded.first[lane] <= page_to));
+  if (a.expanded.n > 32) i += __popc(__ballot_sync(0xffffffffu, lane + 32 < a.expanded.n && a.expanded.first[lane + 32] <= page_to));
+  --i;
+  after_the_last_kernel();
+  const int4 seq = a.seqs.by_value[i];
+  const int b = seq.z, read = __ldcg(a.lens + b), len = min(max(read, 0), a.holds);
+  const int tile = page_to - a.expanded.first[i], p0 = tile * 128;
+  // one that proves longer than its pages here is not read from them
+  if (p0 >= len || len > (a.expanded.first[i + 1] - a.expanded.first[i]) * 128) return;
+  if (a.geom.kind[h] && p0 >= a.geom.S && p0 + 128 <= a.geom.wstart(len - seq.y)) return;
+  const int r0 = threadIdx.x / LPR, ch = threadIdx.x % LPR, lg = a.from.lg_ps;
+#pragma unroll
+  for (int sel = 0; sel < 2; ++sel) {
+    uint4 x[U];
+    int e[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int pos = p0 + r0 + u * ROWS;
+      x[u] = make_uint4(0, 0, 0, 0);
+      e[u] = 0;
+      if (pos >= len) continue;
+      const int page = __ldg(a.table + (size_t)b * a.table_stride + (pos >> lg)), row = pos & (a.from.ps - 1);
+      if ((unsigned)page >= (unsigned)a.from.n_pages) {
+        atomicOr(a.err, kErrPages);
+        continue;
+      }
+      x[u] = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(a.from.data) +
+                                                  (((((size_t)page * 2 + sel) * a.from.Hkv + h) << lg) + row) * D + ch * 16));
+      e[u] = __ldg(a.from.powers + ((((size_t)page * a.from.Hkv + h) * 2 + sel) << lg) + row);
+    }
+    __nv_bfloat16* to = static_cast<__nv_bfloat16*>(a.to.data) + (((size_t)page_to * 2 + sel) * a.to.Hkv + h) * 128 * D + ch * 16;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int row = r0 + u * ROWS;
+      if (p0 + row < len) store16<true>(to + (size_t)row * D, decode(x[u], e[u]));
+    }
+  }
+}
+
 // Rows of a block: the call's rows on four blocks an SM (which run at once), up to 16, or, of
 // few heads, to as many as its threads have on their way at once (written and read, 4 x
 // 2,090-10,231 rows of 2 heads of 64 16.4 -> 12.9 us, 3 x 3,000-9,000 of one of 128 11.8 -> 10.4; 8
@@ -269,6 +316,19 @@ cudaError_t launch_paged_append(const PagedAppendArgs& a, int num_sms, cudaStrea
 cudaError_t launch_paged_read(const PagedReadArgs& a, int num_sms, cudaStream_t s) {
   if (a.pool.D == 128) return a.pool.form ? read<128, true>(a, num_sms, s) : read<128, false>(a, num_sms, s);
   return a.pool.form ? read<64, true>(a, num_sms, s) : read<64, false>(a, num_sms, s);
+}
+
+cudaError_t launch_paged_expand(const PagedExpandArgs& a, cudaStream_t s) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)a.expanded.first[a.expanded.n], (unsigned)a.from.Hkv);
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, a.from.D == 128 ? expand_kernel<128> : expand_kernel<64>, a);
 }
 
 }  // namespace aoh

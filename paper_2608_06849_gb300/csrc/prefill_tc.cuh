@@ -94,11 +94,13 @@ __global__ void __launch_bounds__(CallOf<A>::kThreads, 1)
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   // the append may start once the last CTAs of this grid run (append.cu)
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if constexpr (!PAGED) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if constexpr (Call::kChained) {
     if (threadIdx.x == 0) prefetch_maps(a);
     if (PAGED || a.seqs.table != nullptr) wait_to_start(a);  // the item is read from device memory
   }
+  // (a launch of the same call that follows finds what this one has waited for)
+  if constexpr (PAGED) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   constexpr bool PAIRS = MODE == kPairs, SPLIT = MODE == kSplit;
   const int ctas = SPLIT ? (int)cluster_ctas() : 2;
   const int entry = SPLIT ? (int)blockIdx.x / ctas : blockIdx.x;
@@ -106,6 +108,12 @@ __global__ void __launch_bounds__(CallOf<A>::kThreads, 1)
   if (PAIRS && code == kPrefillNone) return;
   const bool half = SPLIT || (PAIRS && code >= kPrefillHalf);  // alike in all CTAs of a cluster
   const typename Call::ItemT t(a, code & ~kPrefillHalf);
+  if constexpr (PAGED) {
+    if (t.elsewhere(a)) {  // alike in all CTAs of a cluster
+      wait_to_end(a);
+      return;
+    }
+  }
   const CacheGeom& g = a.geom;
   const int n_all = t.tiles();
   // this CTA visits tiles t0 .. t0 + n_tiles - 1 of the item's n_all

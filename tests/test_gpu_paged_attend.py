@@ -297,3 +297,69 @@ def test_same_results_again():
     for _ in range(5):
         c.out.fill_(float("nan"))
         assert torch.equal(c.attend(k_lens=c.k_lens), first)
+
+
+WRITTEN_OUT = [
+    # calls whose items visit the same tiles often: 8-bit pages are written out as bf16 ones first
+    ([1500], [4100], 16, 4, 128, [0, 1, 0, 0], 20, 700, 16),
+    ([900, 1, 2000], [900, 700, 2100], 16, 2, 64, [0, 1], 130, 500, 64),
+    ([700, 650, 800], [5000, 660, 2500], 32, 8, 128, [0, 1] * 4, 64, 512, 128),
+]
+
+
+@pytest.mark.parametrize("case", range(len(WRITTEN_OUT)))
+def test_pages_written_out_first(case):
+    """The outputs are those of the kernel that decodes them itself (a captured call takes no memory, so it
+    is that one), bit by bit, and right for whatever lengths the host takes the sequences to have."""
+    c = Case(*WRITTEN_OUT[case], "e4m3", seed=50 + case, fused=True, spread=1.0)
+    first = c.attend(k_lens=c.k_lens).clone()
+    c.matches("written out")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.c.attend(c.q, c.q_lens, c.lens, c.table, c.out, k_lens=c.k_lens)
+    c.out.fill_(float("nan"))
+    graph.replay()
+    c.c.check()
+    assert torch.equal(c.out, first)
+    for hint in ([n // 2 for n in c.k_lens], [c.k_lens[0] // 3] + c.k_lens[1:], [n + 1000 for n in c.k_lens], None,
+                 [0] + c.k_lens[1:]):
+        c.out.fill_(float("nan"))
+        c.attend(k_lens=hint)
+        c.matches(f"hint {hint}")
+
+
+def test_bad_pages_written_out_first():
+    c = Case([900, 800], [2000, 3000], 16, 4, 128, [0, 1, 0, 0], 20, 700, 32, "e4m3", seed=2)
+    first = c.attend(k_lens=c.k_lens).clone()
+    good = c.table.clone()
+    for page in (-1, c.c.n_pages):
+        c.table.copy_(good)
+        c.table[0, 3] = page
+        c.c.attend(c.q, c.q_lens, c.lens, c.table, c.out, k_lens=c.k_lens)
+        with pytest.raises(aoh.AohError, match="out of range"):
+            c.c.check()
+        assert torch.equal(c.out[900:], first[900:])
+    # NaN where nothing is visible: behind a sequence's end, and between sinks and windows
+    c.table.copy_(good)
+    k, v = c.k.clone(), c.v.clone()
+    k[1000], v[1000] = float("nan"), float("nan")  # position 1000 of the first: before its rows, 1100 .. 1999
+    c.c.append(k, v, c.lens, c.table, cu_rows=ints(sums(c.k_lens)))
+    out = c.attend(k_lens=c.k_lens)
+    hidden = torch.zeros((900, 16), dtype=torch.bool, device="cuda")
+    hidden[600:, 4:8] = True  # KV head 1 streams: rows from position 1100 + 600 = 1700 on see 1001 on
+    assert out[:900][~hidden].isnan().all() and not out[:900][hidden].isnan().any()
+    assert torch.equal(out[900:], first[900:])
+
+
+def test_written_out_after_an_append_in_flight():
+    """An append and the attention that follow each other without a wait: the new rows are seen."""
+    c = Case([1200], [3000], 16, 4, 128, [0, 1, 0, 0], 20, 700, 32, "e4m3", seed=9)
+    for step in range(6):
+        c.k.copy_(randn(tuple(c.k.shape), 100 + step))
+        c.v.copy_(randn(tuple(c.v.shape), 200 + step))
+        torch.cuda.synchronize()
+        c.c.append(c.k, c.v, c.lens, c.table, cu_rows=ints(sums(c.k_lens)))
+        c.c.attend(c.q, c.q_lens, c.lens, c.table, c.out, k_lens=c.k_lens)
+        if step % 3 == 2:
+            c.matches(f"step {step}")
+    c.c.check()

@@ -464,8 +464,8 @@ typedef struct aoh_norms {
  * Norms and rotation of dense rows, e.g. before aoh_prefill, aoh_decode_step or
  * aoh_paged_prefill.
  *   q, k      rows of [n_q_heads][d_head], [n_kv_heads][d_head], q_stride and k_stride
- *             elements apart (multiples of 8: slices of a fused projection will do). 0 heads:
- *             no such rows (their pointers are not looked at)
+ *             elements apart (multiples of 8 below 2^31: slices of a fused projection will do). 0
+ *             heads: no such rows (their pointers are not looked at)
  *   norms     or NULL: none
  *   positions device int32 [n_rows], of any sign
  *   q_out, k_out  likewise rows, q_out_stride and k_out_stride apart; may be q and k
@@ -592,7 +592,8 @@ aoh_status aoh_paged_append(aoh_paged* cache, const void* k, const void* v, int6
  * a projection's rows q, k and v, writes q, normalised and rotated, to q_out, and k, likewise,
  * with v as it is, to the pages. 8-bit rows are encoded from the rotated numbers in 32 bits.
  *   q, q_out   rows of [n_q_heads][d_head], q_stride and q_out_stride elements apart; q_out may
- *              be q with the same stride, and must not overlap q, k or v otherwise
+ *              be q with the same stride, and must not overlap q, k or v otherwise. All strides
+ *              are below 2^31
  *   rope, norms  as for aoh_norm_rotate
  *   positions  device int32 [n_rows], or NULL: a row's place in its sequence
  *   others     as for aoh_paged_append

@@ -14,6 +14,7 @@ configuration; the handle-level functions (``aoh_prefill``,
 
 import array
 import ctypes
+import functools
 import os
 
 import torch
@@ -406,7 +407,7 @@ def aoh_paged_destroy(cache):
 # Grace core and the 13 arguments of a call 1 us: an append of four tensors through
 # layers of checks took 7.2 us, of which the library's call is 2.7 (5.3 so).
 
-_BF16, _I32 = torch.bfloat16, torch.int32
+_BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
 
 
 def _rows(t, name, heads, d):
@@ -472,25 +473,36 @@ class Rope:
 
 
 def _norm(w, name, d):
-    """Pointer and type number of norm weights [d] (None: no norm)."""
-    if w is None:
-        return None, None
+    """Pointer of norm weights [d]."""
     if w.shape != (d,):
         raise ValueError(f"{name} has shape {tuple(w.shape)}; expected [{d}]")
-    if w.dtype not in (_BF16, torch.float32) or not w.is_cuda or not w.is_contiguous():
+    if (w.dtype is not _BF16 and w.dtype is not _F32) or not w.is_cuda or not w.is_contiguous():
         raise ValueError(f"{name} must be a contiguous torch.bfloat16 or torch.float32 CUDA tensor")
-    return w.data_ptr(), 0 if w.dtype is _BF16 else 1
+    return w.data_ptr()
 
 
 def _norms(q_norm, k_norm, eps, d):
-    """The aoh_norms of both sides' weights, or None."""
+    """The aoh_norms of both sides' weights (None: no norm on that side), or None."""
     if q_norm is None and k_norm is None:
         return None
-    qp, qt = _norm(q_norm, "q_norm", d)
-    kp, kt = _norm(k_norm, "k_norm", d)
-    if qt is not None and kt is not None and qt != kt:
+    qp = None if q_norm is None else _norm(q_norm, "q_norm", d)
+    kp = None if k_norm is None else _norm(k_norm, "k_norm", d)
+    kind = (k_norm if q_norm is None else q_norm).dtype
+    if k_norm is not None and k_norm.dtype is not kind:
         raise ValueError(f"q_norm and k_norm must be of one type, not {q_norm.dtype} and {k_norm.dtype}")
-    return ctypes.byref(aoh_norms(qp, kp, kt if qt is None else qt, eps))
+    return ctypes.byref(aoh_norms(qp, kp, 0 if kind is _BF16 else 1, eps))
+
+
+def _side(x, out, name, n, d):
+    """Pointer, token stride and heads of n rows x, pointer and token stride of `out`."""
+    if x is None:
+        return None, 0, 0, None, 0
+    heads = x.shape[1] if len(x.shape) == 3 else 0
+    p, s, rows = _rows(x, name, heads, d)
+    op, os_, orows = _rows(out, name + "_out", heads, d)
+    if rows != n or orows != n:
+        raise ValueError(f"{name} and {name}_out hold {rows} and {orows} rows; expected {n}")
+    return p, s, heads, op, os_
 
 
 def aoh_norm_rotate(rope, q, k, positions, q_out, k_out, q_norm=None, k_norm=None, eps=1e-6, stream=None):
@@ -498,34 +510,30 @@ def aoh_norm_rotate(rope, q, k, positions, q_out, k_out, q_norm=None, k_norm=Non
     in one pass: q, q_out [rows, Hq, d], k, k_out [rows, Hkv, d] (bf16, with any distance between
     tokens; the outputs may be the inputs themselves; q and q_out, or k and k_out, may be None),
     positions int32 [rows], norm weights [d] in bf16 or fp32 (None: no norm on that side)."""
-    some = q if q is not None else k
+    some = k if q is None else q
     if some is None or (q is None) != (q_out is None) or (k is None) != (k_out is None):
         raise ValueError("q with q_out, or k with k_out, or both")
-    if some.dim() != 3:
-        raise ValueError(f"rows have shape {tuple(some.shape)}; expected [rows, heads, d]")
-    n, _, d = some.shape
-    side = []
-    for x, out, name in ((q, q_out, "q"), (k, k_out, "k")):
-        if x is None:
-            side.append((None, 0, 0, None, 0))
-            continue
-        heads = x.shape[1] if x.dim() == 3 else 0
-        p, s, rows = _rows(x, name, heads, d)
-        op, os_, orows = _rows(out, name + "_out", heads, d)
-        if rows != n or orows != n:
-            raise ValueError(f"{name} and {name}_out hold {rows} and {orows} rows; expected {n}")
-        side.append((p, s, heads, op, os_))
+    shape = some.shape
+    if len(shape) != 3:
+        raise ValueError(f"rows have shape {tuple(shape)}; expected [rows, heads, d]")
+    n, d = shape[0], shape[2]
+    qp, qs, hq, qo, qos = _side(q, q_out, "q", n, d)
+    kp, ks, hkv, ko, kos = _side(k, k_out, "k", n, d)
     norms = _norms(q_norm, k_norm, eps, d)
     pp = _ints(positions, "positions", n)
-    if torch.cuda.device_count() > 1:
+    if _several_devices():
         here = torch.cuda.current_device()
         for t in (q, k, positions, q_out, k_out, q_norm, k_norm):
             if t is not None and t.get_device() != here:
                 raise ValueError(f"a tensor is on cuda:{t.get_device()}, the current device is cuda:{here}")
-    (qp, qs, hq, qo, qos), (kp, ks, hkv, ko, kos) = side
     st = load().aoh_norm_rotate(rope.address, norms, qp, kp, qs, ks, pp, n, hq, hkv, d, qo, ko, qos, kos, _stream_ptr(stream))
     if st:
         _check(st)
+
+
+@functools.cache
+def _several_devices():
+    return torch.cuda.device_count() > 1
 
 
 def _device_index(device, pool=None):

@@ -137,6 +137,14 @@ aoh_status check_rotation(const aoh_rope* rope, const aoh_norms* norms, int d) {
   return AOH_OK;
 }
 
+// Rows of a rotation: their strides are 32 bits of bytes.
+aoh_status check_turned_rows(const char* name, const void* p, int64_t stride, int heads, int d) {
+  const aoh_status st = check_rows(name, p, stride, heads, d);
+  if (st == AOH_OK && stride >= (int64_t)1 << 31)
+    return fail(AOH_ERR_INVALID, "the token stride of %s, %lld elements, must be below 2^31", name, (long long)stride);
+  return st;
+}
+
 // Rows written where others are read: in place alone, with the same stride.
 aoh_status check_in_place(const char* name, const void* in, int64_t in_stride, const void* out, int64_t out_stride) {
   if (in == out && in_stride != out_stride)
@@ -374,13 +382,13 @@ aoh_status aoh_norm_rotate(const aoh_rope* rope, const aoh_norms* norms, const v
   aoh_status st = check_rotation(rope, norms, d_head);
   if (st != AOH_OK || n_rows == 0 || n_q_heads + n_kv_heads == 0) return st;
   if (n_q_heads > 0) {
-    st = check_rows("q", q, q_stride, n_q_heads, d_head);
-    if (st == AOH_OK) st = check_rows("q_out", q_out, q_out_stride, n_q_heads, d_head);
+    st = check_turned_rows("q", q, q_stride, n_q_heads, d_head);
+    if (st == AOH_OK) st = check_turned_rows("q_out", q_out, q_out_stride, n_q_heads, d_head);
     if (st == AOH_OK) st = check_in_place("q", q, q_stride, q_out, q_out_stride);
   }
   if (st == AOH_OK && n_kv_heads > 0) {
-    st = check_rows("k", k, k_stride, n_kv_heads, d_head);
-    if (st == AOH_OK) st = check_rows("k_out", k_out, k_out_stride, n_kv_heads, d_head);
+    st = check_turned_rows("k", k, k_stride, n_kv_heads, d_head);
+    if (st == AOH_OK) st = check_turned_rows("k_out", k_out, k_out_stride, n_kv_heads, d_head);
     if (st == AOH_OK) st = check_in_place("k", k, k_stride, k_out, k_out_stride);
   }
   if (st != AOH_OK) return st;
@@ -417,10 +425,10 @@ aoh_status aoh_paged_append_rotated(aoh_paged* cache, const aoh_rope* rope, cons
   if (st == AOH_OK) st = check_cu(cu_rows, n_seqs, n_rows);
   if (st != AOH_OK || n_rows == 0) return st;
   const aoh_paged_config& c = cache->cfg;
-  st = check_rows("q", q, q_stride, c.n_q_heads, c.d_head);
-  if (st == AOH_OK) st = check_rows("k", k, k_stride, c.n_kv_heads, c.d_head);
-  if (st == AOH_OK) st = check_rows("v", v, v_stride, c.n_kv_heads, c.d_head);
-  if (st == AOH_OK) st = check_rows("q_out", q_out, q_out_stride, c.n_q_heads, c.d_head);
+  st = check_turned_rows("q", q, q_stride, c.n_q_heads, c.d_head);
+  if (st == AOH_OK) st = check_turned_rows("k", k, k_stride, c.n_kv_heads, c.d_head);
+  if (st == AOH_OK) st = check_turned_rows("v", v, v_stride, c.n_kv_heads, c.d_head);
+  if (st == AOH_OK) st = check_turned_rows("q_out", q_out, q_out_stride, c.n_q_heads, c.d_head);
   if (st == AOH_OK) st = check_in_place("q", q, q_stride, q_out, q_out_stride);
   if (st == AOH_OK) st = check_table(cache, table, table_stride);
   if (st != AOH_OK) return st;

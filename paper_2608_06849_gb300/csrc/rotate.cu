@@ -12,9 +12,16 @@
 // product, whatever the position; sincospif of its 32 leading bits gives the cosine and sine. A block
 // forms those of its rows once for all heads.
 //
-// Both only move bytes: D / 16 neighbouring lanes hold a row of one head, a lane two runs of 8
-// numbers, so chosen that the numbers of a pair are in one lane: 8 c .. and p + 8 c .. where the pairs
-// are p apart. The vectors of a token lie side by side, four of a thread's on their way at once.
+// D / 16 neighbouring lanes hold a row of one head, a lane two runs of 8 numbers, so chosen that the
+// numbers of a pair are in one lane: 8 c .. and p + 8 c .. where the pairs are p apart. The vectors of a token
+// lie side by side, and token after token: blocks that run at once walk through memory as it lies, next vectors
+// on their way while others are worked on. (With a thread's vector fixed, one row after the other, the
+// addresses cost a third of the instructions and the kernel was 3 to 18% slower.)
+//
+// Bound by HBM and, with norms, by the chain of a vector's sum, shuffles and root: 32,768 rows of 32/8 heads
+// of 128 without norms 111 us (671 MB, 6.1 TB/s), with them 125 (5.4); 22,490 rows with norms to bf16 pages
+// 107 (5.2), to 8-bit ones and read back 138; 16,384 rows of 32/8 heads of 64 to bf16 pages of 16 41 (4.9). One
+// token of 28/4 heads 2.9 us in a graph (10 as calls, the host's time).
 #include <cuda_fp8.h>
 
 #include "paged_rows.cuh"
@@ -25,7 +32,8 @@ namespace {
 using namespace rows;
 
 constexpr int kThreads = 256;
-constexpr int kMostRows = 16;    // rows of a block
+constexpr int kBlocks = 3;       // of an SM
+constexpr int kMostRows = 8;     // rows of a group
 constexpr int kDense = 0, kPagesBf16 = 1, kPagesF8 = 2;
 
 // 16 numbers in 32 bits as e4m3 codes (the first 8 in x and y) with the row's power of two, as
@@ -73,62 +81,91 @@ __device__ __forceinline__ uint4 encode(const float (&f)[16], int* e) {
                     __byte_perm(c[6], c[7], 0x5410));
 }
 
-// A row's cosines and sines as float4 (two neighbouring pairs): for halves [4][8 lanes], so that
-// the lanes of a row read neighbouring ones; for neighbouring pairs [2][16 runs of 8 numbers].
+// A row's cosines and sines as float4 (two neighbouring pairs): for halves [4][8 lanes], so that the lanes of
+// a row read neighbouring ones; for neighbouring pairs [2][16 runs of 8 numbers]. The float of a pair's
+// cosine, which its sine follows.
 __device__ __forceinline__ int turn_at(bool interleaved, int pair) {
-  return interleaved ? ((pair & 3) >> 1) * 32 + (pair >> 2) * 2 + (pair & 1) : ((pair & 7) >> 1) * 16 + (pair >> 3) * 2 + (pair & 1);
+  return 2 * (interleaved ? ((pair & 3) >> 1) * 32 + (pair >> 2) * 2 + (pair & 1)
+                          : ((pair & 7) >> 1) * 16 + (pair >> 3) * 2 + (pair & 1));
+}
+__device__ __forceinline__ void turn_one(float& a, float& b, float c, float s) {
+  const float x = a * c - b * s;
+  b = a * s + b * c;
+  a = x;
 }
 
+// Where a vector comes from and goes to: rows `stride` bytes apart.
+struct Side {
+  const uint8_t* in;
+  uint8_t* out;
+  uint32_t in_stride, out_stride;
+  int first;  // of the token's vectors
+  int norm;   // whether it is normalised: 1
+};
+
+// Blocks that run at once go through groups of rows; a thread through every 32nd (d_head 64: 64th) vector of a
+// group, row after row, two of them in registers while it works on two.
 template <int D, int FORM>
-__global__ void __launch_bounds__(kThreads, 3) rotate_kernel(const __grid_constant__ RotateArgs a, int rows_per_block) {
-  constexpr int LPR = D / 16, GROUPS = kThreads / LPR, U = 4;
-  __shared__ float2 turns[kMostRows][64];
+__global__ void __launch_bounds__(kThreads, kBlocks) rotate_kernel(const __grid_constant__ RotateArgs a, int rows_per_group) {
+  constexpr int LPR = D / 16, SIDE = kThreads / LPR, U = 2;
+  __shared__ __align__(16) float turns[2][kMostRows][128];
   __shared__ __align__(16) float weights[2][D];
-  __shared__ Place place[kMostRows];
-  __shared__ int position[kMostRows], given[kMostRows];  // given: whether the row is of a sequence
-  __shared__ int8_t power[FORM == kPagesF8 ? 2 * kMaxKvHeads * kMostRows : 1];
-  const int r0 = blockIdx.x * rows_per_block, n = min(rows_per_block, a.rows.n_rows - r0);
-  const int ch = threadIdx.x % LPR, group = threadIdx.x / LPR;
+  __shared__ Place place[4][kMostRows];
+  __shared__ int position[4][kMostRows], given[4][kMostRows];  // given: whether the row is of a sequence
+  __shared__ int8_t power[FORM == kPagesF8 ? 2 : 1][FORM == kPagesF8 ? 2 * kMaxKvHeads * kMostRows : 1];
+  __shared__ Side sides[3];  // of q, k and v
+  const int ch = threadIdx.x % LPR, n_rows = a.rows.n_rows, groups = (n_rows + rows_per_group - 1) / rows_per_group;
   const int nq = a.Hq, nk = a.Hkv, per_row = nq + nk + (FORM == kDense ? 0 : nk);
   const bool il = a.rope.interleaved != 0;
-  // the lane's two runs of 8 numbers: numbers 8 * run0 .., 8 * run1 ..
+  // the lane's two runs of 8 numbers: numbers 8 * run0 .., and to_run1 bytes of bf16 behind them
   const int pr = a.rope.n_pairs >> 3, rest = D / 16 - pr;
-  const int run0 = ch < pr ? ch : 2 * pr + (ch - pr), run1 = run0 + (ch < pr ? pr : rest);
-  const bool turned = ch < pr;
+  const int run0 = ch < pr ? ch : 2 * pr + (ch - pr), to_run1 = (ch < pr ? pr : rest) * 16;
+  auto rows_of = [&](int g) { return min(rows_per_group, n_rows - g * rows_per_group); };
+  auto kind_of = [&](int vec) { return vec < nq ? 0 : vec < nq + nk ? 1 : 2; };
+  if (threadIdx.x < 3) {
+    const int k = threadIdx.x;
+    sides[k] = {static_cast<const uint8_t*>(k == 0 ? a.q : k == 1 ? a.k : a.v), static_cast<uint8_t*>(k == 0 ? a.q_out : a.k_out),
+                (uint32_t)(2 * (k == 0 ? a.q_stride : k == 1 ? a.k_stride : a.v_stride)),
+                (uint32_t)(2 * (k == 0 ? a.q_out_stride : a.k_out_stride)), k == 0 ? 0 : k == 1 ? nq : nq + nk,
+                k < 2 && (k == 0 ? a.q_norm : a.k_norm) != nullptr};
+  }
+  __syncthreads();
   after_the_last_kernel();
 
-  // items: row and vector, neighbouring vectors in neighbouring groups
-  int row = 0, vec = group;
-  auto settle = [&]() {
-    while (vec >= per_row) {
-      vec -= per_row;
-      ++row;
-    }
+  struct Batch {
+    uint4 x[U][2];
+    int row[U], vec[U];  // row: of the group, or one beyond
   };
-  settle();
-  struct Item {
-    int row, vec;
-  } it[U];
-  uint4 x[U][2];
-  auto load = [&]() {
+  int at_group = blockIdx.x, at_row = 0, at_vec = threadIdx.x / LPR;  // of the next vector to be loaded
+  auto load = [&](Batch& b) {  // of one group alone
+    const int n = at_group < groups ? rows_of(at_group) : 0;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      it[u] = {row, vec};
-      if (row < n) {
-        const int kind = vec < nq ? 0 : vec < nq + nk ? 1 : 2;
-        const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(kind == 0 ? a.q : kind == 1 ? a.k : a.v) +
-                                   (r0 + row) * (kind == 0 ? a.q_stride : kind == 1 ? a.k_stride : a.v_stride) +
-                                   (vec - (kind == 0 ? 0 : kind == 1 ? nq : nq + nk)) * D;
-        x[u][0] = *reinterpret_cast<const uint4*>(src + run0 * 8);
-        x[u][1] = *reinterpret_cast<const uint4*>(src + run1 * 8);
+      while (at_vec >= per_row) {
+        at_vec -= per_row;
+        ++at_row;
       }
-      vec += GROUPS;
-      settle();
+      b.row[u] = at_row;
+      b.vec[u] = at_vec;
+      if (at_row < n) {
+        const Side& s = sides[kind_of(at_vec)];
+        const uint8_t* from = s.in + (uint64_t)(uint32_t)(at_group * rows_per_group + at_row) * s.in_stride +
+                              (uint32_t)((at_vec - s.first) * (2 * D) + run0 * 16);
+        b.x[u][0] = *reinterpret_cast<const uint4*>(from);
+        b.x[u][1] = *reinterpret_cast<const uint4*>(from + to_run1);
+      }
+      at_vec += SIDE;
     }
   };
-  load();
-  if (threadIdx.x < 32) {
-    const int i = min((int)threadIdx.x, n - 1), r = r0 + i;
+  auto next_group = [&]() {
+    at_group += gridDim.x;
+    at_row = 0;
+    at_vec = threadIdx.x / LPR;
+  };
+  // where group g's rows lie, and their positions; warp 0
+  auto look = [&](int g, int slot) {
+    if (threadIdx.x >= 32 || g >= groups) return;
+    const int n = rows_of(g), r0 = g * rows_per_group, r = r0 + min((int)threadIdx.x, n - 1);
     int pos = 0;
     bool has = true;
     Place p{-1, 0};
@@ -144,11 +181,120 @@ __global__ void __launch_bounds__(kThreads, 3) rotate_kernel(const __grid_consta
     }
     if (a.positions) pos = __ldg(a.positions + r);
     if ((int)threadIdx.x < n) {
-      place[threadIdx.x] = p;
-      position[threadIdx.x] = pos;
-      given[threadIdx.x] = has;
+      place[slot][threadIdx.x] = p;
+      position[slot][threadIdx.x] = pos;
+      given[slot][threadIdx.x] = has;
     }
-  }
+  };
+  auto turn = [&](int g, int slot, int to) {
+    if (g >= groups) return;
+    for (int i = threadIdx.x; i < rows_of(g) * a.rope.n_pairs; i += kThreads) {
+      const int r = i / a.rope.n_pairs, p = i - r * a.rope.n_pairs;
+      const uint64_t t = (uint64_t)(int64_t)position[slot][r] * a.rope.turns[p] + (1ull << 31);
+      float s, c;
+      sincospif((float)(int)(t >> 32) * 0x1p-31f, &s, &c);
+      float* at = turns[to][r] + turn_at(il, p);
+      at[0] = c * a.rope.scale;
+      at[1] = s * a.rope.scale;
+    }
+  };
+
+  const unsigned lanes = ((1u << LPR) - 1u) << (threadIdx.x & 31 & ~(LPR - 1));
+  auto work = [&](const Batch& b, int g, int n, int slot, int buf) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = b.row[u], vec = b.vec[u], kind = kind_of(vec);
+      if (i >= n || (FORM != kDense && !given[slot][i])) continue;  // alike for a row's lanes
+      const Side& side = sides[kind];
+      float f[16];
+      {
+        const uint4 lo = b.x[u][0], hi = b.x[u][1];
+        const uint32_t y[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float2 two = bf16x2_to_float2(y[j]);
+          f[2 * j] = two.x;
+          f[2 * j + 1] = two.y;
+        }
+      }
+      if (side.norm) {
+        float2 s2 = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float2 two = make_float2(f[2 * j], f[2 * j + 1]);
+          s2 = __ffma2_rn(two, two, s2);
+        }
+        float s = s2.x + s2.y;
+#pragma unroll
+        for (int o = LPR / 2; o >= 1; o >>= 1) s += __shfl_xor_sync(lanes, s, o);
+        const float inv = rsqrtf(s * (1.f / D) + a.eps);
+        const float4* wt = reinterpret_cast<const float4*>(weights[kind & 1]) + run0;
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+          const float4 w = wt[(h & 1) * (D / 8) + (h < 2 ? 0 : to_run1 >> 4)];
+          f[4 * h] *= inv * w.x;
+          f[4 * h + 1] *= inv * w.y;
+          f[4 * h + 2] *= inv * w.z;
+          f[4 * h + 3] *= inv * w.w;
+        }
+      }
+      if (kind < 2 && ch < pr) {
+        const float4* tr = reinterpret_cast<const float4*>(turns[buf][i]) + run0;
+        if (il) {
+#pragma unroll
+          for (int h = 0; h < 4; ++h) {
+            const float4 t = tr[(h & 1) * 16 + (h < 2 ? 0 : to_run1 >> 4)];
+            turn_one(f[4 * h], f[4 * h + 1], t.x, t.y);
+            turn_one(f[4 * h + 2], f[4 * h + 3], t.z, t.w);
+          }
+        } else {
+#pragma unroll
+          for (int h = 0; h < 4; ++h) {
+            const float4 t = tr[h * 8];
+            turn_one(f[2 * h], f[8 + 2 * h], t.x, t.y);
+            turn_one(f[2 * h + 1], f[9 + 2 * h], t.z, t.w);
+          }
+        }
+      }
+      if (FORM == kPagesF8 && kind > 0) {
+        int e;
+        const uint4 c = encode<LPR>(f, &e);
+        const int v = vec - nq;
+        if (ch == 0) power[buf][v * kMostRows + i] = (int8_t)e;
+        if (place[slot][i].page < 0) continue;
+        uint8_t* to = static_cast<uint8_t*>(a.pool.data) + data_row(a.pool, place[slot][i], v) * D + run0 * 8;
+        *reinterpret_cast<uint2*>(to) = make_uint2(c.x, c.y);
+        *reinterpret_cast<uint2*>(to + (to_run1 >> 1)) = make_uint2(c.z, c.w);
+        continue;
+      }
+      uint8_t* to;
+      if (FORM == kDense || kind == 0) {
+        to = side.out + (uint64_t)(uint32_t)(g * rows_per_group + i) * side.out_stride +
+             (uint32_t)((vec - side.first) * (2 * D) + run0 * 16);
+      } else {
+        if (place[slot][i].page < 0) continue;
+        to = static_cast<uint8_t*>(a.pool.data) + data_row(a.pool, place[slot][i], vec - nq) * (2 * D) + run0 * 16;
+      }
+      *reinterpret_cast<uint4*>(to) = make_uint4(float2_to_bf16x2(f[0], f[1]), float2_to_bf16x2(f[2], f[3]),
+                                                 float2_to_bf16x2(f[4], f[5]), float2_to_bf16x2(f[6], f[7]));
+      *reinterpret_cast<uint4*>(to + to_run1) = make_uint4(float2_to_bf16x2(f[8], f[9]), float2_to_bf16x2(f[10], f[11]),
+                                                           float2_to_bf16x2(f[12], f[13]), float2_to_bf16x2(f[14], f[15]));
+    }
+  };
+  // a head's powers of neighbouring tokens lie side by side: stored by neighbouring lanes
+  auto store_powers = [&](int g, int slot, int buf) {
+    if constexpr (FORM == kPagesF8) {
+      const int n = rows_of(g);
+      for (int u = threadIdx.x; u < 2 * nk * kMostRows; u += kThreads) {
+        const int v = u / kMostRows, i = u % kMostRows;
+        if (i < n && place[slot][i].page >= 0) a.pool.powers[power_at(a.pool, place[slot][i], v)] = power[buf][u];
+      }
+    }
+  };
+
+  Batch now, next;
+  load(now);
+  look(blockIdx.x, 0);
   for (int i = threadIdx.x; i < 2 * D; i += kThreads) {
     const void* w = i < D ? a.q_norm : a.k_norm;
     const int j = i & (D - 1);
@@ -158,131 +304,40 @@ __global__ void __launch_bounds__(kThreads, 3) rotate_kernel(const __grid_consta
     weights[i >= D][((j >> 2) & 1) * (D / 2) + (j >> 3) * 4 + (j & 3)] = f;
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < n * a.rope.n_pairs; i += kThreads) {
-    const int r = i / a.rope.n_pairs, p = i - r * a.rope.n_pairs;
-    const uint64_t t = (uint64_t)(int64_t)position[r] * a.rope.turns[p] + (1ull << 31);
-    float s, c;
-    sincospif((float)(int)(t >> 32) * 0x1p-31f, &s, &c);
-    turns[r][turn_at(il, p)] = make_float2(c * a.rope.scale, s * a.rope.scale);
-  }
-  __syncthreads();
-
-  const unsigned lanes = ((1u << LPR) - 1u) << (threadIdx.x & 31 & ~(LPR - 1));
-  while (it[0].row < n) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (it[u].row >= n) continue;  // alike for a row's lanes
-      const int i = it[u].row, kind = it[u].vec < nq ? 0 : it[u].vec < nq + nk ? 1 : 2;
-      if (FORM != kDense && !given[i]) continue;
-      float f[16];
-      {
-        const uint32_t w[8] = {x[u][0].x, x[u][0].y, x[u][0].z, x[u][0].w, x[u][1].x, x[u][1].y, x[u][1].z, x[u][1].w};
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float2 y = bf16x2_to_float2(w[j]);
-          f[2 * j] = y.x;
-          f[2 * j + 1] = y.y;
-        }
+  turn(blockIdx.x, 0, 0);
+  look(blockIdx.x + gridDim.x, 1);
+  int k_group = 0;  // of the block's
+  for (int g = blockIdx.x; g < groups; g += gridDim.x, ++k_group) {
+    // the group's turns, and the next one's positions, are there; the last one's powers too
+    __syncthreads();
+    const int slot = k_group & 3, buf = k_group & 1, n = rows_of(g);
+    if (k_group > 0) store_powers(g - gridDim.x, (k_group - 1) & 3, buf ^ 1);
+    const int batches = (n * per_row + SIDE * U - 1) / (SIDE * U);
+    for (int k = 0; k < batches; ++k) {
+      if (k + 1 == batches) next_group();
+      load(next);
+      if (k == 0) {
+        look(g + 2 * (int)gridDim.x, (k_group + 2) & 3);
+        turn(g + gridDim.x, (k_group + 1) & 3, buf ^ 1);
       }
-      if (kind < 2) {
-        if (kind == 0 ? a.q_norm != nullptr : a.k_norm != nullptr) {
-          float2 s2 = make_float2(0.f, 0.f);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float2 y = make_float2(f[2 * j], f[2 * j + 1]);
-            s2 = __ffma2_rn(y, y, s2);
-          }
-          float s = s2.x + s2.y;
-#pragma unroll
-          for (int o = LPR / 2; o >= 1; o >>= 1) s += __shfl_xor_sync(lanes, s, o);
-          const float inv = rsqrtf(s * (1.f / D) + a.eps);
-          const float4* wt = reinterpret_cast<const float4*>(weights[kind]);
-#pragma unroll
-          for (int h = 0; h < 4; ++h) {
-            const float4 w = wt[(h & 1) * (D / 8) + (h < 2 ? run0 : run1)];
-            f[4 * h] *= inv * w.x;
-            f[4 * h + 1] *= inv * w.y;
-            f[4 * h + 2] *= inv * w.z;
-            f[4 * h + 3] *= inv * w.w;
-          }
-        }
-        if (turned) {
-          const float4* tr = reinterpret_cast<const float4*>(turns[i]);
-          if (il) {
-#pragma unroll
-            for (int h = 0; h < 4; ++h) {
-              const float4 t = tr[(h & 1) * 16 + (h < 2 ? run0 : run1)];
-              float* y = f + 4 * h;
-              const float a0 = y[0], b0 = y[1], a1 = y[2], b1 = y[3];
-              y[0] = a0 * t.x - b0 * t.y;
-              y[1] = a0 * t.y + b0 * t.x;
-              y[2] = a1 * t.z - b1 * t.w;
-              y[3] = a1 * t.w + b1 * t.z;
-            }
-          } else {
-#pragma unroll
-            for (int h = 0; h < 4; ++h) {
-              const float4 t = tr[h * 8 + run0];
-              const float a0 = f[2 * h], b0 = f[8 + 2 * h], a1 = f[2 * h + 1], b1 = f[9 + 2 * h];
-              f[2 * h] = a0 * t.x - b0 * t.y;
-              f[8 + 2 * h] = a0 * t.y + b0 * t.x;
-              f[2 * h + 1] = a1 * t.z - b1 * t.w;
-              f[9 + 2 * h] = a1 * t.w + b1 * t.z;
-            }
-          }
-        }
-      }
-      if (FORM == kPagesF8 && kind > 0) {
-        int e;
-        const uint4 c = encode<LPR>(f, &e);
-        const int v = it[u].vec - nq;
-        if (ch == 0) power[v * kMostRows + i] = (int8_t)e;
-        if (place[i].page < 0) continue;
-        uint8_t* dst = static_cast<uint8_t*>(a.pool.data) + data_row(a.pool, place[i], v) * D;
-        *reinterpret_cast<uint2*>(dst + run0 * 8) = make_uint2(c.x, c.y);
-        *reinterpret_cast<uint2*>(dst + run1 * 8) = make_uint2(c.z, c.w);
-        continue;
-      }
-      __nv_bfloat16* dst;
-      if (kind == 0) {
-        dst = static_cast<__nv_bfloat16*>(a.q_out) + (r0 + i) * a.q_out_stride + it[u].vec * D;
-      } else if (FORM == kDense) {
-        dst = static_cast<__nv_bfloat16*>(a.k_out) + (r0 + i) * a.k_out_stride + (it[u].vec - nq) * D;
-      } else {
-        if (place[i].page < 0) continue;
-        dst = static_cast<__nv_bfloat16*>(a.pool.data) + data_row(a.pool, place[i], it[u].vec - nq) * D;
-      }
-      uint4 lo, hi;
-      lo.x = float2_to_bf16x2(f[0], f[1]);
-      lo.y = float2_to_bf16x2(f[2], f[3]);
-      lo.z = float2_to_bf16x2(f[4], f[5]);
-      lo.w = float2_to_bf16x2(f[6], f[7]);
-      hi.x = float2_to_bf16x2(f[8], f[9]);
-      hi.y = float2_to_bf16x2(f[10], f[11]);
-      hi.z = float2_to_bf16x2(f[12], f[13]);
-      hi.w = float2_to_bf16x2(f[14], f[15]);
-      *reinterpret_cast<uint4*>(dst + run0 * 8) = lo;
-      *reinterpret_cast<uint4*>(dst + run1 * 8) = hi;
+      work(now, g, n, slot, buf);
+      now = next;
     }
-    load();
   }
   if constexpr (FORM == kPagesF8) {
-    // a head's powers of neighbouring tokens lie side by side: stored by neighbouring lanes
     __syncthreads();
-    for (int u = threadIdx.x; u < 2 * nk * kMostRows; u += kThreads) {
-      const int v = u / kMostRows, i = u % kMostRows;
-      if (i < n && place[i].page >= 0) a.pool.powers[power_at(a.pool, place[i], v)] = power[u];
-    }
+    store_powers(blockIdx.x + (k_group - 1) * (int)gridDim.x, (k_group - 1) & 3, (k_group - 1) & 1);
   }
 }
 
-// Rows of a block: the call's rows on three blocks an SM (which run at once), up to 16. The launch
-// overlaps the end of the kernel before it.
+// As many blocks as run at once go through groups of up to 8 rows. The launch overlaps the end of the
+// kernel before it.
 template <int D, int FORM>
 cudaError_t launch(const RotateArgs& a, int num_sms, cudaStream_t s) {
-  const int n = a.rows.n_rows, even = (n + 3 * num_sms - 1) / (3 * num_sms), per = even < kMostRows ? even : kMostRows;
+  const int n = a.rows.n_rows, blocks = kBlocks * num_sms, even = (n + blocks - 1) / blocks;
+  const int per = even < kMostRows ? even : kMostRows, groups = (n + per - 1) / per;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((n + per - 1) / per));
+  cfg.gridDim = dim3((unsigned)(groups < blocks ? groups : blocks));
   cfg.blockDim = dim3(kThreads);
   cfg.stream = s;
   cudaLaunchAttribute attr[1];

@@ -140,7 +140,7 @@ def test_library_refuses_on_the_host(lib):
     assert call(n=0) == 0 and call(hq=0, hkv=0) == 0
     assert call(d=96) == 5
     for bad in (dict(rope=None), dict(q=None), dict(q=ctypes.c_void_p((1 << 20) + 8)), dict(qs=511), dict(qs=504),
-                dict(ks=120), dict(qn=p, kind=2), dict(qn=p, eps=-1.0), dict(qn=p, eps=float("nan")), dict(pos=None), dict(n=-1),
+                dict(ks=120), dict(qs=1 << 31), dict(kos=1 << 31), dict(qn=p, kind=2), dict(qn=p, eps=-1.0), dict(qn=p, eps=float("nan")), dict(pos=None), dict(n=-1),
                 dict(hq=-1), dict(hq=1025), dict(ko=None), dict(qos=1024), dict(kos=136), dict(qn=ctypes.c_void_p((1 << 20) + 1)),
                 dict(rope=aoh.Rope(128).c)):
         assert call(**bad) == 1, bad

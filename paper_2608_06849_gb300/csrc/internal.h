@@ -303,6 +303,14 @@ struct PagedDecodeArgs {
   uint32_t* counters;  // [CTAs][3] arrivals: groups of its first and last item, groups of its last
   uint32_t* err;
   float scale_log2;
+  int tokens = 1;      // of a sequence at most (PagedPartsArgs)
+  int rcp = 0;         // (h * rcp) >> 16 = h / G for h < 16 (PagedPartsArgs)
+};
+
+// Parts of sequences, of up to `tokens` tokens each, tokens * G <= 16, on the decode kernel: {first query
+// row, tokens, the sequence's number, tokens of it behind the part's last one}. n_seqs: the parts.
+struct PagedPartsArgs : PagedDecodeArgs {
+  PackedSeqs seqs;
 };
 
 // One warp waits on an mbarrier nothing arrives at, for limit_ns; the timeout
@@ -383,6 +391,7 @@ bool make_pages_map(CUtensorMap* map, const PagePool& p);
 // Floats of PagedDecodeArgs::states.
 size_t paged_state_floats(int num_sms, int D);
 cudaError_t launch_paged_decode(const PagedDecodeArgs& a, int num_sms, cudaStream_t s);
+cudaError_t launch_paged_parts(const PagedPartsArgs& a, int num_sms, cudaStream_t s);
 // The CUDA-core decode kernel: the H2Share reuse step of d_head 64, with its
 // CTA count.
 cudaError_t launch_decode_cc(const DecodeArgs& a, cudaStream_t s);

@@ -208,6 +208,49 @@ void* expand_memory(aoh_paged* h, size_t bytes, cudaStream_t s) {
   return p;
 }
 
+// Tiles of 128 keys that n rows at the end of `keys` positions see, of all KV heads.
+long long seen_tiles(const CacheGeom& g, int n, int keys) {
+  const long long all = ((long long)keys + 127) / 128, window = ((long long)g.S + g.W + n + 255) / 128;
+  return g.n_r * all + g.n_s * std::min(all, window);
+}
+
+// Calls of a few rows a sequence as parts on the decode kernel, of at most 16 columns each (query heads of a KV
+// head times tokens), which reads a sequence's pages once for each part but as they lie, at the rate of HBM. What it
+// takes against the tiles of 256 rows, in nanoseconds of the GPU: 10.6 a tile of 128 keys of d_head 128 and part (8
+// bits: 5.5, but 8 with more than 8 columns, whose softmax takes longer than the tile's transfer) against 14 (18) a
+// tile, and a start of 6 us against 10. work: tiles that the latter visit. Measured, us of a call in tiles / parts: 32 x 2-5
+// rows after 1,000-16,000, 32/8 heads, 8 bits 198 / 121, bf16 154 / 144; 4 rows each, 8 bits - / 98, 2 - / 69; 5 rows after
+// 4,096, 28/4 heads, bf16 12.3 / 9.4.
+bool parts_of(const aoh_paged* h, const std::vector<int4>& seqs, const std::vector<int4>& planned, long long work,
+              std::vector<int4>* parts, int* tokens) {
+  const CacheGeom& g = h->geom;
+  const int most = 16 / g.G;
+  const double scale = g.D / 128.0 * 0.001;
+  long long visits = 0, n = 0, longest = 1;
+  *tokens = 1;
+  for (const int4& s : planned) {
+    const int count = (s.y + most - 1) / most, each = (s.y + count - 1) / count;
+    visits += count * seen_tiles(g, s.y, s.w);
+    n += count;
+    longest = std::max<long long>(longest, (s.w + 127) / 128);
+    *tokens = std::max(*tokens, each);
+    if (count > 16) return false;
+  }
+  const bool f8 = h->cfg.form == AOH_PAGES_E4M3;
+  const double each_ns = !f8 ? 10.6 : g.G * *tokens <= 8 ? 5.5 : 8;
+  if (6 + visits * each_ns * scale > 10 + work * (f8 ? 18 : 14) * scale) return false;
+  if (n > PackedSeqs::kMost && n > h->cfg.max_seqs) return false;  // the device's list holds no more
+  parts->reserve(n);
+  for (const int4& s : seqs) {
+    const int count = (s.y + most - 1) / most, each = (s.y + count - 1) / count;
+    for (int t = 0; t < s.y; t += each) {
+      const int m = std::min(each, s.y - t);
+      parts->push_back(make_int4(s.x + t, m, s.z, s.y - t - m));
+    }
+  }
+  return true;
+}
+
 // Which 8-bit pages of a call to write out as bf16 ones first: none, or those of all its sequences (seqs: as
 // the plan takes them), where its items visit the same tiles often enough. work: tiles that they visit in all.
 // An item's visit costs an SM 1.1 us more with codes (d_head 128; 2,824 us of 8,192 rows after 16,384 of
@@ -221,8 +264,7 @@ bool expand_plan(const aoh_paged* h, const std::vector<int4>& seqs, long long wo
     const int keys = seqs[i].w, all = (int)(((long long)keys + 127) / 128);
     x->first[i] = (int)pages;
     pages += all;
-    const long long seen = (long long)g.S + g.W + seqs[i].y + 256;
-    tiles += (long long)g.n_r * all + (long long)g.n_s * std::min<long long>(all, seen / 128);
+    tiles += seen_tiles(g, seqs[i].y, keys);
   }
   x->first[seqs.size()] = (int)pages;
   const double visit = 7.2 * g.D / 128, write = 16.4 * g.D / 128;
@@ -631,6 +673,48 @@ aoh_status aoh_paged_attend(aoh_paged* cache, const void* q, int64_t q_stride, c
   if (!lens || !aligned(lens, 4)) return fail(AOH_ERR_INVALID, "lens must be a 4-byte aligned device pointer");
   if (holds > (1 << 30)) return fail(AOH_ERR_INVALID, "a table's row must hold at most 2^30 tokens");
 
+  cudaStream_t s = (cudaStream_t)stream;
+  const int span = 128 / cache->geom.G;
+  std::vector<int> costs;
+  const std::vector<uint64_t> items = folded_schedule(cache->geom, planned, span, &costs);
+  long long work = 0;
+  for (int cost : costs) work += cost;
+  std::vector<int4> parts;
+  int tokens = 1;
+  // (the decode kernel counts its tiles, of at least 128 keys, in 32 bits)
+  if (parts_of(cache, seqs, planned, work, &parts, &tokens) &&
+      (int64_t)parts.size() * c.n_kv_heads * ((holds + 127) / 128) <= INT32_MAX) {
+    PagedPartsArgs p;
+    p.pages = cache->pages;
+    p.states = cache->d_states;
+    p.counters = cache->d_counters;
+    p.pool = cache->pool;
+    p.geom = cache->geom;
+    p.q = q;
+    p.q_stride = q_stride;
+    p.out = out;
+    p.lens = lens;
+    p.table = table;
+    p.table_stride = table_stride;
+    p.n_seqs = (int)parts.size();
+    p.max_len = 1;
+    for (const int4& b : planned) p.max_len = std::max(p.max_len, b.w);
+    p.err = cache->d_err;
+    p.scale_log2 = (float)(1.4426950408889634 / sqrt((double)c.d_head));
+    p.tokens = tokens;
+    p.rcp = 65536 / cache->geom.G + 1;
+    cudaError_t e = cudaSuccess;
+    p.seqs.table = nullptr;
+    if (parts.size() <= (size_t)PackedSeqs::kMost) {
+      std::copy(parts.begin(), parts.end(), p.seqs.by_value);
+    } else {
+      p.seqs.table = cache->d_seqs;
+      e = launch_packed_seqs(cache->d_seqs, parts, s);
+    }
+    if (e == cudaSuccess) e = launch_paged_parts(p, cache->num_sms, s);
+    return e == cudaSuccess ? AOH_OK : cuda_fail(e, "paged attention launch");
+  }
+
   PagedAttendArgs a;
   memset(&a, 0, sizeof(a));
   a.geom = cache->geom;
@@ -639,7 +723,7 @@ aoh_status aoh_paged_attend(aoh_paged* cache, const void* q, int64_t q_stride, c
   a.q_stride = q_stride;
   a.err = cache->d_err;
   a.scale_log2 = (float)(1.4426950408889634 / sqrt((double)c.d_head));
-  a.span = 128 / a.geom.G;
+  a.span = span;
   a.rcp = 65536 / a.geom.G + 1;
   a.pages = cache->pages;
   a.pool = cache->pool;
@@ -649,7 +733,6 @@ aoh_status aoh_paged_attend(aoh_paged* cache, const void* q, int64_t q_stride, c
   a.holds = (int)holds;
   if (!make_rows_map(&a.tq, q, 1, n_q, c.n_q_heads, c.d_head, q_stride, a.span, a.geom.G))
     return fail(AOH_ERR_CUDA, "cuTensorMapEncodeTiled failed for q");
-  cudaStream_t s = (cudaStream_t)stream;
   if (seqs.size() <= (size_t)PackedSeqs::kMost) {
     std::copy(seqs.begin(), seqs.end(), a.seqs.by_value);
   } else {
@@ -657,13 +740,9 @@ aoh_status aoh_paged_attend(aoh_paged* cache, const void* q, int64_t q_stride, c
     const cudaError_t e = launch_packed_seqs(cache->d_seqs, seqs, s);
     if (e != cudaSuccess) return cuda_fail(e, "sequence upload launch");
   }
-  std::vector<int> costs;
-  const std::vector<uint64_t> items = folded_schedule(a.geom, planned, a.span, &costs);
   bool lone = true;
   for (const int4& b : seqs) lone = lone && b.y <= a.span;
   const int split = folded_split(costs, lone, decode_tc_max_clusters, cache->num_sms);
-  long long work = 0;
-  for (int cost : costs) work += cost;
   cudaError_t e = cudaSuccess;
   Expanded expanded;
   void* written = nullptr;

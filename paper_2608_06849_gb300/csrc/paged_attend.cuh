@@ -205,29 +205,16 @@ struct CodeWalk<PagedArgs<true>, D> {
   }
 };
 
-// The lane's numbers of key j of K (sel 0) or V (repair_rows; a page out of range: zeros).
+// The lane's numbers of key j of K (sel 0) or V (repair_rows).
 template <int D>
 __device__ __forceinline__ void load_key(const PagedAttendArgs& a, const PagedItem& t, int j, int sel, int lane,
                                          float (&to)[D / 32]) {
-  const int page = t.page_of(a, j), row = j & (a.pool.ps - 1);
-  if ((unsigned)page >= (unsigned)a.pool.n_pages) {
-#pragma unroll
-    for (int n = 0; n < D / 32; ++n) to[n] = 0.f;
-    return;
-  }
-  const size_t at = (((((size_t)page * 2 + sel) * a.pool.Hkv + t.kvh) << a.pool.lg_ps) + row) * D + lane * (D / 32);
-  if (a.pool.form == 0) {
-    load_numbers<D>(static_cast<const bf16*>(a.pool.data) + at, to);
+  // (of written-out pages the table is their numbers, one after the other)
+  if (a.table) {
+    rows::load_key<D>(a.pool, a.table + (size_t)t.b * a.table_stride, t.kvh, j, sel, lane, to);
   } else {
-    const int e = a.pool.powers[((((size_t)page * a.pool.Hkv + t.kvh) * 2 + sel) << a.pool.lg_ps) + row];
-    const float scale = __uint_as_float((uint32_t)(127 + e) << 23);
-#pragma unroll
-    for (int n = 0; n < D / 32; n += 2) {
-      const uint16_t two = *reinterpret_cast<const uint16_t*>(static_cast<const uint8_t*>(a.pool.data) + at + n);
-      const float2 f = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2(two, __NV_E4M3)));
-      to[n] = f.x * scale;
-      to[n + 1] = f.y * scale;
-    }
+    const size_t at = ((((size_t)t.page_of(a, j) * 2 + sel) * a.pool.Hkv + t.kvh) * kBN + (j & (kBN - 1))) * D;
+    load_numbers<D>(static_cast<const bf16*>(a.pool.data) + at + lane * (D / 32), to);
   }
 }
 

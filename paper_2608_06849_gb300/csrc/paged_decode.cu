@@ -5,9 +5,13 @@
 namespace aoh {
 
 cudaError_t launch_paged_decode_f8_128(const PagedDecodeArgs& a, int num_sms, int cluster, cudaStream_t s);
+cudaError_t launch_paged_parts_f8_128(const PagedPartsArgs& a, int num_sms, int cluster, cudaStream_t s);
 cudaError_t launch_paged_decode_f8_64(const PagedDecodeArgs& a, int num_sms, int cluster, cudaStream_t s);
+cudaError_t launch_paged_parts_f8_64(const PagedPartsArgs& a, int num_sms, int cluster, cudaStream_t s);
 cudaError_t launch_paged_decode_bf16_128(const PagedDecodeArgs& a, int num_sms, int cluster, cudaStream_t s);
+cudaError_t launch_paged_parts_bf16_128(const PagedPartsArgs& a, int num_sms, int cluster, cudaStream_t s);
 cudaError_t launch_paged_decode_bf16_64(const PagedDecodeArgs& a, int num_sms, int cluster, cudaStream_t s);
+cudaError_t launch_paged_parts_bf16_64(const PagedPartsArgs& a, int num_sms, int cluster, cudaStream_t s);
 
 // 3D map over a pool as [page, K or V, head][row][D], box one block of up to 128 bytes a row,
 // swizzled over that width.
@@ -61,6 +65,13 @@ cudaError_t launch_paged_decode(const PagedDecodeArgs& a, int num_sms, cudaStrea
   if (a.pool.D == 128)
     return a.pool.form ? launch_paged_decode_f8_128(a, num_sms, c, s) : launch_paged_decode_bf16_128(a, num_sms, c, s);
   return a.pool.form ? launch_paged_decode_f8_64(a, num_sms, c, s) : launch_paged_decode_bf16_64(a, num_sms, c, s);
+}
+
+cudaError_t launch_paged_parts(const PagedPartsArgs& a, int num_sms, cudaStream_t s) {
+  const int c = cluster_size(a, num_sms);
+  if (a.pool.D == 128)
+    return a.pool.form ? launch_paged_parts_f8_128(a, num_sms, c, s) : launch_paged_parts_bf16_128(a, num_sms, c, s);
+  return a.pool.form ? launch_paged_parts_f8_64(a, num_sms, c, s) : launch_paged_parts_bf16_64(a, num_sms, c, s);
 }
 
 }  // namespace aoh

@@ -47,9 +47,12 @@
 #include <cuda_fp8.h>
 #include <math.h>
 
+#include <type_traits>
+
 #include "cluster.cuh"
 #include "common.cuh"
 #include "internal.h"
+#include "paged_rows.cuh"
 #include "tc.cuh"
 
 namespace aoh {
@@ -124,22 +127,27 @@ struct Lay {
   static_assert(TMEM_COLS <= 512, "TMEM columns");
 };
 
+// Sequence b's row of queries, tokens, number, and the tokens behind its last one.
+__device__ __forceinline__ int4 part_of(const PagedDecodeArgs&, int b) { return make_int4(b, 1, b, 0); }
+__device__ __forceinline__ int4 part_of(const PagedPartsArgs& a, int b) { return a.seqs.of(b); }
+
 // What the heads of a sequence of len tokens see, as tiles of 2^LG keys: a retrieval head every
 // page (tr tiles), a streaming head the pages of its sinks and those of its window (ts tiles; from
 // its gslot-th page on, gap pages are left out; w0: first position of the window).
 struct Seq {
   int len, tr, ts, w0, gslot, gap;
 };
-template <int LG>
-__device__ __forceinline__ Seq make_seq(const PagedDecodeArgs& a, int len) {
+// (Of several tokens, a.tokens at most, the window is the first one's.)
+template <int LG, class A>
+__device__ __forceinline__ Seq make_seq(const A& a, int len) {
   const CacheGeom& g = a.geom;
-  const int lg = a.pool.lg_ps, round = (1 << (LG - lg)) - 1;
+  const int lg = a.pool.lg_ps, round = (1 << (LG - lg)) - 1, w0 = len - (a.tokens - 1) - g.W;
   Seq q;
   q.len = len;
   q.w0 = q.gslot = q.gap = 0;
   const int slots = (int)(((unsigned)len + a.pool.ps - 1) >> lg);
-  if (len - g.W > g.S) {
-    q.w0 = len - g.W;
+  if (w0 > g.S) {
+    q.w0 = w0;
     q.gslot = (g.S + a.pool.ps - 1) >> lg;
     q.gap = max((q.w0 >> lg) - q.gslot, 0);
   }
@@ -148,12 +156,17 @@ __device__ __forceinline__ Seq make_seq(const PagedDecodeArgs& a, int len) {
   return q;
 }
 
-// The tokens of sequence b, within what its table holds.
-__device__ __forceinline__ int seq_len(const PagedDecodeArgs& a, int b, bool report) {
-  const int n = __ldcg(a.lens + b), most = a.table_stride << a.pool.lg_ps;
-  if (n >= 0 && n <= most) return n;
-  if (report) atomicOr(a.err, kErrPages);
-  return n < 0 ? 0 : most;
+// The tokens of sequence b, within what its table holds; of a part of a sequence those up to its last one.
+template <class A>
+__device__ __forceinline__ int seq_len(const A& a, int b, bool report) {
+  const int4 part = part_of(a, b);
+  int n = __ldcg(a.lens + part.z);
+  const int most = a.table_stride << a.pool.lg_ps;
+  if (n < 0 || n > most) {
+    if (report) atomicOr(a.err, kErrPages);
+    n = n < 0 ? 0 : most;
+  }
+  return max(n - part.w, 0);
 }
 
 // x / d for 0 <= x, 0 < d: by a reciprocal, put right, where floats hold x.
@@ -176,9 +189,9 @@ struct Deal {
 
 // The items of a CTA's run of tiles [start, end), in order; used by whole warps. Head k of a
 // sequence: retrieval heads before streaming ones.
-template <int LG>
+template <class A, int LG>
 struct Walk {
-  const PagedDecodeArgs& a;
+  const A& a;
   const int* lens_s;       // the lengths in shared memory, or null: lane b of the warp has sequence b's
   const uint8_t* heads_s;  // KV head of head k
   int len_reg;             // (neither above kLensCap sequences: they are loaded)
@@ -186,7 +199,7 @@ struct Walk {
   int b, k, lo, hi, tiles = 0;
   Seq q;
   // seq_off: the first tile of sequence b, which holds tile `start`
-  __device__ __forceinline__ Walk(const PagedDecodeArgs& a_, const int* ls, const uint8_t* hs, int lr, int s, int e, int b0,
+  __device__ __forceinline__ Walk(const A& a_, const int* ls, const uint8_t* hs, int lr, int s, int e, int b0,
                                   int seq_off)
       : a(a_), lens_s(ls), heads_s(hs), len_reg(lr), start(s), end(e), off(seq_off), b(b0), k(-1) {
     if (start >= end) return;
@@ -229,14 +242,14 @@ struct Walk {
 };
 
 // The one item of a cluster: its CTAs have equal runs of its tiles.
-template <int LG>
+template <class A, int LG>
 struct ClusterWalk {
-  const PagedDecodeArgs& a;
+  const A& a;
   const uint8_t* heads_s;
   int b, k, lo, hi, tiles, off = 0;
   bool left;
   Seq q;
-  __device__ __forceinline__ ClusterWalk(const PagedDecodeArgs& a_, const uint8_t* hs, int len, int b_, int k_, int rank,
+  __device__ __forceinline__ ClusterWalk(const A& a_, const uint8_t* hs, int len, int b_, int k_, int rank,
                                          int lg_ctas)
       : a(a_), heads_s(hs), b(b_), k(k_) {
     q = make_seq<LG>(a, len);
@@ -274,12 +287,42 @@ __device__ __forceinline__ float scaled(float l, float d) {
   return l * half * half;
 }
 
+// The outputs of an item: of column h, head h of the KV head's, or of several tokens head h % heads of token
+// h / heads. MULTI: as seqs says.
+template <int D, bool MULTI>
+struct Out {
+  bf16* to;  // null: none
+  int heads, tokens, rcp;
+  size_t stride;  // from a token to the next
+  uint32_t* spoilt;
+  __device__ __forceinline__ bool has(int h) const { return !MULTI || ((h * rcp) >> 16) < tokens; }
+  __device__ __forceinline__ bf16* at(int h) const {
+    if (!MULTI) return to + h * D;
+    const int t = (h * rcp) >> 16;
+    return to + t * stride + (h - t * heads) * D;
+  }
+  // (columns with a value that is not finite are gone over again: repair_columns)
+  __device__ __forceinline__ void look(int h, float x) const {
+    if (MULTI && !(x * 0.f == 0.f)) atomicOr(spoilt, 1u << h);
+  }
+};
+template <int D, bool MULTI, class A>
+__device__ __forceinline__ Out<D, MULTI> out_of(const A& a, int b, int kvh, uint32_t* spoilt) {
+  const CacheGeom& g = a.geom;
+  const size_t stride = (size_t)g.Hq * D;
+  bf16* base = static_cast<bf16*>(a.out) + (size_t)kvh * g.G * D;
+  if constexpr (!MULTI) return {base + b * stride, g.G, 1, 0, stride, nullptr};
+  const int4 part = part_of(a, b);
+  return {base + part.x * stride, g.G, part.y, a.rcp, stride, spoilt};
+}
+
 // Adds up n <= kGroup states and stores the outputs (out) or the sum (dst); 4 warps. State 0
 // is at `first`, state j > 0 at rest + j * stride. A lane owns four values at a time, all
 // states' of them on their way at once, and the lanes of a head hold the states' maxima and
 // sums between them.
-template <int D>
-__device__ __forceinline__ void join(int n, const float* first, const float* rest, int stride, int G, bf16* out, float* dst) {
+template <int D, bool MULTI>
+__device__ __forceinline__ void join(int n, const float* first, const float* rest, int stride, int G,
+                                     const Out<D, MULTI>& out, float* dst) {
   const int lane = threadIdx.x & 31, src = lane & 16;
 #pragma unroll 1
   for (int v = threadIdx.x & 127; v < (G * (D / 4) + 31) / 32 * 32; v += 128) {
@@ -315,10 +358,13 @@ __device__ __forceinline__ void join(int n, const float* first, const float* res
       }
     }
     if (!mine) continue;
-    if (out) {
-      const float inv = 1.f / L;
-      *reinterpret_cast<uint2*>(out + v * 4) =
-          make_uint2(float2_to_bf16x2(O.x * inv, O.y * inv), float2_to_bf16x2(O.z * inv, O.w * inv));
+    if (dst == nullptr) {
+      const float inv = MULTI && L == 0.f ? 0.f : 1.f / L;  // (a token that sees no key)
+      if (out.has(h)) {
+        *reinterpret_cast<uint2*>(out.at(h) + (v % (D / 4)) * 4) =
+            make_uint2(float2_to_bf16x2(O.x * inv, O.y * inv), float2_to_bf16x2(O.z * inv, O.w * inv));
+        out.look(h, (O.x + O.y + O.z + O.w) * inv);
+      }
     } else {
       __stcg(reinterpret_cast<float4*>(dst) + v, O);
       if (v % (D / 4) == 0) {
@@ -331,8 +377,9 @@ __device__ __forceinline__ void join(int n, const float* first, const float* res
 
 // After CTA p stored its state of an item that CTAs f .. last share: the last of a group to
 // arrive joins the group, the last group the item. The 128 threads of named barrier 2.
-template <int D>
-__device__ __forceinline__ void join_item(const PagedDecodeArgs& a, int p, int f, int last, int G, bf16* out,
+// Whether it has stored the outputs.
+template <int D, bool MULTI, class A>
+__device__ __forceinline__ bool join_item(const A& a, int p, int f, int last, int G, const Out<D, MULTI>& out,
                                           volatile int* flag) {
   constexpr int kCta = 4 * state_floats(D);
   const int groups = (last - f) / kGroup + 1, p0 = f + (p - f) / kGroup * kGroup;
@@ -348,11 +395,11 @@ __device__ __forceinline__ void join_item(const PagedDecodeArgs& a, int p, int f
       *flag = done;
     }
     named_barrier_sync(2, 128);
-    if (!*flag) return;
+    if (!*flag) return false;
     const bool whole = step > 1 || groups == 1;
-    join<D>(n, state_slot(a, first, slot, D), state_slot(a, first, slot_rest, D), step * kCta, G, whole ? out : nullptr,
-            state_slot(a, p0, p0 == f ? 3 : 2, D));
-    if (whole) return;
+    join<D, MULTI>(n, state_slot(a, first, slot, D), state_slot(a, first, slot_rest, D), step * kCta, G, out,
+                   whole ? nullptr : state_slot(a, p0, p0 == f ? 3 : 2, D));
+    if (whole) return true;
     first = f;
     slot = 3;
     slot_rest = 2;
@@ -362,12 +409,77 @@ __device__ __forceinline__ void join_item(const PagedDecodeArgs& a, int p, int f
   }
 }
 
+// Several tokens: a key that some of them see and others do not has a weight of zero for these, and zero
+// times a NaN or an infinity of its V row is a NaN. Columns (of `mask`) with an output that is not finite come here; one whose
+// token has such a V row among the keys that only others see (its followers', and those that leave the window) is
+// computed again from the keys that it sees, the newest first, and its numbers d0 .. d1 - 1 stored. The 128
+// threads of named barrier 2, a warp a column.
+template <int D, class A>
+__device__ __noinline__ void repair_columns(const A& a, int b, int kvh, int len, uint32_t mask, int d0, int d1) {
+  constexpr int N = D / 32;
+  const CacheGeom& g = a.geom;
+  const int4 part = part_of(a, b);
+  const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) & 3;
+  const int32_t* pages = a.table + (size_t)part.z * a.table_stride;
+  const bool strm = g.kind[kvh] != 0;
+  float q[N], k[N], v[N];
+  for (int h = 0; mask >> h; ++h) {
+    if (!(mask >> h & 1) || (h & 3) != warp) continue;
+    const int t = (h * a.rcp) >> 16, head = kvh * g.G + h - t * g.G;
+    const int pos = len - part.y + t, w0 = strm ? max(0, pos - g.W + 1) : 0, sinks = strm ? min(g.S, w0) : 0;
+    float bad = 0.f;
+    auto look = [&](int from, int to) {
+      for (int j = max(from, 0); j < to; ++j) {
+        rows::load_key<D>(a.pool, pages, kvh, j, 1, lane, v);
+#pragma unroll
+        for (int n = 0; n < N; ++n) bad = fmaf(v[n], 0.f, bad);
+      }
+    };
+    look(pos + 1, len);
+    if (strm) look(max(w0 - a.tokens, sinks), w0);
+    if (!__any_sync(0xffffffffu, !(bad == 0.f)) || pos < 0) continue;
+    const bf16* from = static_cast<const bf16*>(a.q) + (size_t)(part.x + t) * a.q_stride + head * D + lane * N;
+#pragma unroll
+    for (int n = 0; n < N; ++n) q[n] = __bfloat162float(from[n]);
+    float o[N] = {}, m = -INFINITY, l = 0.f;
+    for (int j = pos; j >= 0; --j) {
+      if (j < w0) j = min(j, sinks - 1);
+      if (j < 0) break;
+      rows::load_key<D>(a.pool, pages, kvh, j, 0, lane, k);
+      rows::load_key<D>(a.pool, pages, kvh, j, 1, lane, v);
+      float x = 0.f;
+#pragma unroll
+      for (int n = 0; n < N; ++n) x = fmaf(q[n], k[n], x);
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+      x *= a.scale_log2;
+      const float top = fmaxf(m, x), base = top == -INFINITY ? 0.f : top;
+      const float f = fast_exp2(m - base), w = fast_exp2(x - base);
+      m = top;
+      l = l * f + w;
+      bool done = l > 0.f;  // with every number a NaN, which it stays
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        o[n] = o[n] * f + w * v[n];
+        done = done && isnan(o[n]);
+      }
+      if (isnan(l) || __all_sync(0xffffffffu, done)) break;
+    }
+    bf16* to = static_cast<bf16*>(a.out) + ((size_t)(part.x + t) * g.Hq + head) * D + lane * N;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+      if (lane * N + n >= d0 && lane * N + n < d1) to[n] = __float2bfloat16_rn(l == 0.f ? 0.f : o[n] / l);
+  }
+}
+
 // Powers of two as floats.
 __device__ __forceinline__ float pow2i(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
 
-template <int D, bool F8, int GP, bool CL>
+// MULTI: parts of sequences (a.seqs), of up to a.tokens tokens whose query heads are the columns.
+template <int D, bool F8, int GP, bool CL, bool MULTI>
 __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
-    paged_decode_kernel(const __grid_constant__ PagedDecodeArgs a) {
+    paged_decode_kernel(const __grid_constant__ std::conditional_t<MULTI, PagedPartsArgs, PagedDecodeArgs> a) {
+  using A = std::conditional_t<MULTI, PagedPartsArgs, PagedDecodeArgs>;
   using C = Lay<D, F8, GP, CL>;
   constexpr int NK = C::NK, NW = C::NW, KP = C::KP, LG = NK == 1 ? 7 : NK == 2 ? 8 : 9;
   static_assert(1 << LG == C::KEYS, "keys of a tile");
@@ -399,6 +511,7 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   volatile int* flag = reinterpret_cast<volatile int*>(tmem_slot + 2);
   int* first_s = reinterpret_cast<int*>(tmem_slot + 3);  // [2] the run's first sequence, and its first tile
+  uint32_t* spoilt = tmem_slot + 5;                      // columns to be gone over again
   int* wsum = reinterpret_cast<int*>(smem + C::OFF_MISC + 32);
   uint8_t* heads_s = smem + C::OFF_MISC + 32 + 128;
   int* lens_s = reinterpret_cast<int*>(smem + C::OFF_LENS);
@@ -407,7 +520,7 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
 
   const CacheGeom& g = a.geom;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int G = g.G, lg = a.pool.lg_ps;
+  const int G = MULTI ? g.G * a.tokens : g.G, lg = a.pool.lg_ps;  // columns
 
   // rows of Q and P that no head fills stay zero for the whole launch
   for (int i = threadIdx.x; i < (C::NQ * C::QBUF + C::NPB * C::PBUF) / 16; i += NT)
@@ -435,6 +548,7 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
     mbar_init(drain, 1);
     *abort_flag = 0;
     first_s[0] = first_s[1] = 0;
+    spoilt[0] = 0;
     fence_mbar_init();
   }
   if (warp == kLoadK && lane == 0) prefetch_tmap(&a.pages);
@@ -459,7 +573,7 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
   auto plan = [&]() {
     if constexpr (CL) {
       const int id = p >> lg_ctas, b = quotient(id, g.Hkv);
-      return ClusterWalk<LG>(a, heads_s, seq_len(a, b, rank == 0 && threadIdx.x == 0), b, id - b * g.Hkv, rank, lg_ctas);
+      return ClusterWalk<A, LG>(a, heads_s, seq_len(a, b, rank == 0 && threadIdx.x == 0), b, id - b * g.Hkv, rank, lg_ctas);
     } else {
       // ---- this CTA's run: a prefix sum of the sequences' tiles; up to 32 sequences every warp
       // forms it for itself, a lane a sequence, without a barrier
@@ -521,7 +635,7 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
         seq_off = first_s[1];
       }
       const bool any = p < deal.P;
-      return Walk<LG>(a, mirrored ? lens_s : nullptr, heads_s, len_reg, any ? deal.first(p) : deal.total,
+      return Walk<A, LG>(a, mirrored ? lens_s : nullptr, heads_s, len_reg, any ? deal.first(p) : deal.total,
                       any ? deal.first(p + 1) : deal.total, b_first, any ? seq_off : deal.total);
     }
   };
@@ -540,7 +654,7 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
     int it = 0;
     bool ok = true;
     while (ok && walk.next()) {
-      const int32_t* row = a.table + (size_t)walk.b * a.table_stride;
+      const int32_t* row = a.table + (size_t)(MULTI ? part_of(a, walk.b).z : walk.b) * a.table_stride;
       const int slots = walk.slots(), kvh = walk.kvh();
       for (int j = walk.lo; j < walk.hi; ++j, ++it) {
         const int st = it % C::NS;
@@ -632,11 +746,18 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
     constexpr int QV = (GP * CPR + 31) / 32;
     uint4 qr[QV];
     auto fetch = [&](int b, int kvh) {
-      const bf16* qg = static_cast<const bf16*>(a.q) + (size_t)b * a.q_stride + (size_t)kvh * G * D;
+      const int4 part = MULTI ? part_of(a, b) : make_int4(b, 1, b, 0);
+      const bf16* qg = static_cast<const bf16*>(a.q) + (size_t)part.x * a.q_stride + (size_t)kvh * g.G * D;
 #pragma unroll
       for (int i = 0; i < QV; ++i) {
         const int c = lane + 32 * i;
-        qr[i] = c < G * CPR ? *reinterpret_cast<const uint4*>(qg + c * 8) : make_uint4(0, 0, 0, 0);
+        if constexpr (MULTI) {
+          const int h = c / CPR, t = (h * a.rcp) >> 16;
+          qr[i] = c < G * CPR && t < part.y ? *reinterpret_cast<const uint4*>(qg + t * a.q_stride + (c - t * g.G * CPR) * 8)
+                                            : make_uint4(0, 0, 0, 0);
+        } else {
+          qr[i] = c < G * CPR ? *reinterpret_cast<const uint4*>(qg + c * 8) : make_uint4(0, 0, 0, 0);
+        }
       }
     };
     bool more = walk.next();
@@ -735,8 +856,9 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
     // sequences without a token
     for (int b = p; !CL && b < a.n_seqs; b += gridDim.x)
       if ((few ? __shfl_sync(0xffffffffu, len_reg, b) : mirrored ? lens_s[b] : seq_len(a, b, false)) == 0)
-        for (int i = r; i < g.Hq * D / 8; i += 128)
-          reinterpret_cast<uint4*>(static_cast<bf16*>(a.out) + (size_t)b * g.Hq * D)[i] = make_uint4(0, 0, 0, 0);
+        for (int i = r; i < g.Hq * D / 8 * (MULTI ? part_of(a, b).y : 1); i += 128)
+          reinterpret_cast<uint4*>(static_cast<bf16*>(a.out) + (size_t)(MULTI ? part_of(a, b).x : b) * g.Hq * D)[i] =
+              make_uint4(0, 0, 0, 0);
     // clusters: row r's values to the CTA that finishes it, head r's state to all
     const int lg_rows = CL ? (D == 128 ? 7 : 6) - lg_ctas : 0;
     auto push = [&](const float (&o)[GP], float m, float l) {
@@ -761,7 +883,7 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
     while (ok && walk.next()) {
       const int x = item & 1;
       const int f = CL ? 0 : deal.cta_of(walk.off), last = CL ? 0 : deal.cta_of(walk.off + walk.tiles - 1);
-      bf16* out = static_cast<bf16*>(a.out) + ((size_t)walk.b * g.Hq + (size_t)walk.kvh() * G) * D;
+      const Out<D, MULTI> out = out_of<D, MULTI>(a, walk.b, walk.kvh(), spoilt);
       ok = wait_bar(&l_full[x], (item >> 1) & 1, a.err, abort_flag);
       ok = wait_bar(&o_full[x], (item >> 1) & 1, a.err, abort_flag) && ok;
       tc_fence_after();
@@ -802,7 +924,11 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
       } else if (f == last) {
 #pragma unroll
         for (int h = 0; h < GP; ++h)
-          if (r < D && h < G) out[h * D + r] = __float2bfloat16_rn(__fdividef(o[h], sum_of(h)));
+          if (r < D && h < G && out.has(h)) {
+            const float L = sum_of(h), y = MULTI && L == 0.f ? 0.f : __fdividef(o[h], L);
+            out.at(h)[r] = __float2bfloat16_rn(y);
+            out.look(h, y);
+          }
         if (D == 64) named_barrier_sync(2, 128);  // `upper` has been read
       } else {
         float* slot = state_slot(a, p, p == f ? 1 : 0, D);
@@ -818,8 +944,19 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
       __syncwarp();
       if (lane == 0) mbar_arrive(&o_free[x]);
       ++item;
-      if (f != last) {
-        join_item<D>(a, p, f, last, G, out, flag);
+      bool stored = !CL && f == last;
+      if (f != last) stored = join_item<D, MULTI>(a, p, f, last, G, out, flag);
+      if constexpr (MULTI && !CL) {
+        if (stored) {  // alike in the 128 threads
+          named_barrier_sync(2, 128);
+          const uint32_t mask = *reinterpret_cast<volatile uint32_t*>(spoilt);
+          if (mask) {
+            named_barrier_sync(2, 128);
+            if ((threadIdx.x & 127) == 0) *spoilt = 0;
+            repair_columns<D>(a, walk.b, walk.kvh(), walk.q.len, mask, 0, D);
+            named_barrier_sync(2, 128);
+          }
+        }
       }
     }
   } else {
@@ -833,6 +970,7 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
     while (ok && walk.next()) {
       const Seq& w = walk.q;
       const bool strm = walk.streaming();
+      const int tokens = MULTI ? part_of(a, walk.b).y : 1;
       float m[GP], l[GP];
       // V powers below this, 90 below the largest of the tiles that moved a maximum: a key of any other whose
       // weight is zero as a float has less than 2^-48 of the weight of the one that is the maximum. (Asking
@@ -847,6 +985,7 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
         const int x = it & 1, st = it % C::NS;
         const bool first = j == walk.lo;
         bool see[KP];
+        uint32_t cols[KP];  // several tokens: the columns that see the key
         int ek[KP], ev[KP];
         if (F8) local_ok = wait_bar(&k_full[st], (it / C::NS) & 1, a.err, abort_flag) && local_ok;
 #pragma unroll
@@ -855,6 +994,13 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
           const int slot = (j << (LG - lg)) + (key >> lg);
           const long long pos = ((long long)walk.page_of_slot(slot) << lg) + (key & (a.pool.ps - 1));
           see[c] = pos < w.len && (!strm || pos < g.S || pos >= w.w0);
+          if constexpr (MULTI) {
+            // token t sits at w.len - tokens + t: it sees the key from `lo` on, up to `hi`
+            const long long d = pos - (w.len - tokens);
+            const int lo = (int)max(d, 0ll), hi = strm && pos >= g.S ? (int)max(min(d + g.W, (long long)tokens), 0ll) : tokens;
+            cols[c] = see[c] && lo < hi ? (1u << hi * g.G) - (1u << lo * g.G) : 0u;
+            see[c] = cols[c] != 0;
+          }
           const unsigned hidden = __ballot_sync(0xffffffffu, !see[c]);
           ek[c] = ev[c] = 0;
           if constexpr (F8) {
@@ -886,6 +1032,7 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&s_free[x]);
+        auto sees = [&](int c, int h) { return MULTI ? (cols[c] >> h & 1) != 0 : see[c]; };
         float s[KP][GP];
 #pragma unroll
         for (int c = 0; c < KP; ++c) {
@@ -897,7 +1044,7 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
                              (float)ev[c]);
             else
               s[c][h] = __uint_as_float(v[c][h]) * a.scale_log2;
-            if (!see[c]) s[c][h] = -INFINITY;
+            if (!sees(c, h)) s[c][h] = -INFINITY;
           }
         }
         // the running maximum moves only when a key is far above it; all threads agree
@@ -975,7 +1122,7 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
 #pragma unroll
             for (int h = 0; h < GP; ++h) {
               const float low = s[c][h] - m[h] + C::kRaise;
-              if (see[c] && low < -126.f) {
+              if (sees(c, h) && low < -126.f) {
                 l[h] += fast_exp2(low - (float)ev[c]);
                 s[c][h] = -INFINITY;
               }
@@ -989,7 +1136,7 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
           const int y = (t + c * C::SOFT) >> 7;
           float pr[GP];
 #pragma unroll
-          for (int h = 0; h < GP; ++h) pr[h] = see[c] ? fast_exp2(s[c][h] - m[h] + C::kRaise) : 0.f;
+          for (int h = 0; h < GP; ++h) pr[h] = sees(c, h) ? fast_exp2(s[c][h] - m[h] + C::kRaise) : 0.f;
           // weights of key r of group y -> column r of the K-major [NPV][128 keys] buffer of its set
           uint8_t* pb = sP + (it % C::NPB) * C::PBUF + (y / C::MB) * C::PSET;
           const int n0 = (y % C::MB) * GP;
@@ -1059,7 +1206,7 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
     cluster_wait();
     if (warp >= kFinish && warp < kFinish + 4) {
       const int lg_rows = (D == 128 ? 7 : 6) - lg_ctas, n = 1 << lg_ctas;
-      bf16* out = static_cast<bf16*>(a.out) + ((size_t)walk.b * g.Hq + (size_t)walk.kvh() * G) * D + (rank << lg_rows);
+      const Out<D, MULTI> out = out_of<D, MULTI>(a, walk.b, walk.kvh(), spoilt);
       for (int i = threadIdx.x & 127; i < G << lg_rows; i += 128) {
         const int h = i >> lg_rows;
         float M = -INFINITY, L = 0.f, O = 0.f;
@@ -1073,7 +1220,16 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
           O += w * recv[((c * G) << lg_rows) + i];
         }
         // (a sequence without a token: zeros)
-        out[(size_t)h * D + (i & ((1 << lg_rows) - 1))] = __float2bfloat16_rn(walk.tiles == 0 ? 0.f : O / L);
+        const float y = walk.tiles == 0 || (MULTI && L == 0.f) ? 0.f : O / L;
+        if (out.has(h)) {
+          out.at(h)[(rank << lg_rows) + (i & ((1 << lg_rows) - 1))] = __float2bfloat16_rn(y);
+          out.look(h, y);
+        }
+      }
+      if constexpr (MULTI) {
+        named_barrier_sync(2, 128);
+        const uint32_t mask = *spoilt;
+        if (mask) repair_columns<D>(a, walk.b, walk.kvh(), walk.q.len, mask, rank << lg_rows, (rank + 1) << lg_rows);
       }
     }
   }
@@ -1083,10 +1239,10 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
 }
 
 // cluster: CTAs of a cluster, 0: no clusters.
-template <int D, bool F8, int GP, bool CL>
-cudaError_t launch(const PagedDecodeArgs& a, int ctas, int cluster, cudaStream_t s) {
+template <int D, bool F8, int GP, bool CL, class A>
+cudaError_t launch(const A& a, int ctas, int cluster, cudaStream_t s) {
   using C = Lay<D, F8, GP, CL>;
-  auto kernel = paged_decode_kernel<D, F8, GP, CL>;
+  auto kernel = paged_decode_kernel<D, F8, GP, CL, std::is_same<A, PagedPartsArgs>::value>;
   static std::atomic<uint64_t> done{0};
   const cudaError_t e = once_per_device(done, [&] {
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
@@ -1111,8 +1267,8 @@ cudaError_t launch(const PagedDecodeArgs& a, int ctas, int cluster, cudaStream_t
   return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
-template <int D, bool F8, int GP>
-cudaError_t launch_split(const PagedDecodeArgs& a, int num_sms, int cluster, cudaStream_t s) {
+template <int D, bool F8, int GP, class A>
+cudaError_t launch_split(const A& a, int num_sms, int cluster, cudaStream_t s) {
   if (cluster > 0) return launch<D, F8, GP, true>(a, a.n_seqs * a.geom.Hkv * cluster, cluster, s);
   return launch<D, F8, GP, false>(a, num_sms, 0, s);
 }
@@ -1123,6 +1279,12 @@ cudaError_t launch_heads(const PagedDecodeArgs& a, int num_sms, int cluster, cud
   if (G <= 2) return launch_split<D, F8, 2>(a, num_sms, cluster, s);
   if (G <= 4) return launch_split<D, F8, 4>(a, num_sms, cluster, s);
   if (G <= 8) return launch_split<D, F8, 8>(a, num_sms, cluster, s);
+  return launch_split<D, F8, 16>(a, num_sms, cluster, s);
+}
+
+template <int D, bool F8>
+cudaError_t launch_parts(const PagedPartsArgs& a, int num_sms, int cluster, cudaStream_t s) {
+  if (a.geom.G * a.tokens <= 8) return launch_split<D, F8, 8>(a, num_sms, cluster, s);
   return launch_split<D, F8, 16>(a, num_sms, cluster, s);
 }
 

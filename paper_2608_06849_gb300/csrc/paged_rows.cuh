@@ -1,5 +1,5 @@
-// What the kernels over rows of a paged cache share (paged_rows.cu, rotate.cu, paged_attend.cuh):
-// where a row of a call lies, and 16 numbers of it.
+// What the kernels over rows of a paged cache share (paged_rows.cu, rotate.cu, paged_attend.cuh,
+// paged_decode.cuh): where a row of a call lies, and numbers of it.
 #pragma once
 
 #include <cuda_fp8.h>
@@ -107,6 +107,38 @@ __device__ __forceinline__ Sixteen decode(const uint4& c, int e) {
     x.w[i] = float2_to_bf16x2(y.x, y.y);
   }
   return x;
+}
+
+// A lane's D / 32 numbers of key j of one head, of K (sel 0) or V, of a sequence with these pages (a page out of
+// range: zeros).
+template <int D>
+__device__ __forceinline__ void load_key(const PagePool& pool, const int32_t* pages, int head, int j, int sel, int lane,
+                                         float (&to)[D / 32]) {
+  const int page = __ldg(pages + (j >> pool.lg_ps)), row = j & (pool.ps - 1);
+  if ((unsigned)page >= (unsigned)pool.n_pages) {
+#pragma unroll
+    for (int n = 0; n < D / 32; ++n) to[n] = 0.f;
+    return;
+  }
+  const size_t at = (((((size_t)page * 2 + sel) * pool.Hkv + head) << pool.lg_ps) + row) * D + lane * (D / 32);
+  if (pool.form == 0) {
+#pragma unroll
+    for (int n = 0; n < D / 32; n += 2) {
+      const float2 f = bf16x2_to_float2(*reinterpret_cast<const uint32_t*>(static_cast<const __nv_bfloat16*>(pool.data) + at + n));
+      to[n] = f.x;
+      to[n + 1] = f.y;
+    }
+  } else {
+    const int e = pool.powers[((((size_t)page * pool.Hkv + head) * 2 + sel) << pool.lg_ps) + row];
+    const float scale = __uint_as_float((uint32_t)(127 + e) << 23);
+#pragma unroll
+    for (int n = 0; n < D / 32; n += 2) {
+      const uint16_t two = *reinterpret_cast<const uint16_t*>(static_cast<const uint8_t*>(pool.data) + at + n);
+      const float2 f = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2(two, __NV_E4M3)));
+      to[n] = f.x * scale;
+      to[n + 1] = f.y * scale;
+    }
+  }
 }
 
 // What earlier kernels wrote is visible from here on; the next one may start its prologue.

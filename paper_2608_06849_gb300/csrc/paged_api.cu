@@ -5,6 +5,7 @@
 #include <stdio.h>
 #include <string.h>
 
+#include <mutex>
 #include <new>
 #include <vector>
 
@@ -14,18 +15,19 @@
 
 using namespace aoh;
 
+constexpr int kPartsASeq = 4;
+
 struct aoh_paged {
   aoh_paged_config cfg;
   CacheGeom geom;  // heads, S and W
   PagePool pool;
   int device = 0, num_sms = 0;
   void* meta = nullptr;  // the device arrays below
-  int4* d_seqs = nullptr;
+  int4* d_seqs = nullptr;  // lists of sequences, or of up to kPartsASeq parts each
   uint32_t* d_err = nullptr;
   uint32_t* d_counters = nullptr;  // decode: arrivals, zero between calls
   float* d_states = nullptr;       // decode: states of items that CTAs share
   CUtensorMap pages;               // of the pool, which does not move
-  cudaMemPool_t expand_pool = nullptr;  // pages written out as bf16, from call to call
 };
 
 namespace {
@@ -178,30 +180,58 @@ cudaError_t sm_count(int* n) {
   return e;
 }
 
-// Device memory of a call that is not captured, ordered on its stream; null if there is none to be had. The
-// handle's own pool keeps it from call to call.
-void* expand_memory(aoh_paged* h, size_t bytes, cudaStream_t s) {
+// Memory for pages written out as bf16: a pool of each device, which keeps it from call to call for all handles
+// (a model's layers use the same), and gives it back with the last handle.
+struct ExpandPools {
+  static constexpr int kMost = 64;
+  std::mutex lock;
+  cudaMemPool_t pool[kMost] = {};
+  int handles[kMost] = {};
+};
+ExpandPools& expand_pools() {
+  static ExpandPools pools;
+  return pools;
+}
+
+// One handle more or less on a device.
+void expand_memories(int device, int handles) {
+  ExpandPools& p = expand_pools();
+  if (device < 0 || device >= ExpandPools::kMost) return;
+  std::lock_guard<std::mutex> hold(p.lock);
+  p.handles[device] += handles;
+  if (p.handles[device] == 0 && p.pool[device]) cudaMemPoolTrimTo(p.pool[device], 0);
+}
+
+// Device memory of a call that is not captured, ordered on its stream; null if there is none to be had.
+void* expand_memory(int device, size_t bytes, cudaStream_t s) {
   cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
   void* p = nullptr;
+  if (device >= ExpandPools::kMost) return nullptr;
   if (cudaStreamIsCapturing(s, &capture) != cudaSuccess || capture != cudaStreamCaptureStatusNone) {
     cudaGetLastError();
     return nullptr;
   }
-  if (!h->expand_pool) {
-    cudaMemPoolProps props;
-    memset(&props, 0, sizeof(props));
-    props.allocType = cudaMemAllocationTypePinned;
-    props.location.type = cudaMemLocationTypeDevice;
-    props.location.id = h->device;
-    uint64_t keep = UINT64_MAX;
-    if (cudaMemPoolCreate(&h->expand_pool, &props) != cudaSuccess) {
-      h->expand_pool = nullptr;
-      cudaGetLastError();
-      return nullptr;
+  cudaMemPool_t pool = nullptr;
+  {
+    ExpandPools& pools = expand_pools();
+    std::lock_guard<std::mutex> hold(pools.lock);
+    if (!pools.pool[device]) {
+      cudaMemPoolProps props;
+      memset(&props, 0, sizeof(props));
+      props.allocType = cudaMemAllocationTypePinned;
+      props.location.type = cudaMemLocationTypeDevice;
+      props.location.id = device;
+      uint64_t keep = UINT64_MAX;
+      if (cudaMemPoolCreate(&pools.pool[device], &props) != cudaSuccess) {
+        pools.pool[device] = nullptr;
+        cudaGetLastError();
+        return nullptr;
+      }
+      cudaMemPoolSetAttribute(pools.pool[device], cudaMemPoolAttrReleaseThreshold, &keep);
     }
-    cudaMemPoolSetAttribute(h->expand_pool, cudaMemPoolAttrReleaseThreshold, &keep);
+    pool = pools.pool[device];
   }
-  if (cudaMallocFromPoolAsync(&p, bytes, h->expand_pool, s) != cudaSuccess) {
+  if (cudaMallocFromPoolAsync(&p, bytes, pool, s) != cudaSuccess) {
     cudaGetLastError();
     return nullptr;
   }
@@ -239,7 +269,7 @@ bool parts_of(const aoh_paged* h, const std::vector<int4>& seqs, const std::vect
   const bool f8 = h->cfg.form == AOH_PAGES_E4M3;
   const double each_ns = !f8 ? 10.6 : g.G * *tokens <= 8 ? 5.5 : 8;
   if (6 + visits * each_ns * scale > 10 + work * (f8 ? 18 : 14) * scale) return false;
-  if (n > PackedSeqs::kMost && n > h->cfg.max_seqs) return false;  // the device's list holds no more
+  if (n > PackedSeqs::kMost && n > (long long)kPartsASeq * h->cfg.max_seqs) return false;  // more than the device's list holds
   parts->reserve(n);
   for (const int4& s : seqs) {
     const int count = (s.y + most - 1) / most, each = (s.y + count - 1) / count;
@@ -340,7 +370,7 @@ aoh_status aoh_paged_init(const aoh_paged_config* cfg, const uint8_t* head_label
   cudaError_t e = cudaGetDevice(&h->device);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&h->num_sms, cudaDevAttrMultiProcessorCount, h->device);
   const size_t counters = ((size_t)h->num_sms * 3 * 4 + 255) / 256 * 256;
-  const size_t seqs = ((size_t)c.max_seqs * sizeof(int4) + 255) / 256 * 256;
+  const size_t seqs = ((size_t)c.max_seqs * kPartsASeq * sizeof(int4) + 255) / 256 * 256;
   const size_t meta = 256 + counters + seqs + paged_state_floats(h->num_sms, c.d_head) * 4;
   if (e == cudaSuccess) e = cudaMalloc(&h->meta, meta);
   if (e == cudaSuccess) e = cudaMemset(h->meta, 0, meta);
@@ -360,6 +390,7 @@ aoh_status aoh_paged_init(const aoh_paged_config* cfg, const uint8_t* head_label
     delete h;
     return fail(AOH_ERR_CUDA, "cuTensorMapEncodeTiled failed for the pages");
   }
+  expand_memories(h->device, 1);
   *out = h;
   return AOH_OK;
 }
@@ -474,7 +505,8 @@ aoh_status aoh_paged_append_rotated(aoh_paged* cache, const aoh_rope* rope, cons
   if (st == AOH_OK) st = check_in_place("q", q, q_stride, q_out, q_out_stride);
   if (st == AOH_OK) st = check_table(cache, table, table_stride);
   if (st != AOH_OK) return st;
-  if (!lens) return fail(AOH_ERR_INVALID, "lens must not be NULL");
+  if (!lens || !aligned(lens, 4) || !aligned(cu_rows, 4) || !aligned(positions, 4))
+    return fail(AOH_ERR_INVALID, "lens, cu_rows and positions must be 4-byte aligned device pointers, lens not NULL");
   RotateArgs a;
   set_rotation(&a, rope, norms);
   a.Hq = c.n_q_heads;
@@ -748,7 +780,7 @@ aoh_status aoh_paged_attend(aoh_paged* cache, const void* q, int64_t q_stride, c
   void* written = nullptr;
   if (expand_plan(cache, planned, work, &expanded)) {
     const size_t pages = (size_t)expanded.first[expanded.n];
-    written = expand_memory(cache, pages * 2 * c.n_kv_heads * 128 * c.d_head * 2, s);
+    written = expand_memory(cache->device, pages * 2 * c.n_kv_heads * 128 * c.d_head * 2, s);
   }
   bool covered = false;  // whether all sequences fit there, whatever their lengths
   if (written) {
@@ -808,7 +840,7 @@ aoh_status aoh_paged_check(aoh_paged* cache, void* stream) {
 
 void aoh_paged_destroy(aoh_paged* cache) {
   if (!cache) return;
-  if (cache->expand_pool) cudaMemPoolDestroy(cache->expand_pool);
+  expand_memories(cache->device, -1);
   if (cache->meta) cudaFree(cache->meta);
   delete cache;
 }

@@ -334,8 +334,9 @@ __global__ void __launch_bounds__(kThreads, kBlocks) rotate_kernel(const __grid_
 // kernel before it.
 template <int D, int FORM>
 cudaError_t launch(const RotateArgs& a, int num_sms, cudaStream_t s) {
+  // as many groups for every block, of as few rows as then do
   const int n = a.rows.n_rows, blocks = kBlocks * num_sms, even = (n + blocks - 1) / blocks;
-  const int per = even < kMostRows ? even : kMostRows, groups = (n + per - 1) / per;
+  const int each = (even + kMostRows - 1) / kMostRows, per = (even + each - 1) / each, groups = (n + per - 1) / per;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(groups < blocks ? groups : blocks));
   cfg.blockDim = dim3(kThreads);

@@ -363,3 +363,73 @@ def test_written_out_after_an_append_in_flight():
         if step % 3 == 2:
             c.matches(f"step {step}")
     c.c.check()
+
+
+FEW = [
+    # a few rows a sequence: parts of it beside one another on the decode kernel
+    # q_lens, k_lens, Hq, Hkv, d, labels, sink, window, page
+    ([4, 1, 3, 2], [4, 500, 2000, 131], 8, 2, 128, [0, 1], 3, 40, 16),
+    ([5], [3000], 28, 4, 128, [1, 0, 0, 1], 16, 300, 64),
+    ([3, 5, 2], [900, 5, 40], 16, 1, 64, [0], 0, 1, 32),
+    ([8, 7], [1030, 260], 4, 2, 64, [1, 0], 100, 129, 128),
+    ([16, 11], [400, 6000], 3, 3, 128, [0, 1, 1], 5, 64, 16),
+    # fewer positions than rows, and none
+    ([4, 3, 2, 4], [2, 0, 1, 0], 8, 2, 64, [0, 1], 3, 40, 16),
+    # more parts than travel by value, windows that move within a part
+    ([1 + i % 4 for i in range(80)], [1 + i % 4 + 53 * (i % 11) for i in range(80)], 32, 8, 128, [0, 1] * 4, 2, 3, 16),
+    ([6] * 30, [40 + 97 * (i % 13) for i in range(30)], 24, 8, 64, [1, 0] * 4, 0, 5, 64),
+    ([2] * 20, [9000 + i for i in range(20)], 32, 8, 64, [0] * 8, 0, 1, 64),
+]
+
+
+@pytest.mark.parametrize("form", ["bf16", "e4m3"])
+@pytest.mark.parametrize("case", range(len(FEW)))
+def test_few_rows(case, form):
+    c = Case(*FEW[case], form, seed=300 + case, fused=case % 2 == 0, spread=1.5)
+    for hint in (c.k_lens, [0] * len(c.k_lens)):  # (the latter takes any of these calls there)
+        c.out.fill_(float("nan"))
+        c.attend(k_lens=hint)
+        c.matches(f"few rows {case}, hint {hint[:3]}")
+
+
+@pytest.mark.parametrize("form", ["bf16", "e4m3"])
+@pytest.mark.parametrize("case", range(len(FEW)))
+def test_spoilt_keys_among_few_rows(case, form):
+    """K and V that are not finite at the rows' own positions and around the beginnings of their windows reach
+    the rows that see them, and no other of the same sequence."""
+    c = Case(*FEW[case], form, seed=400 + case)
+    hint = [0] * len(c.k_lens)
+    clean = f64(c.attend(k_lens=hint))
+    ks, qs, hkv = sums(c.k_lens), sums(c.q_lens), len(c.labels)
+    G = c.q.shape[1] // hkv
+    for what in ("v nan", "v inf", "k nan"):
+        k, v, bad = c.k.clone(), c.v.clone(), []
+        for b, (n, m) in enumerate(zip(c.q_lens, c.k_lens)):
+            # the last rows' keys but the very last; a key that leaves the window within the chunk
+            at = sorted({p for p in (m - 1 - n // 2, m - n - c.window + 2, m - 2) if 0 <= p < m - 1})[:1 + (case + b) % 3]
+            bad.append(at)
+            for j in at:
+                (k if what == "k nan" else v)[ks[b] + j, :, (j * 7) % c.q.shape[2]] = float("inf" if what == "v inf" else "nan")
+        c.c.append(k, v, c.lens, c.table, cu_rows=ints(ks))
+        c.out.fill_(0)
+        out = f64(c.attend(k_lens=hint))
+        for b, (n, m) in enumerate(zip(c.q_lens, c.k_lens)):
+            pos, j = np.arange(m - n, m)[:, None], np.array(bad[b], dtype=int)[None, :]
+            for h in range(c.q.shape[1]):
+                see = j <= pos
+                if c.labels[h // G]:
+                    see &= (j < c.sink) | (pos - j < c.window)
+                rows, hit = np.arange(qs[b], qs[b + 1]), see.any(1)
+                got = out[rows, h]
+                if what == "k nan":
+                    assert np.isnan(got[hit]).all(), (what, b, h)
+                elif hit.any():
+                    assert not np.isfinite(got[hit]).all(1).any(), (what, b, h)
+                ok = clean[rows[~hit], h]
+                # (rows that are gone over again are summed in another order; 8-bit codes of a row whose largest
+                # number became an infinity are those of its other numbers)
+                if form == "bf16" or what != "v inf":
+                    assert (np.abs(got[~hit] - ok) <= 2.0 ** -6 * np.abs(ok) + 0.02).all(), (what, b, h)
+                else:
+                    assert np.isfinite(got[~hit]).all(), (what, b, h)
+        c.c.append(c.k, c.v, c.lens, c.table, cu_rows=ints(ks))

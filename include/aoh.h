@@ -542,8 +542,8 @@ size_t aoh_paged_bytes(const aoh_paged_config* cfg);
 /*
  * Bind a caller-owned device buffer as the pool (256-byte aligned; not freed by the
  * library; contents need not be initialised). head_labels: host [n_kv_heads], copied. Allocates the handle's
- * small device arrays and synchronises the device once; no later call
- * allocates. Errors: INVALID, CAPACITY, UNSUPPORTED, CUDA.
+ * small device arrays and synchronises the device once; no later call but
+ * aoh_paged_attend allocates. Errors: INVALID, CAPACITY, UNSUPPORTED, CUDA.
  */
 aoh_status aoh_paged_init(const aoh_paged_config* cfg, const uint8_t* head_labels, void* pool, size_t pool_bytes,
                           aoh_paged** out);
@@ -644,10 +644,13 @@ aoh_status aoh_paged_decode(aoh_paged* cache, const void* q, int64_t q_stride, c
  *   q_lens   host [n_seqs], >= 0; a captured call replays with the same ones
  *   lens     device [n_seqs]
  *   k_lens   host [n_seqs], or NULL: what the host takes lens to be (NULL: what the table holds). By
- *            them the work is split; the outputs are right whatever they are
+ *            them the work is split; the outputs are right whatever they are, and come soonest with close ones
  *   table    device [n_seqs][table_stride], of at most 2^30 tokens a row
  *   out      [rows][n_q_heads][d_head]
- * Errors: INVALID, CUDA.
+ * Long chunks over 8-bit pages take device memory, ordered on the stream: up to 4 * d_head * n_kv_heads
+ * bytes a token of k_lens (never more than 4 GiB), from a pool of the device that all handles share and that is given
+ * back with the last of them. A captured call takes none, nor does one for which there is none to be had:
+ * these take longer. Errors: INVALID, CUDA.
  */
 aoh_status aoh_paged_attend(aoh_paged* cache, const void* q, int64_t q_stride, const int32_t* q_lens,
                             const int32_t* lens, const int32_t* k_lens, int32_t n_seqs, const int32_t* table,

@@ -433,3 +433,29 @@ def test_spoilt_keys_among_few_rows(case, form):
                 else:
                     assert np.isfinite(got[~hit]).all(), (what, b, h)
         c.c.append(c.k, c.v, c.lens, c.table, cu_rows=ints(ks))
+
+
+def test_two_handles_on_two_streams():
+    """Written-out pages of two handles' calls that run at once lie apart."""
+    cases = [Case([900], [2500], 16, 4, 128, [0, 1, 0, 0], 20, 700, 32, "e4m3", seed=s) for s in (61, 62)]
+    wants = [c.attend(k_lens=c.k_lens).clone() for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    outs = [[torch.full_like(c.out, float("nan")) for _ in range(8)] for c in cases]
+    torch.cuda.synchronize()
+    for i in range(8):
+        for c, s, o in zip(cases, streams, outs):
+            c.c.attend(c.q, c.q_lens, c.lens, c.table, o[i], k_lens=c.k_lens, stream=s)
+    torch.cuda.synchronize()
+    for w, o in zip(wants, outs):
+        assert all(torch.equal(w, x) for x in o)
+
+
+def test_no_rows_and_no_sequences():
+    c = Case([3, 0], [40, 20], 8, 2, 128, [0, 1], 4, 50, 16, "bf16")
+    c.attend(k_lens=c.k_lens)
+    c.matches("a sequence without rows")
+    c.c.attend(c.q[:0], [0, 0], c.lens, c.table, c.out[:0])
+    c.c.attend(c.q[:0], [], c.lens[:0], c.table[:0], c.out[:0])
+    c.c.check()

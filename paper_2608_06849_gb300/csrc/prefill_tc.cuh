@@ -398,10 +398,12 @@ __global__ void __launch_bounds__(CallOf<A>::kThreads, 1)
       end_l = l;
       end_ok = ok && (steps == 0 ||
                       __all_sync(0xffffffffu, wait_bar(&pv_done[SB::bar(x, steps - 1)], SB::phase(steps - 1), a.err, abort_flag)));
-    } else if (ok && ((Call::kEmptyRows && n_tiles == 0) ||
-                      __all_sync(0xffffffffu, wait_bar(&pv_done[SB::bar(x, n_tiles - 1)], SB::phase(n_tiles - 1), a.err, abort_flag)))) {
+    } else if (ok && (Call::kEmptyRows && n_tiles == 0
+                          ? __all_sync(0xffffffffu, wait_bar(q_full, 0, a.err, abort_flag))
+                          : __all_sync(0xffffffffu, wait_bar(&pv_done[SB::bar(x, n_tiles - 1)], SB::phase(n_tiles - 1), a.err,
+                                                             abort_flag)))) {
       tc_fence_after();
-      // Q_X is free: the last S_X was done before the last P V
+      // Q_X is free: the last S_X was done before the last P V, or it came and none reads it
       const uint32_t spoilt =
           store_o<D, D>(a, t, x, q4 * 32, tl + o_col, l, sQ + x * C::QBYTES + q4 * (C::QBYTES / 4), lane);
       if constexpr (Call::kRepairs)

@@ -452,6 +452,21 @@ def test_two_handles_on_two_streams():
         assert all(torch.equal(w, x) for x in o)
 
 
+@pytest.mark.parametrize("form", ["bf16", "e4m3"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_rows_without_any_key(d, form):
+    """Zero, whatever the queries hold, in calls of many items and of one prompt."""
+    c = Case([300 + 7 * (i % 5) for i in range(40)], [0] * 40, 16, 4, d, [0, 1, 0, 1], 4, 100, 64, form, seed=17)
+    for _ in range(10):
+        c.out.fill_(float("nan"))
+        c.attend()
+        assert (c.out == 0).all()
+        c.out.fill_(float("nan"))
+        c.c.prefill(c.q, c.k, c.v, c.q_lens, c.out, k_lens=c.k_lens)
+        c.c.check()
+        assert (c.out == 0).all()
+
+
 def test_no_rows_and_no_sequences():
     c = Case([3, 0], [40, 20], 8, 2, 128, [0, 1], 4, 50, 16, "bf16")
     c.attend(k_lens=c.k_lens)

@@ -200,31 +200,25 @@ struct PagePool {
   int Hkv, D;
 };
 
-// Sequences whose 8-bit pages are first written out as bf16 ones (launch_paged_expand): those of the
-// i-th sequence with rows are pages first[i] .. first[i + 1] - 1 of the written ones, 128 tokens each.
-struct Expanded {
-  static constexpr int kMost = 64;
-  int n;  // 0: none
-  int first[kMost + 1];
-};
-
 // Attention of chunks over a paged cache: folded items (seqs: {first query row, rows, the
-// sequence's number, -}) whose keys are those of the pages.
+// sequence's number, the first of its pages that are written out}) whose keys are those of the pages.
+// 8-bit pages may be written out as bf16 ones of 128 tokens first (launch_paged_expand); the list then
+// has one entry more, for the end of the last sequence's.
 struct PagedAttendArgs : FoldedArgs {
   CUtensorMap pages;  // the pool as [page, K or V, head][row][D] (bf16 pages)
   PagePool pool;
   const int32_t* lens;   // device: tokens of each sequence
-  const int32_t* table;  // device [n_seqs][table_stride]; null: the pages of `expanded`
+  const int32_t* table;  // device [n_seqs][table_stride]; null: the pages written out
   int table_stride;
   int holds;          // tokens that a row of the caller's table holds
-  Expanded expanded;  // with a table: sequences that fit there are left out
+  int written;        // whether pages are written out; with a table: sequences that fit there are left out
 };
 
 struct PagedExpandArgs {
   PagePool from, to;
   CacheGeom geom;
-  PackedSeqs seqs;  // as PagedAttendArgs has them, by value
-  Expanded expanded;
+  PackedSeqs seqs;  // as PagedAttendArgs has them
+  int n_seqs;
   const int32_t* lens;
   const int32_t* table;
   int table_stride, holds;

@@ -281,25 +281,26 @@ bool parts_of(const aoh_paged* h, const std::vector<int4>& seqs, const std::vect
   return true;
 }
 
-// Which 8-bit pages of a call to write out as bf16 ones first: none, or those of all its sequences (seqs: as
-// the plan takes them), where its items visit the same tiles often enough. work: tiles that they visit in all.
+// Whether to write a call's 8-bit pages out as bf16 ones first, of as many tokens as the plan takes its sequences
+// (planned) to have, and which pages they are of each (seqs; the entry behind them has their end): where its items visit the same tiles often enough. work: tiles that they visit in all.
 // An item's visit costs an SM 1.1 us more with codes (d_head 128; 2,824 us of 8,192 rows after 16,384 of
 // 32/8 heads, 1,626 over bf16 pages), a tile's writing 98 KB of traffic, and the two launches some 8 us.
-bool expand_plan(const aoh_paged* h, const std::vector<int4>& seqs, long long work, Expanded* x) {
-  x->n = 0;
-  if (h->cfg.form != AOH_PAGES_E4M3 || seqs.size() > (size_t)Expanded::kMost) return false;
+bool expand_plan(const aoh_paged* h, const std::vector<int4>& planned, long long work, std::vector<int4>* seqs) {
+  if (h->cfg.form != AOH_PAGES_E4M3) return false;
   const CacheGeom& g = h->geom;
   long long pages = 0, tiles = 0;
-  for (size_t i = 0; i < seqs.size(); ++i) {
-    const int keys = seqs[i].w, all = (int)(((long long)keys + 127) / 128);
-    x->first[i] = (int)pages;
-    pages += all;
-    tiles += seen_tiles(g, seqs[i].y, keys);
+  for (const int4& s : planned) {
+    pages += ((long long)s.w + 127) / 128;
+    tiles += seen_tiles(g, s.y, s.w);
   }
-  x->first[seqs.size()] = (int)pages;
   const double visit = 7.2 * g.D / 128, write = 16.4 * g.D / 128;
-  if (pages == 0 || pages * 2 * g.Hkv * 128 * g.D * 2 > (4ll << 30) || work * visit < tiles * write * 1.2 + 8000) return false;
-  x->n = (int)seqs.size();
+  if (pages == 0 || pages > (4ll << 30) / (2 * g.Hkv * 128 * g.D * 2) || work * visit < tiles * write * 1.2 + 8000) return false;
+  pages = 0;
+  for (size_t i = 0; i < planned.size(); ++i) {
+    (*seqs)[i].w = (int)pages;
+    pages += ((long long)planned[i].w + 127) / 128;
+  }
+  seqs->push_back(make_int4(0, 0, 0, (int)pages));
   return true;
 }
 
@@ -765,31 +766,27 @@ aoh_status aoh_paged_attend(aoh_paged* cache, const void* q, int64_t q_stride, c
   a.holds = (int)holds;
   if (!make_rows_map(&a.tq, q, 1, n_q, c.n_q_heads, c.d_head, q_stride, a.span, a.geom.G))
     return fail(AOH_ERR_CUDA, "cuTensorMapEncodeTiled failed for q");
+  bool lone = true;
+  for (const int4& b : planned) lone = lone && b.y <= a.span;
+  const int split = folded_split(costs, lone, decode_tc_max_clusters, cache->num_sms), n_with = (int)seqs.size();
+  void* written = nullptr;
+  if (expand_plan(cache, planned, work, &seqs))
+    written = expand_memory(cache->device, (size_t)seqs[n_with].w * 2 * c.n_kv_heads * 128 * c.d_head * 2, s);
+  cudaError_t e = cudaSuccess;
   if (seqs.size() <= (size_t)PackedSeqs::kMost) {
     std::copy(seqs.begin(), seqs.end(), a.seqs.by_value);
   } else {
     a.seqs.table = cache->d_seqs;
-    const cudaError_t e = launch_packed_seqs(cache->d_seqs, seqs, s);
-    if (e != cudaSuccess) return cuda_fail(e, "sequence upload launch");
-  }
-  bool lone = true;
-  for (const int4& b : seqs) lone = lone && b.y <= a.span;
-  const int split = folded_split(costs, lone, decode_tc_max_clusters, cache->num_sms);
-  cudaError_t e = cudaSuccess;
-  Expanded expanded;
-  void* written = nullptr;
-  if (expand_plan(cache, planned, work, &expanded)) {
-    const size_t pages = (size_t)expanded.first[expanded.n];
-    written = expand_memory(cache->device, pages * 2 * c.n_kv_heads * 128 * c.d_head * 2, s);
+    e = launch_packed_seqs(cache->d_seqs, seqs, s);
   }
   bool covered = false;  // whether all sequences fit there, whatever their lengths
   if (written) {
     PagedAttendArgs w = a;
-    w.expanded = expanded;
+    w.written = 1;
     w.table = nullptr;
     w.pool.data = written;
     w.pool.powers = nullptr;
-    w.pool.n_pages = expanded.first[expanded.n];
+    w.pool.n_pages = seqs[n_with].w;
     w.pool.ps = 128;
     w.pool.lg_ps = 7;
     w.pool.form = AOH_PAGES_BF16;
@@ -798,19 +795,19 @@ aoh_status aoh_paged_attend(aoh_paged* cache, const void* q, int64_t q_stride, c
     x.from = cache->pool;
     x.to = w.pool;
     x.geom = cache->geom;
-    std::copy(seqs.begin(), seqs.end(), x.seqs.by_value);
-    x.expanded = expanded;
+    x.seqs = a.seqs;
+    x.n_seqs = n_with;
     x.lens = lens;
     x.table = table;
     x.table_stride = table_stride;
     x.holds = a.holds;
     x.err = cache->d_err;
     covered = true;
-    for (int i = 0; i < expanded.n; ++i) covered = covered && (expanded.first[i + 1] - expanded.first[i]) * 128ll >= holds;
-    if (!make_pages_map(&w.pages, w.pool)) e = cudaErrorInvalidValue;
+    for (int i = 0; i < n_with; ++i) covered = covered && (seqs[i + 1].w - seqs[i].w) * 128ll >= holds;
+    if (e == cudaSuccess && !make_pages_map(&w.pages, w.pool)) e = cudaErrorInvalidValue;
     if (e == cudaSuccess) e = launch_paged_expand(x, s);
     if (e == cudaSuccess) e = launch_paged_attend(w, items, split, s);
-    a.expanded = expanded;
+    a.written = 1;
   }
   if (e == cudaSuccess && !covered) e = launch_paged_attend(a, items, split, s);
   if (written) {

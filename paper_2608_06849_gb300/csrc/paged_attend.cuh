@@ -29,20 +29,20 @@ __device__ __forceinline__ int attend_len(const PagedAttendArgs& a, int b) {
 }
 
 struct PagedItem : FoldedItem {
-  int index, b;  // among the sequences with rows, and the sequence's number
+  int index, b, first;  // among the sequences with rows, the sequence's number, its first page written out
   __device__ __forceinline__ PagedItem(const PagedAttendArgs& a, uint64_t code)
       : PagedItem(a, code, a.seqs.of((int)(code >> 34))) {}
   __device__ __forceinline__ PagedItem(const PagedAttendArgs& a, uint64_t code, const int4& s)
-      : FoldedItem(a, code, make_int4(s.x, s.y, 0, attend_len(a, s.z))), index((int)(code >> 34)), b(s.z) {}
+      : FoldedItem(a, code, make_int4(s.x, s.y, 0, attend_len(a, s.z))), index((int)(code >> 34)), b(s.z), first(s.w) {}
   // whether another kernel of the call computes it
   __device__ __forceinline__ bool elsewhere(const PagedAttendArgs& a) const {
-    if (a.expanded.n == 0) return false;
-    return (klen <= (a.expanded.first[index + 1] - a.expanded.first[index]) * kBN) == (a.table != nullptr);
+    if (!a.written) return false;
+    return (klen <= (a.seqs.of(index + 1).w - first) * kBN) == (a.table != nullptr);
   }
   // the page with position pos
   __device__ __forceinline__ int page_of(const PagedAttendArgs& a, int pos) const {
     const int slot = pos >> a.pool.lg_ps;
-    return a.table ? __ldg(a.table + (size_t)b * a.table_stride + slot) : a.expanded.first[index] + slot;
+    return a.table ? __ldg(a.table + (size_t)b * a.table_stride + slot) : first + slot;
   }
 };
 

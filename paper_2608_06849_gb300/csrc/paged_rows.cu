@@ -231,16 +231,20 @@ template <int D>
 __global__ void __launch_bounds__(kThreads, 4) expand_kernel(const __grid_constant__ PagedExpandArgs a) {
   constexpr int LPR = D / 16, ROWS = kThreads / LPR, U = 128 / ROWS;
   const int page_to = blockIdx.x, h = blockIdx.y, lane = threadIdx.x & 31;
-  // the sequence: the last one that begins at or before the page
-  int i = __popc(__ballot_sync(0xffffffffu, lane < a.expanded.n && a.expanded.first[lane] <= page_to));
-  if (a.expanded.n > 32) i += __popc(__ballot_sync(0xffffffffu, lane + 32 < a.expanded.n && a.expanded.first[lane + 32] <= page_to));
-  --i;
   after_the_last_kernel();
-  const int4 seq = a.seqs.by_value[i];
+  // the sequence: the last one that begins at or before the page, among a 32nd of those left in each round
+  int i = 0;
+  for (int n = a.n_seqs; n > 1;) {
+    const int step = (n + 31) / 32, at = lane * step;
+    const int skip = (__popc(__ballot_sync(0xffffffffu, at < n && a.seqs.of(i + at).w <= page_to)) - 1) * step;
+    i += skip;
+    n = min(step, n - skip);
+  }
+  const int4 seq = a.seqs.of(i);
   const int b = seq.z, read = __ldcg(a.lens + b), len = min(max(read, 0), a.holds);
-  const int tile = page_to - a.expanded.first[i], p0 = tile * 128;
+  const int tile = page_to - seq.w, p0 = tile * 128;
   // one that proves longer than its pages here is not read from them
-  if (p0 >= len || len > (a.expanded.first[i + 1] - a.expanded.first[i]) * 128) return;
+  if (p0 >= len || len > (a.seqs.of(i + 1).w - seq.w) * 128) return;
   if (a.geom.kind[h] && p0 >= a.geom.S && p0 + 128 <= a.geom.wstart(len - seq.y)) return;
   const int r0 = threadIdx.x / LPR, ch = threadIdx.x % LPR, lg = a.from.lg_ps;
 #pragma unroll
@@ -320,7 +324,7 @@ cudaError_t launch_paged_read(const PagedReadArgs& a, int num_sms, cudaStream_t 
 
 cudaError_t launch_paged_expand(const PagedExpandArgs& a, cudaStream_t s) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)a.expanded.first[a.expanded.n], (unsigned)a.from.Hkv);
+  cfg.gridDim = dim3((unsigned)a.to.n_pages, (unsigned)a.from.Hkv);
   cfg.blockDim = dim3(kThreads);
   cfg.stream = s;
   cudaLaunchAttribute attr[1];

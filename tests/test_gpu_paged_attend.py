@@ -351,6 +351,18 @@ def test_bad_pages_written_out_first():
     assert torch.equal(out[900:], first[900:])
 
 
+@pytest.mark.parametrize("n", [63, 64, 100])
+def test_pages_of_many_sequences_written_out(n):
+    """Lists of sequences that travel by value or by way of the device, some without rows or keys and some
+    longer than the host takes them to be."""
+    q_lens = [0 if i % 13 == 5 else 290 + 7 * (i % 6) for i in range(n)]
+    k_lens = [0 if i % 17 == 3 else q + 61 * (i % 9) for i, q in enumerate(q_lens)]
+    hint = [max(0, k - 200) if i % 11 == 2 else k for i, k in enumerate(k_lens)]
+    c = Case(q_lens, k_lens, 16, 2, 128, [0, 1], 10, 260, 32, "e4m3", seed=70 + n)
+    c.attend(k_lens=hint)
+    c.matches(f"{n} sequences written out")
+
+
 def test_written_out_after_an_append_in_flight():
     """An append and the attention that follow each other without a wait: the new rows are seen."""
     c = Case([1200], [3000], 16, 4, 128, [0, 1, 0, 0], 20, 700, 32, "e4m3", seed=9)

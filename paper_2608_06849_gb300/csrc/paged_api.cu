@@ -248,11 +248,14 @@ long long seen_tiles(const CacheGeom& g, int n, int keys) {
 // head times tokens), which reads a sequence's pages once for each part but as they lie, at the rate of HBM. What it
 // takes against the tiles of 256 rows, in nanoseconds of the GPU: 10.6 a tile of 128 keys of d_head 128 and part (8
 // bits: 5.5, but 8 with more than 8 columns, whose softmax takes longer than the tile's transfer) against 14 (18) a
-// tile, and a start of 6 us against 10. work: tiles that the latter visit. Measured, us of a call in tiles / parts: 32 x 2-5
+// tile, a start of 6 us against 9, and, since a short item is a chain of waits on its SM, 30 (28, 38) a part of a KV
+// head against 25 an item. work: tiles that the latter's `items` visit. Measured, us of a call in tiles / parts: 32 x 2-5
 // rows after 1,000-16,000, 32/8 heads, 8 bits 198 / 121, bf16 154 / 144; 4 rows each, 8 bits - / 98, 2 - / 69; 5 rows after
-// 4,096, 28/4 heads, bf16 12.3 / 9.4.
-bool parts_of(const aoh_paged* h, const std::vector<int4>& seqs, const std::vector<int4>& planned, long long work,
-              std::vector<int4>* parts, int* tokens) {
+// 4,096, 28/4 heads, bf16 12.3 / 9.4; 32/8 heads, 128 x 2 rows after 20-36, 8 bits 59 / 42, 10-15 rows 61 / 181, 64 x 2-5
+// after 20-100 31 / 44, bf16 26 / 31, 256 x 2-4 after 100-300 165 / 160, bf16 122 / 119; of 64, 128 x 2-5 after
+// 200-500 84 / 132, bf16 65 / 94.
+bool parts_of(const aoh_paged* h, const std::vector<int4>& seqs, const std::vector<int4>& planned, size_t items,
+              long long work, std::vector<int4>* parts, int* tokens) {
   const CacheGeom& g = h->geom;
   const int most = 16 / g.G;
   const double scale = g.D / 128.0 * 0.001;
@@ -267,8 +270,11 @@ bool parts_of(const aoh_paged* h, const std::vector<int4>& seqs, const std::vect
     if (count > 16) return false;
   }
   const bool f8 = h->cfg.form == AOH_PAGES_E4M3;
-  const double each_ns = !f8 ? 10.6 : g.G * *tokens <= 8 ? 5.5 : 8;
-  if (6 + visits * each_ns * scale > 10 + work * (f8 ? 18 : 14) * scale) return false;
+  const bool narrow = g.G * *tokens <= 8;
+  const double tile_ns = !f8 ? 10.6 : narrow ? 5.5 : 8, part_ns = !f8 ? 30 : narrow ? 28 : 38;
+  if (6 + n * g.Hkv * part_ns * 0.001 + visits * tile_ns * scale >
+      9 + items * 25 * 0.001 + work * (f8 ? 18 : 14) * scale)
+    return false;
   if (n > PackedSeqs::kMost && n > (long long)kPartsASeq * h->cfg.max_seqs) return false;  // more than the device's list holds
   parts->reserve(n);
   for (const int4& s : seqs) {
@@ -715,7 +721,7 @@ aoh_status aoh_paged_attend(aoh_paged* cache, const void* q, int64_t q_stride, c
   std::vector<int4> parts;
   int tokens = 1;
   // (the decode kernel counts its tiles, of at least 128 keys, in 32 bits)
-  if (parts_of(cache, seqs, planned, work, &parts, &tokens) &&
+  if (parts_of(cache, seqs, planned, items.size(), work, &parts, &tokens) &&
       (int64_t)parts.size() * c.n_kv_heads * ((holds + 127) / 128) <= INT32_MAX) {
     PagedPartsArgs p;
     p.pages = cache->pages;

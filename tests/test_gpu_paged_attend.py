@@ -391,6 +391,7 @@ FEW = [
     ([1 + i % 4 for i in range(80)], [1 + i % 4 + 53 * (i % 11) for i in range(80)], 32, 8, 128, [0, 1] * 4, 2, 3, 16),
     ([6] * 30, [40 + 97 * (i % 13) for i in range(30)], 24, 8, 64, [1, 0] * 4, 0, 5, 64),
     ([2] * 20, [9000 + i for i in range(20)], 32, 8, 64, [0] * 8, 0, 1, 64),
+    ([6] * 3, [40, 1007, 300], 24, 8, 64, [1, 0] * 4, 0, 5, 64),
 ]
 
 
@@ -398,7 +399,8 @@ FEW = [
 @pytest.mark.parametrize("case", range(len(FEW)))
 def test_few_rows(case, form):
     c = Case(*FEW[case], form, seed=300 + case, fused=case % 2 == 0, spread=1.5)
-    for hint in (c.k_lens, [0] * len(c.k_lens)):  # (the latter takes any of these calls there)
+    # (calls of one part a sequence run there by the last, others of a few parts by the one before)
+    for hint in (c.k_lens, [0] * len(c.k_lens), [1 << 17] * len(c.k_lens)):
         c.out.fill_(float("nan"))
         c.attend(k_lens=hint)
         c.matches(f"few rows {case}, hint {hint[:3]}")
@@ -410,7 +412,7 @@ def test_spoilt_keys_among_few_rows(case, form):
     """K and V that are not finite at the rows' own positions and around the beginnings of their windows reach
     the rows that see them, and no other of the same sequence."""
     c = Case(*FEW[case], form, seed=400 + case)
-    hint = [0] * len(c.k_lens)
+    hint = [1 << 17 if max(c.q_lens) * (c.q.shape[1] // len(c.labels)) <= 16 else 0] * len(c.k_lens)
     clean = f64(c.attend(k_lens=hint))
     ks, qs, hkv = sums(c.k_lens), sums(c.q_lens), len(c.labels)
     G = c.q.shape[1] // hkv

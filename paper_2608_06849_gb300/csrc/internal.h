@@ -376,7 +376,9 @@ cudaError_t launch_prefill_packed(const PackedArgs& a, const std::vector<uint64_
 cudaError_t launch_prefill_folded(const FoldedArgs& a, const std::vector<uint64_t>& items, int split, bool is_short,
                                   int num_sms, cudaStream_t s);
 // Chunks over pages, as launch_prefill_folded takes its items.
-cudaError_t launch_paged_attend(const PagedAttendArgs& a, const std::vector<uint64_t>& items, int split, cudaStream_t s);
+// is_short (bf16 pages): one CTA an SM goes through all items in one pipeline (prefill_is_short).
+cudaError_t launch_paged_attend(const PagedAttendArgs& a, const std::vector<uint64_t>& items, int split, bool is_short,
+                                int num_sms, cudaStream_t s);
 cudaError_t launch_paged_expand(const PagedExpandArgs& a, cudaStream_t s);
 cudaError_t launch_paged_append(const PagedAppendArgs& a, int num_sms, cudaStream_t s);
 cudaError_t launch_paged_read(const PagedReadArgs& a, int num_sms, cudaStream_t s);

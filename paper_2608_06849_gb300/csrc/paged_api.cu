@@ -775,6 +775,7 @@ aoh_status aoh_paged_attend(aoh_paged* cache, const void* q, int64_t q_stride, c
   bool lone = true;
   for (const int4& b : planned) lone = lone && b.y <= a.span;
   const int split = folded_split(costs, lone, decode_tc_max_clusters, cache->num_sms), n_with = (int)seqs.size();
+  const bool is_short = split == 1 && prefill_is_short(costs, cache->num_sms);
   void* written = nullptr;
   if (expand_plan(cache, planned, work, &seqs))
     written = expand_memory(cache->device, (size_t)seqs[n_with].w * 2 * c.n_kv_heads * 128 * c.d_head * 2, s);
@@ -812,10 +813,10 @@ aoh_status aoh_paged_attend(aoh_paged* cache, const void* q, int64_t q_stride, c
     for (int i = 0; i < n_with; ++i) covered = covered && (seqs[i + 1].w - seqs[i].w) * 128ll >= holds;
     if (e == cudaSuccess && !make_pages_map(&w.pages, w.pool)) e = cudaErrorInvalidValue;
     if (e == cudaSuccess) e = launch_paged_expand(x, s);
-    if (e == cudaSuccess) e = launch_paged_attend(w, items, split, s);
+    if (e == cudaSuccess) e = launch_paged_attend(w, items, split, is_short, cache->num_sms, s);
     a.written = 1;
   }
-  if (e == cudaSuccess && !covered) e = launch_paged_attend(a, items, split, s);
+  if (e == cudaSuccess && !covered) e = launch_paged_attend(a, items, split, is_short, cache->num_sms, s);
   if (written) {
     const cudaError_t f = cudaFreeAsync(written, s);
     if (e == cudaSuccess) e = f;

@@ -21,19 +21,22 @@ template <bool F8>
 struct PagedArgs : PagedAttendArgs {};
 
 // The tokens of sequence b, within what its table holds.
-__device__ __forceinline__ int attend_len(const PagedAttendArgs& a, int b) {
+__device__ __forceinline__ int attend_len(const PagedAttendArgs& a, int b, bool tells) {
   const int n = __ldcg(a.lens + b);
   if (n >= 0 && n <= a.holds) return n;
-  if (threadIdx.x == 0) atomicOr(a.err, kErrPages);
+  if (tells) atomicOr(a.err, kErrPages);
   return n < 0 ? 0 : a.holds;
 }
 
 struct PagedItem : FoldedItem {
   int index, b, first;  // among the sequences with rows, the sequence's number, its first page written out
-  __device__ __forceinline__ PagedItem(const PagedAttendArgs& a, uint64_t code)
-      : PagedItem(a, code, a.seqs.of((int)(code >> 34))) {}
-  __device__ __forceinline__ PagedItem(const PagedAttendArgs& a, uint64_t code, const int4& s)
-      : FoldedItem(a, code, make_int4(s.x, s.y, 0, attend_len(a, s.z))), index((int)(code >> 34)), b(s.z), first(s.w) {}
+  // (of the CTA's threads one, or each with tells, reports a length out of range)
+  __device__ __forceinline__ PagedItem(const PagedAttendArgs& a, uint64_t code, bool tells = false)
+      : PagedItem(a, code, a.seqs.of((int)(code >> 34)), tells || threadIdx.x == 0) {}
+  __device__ __forceinline__ PagedItem(const PagedAttendArgs& a, uint64_t code, const int4& s, bool tells)
+      : PagedItem(a, code, s, attend_len(a, s.z, tells)) {}
+  __device__ __forceinline__ PagedItem(const PagedAttendArgs& a, uint64_t code, const int4& s, int keys)
+      : FoldedItem(a, code, make_int4(s.x, s.y, 0, keys)), index((int)(code >> 34)), b(s.z), first(s.w) {}
   // whether another kernel of the call computes it
   __device__ __forceinline__ bool elsewhere(const PagedAttendArgs& a) const {
     if (!a.written) return false;
@@ -68,7 +71,7 @@ struct PageWalk<PagedArgs<false>, D> {
   int lane, rows, page;  // page: the lane's, at key lane * rows, or -1: out of range
   int ahead;             // the entry of the tile after it, which is on its way meanwhile
   bool has;              // whether the lane has a page with keys
-  __device__ __forceinline__ PageWalk(const PagedAttendArgs& a, const PagedItem&, int lane_)
+  __device__ __forceinline__ PageWalk(int lane_, const PagedAttendArgs& a)
       : lane(lane_), rows(a.pool.ps), page(-1), ahead(-1), has(false) {}
   __device__ __forceinline__ int key() const { return lane * rows; }
   __device__ __forceinline__ bool position(const PagedItem& t, int i, int* pos) const {
@@ -76,10 +79,11 @@ struct PageWalk<PagedArgs<false>, D> {
     return key() < kBN && *pos < t.klen;
   }
   // visited tile i of the item, the first that is looked up or the one after the last that was
-  __device__ __forceinline__ void fetch(const PagedAttendArgs& a, const PagedItem& t, int i) {
+  __device__ __forceinline__ int entry(const PagedAttendArgs& a, const PagedItem& t, int i) const {
     int pos;
-    ahead = position(t, i, &pos) ? t.page_of(a, pos) : -1;
+    return position(t, i, &pos) ? t.page_of(a, pos) : -1;
   }
+  __device__ __forceinline__ void fetch(const PagedAttendArgs& a, const PagedItem& t, int i) { ahead = entry(a, t, i); }
   __device__ __forceinline__ void look(const PagedAttendArgs& a, const PagedItem& t, int i, bool more) {
     int pos;
     has = position(t, i, &pos);
@@ -223,12 +227,20 @@ constexpr int kAttendByValue = 3200;
 
 // The items of a call: `split` CTAs each (1: one), as launch_prefill_folded has them.
 template <bool F8, int D>
-cudaError_t launch_attend(const PagedAttendArgs& args, const std::vector<uint64_t>& items, int split, cudaStream_t s) {
+cudaError_t launch_attend(const PagedAttendArgs& args, const std::vector<uint64_t>& items, int split, bool is_short, int num_sms,
+                          cudaStream_t s) {
   PagedArgs<F8> a;
   static_cast<PagedAttendArgs&>(a) = args;
   if (split > 1)
     return launch_items<PagedArgs<F8>, D, kSplit, kPrefillSplitMost>(a, items.data(), (int)items.size(), split, s);
   const size_t n = items.size();
+  if constexpr (!F8)
+    for (size_t i = 0; is_short && i < n; i += kAttendByValue) {
+      const int m = (int)(n - i < (size_t)kAttendByValue ? n - i : (size_t)kAttendByValue);
+      a.follows = i > 0;
+      const cudaError_t e = launch_short<PagedArgs<F8>, D, kAttendByValue>(a, items.data() + i, m, num_sms, s);
+      if (e != cudaSuccess || i + m == n) return e;
+    }
   if (n <= kTiny) return launch_items<PagedArgs<F8>, D, kWhole, kTiny>(a, items.data(), (int)n, 1, s);
   if (n <= kSmall) return launch_items<PagedArgs<F8>, D, kWhole, kSmall>(a, items.data(), (int)n, 1, s);
   for (size_t i = 0; i < n; i += kAttendByValue) {

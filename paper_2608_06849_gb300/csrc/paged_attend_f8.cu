@@ -3,8 +3,9 @@
 #include "paged_attend.cuh"
 
 namespace aoh {
-cudaError_t launch_paged_attend_f8(const PagedAttendArgs& a, const std::vector<uint64_t>& items, int split, cudaStream_t s) {
-  return a.pool.D == 128 ? pf::launch_attend<true, 128>(a, items, split, s)
-                         : pf::launch_attend<true, 64>(a, items, split, s);
+cudaError_t launch_paged_attend_f8(const PagedAttendArgs& a, const std::vector<uint64_t>& items, int split, bool is_short,
+                                     int num_sms, cudaStream_t s) {
+  return a.pool.D == 128 ? pf::launch_attend<true, 128>(a, items, split, is_short, num_sms, s)
+                         : pf::launch_attend<true, 64>(a, items, split, is_short, num_sms, s);
 }
 }  // namespace aoh

@@ -60,16 +60,15 @@ cudaError_t launch_items(const A& a, const uint64_t* items, int n, int each, cud
   return launch<A, decltype(kernel), CAP>(kernel, smem, n * each, MODE == kPairs ? 2 : each, a, items, n, s);
 }
 
-template <class A, int D>
+template <class A, int D, int CAP = kPrefillByValue>
 cudaError_t launch_short(const A& a, const uint64_t* items, int n, int num_sms, cudaStream_t s) {
-  auto kernel = prefill_short_kernel<A, D, kPrefillByValue>;
+  auto kernel = prefill_short_kernel<A, D, CAP>;
   constexpr int smem = ShortCfg<D>::SMEM;
   static std::atomic<uint64_t> done{0};
   const cudaError_t e = once_per_device(
       done, [&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem); });
   if (e != cudaSuccess) return e;
-  return launch<A, decltype(kernel), kPrefillByValue>(kernel, smem, n < num_sms ? n : num_sms, 1, a, items, n, s,
-                                                   n);
+  return launch<A, decltype(kernel), CAP>(kernel, smem, n < num_sms ? n : num_sms, 1, a, items, n, s, n);
 }
 
 // The items travel as kernel arguments, at most kPrefillByValue a launch.

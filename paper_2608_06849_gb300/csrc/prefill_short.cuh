@@ -16,6 +16,11 @@
 // 64, W = 512): 276 us with a CTA an item, 244 so; heads of 64 230 -> 210; 16 sequences
 // of up to 700 tokens 89 -> 71. What is left of an item's start and end is the chain
 // from its last S to the next item's first P V: Q's buffer, S and its softmax.
+//
+// Over pages (of bf16; paged_attend.cuh) the items' sequences are read before the roles begin, and the first
+// entries of the table of the next item are on their way while this one's tiles are: 128 sequences of 2-5 rows
+// after 20-36 tokens, 32/8 heads of 64, 45 -> 38 us, 64 of 100-300 rows after up to 1,000 145 -> 130, 16 of 300-700 after up
+// to 500, heads of 128, 99 -> 85.
 #pragma once
 
 #include <string.h>
@@ -25,6 +30,9 @@
 namespace aoh {
 namespace pf {
 
+// Items of a CTA over pages at most: their sequences are read once, before the roles begin.
+constexpr int kShortItems = 32;
+
 template <int D>
 struct ShortCfg {
   using C = PfCfg<D>;
@@ -33,7 +41,8 @@ struct ShortCfg {
   static constexpr int OFF_STAGE = C::OFF_BAR;   // 8 warps
   static constexpr int OFF_BAR = OFF_STAGE + 8 * STAGE;
   static constexpr int NBAR = 2 + 2 * kNS + 4 + 8 + 4 + 2 + 1;
-  static constexpr int SMEM = OFF_BAR + NBAR * 8 + 16 + 1024;
+  static constexpr int OFF_ITEMS = OFF_BAR + (NBAR * 8 + 15) / 16 * 16 + 16;  // pages: sequences of the CTA's items
+  static constexpr int SMEM = OFF_ITEMS + kShortItems * 20 + 1024;
   static_assert(SMEM <= 232448, "shared memory");
 };
 
@@ -44,6 +53,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   using X = ShortCfg<D>;
   using Call = CallOf<A>;
   using SB = SBuf<A, D>;
+  constexpr bool PAGED = Call::kPaged;
+  static_assert(!Call::kF8, "pages of bf16");
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
   uint8_t* sQ = smem + C::OFF_Q;
@@ -60,6 +71,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   uint32_t* spoilt = tmem_slot + 2;  // this CTA's items with a value that is not finite: bit k mod 32
+  int4* seq_s = reinterpret_cast<int4*>(smem + X::OFF_ITEMS);  // pages: the k-th item's sequence
+  int* klen_s = reinterpret_cast<int*>(seq_s + kShortItems);   // and its keys, or -1: another kernel's
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const CacheGeom& g = a.geom;
@@ -69,6 +82,13 @@ __global__ void __launch_bounds__(kThreads, 1)
   // this CTA's k-th item
   auto item_index = [&](int k) { return k * P + ((k & 1) ? P - 1 - cta : cta); };
   auto item_code = [&](int i) { return CAP > 0 ? wl.item[i] : a.work[i]; };
+  auto item = [&](int k) {
+    if constexpr (PAGED)
+      return typename Call::ItemT(a, item_code(item_index(k)), seq_s[k], klen_s[k]);
+    else
+      return typename Call::ItemT(a, item_code(item_index(k)));
+  };
+  auto elsewhere = [&](int k) { return PAGED && klen_s[k] < 0; };
   if (threadIdx.x == 0) {
     mbar_init(q_full, 2);
     mbar_init(q_empty, 1);
@@ -90,6 +110,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     *spoilt = 0;
     fence_mbar_init();
   }
+  if constexpr (PAGED) {
+    if (warp == 2 && item_index(lane) < n_items) {
+      wait_to_start(a);
+      const typename Call::ItemT t(a, item_code(item_index(lane)), true);
+      seq_s[lane] = make_int4(t.qrow, t.len, t.b, t.first);
+      klen_s[lane] = t.elsewhere(a) ? -1 : t.klen;
+    }
+  }
   if (warp == 1) {
     tmem_alloc(tmem_slot, kTmemCols);
     tmem_relinquish();
@@ -104,19 +132,49 @@ __global__ void __launch_bounds__(kThreads, 1)
     // ------------------------------------------------------------ producer
     int it = 0;         // copies of the KV ring so far (K, V, K, V, ...)
     int n_partial = 0;  // partial V tiles so far
-    int issued = 0, nq = 0;
+    int issued = 0, nq = 0;  // nq: items whose Q was loaded
     bool ok = true;
+    PageWalk<A, D> pages(lane, a);
+    int early = -1, entry = -1;  // pages: the item whose first entry of the table is on its way, and that
     for (int k = 0; ok; ++k) {
       const int ii = item_index(k);
       if (ii >= n_items) break;
       // the append may start once every CTA is at its last item (append.cu)
       if (item_index(k + 1) >= n_items) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-      const typename Call::ItemT t(a, item_code(ii));
+      if (elsewhere(k)) continue;
+      const auto t = item(k);
       const int n = t.tiles();
+      if constexpr (PAGED) {
+        if (early == k)
+          pages.ahead = entry;
+        else if (n > 0)
+          pages.fetch(a, t, 0);
+      }
       for (int jj = 0; jj < n && ok; ++jj) {
+        if constexpr (PAGED) {
+          pages.look(a, t, jj, jj + 1 < n);
+          if (jj == 0 && item_index(k + 1) < n_items && !elsewhere(k + 1)) {
+            early = k + 1;
+            entry = pages.entry(a, item(k + 1), 0);
+          }
+        }
         for (int sel = 0; sel < 2; ++sel, ++it) {
           const int st = it % kNS;
-          if (lane == 0) {
+          if constexpr (PAGED) {
+            if (it >= kNS) ok = __all_sync(0xffffffffu, wait_bar(&kv_empty[st], ((it / kNS) & 1) ^ 1, a.err, abort_flag));
+            if (ok) {
+              pages.load(a, t, sel, sKV + st * C::KVBYTES, &kv_full[st]);
+              issued = it + 1;
+            }
+            if (lane == 0 && ok && jj == 0 && sel == 0) {
+              if (nq >= 1) ok = wait_bar(q_empty, (nq - 1) & 1, a.err, abort_flag);
+              if (ok) {
+                load_q<D>(a, t, 0, sQ, q_full);
+                load_q<D>(a, t, 1, sQ + C::QBYTES, q_full);
+              }
+            }
+            if (jj == 0 && sel == 0 && __all_sync(0xffffffffu, ok)) ++nq;
+          } else if (lane == 0) {
             if (it >= kNS) ok = wait_bar(&kv_empty[st], ((it / kNS) & 1) ^ 1, a.err, abort_flag);
             if (ok) {
               load_kv<D>(a, t, jj, sel, sKV + st * C::KVBYTES, &kv_full[st]);
@@ -160,6 +218,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint64_t v_desc0 = sdesc_sw128(smem_u32(sKV), C::BOX, 1024);
     int kt = 0;         // KV tiles before this one, over all items
     int n_partial = 0;  // partial V tiles so far
+    int nq = 0;         // items with tiles so far
     bool ok = true;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
       if (ok) ok = __all_sync(0xffffffffu, wait_bar(bar, parity, a.err, abort_flag));
@@ -195,11 +254,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int k = 0; ok; ++k) {
       const int ii = item_index(k);
       if (ii >= n_items) break;
-      const typename Call::ItemT t(a, item_code(ii));
+      if (elsewhere(k)) continue;
+      const auto t = item(k);
       const int n = t.tiles();
+      if (PAGED && n == 0) continue;
       const int part0 = t.n_c > 0 && t.valid(g, t.n_c - 1) < kBN ? t.n_c - 1 : -1;
       const int part1 = t.valid(g, n - 1) < kBN ? n - 1 : -1;
-      if (!wait(q_full, k & 1) || !wait_k(kt)) break;
+      if (!wait(q_full, nq & 1) || !wait_k(kt)) break;
+      ++nq;
       tc_fence_after();
       if constexpr (SB::N == 3) {
         auto on = [](int b) { return b == 2 ? 0 : b + 1; };
@@ -282,7 +344,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int k = 0; ok; ++k) {
       const int ii = item_index(k);
       if (ii >= n_items) break;
-      const typename Call::ItemT t(a, item_code(ii));
+      if (elsewhere(k)) continue;
+      const auto t = item(k);
       const int qx0 = t.row0(x), i = t.row(x, r), n = t.tiles();
       const int rot = t.rot(g);
       float m = -INFINITY, l = 0.f;
@@ -296,7 +359,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (SB::N == 3) s_col = s_col >= 128 ? s_col - 128 : 256;  // two buffers on
       }
       if (!ok) break;
-      ok = __all_sync(0xffffffffu, wait_bar(&pv_done[SB::bar(x, kt - 1)], SB::phase(kt - 1), a.err, abort_flag));
+      // (without a tile: zeros)
+      if (!PAGED || n > 0)
+        ok = __all_sync(0xffffffffu, wait_bar(&pv_done[SB::bar(x, kt - 1)], SB::phase(kt - 1), a.err, abort_flag));
       if (!ok) break;
       tc_fence_after();
       if (store_o<D, X::COLS>(a, t, x, q4 * 32, tl + o_col, l, stage, lane) && lane == 0)

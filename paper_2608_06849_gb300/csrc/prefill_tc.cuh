@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(CallOf<A>::kThreads, 1)
   const int t0 = rank * per;
   const int n_tiles = !half ? n_all : SPLIT ? max(0, min(per, n_all - t0)) : rank == 0 ? (n_all + 1) / 2 : n_all / 2;
   const bool lone = SPLIT && !t.has_row(1, 0);
-  PageWalk<A, D> pages(a, t, warp == 0 ? lane : -1);
+  PageWalk<A, D> pages(warp == 0 ? lane : -1, a);
   if (threadIdx.x == 0) {
     mbar_init(q_full, 2);
     for (int s = 0; s < kNS; ++s) {

@@ -44,8 +44,7 @@ struct PfCfg {
 // Calls over pages alone (paged_attend.cuh): the walks through a sequence's pages of bf16, and of 8 bits.
 template <class A, int D>
 struct PageWalk {
-  template <class T>
-  __device__ __forceinline__ PageWalk(const A&, const T&, int) {}
+  __device__ __forceinline__ PageWalk(int, const A&) {}
 };
 template <class A, int D>
 struct CodeWalk {};

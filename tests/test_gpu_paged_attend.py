@@ -466,6 +466,70 @@ def test_two_handles_on_two_streams():
         assert all(torch.equal(w, x) for x in o)
 
 
+MANY = [
+    # many short items, which one pipeline an SM goes through: q_lens, k_lens, Hq, Hkv, d, labels, sink, window, page
+    ([1 + 7 * i % 60 for i in range(64)], [1 + 7 * i % 60 + 37 * (i % 9) for i in range(64)], 32, 8, 64, [0, 1] * 4, 4, 50, 16),
+    # without rows, without keys, fewer positions than rows
+    ([(i % 7) * 6 for i in range(90)], [0 if i % 5 == 1 else 13 * (i % 23) for i in range(90)], 32, 8, 128, [1, 0] * 4, 9, 70, 32),
+    ([1 + 11 * (i % 29) for i in range(60)], [1 + 11 * (i % 29) + 61 * (i % 4) for i in range(60)], 8, 8, 128, [0] * 7 + [1], 0, 130, 128),
+    ([40 + i % 3 for i in range(70)], [40 + i % 3 + 128 * (i % 5) for i in range(70)], 24, 8, 64, [0, 0, 1, 1] * 2, 130, 200, 64),
+]
+
+
+@pytest.mark.parametrize("form", ["bf16", "e4m3"])
+@pytest.mark.parametrize("case", range(len(MANY)))
+def test_many_short_items(case, form):
+    c = Case(*MANY[case], form, seed=500 + case, fused=case % 2 == 0, spread=1.0)
+    for hint in (c.k_lens, [0] * len(c.k_lens), [n // 2 for n in c.k_lens]):
+        c.out.fill_(float("nan"))
+        c.attend(k_lens=hint)
+        c.matches(f"many short items {case}, hint {hint[:3]}")
+
+
+@pytest.mark.parametrize("form", ["bf16", "e4m3"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_bad_sequences_among_many_short_items(d, form):
+    """V rows that are NaN reach the rows that see them and no others; lengths and pages out of range are told, and the
+    other sequences' rows are what they were."""
+    n, past = 70, 150
+    q_lens, labels, sink, window = [33] * n, [0, 1] * 4, 5, 60
+    c = Case(q_lens, [past + 33] * n, 32, 8, d, labels, sink, window, 16, form, seed=8 + d)
+    clean = c.attend(k_lens=c.k_lens).clone()
+    v = c.v.clone().view(n, past + 33, 8, d)
+    at = {3: past + 20, 41: past - 10, 69: 2}  # sequence: position
+    for b, p in at.items():
+        v[b, p] = float("nan")
+    c.c.append(c.k, v.view(-1, 8, d), c.lens, c.table, cu_rows=ints(sums(c.k_lens)))
+    got = c.attend(k_lens=c.k_lens).view(n, 33, 8, 4, d)
+    want = clean.view(n, 33, 8, 4, d)
+    pos = torch.arange(past, past + 33, device="cuda")
+    for b in range(n):
+        for h in range(8):
+            sees = torch.zeros(33, dtype=torch.bool, device="cuda")
+            if b in at:
+                sees = at[b] <= pos
+                if labels[h] and at[b] >= sink:
+                    sees = sees & (pos - at[b] < window)
+            assert got[b, sees, h].isnan().all(), (b, h)
+            x, y = got[b, ~sees, h].double(), want[b, ~sees, h].double()
+            # rows that are gone over again are summed in another order: two roundings to bf16, of weights and of sums
+            assert ((x - y).abs() <= 2.0 ** -6 * y.abs() + 0.02).all(), (b, h)
+    c.c.append(c.k, c.v, c.lens, c.table, cu_rows=ints(sums(c.k_lens)))
+    table, lens = c.table.clone(), c.lens.clone()
+    for what in ("page", "long", "negative"):
+        c.table.copy_(table)
+        c.lens.copy_(lens)
+        if what == "page":
+            c.table[17, 4] = c.c.n_pages
+        else:
+            c.lens[17] = 1 << 20 if what == "long" else -5
+        c.c.attend(c.q, c.q_lens, c.lens, c.table, c.out, k_lens=c.k_lens)
+        with pytest.raises(aoh.AohError, match="out of range"):
+            c.c.check()
+        keep = torch.arange(n * 33, device="cuda") // 33 != 17
+        assert torch.equal(c.out[keep], clean[keep]), what
+
+
 @pytest.mark.parametrize("form", ["bf16", "e4m3"])
 @pytest.mark.parametrize("d", [64, 128])
 def test_rows_without_any_key(d, form):

@@ -1,5 +1,6 @@
 // Host runtime of the paged cache (include/aoh.h): argument validation, the plan of
 // packed prompts and kernel launches on the caller's stream.
+#include <limits.h>
 #include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
@@ -238,42 +239,47 @@ void* expand_memory(int device, size_t bytes, cudaStream_t s) {
   return p;
 }
 
-// Tiles of 128 keys that n rows at the end of `keys` positions see, of all KV heads.
-long long seen_tiles(const CacheGeom& g, int n, int keys) {
+// Groups of `per` tiles of 128 keys that n rows at the end of `keys` positions see, `most` of a KV head at most, of all
+// KV heads.
+long long seen_tiles(const CacheGeom& g, int n, int keys, int per = 1, long long most = LLONG_MAX) {
   const long long all = ((long long)keys + 127) / 128, window = ((long long)g.S + g.W + n + 255) / 128;
-  return g.n_r * all + g.n_s * std::min(all, window);
+  auto of = [&](long long tiles) { return std::min((tiles + per - 1) / per, most); };
+  return g.n_r * of(all) + g.n_s * of(std::min(all, window));
 }
 
 // Calls of a few rows a sequence as parts on the decode kernel, of at most 16 columns each (query heads of a KV
 // head times tokens), which reads a sequence's pages once for each part but as they lie, at the rate of HBM. What it
 // takes against the tiles of 256 rows, in nanoseconds of the GPU: 10.6 a tile of 128 keys of d_head 128 and part (8
-// bits: 5.5, but 8 with more than 8 columns, whose softmax takes longer than the tile's transfer) against 14 (18) a
-// tile, a start of 6 us against 9, and, since a short item is a chain of waits on its SM, 30 (28, 38) a part of a KV
-// head against 25 an item. work: tiles that the latter's `items` visit. Measured, us of a call in tiles / parts: 32 x 2-5
-// rows after 1,000-16,000, 32/8 heads, 8 bits 198 / 121, bf16 154 / 144; 4 rows each, 8 bits - / 98, 2 - / 69; 5 rows after
-// 4,096, 28/4 heads, bf16 12.3 / 9.4; 32/8 heads, 128 x 2 rows after 20-36, 8 bits 59 / 42, 10-15 rows 61 / 181, 64 x 2-5
-// after 20-100 31 / 44, bf16 26 / 31, 256 x 2-4 after 100-300 165 / 160, bf16 122 / 119; of 64, 128 x 2-5 after
-// 200-500 84 / 132, bf16 65 / 94.
+// bits: 5.5, but 8 with more than 8 columns, whose softmax takes longer than the tile's transfer) against 14 (18), and a
+// start of 6 us against 10. A short item is a chain of waits on its SM: the first two tiles of the decode kernel's, of 32 KB
+// of K, of each part and KV head cost 31 more (28, 38), one of the latter's 25 more, 20 in one pipeline an SM (in_line).
+// work: tiles that these `items` visit. Measured, us of a call in tiles / parts: 32 x 2-5 rows after 1,000-16,000, 32/8
+// heads, 8 bits 198 / 121, bf16 154 / 144; 4 rows each, 8 bits - / 98, 2 - / 69; 5 rows after 4,096, 28/4 heads, bf16 12.3 /
+// 9.4; 32/8 heads, 128 x 2 rows after 20-36, 8 bits 59 / 42, 2-5 after 200-500 111 / 145, 10-15 after 9-16 61 / 181, 64 x
+// 2-5 after 20-100 31 / 44, bf16 26 / 31, 256 x 2-4 after 100-300 165 / 160.
 bool parts_of(const aoh_paged* h, const std::vector<int4>& seqs, const std::vector<int4>& planned, size_t items,
-              long long work, std::vector<int4>* parts, int* tokens) {
+              long long work, bool in_line, std::vector<int4>* parts, int* tokens) {
   const CacheGeom& g = h->geom;
   const int most = 16 / g.G;
   const double scale = g.D / 128.0 * 0.001;
-  long long visits = 0, n = 0, longest = 1;
+  const bool f8 = h->cfg.form == AOH_PAGES_E4M3;
   *tokens = 1;
   for (const int4& s : planned) {
-    const int count = (s.y + most - 1) / most, each = (s.y + count - 1) / count;
-    visits += count * seen_tiles(g, s.y, s.w);
-    n += count;
-    longest = std::max<long long>(longest, (s.w + 127) / 128);
-    *tokens = std::max(*tokens, each);
+    const int count = (s.y + most - 1) / most;
     if (count > 16) return false;
+    *tokens = std::max(*tokens, (s.y + count - 1) / count);
   }
-  const bool f8 = h->cfg.form == AOH_PAGES_E4M3;
   const bool narrow = g.G * *tokens <= 8;
-  const double tile_ns = !f8 ? 10.6 : narrow ? 5.5 : 8, part_ns = !f8 ? 30 : narrow ? 28 : 38;
-  if (6 + n * g.Hkv * part_ns * 0.001 + visits * tile_ns * scale >
-      9 + items * 25 * 0.001 + work * (f8 ? 18 : 14) * scale)
+  const int per = !f8 ? 128 / g.D : narrow ? 256 / g.D : 2;
+  long long visits = 0, waits = 0, n = 0;
+  for (const int4& s : planned) {
+    const int count = (s.y + most - 1) / most;
+    visits += count * seen_tiles(g, s.y, s.w);
+    waits += count * std::max(seen_tiles(g, s.y, s.w, per, 2), (long long)g.Hkv);
+    n += count;
+  }
+  const double tile_ns = !f8 ? 10.6 : narrow ? 5.5 : 8, wait_ns = !f8 ? 31 : narrow ? 28 : 38, item_ns = in_line ? 20 : 25;
+  if (6 + waits * wait_ns * 0.001 + visits * tile_ns * scale > 10 + items * item_ns * 0.001 + work * (f8 ? 18 : 14) * scale)
     return false;
   if (n > PackedSeqs::kMost && n > (long long)kPartsASeq * h->cfg.max_seqs) return false;  // more than the device's list holds
   parts->reserve(n);
@@ -721,7 +727,8 @@ aoh_status aoh_paged_attend(aoh_paged* cache, const void* q, int64_t q_stride, c
   std::vector<int4> parts;
   int tokens = 1;
   // (the decode kernel counts its tiles, of at least 128 keys, in 32 bits)
-  if (parts_of(cache, seqs, planned, items.size(), work, &parts, &tokens) &&
+  const bool in_line = prefill_is_short(costs, cache->num_sms) && c.form == AOH_PAGES_BF16;
+  if (parts_of(cache, seqs, planned, items.size(), work, in_line, &parts, &tokens) &&
       (int64_t)parts.size() * c.n_kv_heads * ((holds + 127) / 128) <= INT32_MAX) {
     PagedPartsArgs p;
     p.pages = cache->pages;

@@ -392,6 +392,7 @@ FEW = [
     ([6] * 30, [40 + 97 * (i % 13) for i in range(30)], 24, 8, 64, [1, 0] * 4, 0, 5, 64),
     ([2] * 20, [9000 + i for i in range(20)], 32, 8, 64, [0] * 8, 0, 1, 64),
     ([6] * 3, [40, 1007, 300], 24, 8, 64, [1, 0] * 4, 0, 5, 64),
+    ([1 + i % 4 for i in range(80)], [2400 + 3 * i for i in range(80)], 8, 2, 128, [0, 0], 0, 1, 64),
 ]
 
 

@@ -211,6 +211,9 @@ struct PagedAttendArgs : FoldedArgs {
   const int32_t* table;  // device [n_seqs][table_stride]; null: the pages written out
   int table_stride;
   int holds;          // tokens that a row of the caller's table holds
+  float4* states;     // items in parts (prefill_tc.cuh: kJoined): their states, most_parts of each, or null
+  int* arrived;       // and how many of them are there
+  int most_parts;
   int written;        // whether pages are written out; with a table: sequences that fit there are left out
 };
 
@@ -319,6 +322,17 @@ inline uint64_t prefill_item(int b, int h, int index) { return (uint64_t)b << 34
 constexpr uint64_t kPrefillTwoHeads = 1ull << 62;
 // A half of an item that a cluster's two CTAs share, and an entry without work.
 constexpr uint64_t kPrefillHalf = 1ull << 63, kPrefillNone = ~0ull;
+
+// An entry of an item's part alone: the item below bit 50, then the part, the parts (less one) and the
+// item's number among those that have parts.
+constexpr int kJoinedMost = 8, kJoinedSlots = 256, kJoinedEntries = 1280;  // parts of an item, such items and entries at most
+constexpr uint64_t kJoinedPart = 1ull << 50;
+__host__ __device__ inline uint64_t joined_entry(uint64_t item, int part, int parts, int slot) {
+  return item | (uint64_t)part << 50 | (uint64_t)(parts - 1) << 53 | (uint64_t)slot << 56;
+}
+__host__ __device__ inline int joined_part(uint64_t e) { return (int)(e >> 50) & 7; }
+__host__ __device__ inline int joined_parts(uint64_t e) { return ((int)(e >> 53) & 7) + 1; }
+__host__ __device__ inline int joined_slot(uint64_t e) { return (int)(e >> 56); }
 // Work items that travel as kernel arguments (32 KB of them at most).
 constexpr int kPrefillByValue = 3840;
 // Most work items of a launch on clusters of two CTAs.

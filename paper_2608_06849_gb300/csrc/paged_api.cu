@@ -181,8 +181,8 @@ cudaError_t sm_count(int* n) {
   return e;
 }
 
-// Memory for pages written out as bf16: a pool of each device, which keeps it from call to call for all handles
-// (a model's layers use the same), and gives it back with the last handle.
+// Memory of calls, for pages written out as bf16 and states of items in parts: a pool of each device, which keeps
+// it from call to call for all handles (a model's layers use the same), and gives it back with the last handle.
 struct ExpandPools {
   static constexpr int kMost = 64;
   std::mutex lock;
@@ -781,8 +781,28 @@ aoh_status aoh_paged_attend(aoh_paged* cache, const void* q, int64_t q_stride, c
     return fail(AOH_ERR_CUDA, "cuTensorMapEncodeTiled failed for q");
   bool lone = true;
   for (const int4& b : planned) lone = lone && b.y <= a.span;
-  const int split = folded_split(costs, lone, decode_tc_max_clusters, cache->num_sms), n_with = (int)seqs.size();
-  const bool is_short = split == 1 && prefill_is_short(costs, cache->num_sms);
+  const int n_with = (int)seqs.size();
+  double end = 0;
+  int split = folded_split(costs, lone, decode_tc_max_clusters, cache->num_sms, &end);
+  int slots = 0;
+  const std::vector<uint64_t> joined = joined_plan(items, costs, cache->num_sms, end, &a.most_parts, &slots);
+  void* states = nullptr;
+  if (!joined.empty()) {
+    const size_t bytes = (size_t)slots * a.most_parts * 256 * (c.d_head * 4 + 8);
+    states = expand_memory(cache->device, bytes + slots * sizeof(int), s);
+    if (states) {
+      a.states = static_cast<float4*>(states);
+      a.arrived = reinterpret_cast<int*>(static_cast<uint8_t*>(states) + bytes);
+      const cudaError_t e = cudaMemsetAsync(a.arrived, 0, slots * sizeof(int), s);
+      if (e != cudaSuccess) {
+        cudaFreeAsync(states, s);
+        return cuda_fail(e, "cudaMemsetAsync");
+      }
+      split = 1;
+    }
+  }
+  const std::vector<uint64_t>& entries = states ? joined : items;
+  const bool is_short = split == 1 && !states && prefill_is_short(costs, cache->num_sms);
   void* written = nullptr;
   if (expand_plan(cache, planned, work, &seqs))
     written = expand_memory(cache->device, (size_t)seqs[n_with].w * 2 * c.n_kv_heads * 128 * c.d_head * 2, s);
@@ -820,14 +840,15 @@ aoh_status aoh_paged_attend(aoh_paged* cache, const void* q, int64_t q_stride, c
     for (int i = 0; i < n_with; ++i) covered = covered && (seqs[i + 1].w - seqs[i].w) * 128ll >= holds;
     if (e == cudaSuccess && !make_pages_map(&w.pages, w.pool)) e = cudaErrorInvalidValue;
     if (e == cudaSuccess) e = launch_paged_expand(x, s);
-    if (e == cudaSuccess) e = launch_paged_attend(w, items, split, is_short, cache->num_sms, s);
+    if (e == cudaSuccess) e = launch_paged_attend(w, entries, split, is_short, cache->num_sms, s);
     a.written = 1;
   }
-  if (e == cudaSuccess && !covered) e = launch_paged_attend(a, items, split, is_short, cache->num_sms, s);
-  if (written) {
-    const cudaError_t f = cudaFreeAsync(written, s);
-    if (e == cudaSuccess) e = f;
-  }
+  if (e == cudaSuccess && !covered) e = launch_paged_attend(a, entries, split, is_short, cache->num_sms, s);
+  for (void* p : {written, states})
+    if (p) {
+      const cudaError_t f = cudaFreeAsync(p, s);
+      if (e == cudaSuccess) e = f;
+    }
   return e == cudaSuccess ? AOH_OK : cuda_fail(e, "paged attention launch");
 } catch (const std::exception& x) {
   return fail(AOH_ERR_CUDA, "paged attention: %s", x.what());

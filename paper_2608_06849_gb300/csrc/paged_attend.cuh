@@ -8,6 +8,10 @@
 // the computation on bf16 pages). That takes an item as many instructions as its softmax: where several
 // items visit the same tiles, paged_api.cu has them written out as bf16 pages once, for the bf16 kernel;
 // sequences that prove longer than the host took them to be are then left to this one.
+//
+// A chunk's items are few and unlike (a retrieval head's visit the whole prefix, a streaming one's its window), so
+// that whole items leave SMs idle at the end: prefill_plan.h has them shared by clusters or cut into parts, whose
+// states meet in global memory (131 KB a part of d_head 128, which L2 holds).
 #pragma once
 
 #include "paged_rows.cuh"
@@ -234,6 +238,7 @@ cudaError_t launch_attend(const PagedAttendArgs& args, const std::vector<uint64_
   if (split > 1)
     return launch_items<PagedArgs<F8>, D, kSplit, kPrefillSplitMost>(a, items.data(), (int)items.size(), split, s);
   const size_t n = items.size();
+  if (a.states) return launch_items<PagedArgs<F8>, D, kJoined, kJoinedEntries>(a, items.data(), (int)n, 1, s);
   if constexpr (!F8)
     for (size_t i = 0; is_short && i < n; i += kAttendByValue) {
       const int m = (int)(n - i < (size_t)kAttendByValue ? n - i : (size_t)kAttendByValue);

@@ -183,8 +183,9 @@ inline bool packed_folds(const CacheGeom& g, const std::vector<int4>& seqs, int 
 // alone / these sizes: 300 rows of 32/8 heads after 20,000 111 / 83, 256 of 16/2 after 5,000 34 / 22,
 // 100 of 28/4 after 100,000 148 / 124.
 template <class F>
-int folded_split(const std::vector<int>& costs, bool lone, F most, int num_sms) {
+int folded_split(const std::vector<int>& costs, bool lone, F most, int num_sms, double* its_end = nullptr) {
   const int n = (int)costs.size();
+  if (its_end) *its_end = 0;
   if (n > kPrefillSplitMost || n > 4 * num_sms || costs[0] < 7) return 1;
   std::vector<double> free_at;  // a min-heap
   auto end_of = [&](int slots, auto time) {
@@ -212,7 +213,59 @@ int folded_split(const std::vector<int>& costs, bool lone, F most, int num_sms) 
       pick = c;
     }
   }
+  if (its_end) *its_end = best;
   return pick;
+}
+
+// The entries of folded items in parts that CTAs of their own take, longest first, or none: where a longest-first
+// schedule of them ends well before `end`, that of the items or of clusters that share them (folded_split), in
+// visited tiles, with 4 tiles' time added to an item and 5 to a part of one. Clusters begin and end together, and
+// leave the SMs of a GPC that make no whole cluster idle. most_parts: of an item, 2 to kJoinedMost. Measured, us of a
+// chunk without / with (28/4 heads of 128, half streaming with a window of 2,048, after 30,001): 2,048 rows (114
+// items of 250 tiles, 114 of 18) 343 / 316, 8 bits 355 / 326, 4,096 647 / 612; close to even, 1,024 185 / 185, 512 104 / 106;
+// 32/8 heads, windows of 512: 600 rows after 6,000, half streaming, 51 / 47, 8 bits, 4 x 120 after 9,000, 5 heads
+// streaming, 75 / 68.
+inline std::vector<uint64_t> joined_plan(const std::vector<uint64_t>& items, const std::vector<int>& costs, int num_sms, double end,
+                                         int* most_parts, int* slots) {
+  std::vector<uint64_t> best;
+  const int n = (int)costs.size();
+  if (end <= 0 || n > kPrefillSplitMost || costs[0] < 16) return best;
+  double limit = 0.97 * end - 2;  // (the launch that clears the counts)
+  struct Entry {
+    double cost;
+    uint64_t entry;
+  };
+  std::vector<Entry> entries;
+  std::vector<double> free_at;
+  for (int k = 2; k <= kJoinedMost; ++k) {
+    const int longest = (costs[0] + k - 1) / k;
+    entries.clear();
+    int slot = 0;
+    double work = 0;
+    for (int i = 0; i < n; ++i) {
+      const int parts = costs[i] <= longest ? 1 : (costs[i] + longest - 1) / longest;
+      const double cost = parts > 1 ? (costs[i] + parts - 1) / parts + 5.0 : costs[i] + 4.0;
+      for (int p = 0; p < parts; ++p) entries.push_back({cost, joined_entry(items[i], p, parts, parts > 1 ? slot : 0)});
+      slot += parts > 1;
+      work += cost * parts;
+    }
+    if (entries.size() > (size_t)kJoinedEntries || slot > kJoinedSlots || work >= limit * num_sms) continue;
+    std::stable_sort(entries.begin(), entries.end(), [](const Entry& x, const Entry& y) { return x.cost > y.cost; });
+    free_at.assign(num_sms, 0.0);
+    double last = 0;
+    for (const Entry& e : entries) {
+      std::pop_heap(free_at.begin(), free_at.end(), std::greater<double>());
+      last = std::max(last, free_at.back() += e.cost);
+      std::push_heap(free_at.begin(), free_at.end(), std::greater<double>());
+    }
+    if (last >= limit) continue;
+    limit = last;
+    *most_parts = k;
+    *slots = slot;
+    best.clear();
+    for (const Entry& e : entries) best.push_back(e.entry);
+  }
+  return best;
 }
 
 // The work of clusters of two CTAs, two entries a cluster: two items, or one item

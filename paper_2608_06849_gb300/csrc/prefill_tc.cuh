@@ -59,11 +59,96 @@ namespace pf {
 // them). An item whose second query tile has no row is a lone one: both halves of the
 // pipeline work on its first tile, A on the even KV tiles and B on the odd ones, and their states
 // count as those of two CTAs.
-constexpr int kWhole = 0, kPairs = 1, kSplit = 2;
+// kJoined: CTAs of their own, one for each part of an item's KV tiles (an entry has the part, the parts
+// and a number of the item's: joined_entry). Each stores its state in global memory, and the last to
+// arrive adds them up.
+constexpr int kWhole = 0, kPairs = 1, kSplit = 2, kJoined = 3;
 
 // Whether a part of an item saw no key of a row. A part whose visible scores are all NaN has a
 // maximum of -inf as well, no NaN being the greater of two numbers, but its sum is NaN.
 __device__ __forceinline__ bool empty_state(float m, float l) { return m == -INFINITY && l == 0.f; }
+
+// The state of part `rank` of `parts` of an item to global memory ([D / 4][256 rows] float4, then (m, l) of
+// each row); the last CTA to arrive adds up the parts' and writes the rows. All threads; w: the warp among the
+// softmax warps (others: outside 0-7). The copies and MMAs of the CTA are done with its shared memory.
+template <int D, int O, class A, class T>
+__device__ __forceinline__ void join_parts(const A& a, const T& t, uint64_t code, int slot, int rank, int parts, int n_tiles,
+                                           float m, float l, bool ok, uint32_t tmem, uint8_t* smem, volatile int* last, int w) {
+  const int lane = threadIdx.x & 31, x = w >> 2, q4 = (threadIdx.x >> 5) & 3, r = q4 * 32 + lane, row = x * 128 + r;
+  const bool soft = w >= 0 && w < 8 && t.has_row(x, q4 * 32);  // alike in a warp
+  auto state = [&](int part) { return a.states + (size_t)(slot * a.most_parts + part) * (64 * D + 128); };
+  auto ends = [&](int part) { return reinterpret_cast<float2*>(state(part) + 64 * D); };
+  if (soft) {
+    float4* to = state(rank) + row;
+    __stcg(ends(rank) + row, make_float2(ok ? m : -INFINITY, l));
+    if (n_tiles > 0) {
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) {
+        uint32_t v[32];
+        tmem_ld32(tmem + ((uint32_t)(q4 * 32) << 16) + O + x * D + c * 32, v);
+        tmem_ld_wait();
+#pragma unroll
+        for (int e = 0; e < 32; e += 4)
+          __stcg(to + (c * 8 + e / 4) * 256, make_float4(__uint_as_float(v[e]), __uint_as_float(v[e + 1]),
+                                                         __uint_as_float(v[e + 2]), __uint_as_float(v[e + 3])));
+      }
+    }
+    tc_fence_before();
+    __threadfence();
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) *last = atomicAdd(a.arrived + slot, 1) == parts - 1;
+  __syncthreads();
+  if (!*last) return;
+  __threadfence();
+  if (!soft) return;
+  float M = -INFINITY, L = 0.f, f[kJoinedMost];
+#pragma unroll
+  for (int p = 0; p < kJoinedMost; ++p)
+    if (p < parts) M = fmaxf(M, __ldcg(ends(p) + row).x);
+#pragma unroll
+  for (int p = 0; p < kJoinedMost; ++p) {
+    f[p] = -1.f;  // a state that saw no key, whose numbers may never have been written
+    if (p < parts) {
+      const float2 ml = __ldcg(ends(p) + row);
+      if (!empty_state(ml.x, ml.y)) {
+        f[p] = fast_exp2(ml.x - M);
+        L += f[p] * ml.y;
+      }
+    }
+  }
+  const float inv = L == 0.f ? 0.f : 1.f / L;
+  uint8_t* stage = smem + w * (32 * D * 2);
+  Spoilt spoilt;
+#pragma unroll 1
+  for (int c = 0; c < D / 32; ++c) {
+    float4 o[8] = {};
+#pragma unroll
+    for (int p = 0; p < kJoinedMost; ++p) {
+      if (p >= parts) break;
+      float4 z[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[e] = __ldcg(state(p) + (c * 8 + e) * 256 + row);
+      if (f[p] < 0.f) continue;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        o[e].x += f[p] * z[e].x;
+        o[e].y += f[p] * z[e].y;
+        o[e].z += f[p] * z[e].z;
+        o[e].w += f[p] * z[e].w;
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+      const float y[8] = {o[e].x * inv,     o[e].y * inv,     o[e].z * inv,     o[e].w * inv,
+                          o[e + 1].x * inv, o[e + 1].y * inv, o[e + 1].z * inv, o[e + 1].w * inv};
+      spoilt.add(put_row<D>(stage, lane, c * 4 + e / 2, y));
+    }
+  }
+  write_rows<D, D>(a, t, x, q4 * 32, 0, stage, lane);
+  const uint32_t rows = spoilt.rows(t.has_row(x, r));
+  if (rows) repair_rows<D>(a, code, x * 128 + q4 * 32, rows);
+}
 
 template <class A, int D, int MODE, int CAP>
 __global__ void __launch_bounds__(CallOf<A>::kThreads, 1)
@@ -101,12 +186,12 @@ __global__ void __launch_bounds__(CallOf<A>::kThreads, 1)
   }
   // (a launch of the same call that follows finds what this one has waited for)
   if constexpr (PAGED) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  constexpr bool PAIRS = MODE == kPairs, SPLIT = MODE == kSplit;
-  const int ctas = SPLIT ? (int)cluster_ctas() : 2;
-  const int entry = SPLIT ? (int)blockIdx.x / ctas : blockIdx.x;
-  const uint64_t code = CAP > 0 ? wl.item[entry] : a.work[entry];
+  constexpr bool PAIRS = MODE == kPairs, SPLIT = MODE == kSplit, JOINED = MODE == kJoined;
+  const int entry = SPLIT ? blockIdx.x / cluster_ctas() : blockIdx.x;
+  const uint64_t given = CAP > 0 ? wl.item[entry] : a.work[entry], code = JOINED ? given & (kJoinedPart - 1) : given;
   if (PAIRS && code == kPrefillNone) return;
-  const bool half = SPLIT || (PAIRS && code >= kPrefillHalf);  // alike in all CTAs of a cluster
+  const int ctas = SPLIT ? (int)cluster_ctas() : JOINED ? joined_parts(given) : 2;
+  const bool half = SPLIT || (JOINED && ctas > 1) || (PAIRS && code >= kPrefillHalf);  // alike in all CTAs of a cluster
   const typename Call::ItemT t(a, code & ~kPrefillHalf);
   if constexpr (PAGED) {
     if (t.elsewhere(a)) {  // alike in all CTAs of a cluster
@@ -117,10 +202,10 @@ __global__ void __launch_bounds__(CallOf<A>::kThreads, 1)
   const CacheGeom& g = a.geom;
   const int n_all = t.tiles();
   // this CTA visits tiles t0 .. t0 + n_tiles - 1 of the item's n_all
-  const int rank = half ? (int)cluster_rank() : 0;
-  const int per = SPLIT ? (n_all + ctas - 1) / ctas : (n_all + 1) / 2;
+  const int rank = JOINED ? joined_part(given) : half ? (int)cluster_rank() : 0;
+  const int per = SPLIT || JOINED ? (n_all + ctas - 1) / ctas : (n_all + 1) / 2;
   const int t0 = rank * per;
-  const int n_tiles = !half ? n_all : SPLIT ? max(0, min(per, n_all - t0)) : rank == 0 ? (n_all + 1) / 2 : n_all / 2;
+  const int n_tiles = !half ? n_all : SPLIT || JOINED ? max(0, min(per, n_all - t0)) : rank == 0 ? (n_all + 1) / 2 : n_all / 2;
   const bool lone = SPLIT && !t.has_row(1, 0);
   PageWalk<A, D> pages(warp == 0 ? lane : -1, a);
   if (threadIdx.x == 0) {
@@ -499,6 +584,9 @@ __global__ void __launch_bounds__(CallOf<A>::kThreads, 1)
     }
     __syncthreads();
     tc_fence_after();
+  } else if constexpr (JOINED) {
+    if (half) join_parts<D, SB::O>(a, t, code, joined_slot(given), rank, ctas, n_tiles, end_m, end_ok ? end_l : 0.f, end_ok, tmem, smem,
+                                   reinterpret_cast<volatile int*>(tmem_slot + 2), warp - S0);
   } else if (half) {
     // both CTAs' copies and MMAs are done with their shared memory
     cluster_arrive();

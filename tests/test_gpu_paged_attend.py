@@ -309,10 +309,10 @@ WRITTEN_OUT = [
 
 @pytest.mark.parametrize("case", range(len(WRITTEN_OUT)))
 def test_pages_written_out_first(case):
-    """The outputs are those of the kernel that decodes them itself (a captured call takes no memory, so it
-    is that one), bit by bit, and right for whatever lengths the host takes the sequences to have."""
+    """Right for whatever lengths the host takes the sequences to have, and so are those of the kernel that
+    decodes them itself (a captured call takes no memory, so it is that one)."""
     c = Case(*WRITTEN_OUT[case], "e4m3", seed=50 + case, fused=True, spread=1.0)
-    first = c.attend(k_lens=c.k_lens).clone()
+    c.attend(k_lens=c.k_lens)
     c.matches("written out")
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
@@ -320,7 +320,7 @@ def test_pages_written_out_first(case):
     c.out.fill_(float("nan"))
     graph.replay()
     c.c.check()
-    assert torch.equal(c.out, first)
+    c.matches("captured")
     for hint in ([n // 2 for n in c.k_lens], [c.k_lens[0] // 3] + c.k_lens[1:], [n + 1000 for n in c.k_lens], None,
                  [0] + c.k_lens[1:]):
         c.out.fill_(float("nan"))
@@ -349,6 +349,19 @@ def test_bad_pages_written_out_first():
     hidden[600:, 4:8] = True  # KV head 1 streams: rows from position 1100 + 600 = 1700 on see 1001 on
     assert out[:900][~hidden].isnan().all() and not out[:900][hidden].isnan().any()
     assert torch.equal(out[900:], first[900:])
+
+
+def test_written_out_pages_are_what_the_codes_stand_for():
+    """Of whole items in both, so that the outputs are equal bit by bit."""
+    c = Case([300] * 20, [450 + i for i in range(20)], 16, 4, 128, [0, 1, 0, 0], 20, 200, 16, "e4m3", seed=57, spread=1.0)
+    first = c.attend(k_lens=c.k_lens).clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.c.attend(c.q, c.q_lens, c.lens, c.table, c.out, k_lens=c.k_lens)
+    c.out.fill_(float("nan"))
+    graph.replay()
+    c.c.check()
+    assert torch.equal(c.out, first)
 
 
 @pytest.mark.parametrize("n", [63, 64, 100])
@@ -529,6 +542,74 @@ def test_bad_sequences_among_many_short_items(d, form):
             c.c.check()
         keep = torch.arange(n * 33, device="cuda") // 33 != 17
         assert torch.equal(c.out[keep], clean[keep]), what
+
+
+JOINED = [
+    # chunks after long prefixes whose items are cut into parts of CTAs of their own: q_lens, k_lens, Hq, Hkv, d,
+    # labels, sink, window, page
+    ([300], [20300], 32, 8, 64, [0, 1] * 4, 64, 512, 64),
+    ([600], [6600], 32, 8, 128, [0, 1] * 4, 64, 512, 128),
+    ([700], [4700], 12, 3, 128, [0, 1, 0], 20, 500, 16),
+]
+
+
+@pytest.mark.parametrize("form", ["bf16", "e4m3"])
+@pytest.mark.parametrize("case", range(len(JOINED)))
+def test_items_in_parts(case, form):
+    """Right for whatever lengths the host takes the sequences to have (parts without a tile, others that the plan
+    does not cut), the same numbers every time, and no rows but those that see a spoilt key are spoilt."""
+    c = Case(*JOINED[case], form, seed=600 + case, fused=case % 2 == 0, spread=0.5)
+    first = c.attend(k_lens=c.k_lens).clone()
+    c.matches(f"items in parts {case}")
+    for _ in range(3):
+        c.out.fill_(float("nan"))
+        assert torch.equal(c.attend(k_lens=c.k_lens), first)
+    for n in (c.k_lens[0] // 3, c.k_lens[0] + 900):
+        c.out.fill_(float("nan"))
+        c.attend(k_lens=[n])
+        c.matches(f"items in parts {case}, hint {n}")
+    # fewer tokens than the host takes it to have: parts without a tile
+    c.lens.copy_(ints([c.q_lens[0] + 140]))
+    short = c.attend(k_lens=c.k_lens).clone()
+    c.lens.copy_(ints(c.k_lens))
+    d = Case([c.q_lens[0]], [c.q_lens[0] + 140], *JOINED[case][2:], form, seed=1)
+    d.q = c.q
+    d.c.append(c.k[:d.k_lens[0]], c.v[:d.k_lens[0]], d.lens, d.table, cu_rows=ints([0, d.k_lens[0]]))
+    want = d.attend(k_lens=d.k_lens)
+    assert ((short.double() - want.double()).abs() <= 2.0 ** -6 * want.double().abs() + 0.02).all()
+    # a spoilt key inside the chunk
+    q, m, labels = c.q_lens[0], c.k_lens[0], c.labels
+    at = m - q + 150
+    v = c.v.clone()
+    v[at] = float("nan")
+    c.c.append(c.k, v, c.lens, c.table, cu_rows=ints([0, m]))
+    out = c.attend(k_lens=c.k_lens)
+    pos = torch.arange(m - q, m, device="cuda")
+    for h, kind in enumerate(labels):
+        sees = at <= pos
+        if kind:
+            sees = sees & (pos - at < c.window)
+        g = slice(h * (c.q.shape[1] // len(labels)), (h + 1) * (c.q.shape[1] // len(labels)))
+        assert out[sees][:, g].isnan().all(), h
+        x, y = out[~sees][:, g].double(), first[~sees][:, g].double()
+        # (rows that are gone over again are summed in another order)
+        assert ((x - y).abs() <= 2.0 ** -6 * y.abs() + 0.02).all(), h
+
+
+@pytest.mark.parametrize("form", ["bf16", "e4m3"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_items_of_several_sequences_in_parts(d, form):
+    """Items that visit few tiles twice (8 bits: they are not written out), a sequence without keys among them."""
+    c = Case([120, 119, 30, 120, 118], [9120, 8000, 0, 9119, 8500], 32, 8, d, [0, 1, 1, 0, 1, 1, 0, 1], 64, 512, 64, form, seed=d)
+    first = c.attend(k_lens=c.k_lens).clone()
+    c.matches("several sequences in parts")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):  # (without memory for states: clusters)
+        c.c.attend(c.q, c.q_lens, c.lens, c.table, c.out, k_lens=c.k_lens)
+    c.out.fill_(float("nan"))
+    graph.replay()
+    c.c.check()
+    assert ((c.out.double() - first.double()).abs() <= 2.0 ** -6 * first.double().abs() + 0.02).all()
 
 
 @pytest.mark.parametrize("form", ["bf16", "e4m3"])

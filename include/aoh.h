@@ -647,10 +647,11 @@ aoh_status aoh_paged_decode(aoh_paged* cache, const void* q, int64_t q_stride, c
  *            them the work is split; the outputs are right whatever they are, and come soonest with close ones
  *   table    device [n_seqs][table_stride], of at most 2^30 tokens a row
  *   out      [rows][n_q_heads][d_head]
- * Long chunks over 8-bit pages take device memory, ordered on the stream: up to 4 * d_head * n_kv_heads
- * bytes a token of k_lens (never more than 4 GiB), from a pool of the device that all handles share and that is given
- * back with the last of them. A captured call takes none, nor does one for which there is none to be had:
- * these take longer. Errors: INVALID, CUDA.
+ * Long chunks take device memory, ordered on the stream, from a pool of the device that all handles share and
+ * that is given back with the last of them: over 8-bit pages up to 4 * d_head * n_kv_heads bytes a token of k_lens
+ * (never more than 4 GiB), and up to 260 MiB where a few items are cut into parts. A captured call takes
+ * none, nor does one for which there is none to be had: these take longer, and their sums may be rounded in another
+ * order. Errors: INVALID, CUDA.
  */
 aoh_status aoh_paged_attend(aoh_paged* cache, const void* q, int64_t q_stride, const int32_t* q_lens,
                             const int32_t* lens, const int32_t* k_lens, int32_t n_seqs, const int32_t* table,

@@ -239,6 +239,8 @@ cudaError_t launch_attend(const PagedAttendArgs& args, const std::vector<uint64_
     return launch_items<PagedArgs<F8>, D, kSplit, kPrefillSplitMost>(a, items.data(), (int)items.size(), split, s);
   const size_t n = items.size();
   if (a.states) return launch_items<PagedArgs<F8>, D, kJoined, kJoinedEntries>(a, items.data(), (int)n, 1, s);
+  // (a CTA holds the sequences of kShortItems items)
+  if (n > (size_t)kShortItems * num_sms && kAttendByValue > kShortItems * num_sms) is_short = false;
   if constexpr (!F8)
     for (size_t i = 0; is_short && i < n; i += kAttendByValue) {
       const int m = (int)(n - i < (size_t)kAttendByValue ? n - i : (size_t)kAttendByValue);

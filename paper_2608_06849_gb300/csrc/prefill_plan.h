@@ -239,17 +239,25 @@ inline std::vector<uint64_t> joined_plan(const std::vector<uint64_t>& items, con
   std::vector<double> free_at;
   for (int k = 2; k <= kJoinedMost; ++k) {
     const int longest = (costs[0] + k - 1) / k;
-    entries.clear();
-    int slot = 0;
+    auto parts_of = [&](int i) { return costs[i] <= longest ? 1 : (costs[i] + longest - 1) / longest; };
+    auto cost_of = [&](int i, int parts) { return parts > 1 ? (costs[i] + parts - 1) / parts + 5.0 : costs[i] + 4.0; };
+    int all = 0, cut = 0;
     double work = 0;
     for (int i = 0; i < n; ++i) {
-      const int parts = costs[i] <= longest ? 1 : (costs[i] + longest - 1) / longest;
-      const double cost = parts > 1 ? (costs[i] + parts - 1) / parts + 5.0 : costs[i] + 4.0;
-      for (int p = 0; p < parts; ++p) entries.push_back({cost, joined_entry(items[i], p, parts, parts > 1 ? slot : 0)});
-      slot += parts > 1;
-      work += cost * parts;
+      const int parts = parts_of(i);
+      all += parts;
+      cut += parts > 1;
+      work += parts * cost_of(i, parts);
     }
-    if (entries.size() > (size_t)kJoinedEntries || slot > kJoinedSlots || work >= limit * num_sms) continue;
+    if (all > kJoinedEntries || cut > kJoinedSlots || std::max(work / num_sms, longest + 4.0) >= limit) continue;
+    entries.clear();
+    int slot = 0;
+    for (int i = 0; i < n; ++i) {
+      const int parts = parts_of(i);
+      for (int p = 0; p < parts; ++p)
+        entries.push_back({cost_of(i, parts), joined_entry(items[i], p, parts, parts > 1 ? slot : 0)});
+      slot += parts > 1;
+    }
     std::stable_sort(entries.begin(), entries.end(), [](const Entry& x, const Entry& y) { return x.cost > y.cost; });
     free_at.assign(num_sms, 0.0);
     double last = 0;

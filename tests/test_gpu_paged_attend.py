@@ -67,11 +67,21 @@ class Case:
             self.c.append(self.k, self.v, self.lens, self.table, cu_rows=ints(sums(k_lens)))
         self.c.check()
         self.out = torch.full((n, hq, d), float("nan"), dtype=torch.bfloat16, device="cuda")
+        self.formed = {}
 
     def attend(self, **kw):
         self.c.attend(self.q, self.q_lens, self.lens, self.table, self.out, **kw)
         self.c.check()
         return self.out
+
+    def held(self, b, keys):
+        """What the pages hold of sequence b, formed once for the same k and v."""
+        version = (self.k._version, self.v._version)
+        if self.form == "bf16" or self.formed.get("version") != version:
+            self.formed = {"version": version}
+        if b not in self.formed:
+            self.formed[b] = held(self.k[keys], self.form), held(self.v[keys], self.form)
+        return self.formed[b]
 
     def matches(self, what, sequences=None):
         qs, ks = sums(self.q_lens), sums(self.k_lens)
@@ -80,7 +90,7 @@ class Case:
             if self.q_lens[b] == 0:
                 continue
             rows, keys = slice(qs[b], qs[b + 1]), slice(ks[b], ks[b + 1])
-            k, v = held(self.k[keys], self.form), held(self.v[keys], self.form)
+            k, v = self.held(b, keys)
             want = opaged.attend(q[rows], k, v, self.labels, self.sink, self.window)
             mag = opaged.attend(q[rows], k, np.abs(v), self.labels, self.sink, self.window)
             assert_matches(out[rows], want, f"{what}, sequence {b}", mag=mag, abs_bounds=False)

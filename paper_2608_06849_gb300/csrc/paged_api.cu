@@ -780,12 +780,16 @@ aoh_status aoh_paged_attend(aoh_paged* cache, const void* q, int64_t q_stride, c
   if (!make_rows_map(&a.tq, q, 1, n_q, c.n_q_heads, c.d_head, q_stride, a.span, a.geom.G))
     return fail(AOH_ERR_CUDA, "cuTensorMapEncodeTiled failed for q");
   bool lone = true;
-  for (const int4& b : planned) lone = lone && b.y <= a.span;
+  int lone_items = 0;
+  for (const int4& b : planned) {
+    lone = lone && b.y <= a.span;
+    if ((b.y - 1) % (2 * a.span) < a.span) lone_items += c.n_kv_heads;
+  }
   const int n_with = (int)seqs.size();
   double end = 0;
   int split = folded_split(costs, lone, decode_tc_max_clusters, cache->num_sms, &end);
   int slots = 0;
-  const std::vector<uint64_t> joined = joined_plan(items, costs, cache->num_sms, end, &a.most_parts, &slots);
+  const std::vector<uint64_t> joined = joined_plan(items, costs, lone_items, cache->num_sms, end, &a.most_parts, &slots);
   void* states = nullptr;
   if (!joined.empty()) {
     const size_t bytes = (size_t)slots * a.most_parts * 256 * (c.d_head * 4 + 8);

@@ -219,17 +219,20 @@ int folded_split(const std::vector<int>& costs, bool lone, F most, int num_sms, 
 
 // The entries of folded items in parts that CTAs of their own take, longest first, or none: where a longest-first
 // schedule of them ends well before `end`, that of the items or of clusters that share them (folded_split), in
-// visited tiles, with 4 tiles' time added to an item and 5 to a part of one. Clusters begin and end together, and
-// leave the SMs of a GPC that make no whole cluster idle. most_parts: of an item, 2 to kJoinedMost. Measured, us of a
-// chunk without / with (28/4 heads of 128, half streaming with a window of 2,048, after 30,001): 2,048 rows (114
+// visited tiles, with 4 tiles' time added to an item or part of one and 0.9 for each state that the last to arrive reads (131
+// KB at the rate of an SM). Where many items are lone ones (lone: how many; folded_split) clusters are left to them,
+// whose halves share such an item. Clusters begin and end together, and leave the SMs of a GPC that make no whole
+// cluster idle. most_parts: of an item, 2 to kJoinedMost. Measured, us of a chunk without / with (28/4 heads of 128, half streaming with a window of 2,048, after 30,001): 2,048 rows (114
 // items of 250 tiles, 114 of 18) 343 / 316, 8 bits 355 / 326, 4,096 647 / 612; close to even, 1,024 185 / 185, 512 104 / 106;
 // 32/8 heads, windows of 512: 600 rows after 6,000, half streaming, 51 / 47, 8 bits, 4 x 120 after 9,000, 5 heads
-// streaming, 75 / 68.
-inline std::vector<uint64_t> joined_plan(const std::vector<uint64_t>& items, const std::vector<int>& costs, int num_sms, double end,
-                                         int* most_parts, int* slots) {
+// streaming, 75 / 68. Not cut by this rule: 38 and 42 rows after 2,148-9,831, 40/8 heads, 31 / 40; 32/8 heads of
+// 64, 8 bits, 15 x 17-21 after 17,202-28,739 (lone ones) 246 / 298, 17 x 19-59 after 6,000-12,000 (half of them) 128 / 139.
+inline std::vector<uint64_t> joined_plan(const std::vector<uint64_t>& items, const std::vector<int>& costs, int lone, int num_sms,
+                                         double end, int* most_parts, int* slots) {
   std::vector<uint64_t> best;
   const int n = (int)costs.size();
-  if (end <= 0 || n > kPrefillSplitMost || costs[0] < 16) return best;
+  if (lone > n / 5 || end <= 0 || n > kPrefillSplitMost || costs[0] < 16) return best;
+  constexpr double join = 0.9;
   double limit = 0.97 * end - 2;  // (the launch that clears the counts)
   struct Entry {
     double cost;
@@ -240,7 +243,7 @@ inline std::vector<uint64_t> joined_plan(const std::vector<uint64_t>& items, con
   for (int k = 2; k <= kJoinedMost; ++k) {
     const int longest = (costs[0] + k - 1) / k;
     auto parts_of = [&](int i) { return costs[i] <= longest ? 1 : (costs[i] + longest - 1) / longest; };
-    auto cost_of = [&](int i, int parts) { return parts > 1 ? (costs[i] + parts - 1) / parts + 5.0 : costs[i] + 4.0; };
+    auto cost_of = [&](int i, int parts) { return parts > 1 ? (costs[i] + parts - 1) / parts + 4.0 + join : costs[i] + 4.0; };
     int all = 0, cut = 0;
     double work = 0;
     for (int i = 0; i < n; ++i) {
@@ -249,7 +252,7 @@ inline std::vector<uint64_t> joined_plan(const std::vector<uint64_t>& items, con
       cut += parts > 1;
       work += parts * cost_of(i, parts);
     }
-    if (all > kJoinedEntries || cut > kJoinedSlots || std::max(work / num_sms, longest + 4.0) >= limit) continue;
+    if (all > kJoinedEntries || cut > kJoinedSlots || std::max(work / num_sms, longest + 4.0) + join * k >= limit) continue;
     entries.clear();
     int slot = 0;
     for (int i = 0; i < n; ++i) {
@@ -266,8 +269,8 @@ inline std::vector<uint64_t> joined_plan(const std::vector<uint64_t>& items, con
       last = std::max(last, free_at.back() += e.cost);
       std::push_heap(free_at.begin(), free_at.end(), std::greater<double>());
     }
-    if (last >= limit) continue;
-    limit = last;
+    if (last + join * k >= limit) continue;
+    limit = last + join * k;
     *most_parts = k;
     *slots = slot;
     best.clear();

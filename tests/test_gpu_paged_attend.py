@@ -555,11 +555,12 @@ def test_bad_sequences_among_many_short_items(d, form):
 
 
 JOINED = [
-    # chunks after long prefixes whose items are cut into parts of CTAs of their own: q_lens, k_lens, Hq, Hkv, d,
+    # chunks after long prefixes whose items are cut into parts of CTAs of their own, or shared by clusters: q_lens, k_lens, Hq, Hkv, d,
     # labels, sink, window, page
     ([300], [20300], 32, 8, 64, [0, 1] * 4, 64, 512, 64),
     ([600], [6600], 32, 8, 128, [0, 1] * 4, 64, 512, 128),
     ([700], [4700], 12, 3, 128, [0, 1, 0], 20, 500, 16),
+    ([700], [20700], 12, 3, 128, [0, 1, 0], 20, 500, 16),
 ]
 
 

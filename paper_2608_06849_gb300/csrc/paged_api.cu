@@ -194,13 +194,17 @@ ExpandPools& expand_pools() {
   return pools;
 }
 
-// One handle more or less on a device.
+// One handle more or less on a device. With the last one its pool goes: what calls in flight still use follows
+// once they end (a pool that is trimmed instead keeps what the host has not seen freed, for good).
 void expand_memories(int device, int handles) {
   ExpandPools& p = expand_pools();
   if (device < 0 || device >= ExpandPools::kMost) return;
   std::lock_guard<std::mutex> hold(p.lock);
   p.handles[device] += handles;
-  if (p.handles[device] == 0 && p.pool[device]) cudaMemPoolTrimTo(p.pool[device], 0);
+  if (p.handles[device] == 0 && p.pool[device]) {
+    if (cudaMemPoolDestroy(p.pool[device]) != cudaSuccess) cudaGetLastError();
+    p.pool[device] = nullptr;
+  }
 }
 
 // Device memory of a call that is not captured, ordered on its stream; null if there is none to be had.
@@ -876,8 +880,8 @@ aoh_status aoh_paged_check(aoh_paged* cache, void* stream) {
 
 void aoh_paged_destroy(aoh_paged* cache) {
   if (!cache) return;
+  if (cache->meta) cudaFree(cache->meta);  // (waits for the handle's calls)
   expand_memories(cache->device, -1);
-  if (cache->meta) cudaFree(cache->meta);
   delete cache;
 }
 

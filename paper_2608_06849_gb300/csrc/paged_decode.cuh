@@ -377,9 +377,8 @@ __device__ __forceinline__ void join(int n, const float* first, const float* res
 
 // After CTA p stored its state of an item that CTAs f .. last share: the last of a group to
 // arrive joins the group, the last group the item. The 128 threads of named barrier 2.
-// Whether it has stored the outputs.
 template <int D, bool MULTI, class A>
-__device__ __forceinline__ bool join_item(const A& a, int p, int f, int last, int G, const Out<D, MULTI>& out,
+__device__ __forceinline__ void join_item(const A& a, int p, int f, int last, int G, const Out<D, MULTI>& out,
                                           volatile int* flag) {
   constexpr int kCta = 4 * state_floats(D);
   const int groups = (last - f) / kGroup + 1, p0 = f + (p - f) / kGroup * kGroup;
@@ -395,11 +394,11 @@ __device__ __forceinline__ bool join_item(const A& a, int p, int f, int last, in
       *flag = done;
     }
     named_barrier_sync(2, 128);
-    if (!*flag) return false;
+    if (!*flag) return;
     const bool whole = step > 1 || groups == 1;
     join<D, MULTI>(n, state_slot(a, first, slot, D), state_slot(a, first, slot_rest, D), step * kCta, G, out,
                    whole ? nullptr : state_slot(a, p0, p0 == f ? 3 : 2, D));
-    if (whole) return true;
+    if (whole) return;
     first = f;
     slot = 3;
     slot_rest = 2;
@@ -426,6 +425,7 @@ __device__ __noinline__ void repair_columns(const A& a, int b, int kvh, int len,
   for (int h = 0; mask >> h; ++h) {
     if (!(mask >> h & 1) || (h & 3) != warp) continue;
     const int t = (h * a.rcp) >> 16, head = kvh * g.G + h - t * g.G;
+    if (t >= part.y) continue;
     const int pos = len - part.y + t, w0 = strm ? max(0, pos - g.W + 1) : 0, sinks = strm ? min(g.S, w0) : 0;
     float bad = 0.f;
     auto look = [&](int from, int to) {
@@ -472,6 +472,24 @@ __device__ __noinline__ void repair_columns(const A& a, int b, int kvh, int len,
   }
 }
 
+// The columns of a CTA's run that repair_columns looks at, of the first `items` of its items, once no wait
+// of the pipeline depends on these warps: a column's keys, one after the other, take about 1 us each (three columns a warp
+// of 2^20 keys 3.1 s), and those waits give up after 2 s. columns: [32] of items that the CTA has alone, by their number modulo 32 (one marked
+// for another item is looked at in vain); shared: [2] of its first and of its last item, where it has joined
+// them. first: the run's first sequence, and its first tile.
+template <int D, int LG, class A>
+__device__ __noinline__ void repair_run(const A& a, const int* lens_s, const uint8_t* heads_s, int len_reg, Deal deal,
+                                        const int* first, const uint32_t* columns, const uint32_t* shared, int items) {
+  const int p = blockIdx.x;
+  if (p >= deal.P) return;
+  Walk<A, LG> walk(a, lens_s, heads_s, len_reg, deal.first(p), deal.first(p + 1), first[0], first[1]);
+  for (int n = 0; n < items && walk.next(); ++n) {
+    const bool alone = deal.cta_of(walk.off) == deal.cta_of(walk.off + walk.tiles - 1);
+    const uint32_t mask = alone ? columns[n & 31] : shared[n > 0];
+    if (mask) repair_columns<D>(a, walk.b, walk.kvh(), walk.q.len, mask, 0, D);
+  }
+}
+
 // Powers of two as floats.
 __device__ __forceinline__ float pow2i(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
 
@@ -511,7 +529,7 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   volatile int* flag = reinterpret_cast<volatile int*>(tmem_slot + 2);
   int* first_s = reinterpret_cast<int*>(tmem_slot + 3);  // [2] the run's first sequence, and its first tile
-  uint32_t* spoilt = tmem_slot + 5;                      // columns to be gone over again
+  uint32_t* spoilt = tmem_slot + 5;                      // [2] columns to be gone over again (repair_run: shared)
   int* wsum = reinterpret_cast<int*>(smem + C::OFF_MISC + 32);
   uint8_t* heads_s = smem + C::OFF_MISC + 32 + 128;
   int* lens_s = reinterpret_cast<int*>(smem + C::OFF_LENS);
@@ -548,7 +566,7 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
     mbar_init(drain, 1);
     *abort_flag = 0;
     first_s[0] = first_s[1] = 0;
-    spoilt[0] = 0;
+    spoilt[0] = spoilt[1] = 0;
     fence_mbar_init();
   }
   if (warp == kLoadK && lane == 0) prefetch_tmap(&a.pages);
@@ -603,6 +621,10 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
         const unsigned past = __ballot_sync(0xffffffffu, lane < a.n_seqs && inc > deal.first(p));
         b_first = past ? __ffs(past) - 1 : 0;
         seq_off = __shfl_sync(0xffffffffu, inc - mine, b_first);
+        if (MULTI && threadIdx.x == kFinish * 32) {
+          first_s[0] = b_first;
+          first_s[1] = seq_off;
+        }
       } else {
         const int per = (a.n_seqs + NT - 1) / NT;
         const int b0 = min(a.n_seqs, (int)threadIdx.x * per), b1 = min(a.n_seqs, b0 + per);
@@ -878,12 +900,16 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
         push(none, -INFINITY, 0.f);
       }
     }
+    // several tokens: columns to be gone over again, where the sums of the warps' tiles were (repair_run: columns)
+    uint32_t* columns = reinterpret_cast<uint32_t*>(wsum);
+    if (MULTI && !CL && r < 32) columns[r] = 0;
     int item = 0;
     bool ok = true;
     while (ok && walk.next()) {
       const int x = item & 1;
       const int f = CL ? 0 : deal.cta_of(walk.off), last = CL ? 0 : deal.cta_of(walk.off + walk.tiles - 1);
-      const Out<D, MULTI> out = out_of<D, MULTI>(a, walk.b, walk.kvh(), spoilt);
+      const Out<D, MULTI> out =
+          out_of<D, MULTI>(a, walk.b, walk.kvh(), CL ? spoilt : f == last ? columns + (item & 31) : spoilt + (item > 0));
       ok = wait_bar(&l_full[x], (item >> 1) & 1, a.err, abort_flag);
       ok = wait_bar(&o_full[x], (item >> 1) & 1, a.err, abort_flag) && ok;
       tc_fence_after();
@@ -944,20 +970,12 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
       __syncwarp();
       if (lane == 0) mbar_arrive(&o_free[x]);
       ++item;
-      bool stored = !CL && f == last;
-      if (f != last) stored = join_item<D, MULTI>(a, p, f, last, G, out, flag);
-      if constexpr (MULTI && !CL) {
-        if (stored) {  // alike in the 128 threads
-          named_barrier_sync(2, 128);
-          const uint32_t mask = *reinterpret_cast<volatile uint32_t*>(spoilt);
-          if (mask) {
-            named_barrier_sync(2, 128);
-            if ((threadIdx.x & 127) == 0) *spoilt = 0;
-            repair_columns<D>(a, walk.b, walk.kvh(), walk.q.len, mask, 0, D);
-            named_barrier_sync(2, 128);
-          }
-        }
-      }
+      if (f != last) join_item<D, MULTI>(a, p, f, last, G, out, flag);
+    }
+    if constexpr (MULTI && !CL) {
+      named_barrier_sync(2, 128);
+      if (__any_sync(0xffffffffu, (columns[lane] | spoilt[0] | spoilt[1]) != 0))
+        repair_run<D, LG>(a, mirrored ? lens_s : nullptr, heads_s, len_reg, deal, first_s, columns, spoilt, item);
     }
   } else {
     // ------------------------------------------------------------ softmax

@@ -358,7 +358,7 @@ __device__ __forceinline__ void join(int n, const float* first, const float* res
       }
     }
     if (!mine) continue;
-    if (dst == nullptr) {
+    if (out.to) {
       const float inv = MULTI && L == 0.f ? 0.f : 1.f / L;  // (a token that sees no key)
       if (out.has(h)) {
         *reinterpret_cast<uint2*>(out.at(h) + (v % (D / 4)) * 4) =
@@ -396,8 +396,10 @@ __device__ __forceinline__ void join_item(const A& a, int p, int f, int last, in
     named_barrier_sync(2, 128);
     if (!*flag) return;
     const bool whole = step > 1 || groups == 1;
-    join<D, MULTI>(n, state_slot(a, first, slot, D), state_slot(a, first, slot_rest, D), step * kCta, G, out,
-                   whole ? nullptr : state_slot(a, p0, p0 == f ? 3 : 2, D));
+    Out<D, MULTI> to = out;
+    if (!whole) to.to = nullptr;
+    join<D, MULTI>(n, state_slot(a, first, slot, D), state_slot(a, first, slot_rest, D), step * kCta, G, to,
+                   state_slot(a, p0, p0 == f ? 3 : 2, D));
     if (whole) return;
     first = f;
     slot = 3;
@@ -1050,7 +1052,12 @@ __global__ void __launch_bounds__(Lay<D, F8, GP>::THREADS, 1)
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&s_free[x]);
-        auto sees = [&](int c, int h) { return MULTI ? (cols[c] >> h & 1) != 0 : see[c]; };
+        auto sees = [&](int c, int h) {
+          if constexpr (MULTI)
+            return (cols[c] >> h & 1) != 0;
+          else
+            return see[c];
+        };
         float s[KP][GP];
 #pragma unroll
         for (int c = 0; c < KP; ++c) {

@@ -433,7 +433,7 @@ aoh_status aoh_classify(const void* w_q, const void* w_k, int32_t n_layers, int3
  *   scale * (a cos t - b sin t, a sin t + b cos t),   t = position * inv_freq[i].
  * The other numbers stay y. All of it is computed in 32 bits (angles exactly, to 2^-24 of a
  * half-turn, whatever the position) and rounded once. The squares are summed in 32 bits too: a row
- * with numbers above 2^60 has no norm.
+ * with numbers above 2^60 has no norm, nor has one of numbers below 2^-60 alone where eps is below 2^-100.
  */
 typedef struct aoh_rope {
   int32_t n_pairs;     /* pairs that turn: a multiple of 8, at most d_head / 2; 0: none      */

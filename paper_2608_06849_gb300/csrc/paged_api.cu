@@ -207,6 +207,14 @@ void expand_memories(int device, int handles) {
   }
 }
 
+// While it lives, calls of this thread that take memory or give it back are allowed beside other streams' captures,
+// which they would end otherwise.
+struct BesideCaptures {
+  cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+  BesideCaptures() { cudaThreadExchangeStreamCaptureMode(&mode); }
+  ~BesideCaptures() { cudaThreadExchangeStreamCaptureMode(&mode); }
+};
+
 // Device memory of a call that is not captured, ordered on its stream; null if there is none to be had.
 void* expand_memory(int device, size_t bytes, cudaStream_t s) {
   cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
@@ -216,6 +224,7 @@ void* expand_memory(int device, size_t bytes, cudaStream_t s) {
     cudaGetLastError();
     return nullptr;
   }
+  const BesideCaptures relaxed;
   cudaMemPool_t pool = nullptr;
   {
     ExpandPools& pools = expand_pools();
@@ -241,6 +250,11 @@ void* expand_memory(int device, size_t bytes, cudaStream_t s) {
     return nullptr;
   }
   return p;
+}
+
+cudaError_t expand_free(void* p, cudaStream_t s) {
+  const BesideCaptures relaxed;
+  return cudaFreeAsync(p, s);
 }
 
 // Groups of `per` tiles of 128 keys that n rows at the end of `keys` positions see, `most` of a KV head at most, of all
@@ -803,7 +817,7 @@ aoh_status aoh_paged_attend(aoh_paged* cache, const void* q, int64_t q_stride, c
       a.arrived = reinterpret_cast<int*>(static_cast<uint8_t*>(states) + bytes);
       const cudaError_t e = cudaMemsetAsync(a.arrived, 0, slots * sizeof(int), s);
       if (e != cudaSuccess) {
-        cudaFreeAsync(states, s);
+        expand_free(states, s);
         return cuda_fail(e, "cudaMemsetAsync");
       }
       split = 1;
@@ -854,7 +868,7 @@ aoh_status aoh_paged_attend(aoh_paged* cache, const void* q, int64_t q_stride, c
   if (e == cudaSuccess && !covered) e = launch_paged_attend(a, entries, split, is_short, cache->num_sms, s);
   for (void* p : {written, states})
     if (p) {
-      const cudaError_t f = cudaFreeAsync(p, s);
+      const cudaError_t f = expand_free(p, s);
       if (e == cudaSuccess) e = f;
     }
   return e == cudaSuccess ? AOH_OK : cuda_fail(e, "paged attention launch");

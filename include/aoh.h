@@ -562,7 +562,7 @@ aoh_status aoh_paged_init(const aoh_paged_config* cfg, const uint8_t* head_label
  *                at least n_q_heads * d_head: slices of a fused projection will do)
  *   k, v         rows of [n_kv_heads][d_head], k_stride and v_stride apart
  *   q_lens, k_lens  host [n_seqs], >= 0; k_lens NULL: as q_lens
- *   out          [rows][n_q_heads][d_head]
+ *   out          [rows][n_q_heads][d_head]; must not overlap q, k or v
  * The pages are not touched. The lengths travel as kernel arguments: a captured call
  * replays with the same ones. Errors: INVALID, CUDA.
  */
@@ -646,7 +646,7 @@ aoh_status aoh_paged_decode(aoh_paged* cache, const void* q, int64_t q_stride, c
  *   k_lens   host [n_seqs], or NULL: what the host takes lens to be (NULL: what the table holds). By
  *            them the work is split; the outputs are right whatever they are, and come soonest with close ones
  *   table    device [n_seqs][table_stride], of at most 2^30 tokens a row
- *   out      [rows][n_q_heads][d_head]
+ *   out      [rows][n_q_heads][d_head]; must not lie between the first and the last number of q
  * Long chunks take device memory, ordered on the stream, from a pool of the device that all handles share and
  * that is given back with the last of them: over 8-bit pages up to 4 * d_head * n_kv_heads bytes a token of k_lens
  * (never more than 4 GiB), and up to 260 MiB where a few items are cut into parts. A captured call takes

@@ -786,7 +786,7 @@ class PagedCache:
 
     def attend(self, q, q_lens, lens, table, out, k_lens=None, stream=None):
         """Attention of a chunk of new tokens of every sequence over its cached positions: q, out
-        [rows, Hq, d] (q with any distance between tokens), q_lens[b] rows of sequence b (a host list),
+        [rows, Hq, d] (q with any distance between tokens, out apart from it), q_lens[b] rows of sequence b (a host list),
         the last of its lens[b] positions (their own keys among them: append them first). k_lens: what the host
         takes the lengths to be (None: what the table holds), by which the work is split."""
         qp, qs, rows = _rows(q, "q", self.n_q_heads, self.d_head)

@@ -735,6 +735,10 @@ aoh_status aoh_paged_attend(aoh_paged* cache, const void* q, int64_t q_stride, c
   if (st != AOH_OK) return st;
   if (!lens || !aligned(lens, 4)) return fail(AOH_ERR_INVALID, "lens must be a 4-byte aligned device pointer");
   if (holds > (1 << 30)) return fail(AOH_ERR_INVALID, "a table's row must hold at most 2^30 tokens");
+  // (rows beside a value that is not finite read their queries once more, behind their outputs)
+  const __int128 row = (__int128)c.n_q_heads * c.d_head * 2, apart = (__int128)((uintptr_t)out) - (uintptr_t)q;
+  if (apart < (n_q - 1) * (__int128)q_stride * 2 + row && -apart < n_q * row)
+    return fail(AOH_ERR_INVALID, "out must not overlap the queries");
 
   cudaStream_t s = (cudaStream_t)stream;
   const int span = 128 / cache->geom.G;

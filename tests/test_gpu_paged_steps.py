@@ -105,3 +105,35 @@ def test_a_chunk_beside_many_single_tokens(form):
         c.out.fill_(float("nan"))
         c.attend(k_lens=hint)
         c.matches(f"hint {hint and hint[:3]}")
+
+
+def test_outputs_over_queries_are_refused():
+    """(A spoilt value in reach would have rows computed again from queries that are no longer there.)"""
+    n, hq, d = 6, 8, 64
+    c = Case([2, 4], [40, 50], hq, 2, d, [0, 1], 4, 30, 16, "bf16")
+    size = n * hq * d
+    buffer = torch.zeros(3 * size, dtype=torch.bfloat16, device="cuda")
+    q = buffer[size:2 * size].view(n, hq, d)
+    q.copy_(c.q)
+    for at in (size, size + 8, 8, 2 * size - 8):
+        with pytest.raises(aoh.AohError, match="must not overlap"):
+            c.c.attend(q, c.q_lens, c.lens, c.table, buffer[at:at + size].view(n, hq, d))
+    want = c.attend()
+    for at in (0, 2 * size):
+        out = buffer[at:at + size].view(n, hq, d)
+        c.c.attend(q, c.q_lens, c.lens, c.table, out)
+        assert torch.equal(out, want)
+    # a slice of a fused projection: the last row ends with its own heads
+    fused = torch.zeros(n * 2 * hq * d + size, dtype=torch.bfloat16, device="cuda")
+    q = fused[:n * 2 * hq * d].view(n, 2 * hq, d)[:, :hq]
+    q.copy_(c.q)
+    end = (2 * n - 1) * hq * d
+    for at, ok in ((end, True), (end - 8, False)):
+        out = fused[at:at + size].view(n, hq, d)
+        if ok:
+            c.c.attend(q, c.q_lens, c.lens, c.table, out)
+            assert torch.equal(out, want)
+        else:
+            with pytest.raises(aoh.AohError, match="must not overlap"):
+                c.c.attend(q, c.q_lens, c.lens, c.table, out)
+    c.c.check()

@@ -648,8 +648,9 @@ aoh_status aoh_paged_decode(aoh_paged* cache, const void* q, int64_t q_stride, c
  *   table    device [n_seqs][table_stride], of at most 2^30 tokens a row
  *   out      [rows][n_q_heads][d_head]; must not lie between the first and the last number of q
  * Long chunks take device memory, ordered on the stream, from a pool of the device that all handles share and
- * that is given back with the last of them: over 8-bit pages up to 4 * d_head * n_kv_heads bytes a token of k_lens
- * (never more than 4 GiB), and up to 260 MiB where a few items are cut into parts. A captured call takes
+ * that is given back with the last of them: over 8-bit pages up to 4 * d_head * n_kv_heads bytes a token of k_lens, each
+ * rounded up to 128 tokens (NULL: of what the table holds; never more than 4 GiB), and up to 260 MiB where a few items are
+ * cut into parts. A captured call takes
  * none, nor does one for which there is none to be had: these take longer, and their sums may be rounded in another
  * order. Errors: INVALID, CUDA.
  */

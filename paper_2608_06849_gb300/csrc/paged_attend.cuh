@@ -11,7 +11,8 @@
 //
 // A chunk's items are few and unlike (a retrieval head's visit the whole prefix, a streaming one's its window), so
 // that whole items leave SMs idle at the end: prefill_plan.h has them shared by clusters or cut into parts, whose
-// states meet in global memory (131 KB a part of d_head 128, which L2 holds).
+// states meet in global memory: 133 KB a part of d_head 128, most of which L2 holds (456 parts of a chunk of 2,048 rows, 61 MB
+// of states: 41 MB written to HBM, of which 15 are the outputs).
 #pragma once
 
 #include "paged_rows.cuh"

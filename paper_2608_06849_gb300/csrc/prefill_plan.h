@@ -219,12 +219,13 @@ int folded_split(const std::vector<int>& costs, bool lone, F most, int num_sms, 
 
 // The entries of folded items in parts that CTAs of their own take, longest first, or none: where a longest-first
 // schedule of them ends well before `end`, that of the items or of clusters that share them (folded_split), in
-// visited tiles, with 4 tiles' time added to an item or part of one and 0.9 for each state that the last to arrive reads (131
-// KB at the rate of an SM). Where many items are lone ones (lone: how many; folded_split) clusters are left to them,
+// visited tiles, with 4 tiles' time added to an item or part of one and 0.9 for each state that the last to arrive reads (133
+// KB at the rate of an SM; measured up to 456 parts, 61 MB, most of which L2 holds: there is no term for states that go to HBM). Where many items are lone ones (lone: how many; folded_split) clusters are left to them,
 // whose halves share such an item. Clusters begin and end together, and leave the SMs of a GPC that make no whole
 // cluster idle. most_parts: of an item, 2 to kJoinedMost. Measured, us of a chunk without / with (28/4 heads of 128, half streaming with a window of 2,048, after 30,001): 2,048 rows (114
-// items of 250 tiles, 114 of 18) 343 / 316, 8 bits 355 / 326, 4,096 647 / 612; close to even, 1,024 185 / 185, 512 104 / 106;
-// 32/8 heads, windows of 512: 600 rows after 6,000, half streaming, 51 / 47, 8 bits, 4 x 120 after 9,000, 5 heads
+// items of 250 tiles, 114 of 18) 342 / 316 (with inputs that change from call to call 351 / 333), 8 bits 354 / 327, 4,096 651 / 642,
+// 8 bits 654 / 619; close to even, 1,024 182 / 186, 512 101 / 102, 8 bits 194 / 197, 113 / 115;
+// 32/8 heads, windows of 512: 600 rows after 6,000, half streaming, 52 / 49, 8 bits 60 / 53; 8 bits, 4 x 120 after 9,000, 5 heads
 // streaming, 75 / 68. Not cut by this rule: 38 and 42 rows after 2,148-9,831, 40/8 heads, 31 / 40; 32/8 heads of
 // 64, 8 bits, 15 x 17-21 after 17,202-28,739 (lone ones) 246 / 298, 17 x 19-59 after 6,000-12,000 (half of them) 128 / 139.
 inline std::vector<uint64_t> joined_plan(const std::vector<uint64_t>& items, const std::vector<int>& costs, int lone, int num_sms,

@@ -334,7 +334,8 @@ __global__ void __launch_bounds__(kThreads, kBlocks) rotate_kernel(const __grid_
 // kernel before it.
 template <int D, int FORM>
 cudaError_t launch(const RotateArgs& a, int num_sms, cudaStream_t s) {
-  // as many groups for every block, of as few rows as then do
+  // groups of as few rows as take no more rounds of the blocks than groups of 8 would. (The last round is not
+  // full: 19,277 rows are 5.3 groups a block, 22,490 6.2, 16,384 4.5, where 32,768 are 8.98; 10 to 12% of the blocks' time.)
   const int n = a.rows.n_rows, blocks = kBlocks * num_sms, even = (n + blocks - 1) / blocks;
   const int each = (even + kMostRows - 1) / kMostRows, per = (even + each - 1) / each, groups = (n + per - 1) / per;
   cudaLaunchConfig_t cfg = {};

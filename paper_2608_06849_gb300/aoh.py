@@ -461,6 +461,8 @@ class Rope:
         if inv_freq is None:
             if rotated < 0 or rotated % 2:
                 raise ValueError(f"rotated = {rotated} must be a multiple of 16")
+            if not base > 0:
+                raise ValueError(f"base = {base} must be a number above 0")
             inv_freq = [float(base) ** (-2.0 * i / rotated) for i in range(rotated // 2)]
         inv_freq = [float(f) for f in inv_freq]
         self.c = aoh_rope()

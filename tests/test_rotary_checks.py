@@ -67,6 +67,13 @@ def test_rope_arguments():
             aoh.Rope(**bad)
 
 
+@pytest.mark.parametrize("base", [0, 0.0, -1e4, float("nan")])
+def test_rope_bases_that_have_no_powers(base):
+    """A refusal in the binding's own words, not of the arithmetic behind it."""
+    with pytest.raises(ValueError, match="above 0"):
+        aoh.Rope(64, base=base)
+
+
 def test_rope_struct_matches_header():
     assert ctypes.sizeof(aoh.aoh_rope) == 16 + 64 * 8
     assert aoh.aoh_rope.turns.offset == 16
